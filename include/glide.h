@@ -307,6 +307,119 @@ int glide_decode_launch_info(glide_ctx *ctx, int32_t *n_launches, int32_t *n_wor
 int glide_stream_schedule(const glide_config *cfg, int32_t n_sms, int64_t smem_limit, int32_t *rows_out, int32_t max_rows,
                           int32_t *n_rows);
 
+/* ---- softmax attention over a paged cache -----------------------------------------------------------------------
+ * For the layers beside the hybrid ones: layers that keep every token (w_l >= context, of which a ring would hold
+ * max_tokens rows for each sequence whatever its length), or a sliding window and a few first tokens that stay visible
+ * (sinks), and caches that may not grow and give up the slots whose accumulated attention weight is least.
+ *
+ * Keys and values live in pages of page_size tokens that the caller owns and hands out; a sequence's page table lists its
+ * pages in order, so slot s of sequence b is row s % page_size of page table[b][s / page_size].  Slots are the places of a
+ * sequence's tokens in its cache: positions, until glide_paged_evict has moved some.  The query of a sequence's newest
+ * token stands at slot lens[b] - 1, and query slot i sees slot j when
+ *     j <= i   and   (window < 0   or   j > i - window   or   j < n_sink)
+ *     out_i = sum_j e^(scale q_i.k_j - lse_i) v_j,    lse_i = log sum_j e^(scale q_i.k_j)
+ * A row that sees nothing (window 0 without sinks, an empty sequence) is 0 with lse -inf.  Query head h reads KV head
+ * h / (n_q_heads / n_kv_heads).  The account of attention weights, if one is kept, is
+ *     weight[b][g][j] += sum over the queries i and the query heads of KV head g of e^(scale q_i.k_j - lse_i).
+ *
+ *   - lens, starts, seen and the table are device arrays, read when the kernels run: a captured call can be replayed with
+ *     other lengths and pages.  Table entries of slots that no query sees are not read as pages and may hold anything.  A
+ *     page id outside [0, n_pages), a length outside [0, max_tokens], starts that do not ascend, or more new tokens than
+ *     the length are recorded in the status word; no memory outside the pool is touched, and that sequence's results are
+ *     unspecified.
+ *   - What a slot holds that a query does not see does not reach its output, infinities and NaN included.
+ *   - Offsets into the pool are 64 bits wide.  Rows of out, lse, weight and pos that belong to no sequence are left alone.
+ *   - The calls allocate nothing and do not synchronise.  The workspace holds what the kernels of one call hand to each
+ *     other: calls of one handle, replayed ones included, have to follow one another (stream order); calls that may run at
+ *     the same time need handles of their own, which may share the pages.  Nothing in it outlives a call but the status word.
+ *   - Results do not depend on timing: sums are joined in a fixed order, without atomics.
+ */
+typedef struct glide_paged glide_paged; /* opaque, host side */
+
+typedef struct {
+  int32_t n_layers;        /* layers of the pool, >= 1: page ids are the same in all of them */
+  int32_t n_q_heads;       /* H; H / H_kv in {1, 2, 4, 8} */
+  int32_t n_kv_heads;      /* H_kv */
+  int32_t head_dim;        /* d in {64, 128} */
+  int32_t io_dtype;        /* glide_dtype of q, k, v, out and the pages */
+  int32_t page_size;       /* tokens of a page: 16, 32, 64, 128 or 256 */
+  int32_t n_pages;         /* pages of the pool, per layer */
+  int32_t max_batch;       /* most sequences of a call, <= 1024 */
+  int64_t max_tokens;      /* most slots of a sequence, <= 2^30 */
+  int64_t layer_stride, page_stride, head_stride, row_stride; /* elements between layers, pages, KV heads and slots of the
+                              pool, multiples of 16 bytes, layer_stride a multiple of page_stride; all 0:
+                              [n_layers][n_pages][H_kv][page_size][d] */
+  float softmax_scale;     /* 0 selects 1/sqrt(head_dim) */
+  int32_t weights;         /* 1: the account of weights can be kept (a decode step then needs max_batch * H * max_tokens
+                              floats of workspace) */
+} glide_paged_config;
+
+/* What the calls below share.  Fields that a call does not name are ignored. */
+typedef struct {
+  int32_t layer;
+  int32_t batch;             /* sequences B, 1 <= B <= max_batch */
+  const int32_t *dev_table;  /* device [B][table_cols] page ids, rows table_stride apart */
+  int32_t table_cols;
+  int32_t n_sink;            /* first slots that stay visible, >= 0 (evict: first positions that are kept) */
+  int64_t table_stride;
+  const int32_t *dev_lens;   /* device [B]: slots each sequence holds, this call's new tokens among them */
+  const int32_t *dev_starts; /* device [B + 1]: the new tokens of sequence b are rows starts[b] .. starts[b + 1] - 1 */
+  int64_t n_tokens;          /* rows of q, k, v, out (prefill, weights): at least starts[B] */
+  int64_t q_stride, kv_stride, out_stride; /* elements between tokens of q, of k and v, of out; 0: H d, H_kv d, H d.  The
+                              heads of a token lie side by side; strides are multiples of 16 bytes */
+  int64_t window;            /* newest slots that a query sees, its own among them; < 0: all */
+  float *dev_weight;         /* device fp32 [B][H_kv][.], rows track_stride apart, one entry per slot; NULL: no account */
+  int32_t *dev_pos;          /* device int32, likewise: the position of each slot's token */
+  const int32_t *dev_seen;   /* device [B]: tokens each sequence has absorbed, this call's among them (NULL: lens) */
+  int64_t track_stride;
+} glide_paged_call;
+
+/* Bytes of device workspace a handle needs.  Host only, no CUDA calls. */
+int glide_paged_workspace_bytes(const glide_paged_config *cfg, size_t *bytes_out);
+
+/* Build a handle over the caller's pages and a workspace (256-byte aligned).  Both must stay alive until
+ * glide_paged_destroy.  The status word is cleared on `stream`. */
+int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *dev_v_pages, void *dev_workspace,
+                       size_t workspace_bytes, void *stream, glide_paged **out);
+int glide_paged_destroy(glide_paged *p);
+
+/* Store the new tokens of every sequence (dev_k, dev_v [n_tokens][H_kv][d]) in the last slots of its length and, unless
+ * dev_out is NULL, attend: dev_q, dev_out [n_tokens][H][d], dev_lse fp32 [n_tokens][H] or NULL.  With dev_k and dev_v NULL
+ * the tokens are in the cache already.  Where dev_weight / dev_pos are given, the new slots' account starts at 0 and
+ * their positions are seen - T_b ... seen - 1; the weights of this call are not added (glide_paged_weights does that). */
+int glide_paged_prefill(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
+                        void *dev_out, float *dev_lse, void *stream);
+
+/* One new token for every sequence: row b of dev_q, dev_out [B][H][d], dev_k, dev_v [B][H_kv][d], dev_lse [B][H] or NULL.
+ * The token is stored at slot lens[b] - 1 and attends; with dev_k and dev_v NULL it is in the cache already.  Where
+ * dev_weight is given, the weights of the step are added to the account (the new slot's starts at 0), and dev_pos, if
+ * given, receives the new slot's position.  A sequence of length 0 stores nothing.  The cache is read once, split over
+ * its length across the GPU and joined. */
+int glide_paged_decode(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
+                       void *dev_out, float *dev_lse, void *stream);
+
+/* Add the weights that the queries dev_q [n_tokens][H][d] with the row sums dev_lse [n_tokens][H] (of glide_paged_prefill
+ * over the same tokens, mask and scale) give every slot to the account dev_weight. */
+int glide_paged_weights(glide_paged *p, const glide_paged_call *call, const void *dev_q, const float *dev_lse, void *stream);
+
+/* Every sequence keeps min(lens[b], budget) slots; each KV head chooses its own.  Slots with a position below n_sink or at
+ * or above seen[b] - recent are protected (n_sink + recent <= budget); of the others those of least dev_weight leave, of
+ * equal ones the lowest slots first (a NaN counts as larger than any number; protected slots leave, lowest first, only
+ * when there are not enough others).  Of the kept slots those at or behind the new length move, in ascending order, into the
+ * freed slots below it, in ascending order: keys, values, weight and position; the rest stay where they are.
+ * dev_weight_out and dev_pos_out (same layout and stride) receive the account of the kept slots; they may be dev_weight and
+ * dev_pos themselves (both or neither).  dev_new_lens [B] receives the new lengths and may be dev_lens.  Pages
+ * behind them are the caller's again. */
+int glide_paged_evict(glide_paged *p, const glide_paged_call *call, int64_t budget, int64_t recent, float *dev_weight_out,
+                      int32_t *dev_pos_out, int32_t *dev_new_lens, void *stream);
+
+/* What a call with these fields would be refused with (GLIDE_OK: it would not).  The fields that only prefill and
+ * weights read are looked at when dev_starts is given.  Host only, no CUDA calls. */
+int glide_paged_check_call(const glide_paged_config *cfg, const glide_paged_call *call);
+
+/* The handle's status word (0: nothing was recorded since the last call), read and cleared.  Synchronises `stream`. */
+int glide_paged_device_status(glide_paged *p, void *stream, int32_t *status_out);
+
 /* Static, NUL-terminated description of a status code. */
 const char *glide_strerror(int code);
 

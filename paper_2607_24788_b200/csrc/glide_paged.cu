@@ -1,0 +1,207 @@
+// Paged attention: storing new tokens, and the forms that take one query token, or one slot, at a time.
+#include <algorithm>
+
+#include "glide_paged_rows.cuh"
+
+namespace glide {
+
+namespace {
+
+constexpr int kWarps = 8;
+
+// Sequence of row r of the call, its slot; false for rows of no sequence.
+__device__ bool row_of(const PagedParams &p, int64_t r, int &b, int &slot) {
+  int lo = 0, hi = p.batch;
+  while (hi - lo > 1) {   // the last sequence that starts at or before r
+    const int mid = (lo + hi) >> 1;
+    if (p.starts[mid] <= r) lo = mid; else hi = mid;
+  }
+  b = lo;
+  const int len = paged_len(p, b);
+  int row0;
+  const int n = paged_new(p, b, len, row0);
+  slot = len - n + int(r - row0);
+  return r >= row0 && r < row0 + n;
+}
+
+// One warp per (new token, KV head): its rows of K and V, its place in the account.
+template <typename T, int D>
+__global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int kChunks = D * int(sizeof(T)) / 16;
+  const int lane = threadIdx.x & 31;
+  const int64_t item = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t r = item / p.Hkv;
+  const int g = int(item - r * p.Hkv);
+  int b, slot;
+  if (r >= p.n_tokens || !row_of(p, r, b, slot)) return;
+  const int page = paged_page(p, b, slot);
+  if (page < 0) return;
+  const size_t to = paged_row(p, page, slot, g), from = size_t(r) * size_t(p.kv_stride) + size_t(g) * D;
+  if (lane < kChunks) {
+    reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.k) + to)[lane] = reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.new_k) + from)[lane];
+    reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.v) + to)[lane] = reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.new_v) + from)[lane];
+  }
+  const size_t at = (size_t(b) * p.Hkv + g) * size_t(p.track_stride) + slot;
+  if (lane == 0 && p.weight) p.weight[at] = 0.f;
+  if (lane == 0 && p.pos) p.pos[at] = p.seen[b] - paged_len(p, b) + slot;
+}
+
+// One warp per (new token, KV head).
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kWarps * 32) paged_prefill_row_kernel(const __grid_constant__ PagedParams p) {
+  const int64_t item = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t r = item / p.Hkv;
+  const int g = int(item - r * p.Hkv);
+  int b, i;
+  if (r >= p.n_tokens || !row_of(p, r, b, i)) return;
+  PagedRow<T, D, G> row;
+  row.load_q(p, size_t(r), g);
+  int first, second;
+  paged_ranges(p, i, first, second);
+  for_slots(0, first, 0, 1, [&](int j) { row.slot(p, b, g, j, nullptr); });
+  for_slots(second, i + 1, 0, 1, [&](int j) { row.slot(p, b, g, j, nullptr); });
+  row.store(p, size_t(r), g);
+}
+
+// One warp per (sequence, KV head, slot): the weights of all queries that see the slot.
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kWarps * 32) paged_weights_row_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31, b = blockIdx.y / p.Hkv, g = blockIdx.y % p.Hkv;
+  const int len = paged_len(p, b);
+  int row0;
+  const int n = paged_new(p, b, len, row0);
+  for (int j = blockIdx.x * kWarps + (threadIdx.x >> 5); j < len; j += gridDim.x * kWarps) {
+    float k[E], sum = 0.f;
+    bool seen = false;
+    for (int t = 0; t < n; ++t) {
+      const int i = len - n + t;
+      if (!paged_sees(p, i, j)) continue;
+      if (!seen) load_elems<T, E>(reinterpret_cast<const T *>(p.k) + paged_row(p, paged_page(p, b, j), j, g) + lane * E, k);
+      seen = true;
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        float q[E], part = 0.f;
+        load_elems<T, E>(reinterpret_cast<const T *>(p.q) + size_t(row0 + t) * size_t(p.q_stride) + size_t(g * G + h) * D + lane * E, q);
+#pragma unroll
+        for (int e = 0; e < E; ++e) part = fmaf(q[e] * p.scale_log2, k[e], part);
+        const float lse = p.lse[size_t(row0 + t) * size_t(p.H) + g * G + h];
+        sum += exp2f(warp_sum(part) - lse * kLog2e);
+      }
+    }
+    if (seen && lane == 0) p.weight[(size_t(b) * p.Hkv + g) * size_t(p.track_stride) + j] += sum;
+  }
+}
+
+// One block per (sequence, KV head): the new token is stored, the warps take the slots in turns and join.
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kWarps * 32) paged_decode_unit_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int E = D / 32;
+  __shared__ float sm_m[kWarps][G], sm_l[kWarps][G], sm_acc[kWarps][G][D];
+  __shared__ float sm_lse[G];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;
+  const int len = paged_len(p, b), i = len - 1;
+  PagedRow<T, D, G> row;
+  row.load_q(p, size_t(b), g);
+  float *scores = p.weight ? p.logits + size_t(blockIdx.x) * size_t(p.most) * G : nullptr;
+  int first = 0, second = 0;
+  if (len > 0) {
+    if (p.new_k && warp == 0) {
+      const int page = paged_page(p, b, i);
+      const size_t to = paged_row(p, page, i, g) + lane * E, from = size_t(b) * size_t(p.kv_stride) + size_t(g) * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (page < 0) break;
+        reinterpret_cast<T *>(p.k)[to + e] = reinterpret_cast<const T *>(p.new_k)[from + e];
+        reinterpret_cast<T *>(p.v)[to + e] = reinterpret_cast<const T *>(p.new_v)[from + e];
+      }
+    }
+    __syncthreads();
+    paged_ranges(p, i, first, second);
+    for_slots(0, first, warp, kWarps, [&](int j) { row.slot(p, b, g, j, scores ? scores + size_t(j) * G : nullptr); });
+    for_slots(second, len, warp, kWarps, [&](int j) { row.slot(p, b, g, j, scores ? scores + size_t(j) * G : nullptr); });
+  }
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    if (lane == 0) sm_m[warp][h] = row.m[h], sm_l[warp][h] = row.l[h];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sm_acc[warp][h][lane * E + e] = row.acc[h][e];
+  }
+  __syncthreads();
+  if (warp == 0) {
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      float m = -CUDART_INF_F, l = 0.f;
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm_m[w][h]);
+      const float ref = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < E; ++e) row.acc[h][e] = 0.f;
+      for (int w = 0; w < kWarps; ++w) {
+        const float c = exp2f(sm_m[w][h] - ref);
+        l = fmaf(sm_l[w][h], c, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) row.acc[h][e] = fmaf(sm_acc[w][h][lane * E + e], c, row.acc[h][e]);
+      }
+      row.m[h] = m, row.l[h] = l;
+      if (lane == 0) sm_lse[h] = ref + (l == 0.f ? 0.f : log2f(l));
+    }
+    row.store(p, size_t(b), g);
+  }
+  __syncthreads();
+  const size_t at = (size_t(b) * p.Hkv + g) * size_t(p.track_stride);
+  if (scores) {
+    for (int j = threadIdx.x; j < len; j += kWarps * 32) {
+      if (!paged_sees(p, i, j)) continue;
+      float sum = 0.f;   // (the step's weights first: the account is rounded once)
+#pragma unroll
+      for (int h = 0; h < G; ++h) sum += exp2f(scores[size_t(j) * G + h] - sm_lse[h]);
+      p.weight[at + j] = p.new_k && j == i ? sum : p.weight[at + j] + sum;
+    }
+    if (threadIdx.x == 0 && len > 0 && p.new_k && !paged_sees(p, i, i)) p.weight[at + i] = 0.f;
+  }
+  if (p.pos && threadIdx.x == 0 && len > 0 && p.new_k) p.pos[at + i] = p.seen[b] - 1;
+}
+
+unsigned blocks_of(int64_t items) { return unsigned((items + kWarps - 1) / kWarps); }
+int launched() {
+  if (cudaGetLastError() == cudaSuccess) return GLIDE_OK;
+  return GLIDE_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t paged_record_bytes(const glide_paged_config &) { return 0; }
+int setup_paged_decode(const glide_paged *) { return GLIDE_OK; }
+
+int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
+    paged_store_kernel<typename decltype(t)::type, decltype(d)::value><<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);
+    return launched();
+  });
+}
+
+int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
+    paged_prefill_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>
+        <<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);
+    return launched();
+  });
+}
+
+int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
+    const dim3 grid(unsigned(std::min<int64_t>(blocks_of(p.most), 1024)), unsigned(p.batch * p.Hkv));
+    paged_weights_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value><<<grid, kWarps * 32, 0, st>>>(p);
+    return launched();
+  });
+}
+
+int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
+    paged_decode_unit_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>
+        <<<unsigned(p.batch * p.Hkv), kWarps * 32, 0, st>>>(p);
+    return launched();
+  });
+}
+
+}  // namespace glide

@@ -1,0 +1,104 @@
+// Internal structures of the paged softmax attention (glide_paged_* of include/glide.h).
+#pragma once
+
+#include <cuda.h>
+
+#include "glide_internal.h"
+
+struct glide_paged {
+  glide_paged_config cfg;
+  int device = 0;
+  int sm_count = 0;
+  int group = 1;
+  int page_shift = 4;
+  int64_t layer_pages = 0;          // page numbers from one layer to the next: layer_stride / page_stride
+  unsigned char *ws = nullptr;
+  unsigned char *k = nullptr, *v = nullptr;
+  size_t off_records = 0, off_track = 0, total = 0;   // byte offsets in the workspace
+  CUtensorMap k16, v16;             // pages as {64 columns, halves, slots, KV heads, pages}: boxes of 16 slots x all columns
+  CUtensorMap kpage, vpage;         // boxes of min(page_size, 128) slots x 64 columns
+  bool maps = false;                // bf16 only
+};
+
+namespace glide {
+
+enum : int { kDevBadPage = 4, kDevBadLength = 5 };   // status codes beside glide_internal.h's
+
+constexpr int kMaxPagedBatch = 1024;
+constexpr int kPagedTile = 16;        // slots of a decode tile: no tile crosses a page
+
+// One call, as the kernels get it.
+struct PagedParams {
+  const int32_t *table;
+  int64_t table_stride;
+  const int32_t *lens, *starts, *seen;
+  int32_t batch, H, Hkv, n_pages;
+  int32_t page_shift, most;           // most: slots that a sequence may hold here, min(max_tokens, table_cols * page_size)
+  int32_t window, n_sink;             // window: < 0 none; both at most 2^30
+  float scale_log2;                   // softmax_scale * log2(e)
+  int32_t page0;                      // number of the layer's first page in the tensor maps
+  void *k, *v;                        // the layer's pages
+  int64_t page_stride, head_stride, row_stride;
+  const void *q, *new_k, *new_v;
+  void *out;
+  float *lse;                         // prefill, decode: written; weights: read
+  int64_t q_stride, kv_stride, out_stride;
+  int64_t n_tokens;
+  float *weight;
+  int32_t *pos;
+  int64_t track_stride;
+  int32_t *status;
+  float *records;                     // partial records of units that several blocks share
+  float *logits;                      // [batch][Hkv][most][G]: scores of a decode step whose weights are kept
+  int32_t *moves;                     // (the same memory) evict: [batch][Hkv] counts, then [batch][Hkv][most / 2] pairs of slots
+  int32_t sm_count;
+};
+
+// Lengths as the kernels use them: what is out of range is recorded and clamped.
+__device__ __forceinline__ int paged_len(const PagedParams &p, int b) {
+  const int n = p.lens[b];
+  if (n < 0 || n > p.most) {
+    atomicExch(p.status, kDevBadLength);
+    return n < 0 ? 0 : p.most;
+  }
+  return n;
+}
+// The new tokens of sequence b: row of the first one, and how many.
+__device__ __forceinline__ int paged_new(const PagedParams &p, int b, int len, int &row0) {
+  row0 = p.starts[b];
+  int n = p.starts[b + 1] - row0;
+  if (n < 0 || n > len || row0 < 0 || int64_t(row0) + n > p.n_tokens) {
+    atomicExch(p.status, kDevBadLength);
+    n = 0;
+  }
+  return n;
+}
+// Page of a slot; a bad id is recorded and gives -1.
+__device__ __forceinline__ int paged_page(const PagedParams &p, int b, int slot) {
+  const int id = p.table[size_t(b) * size_t(p.table_stride) + size_t(slot >> p.page_shift)];
+  if (unsigned(id) >= unsigned(p.n_pages)) {
+    atomicExch(p.status, kDevBadPage);
+    return -1;
+  }
+  return id;
+}
+// Element offset of a slot's row in the layer's pages (a bad page: row 0 of the pool, which is memory of the pool).
+__device__ __forceinline__ size_t paged_row(const PagedParams &p, int page, int slot, int g) {
+  if (page < 0) return 0;
+  return size_t(page) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) +
+         size_t(slot & ((1 << p.page_shift) - 1)) * size_t(p.row_stride);
+}
+__device__ __forceinline__ bool paged_sees(const PagedParams &p, int i, int j) {
+  return j <= i && (p.window < 0 || j > i - p.window || j < p.n_sink);
+}
+
+int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, int recent, float *weight_out, int32_t *pos_out,
+                       int32_t *new_lens, cudaStream_t st);
+size_t paged_record_bytes(const glide_paged_config &cfg);
+int setup_paged_decode(const glide_paged *h);
+
+}  // namespace glide

@@ -50,6 +50,19 @@ class glide_config(ctypes.Structure):
     ]
 
 
+class glide_paged_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "io_dtype", "page_size", "n_pages", "max_batch")] + \
+               [(n, ctypes.c_int64) for n in ("max_tokens", "layer_stride", "page_stride", "head_stride", "row_stride")] + \
+               [("softmax_scale", ctypes.c_float), ("weights", ctypes.c_int32)]
+
+
+class glide_paged_call(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int32), ("batch", ctypes.c_int32), ("dev_table", ctypes.c_void_p), ("table_cols", ctypes.c_int32),
+                ("n_sink", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("dev_lens", ctypes.c_void_p), ("dev_starts", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("n_tokens", "q_stride", "kv_stride", "out_stride", "window")] + \
+               [(n, ctypes.c_void_p) for n in ("dev_weight", "dev_pos", "dev_seen")] + [("track_stride", ctypes.c_int64)]
+
+
 class glide_layer_info_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("window", "capacity", "n", "count", "head_slot", "n_evicted")]
 
@@ -92,13 +105,25 @@ def load_library() -> ctypes.CDLL:
     lib.glide_decode_launch_info.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]
     lib.glide_stream_schedule.argtypes = [cfgp, i32, i64, ctypes.POINTER(i32), i32, ctypes.POINTER(i32)]
     lib.glide_stream_schedule.restype = ctypes.c_int
+    pagedp, callp = ctypes.POINTER(glide_paged_config), ctypes.POINTER(glide_paged_call)
+    lib.glide_paged_workspace_bytes.argtypes = [pagedp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.glide_paged_create.argtypes = [pagedp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
+    lib.glide_paged_destroy.argtypes = [vp]
+    lib.glide_paged_prefill.argtypes = [vp, callp, vp, vp, vp, vp, vp, vp]
+    lib.glide_paged_decode.argtypes = [vp, callp, vp, vp, vp, vp, vp, vp]
+    lib.glide_paged_weights.argtypes = [vp, callp, vp, vp, vp]
+    lib.glide_paged_evict.argtypes = [vp, callp, i64, i64, vp, vp, vp, vp]
+    lib.glide_paged_check_call.argtypes = [pagedp, callp]
+    lib.glide_paged_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.glide_strerror.argtypes = [ctypes.c_int]
     lib.glide_strerror.restype = ctypes.c_char_p
     for name in ("glide_workspace_bytes", "glide_create", "glide_prefill", "glide_decode_step", "glide_destroy",
                  "glide_decode_step_noalloc", "glide_decode_step_layers", "glide_prefill_gated",
                  "glide_decode_step_gated", "glide_export_gates", "glide_import_gates",
                  "glide_layer_info", "glide_export_state", "glide_import_state", "glide_reset",
-                 "glide_device_status", "glide_decode_launch_info"):
+                 "glide_device_status", "glide_decode_launch_info", "glide_paged_workspace_bytes", "glide_paged_create",
+                 "glide_paged_destroy", "glide_paged_prefill", "glide_paged_decode", "glide_paged_weights", "glide_paged_evict",
+                 "glide_paged_check_call", "glide_paged_device_status"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -365,3 +390,168 @@ class Glide:
         _check(self.lib.glide_decode_launch_info(self._h, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c)),
                "glide_decode_launch_info")
         return dict(launches=a.value, work_items=b.value, grid=c.value)
+
+
+def make_paged_config(k_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int, softmax_scale: float = 0.0,
+                      weights: bool = True) -> glide_paged_config:
+    """The configuration of pages k_pages [L][n_pages][H_kv][page_size][d], which may be a view with other strides."""
+    assert k_pages.dim() == 5 and k_pages.stride(4) == 1, "pages are [L][n_pages][H_kv][page_size][d], features side by side"
+    L, n, hkv, page, d = k_pages.shape
+    cfg = glide_paged_config(n_layers=L, n_q_heads=n_q_heads, n_kv_heads=hkv, head_dim=d,
+                             io_dtype={torch.float32: GLIDE_F32, torch.bfloat16: GLIDE_BF16}[k_pages.dtype], page_size=page, n_pages=n,
+                             max_batch=int(max_batch), max_tokens=int(max_tokens), softmax_scale=float(softmax_scale), weights=int(bool(weights)))
+    cfg.layer_stride, cfg.page_stride, cfg.head_stride, cfg.row_stride = (int(k_pages.stride(i)) for i in range(4))
+    if L == 1:   # (of a single layer any distance will do)
+        cfg.layer_stride = max(1, n) * cfg.page_stride
+    return cfg
+
+
+def glide_paged_workspace_bytes(cfg: glide_paged_config) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().glide_paged_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)), "glide_paged_workspace_bytes")
+    return int(out.value)
+
+
+class GlidePaged:
+    """Softmax attention over a paged cache (include/glide.h): k_pages, v_pages [L][n_pages][H_kv][page_size][d] are the
+    caller's (views of equal strides will do), a torch workspace and the handle are owned here.  Tables are int32 [B][cols], lens,
+    seen and new_lens int32 [B], starts int32 [B + 1], weight fp32 and pos int32 [B][H_kv][slots], all on the pages' device.
+    Calls of one object must follow one another on the GPU; objects of their own may share pages."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int,
+                 softmax_scale: float = 0.0, weights: bool = True):
+        self.lib = load_library()
+        assert k_pages.is_cuda and v_pages.device == k_pages.device and v_pages.dtype == k_pages.dtype
+        assert v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
+        self.device, self.dtype = k_pages.device, k_pages.dtype
+        self.L, _, self.Hkv, self.page_size, self.d = k_pages.shape
+        self.H, self.max_batch, self.max_tokens = int(n_q_heads), int(max_batch), int(max_tokens)
+        self.cfg = make_paged_config(k_pages, n_q_heads, max_batch, max_tokens, softmax_scale, weights)
+        self.workspace_bytes = glide_paged_workspace_bytes(self.cfg)
+        self._keep = (k_pages, v_pages)
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
+            base = (self.workspace.data_ptr() + 255) // 256 * 256
+            handle = ctypes.c_void_p()
+            _check(self.lib.glide_paged_create(ctypes.byref(self.cfg), k_pages.data_ptr(), v_pages.data_ptr(), base, self.workspace_bytes,
+                                               _stream(None), ctypes.byref(handle)), "glide_paged_create")
+        self._h = handle
+        self._call = glide_paged_call()
+        self._callp = ctypes.byref(self._call)
+
+    def _ints(self, t: torch.Tensor, n: int, what: str) -> int:
+        assert t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous() and t.device == self.device, f"{what}: int32 [{n}] on {self.device}"
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, heads: int, what: str):
+        """Address and token stride of [tokens][heads][d] whose heads lie side by side."""
+        assert t.dtype is self.dtype and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.d and t.device == self.device, what
+        assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.d), f"{what}: a token's heads have to lie side by side"
+        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+
+    def _begin(self, layer: int, table: torch.Tensor, lens: torch.Tensor, window: int, n_sink: int, weight, pos, seen) -> glide_paged_call:
+        c = self._call
+        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.device == self.device, "table: int32 [B][cols]"
+        B, cols = table.shape
+        c.layer, c.batch, c.dev_table, c.table_cols = layer, B, table.data_ptr(), cols
+        c.table_stride = table.stride(0) if B > 1 else cols
+        c.dev_lens = self._ints(lens, B, "lens")
+        c.window, c.n_sink = window, n_sink
+        c.track_stride, c.dev_weight, c.dev_pos = 0, None, None
+        for t, dt in ((weight, torch.float32), (pos, torch.int32)):
+            if t is None:
+                continue
+            assert t.dtype is dt and t.dim() == 3 and t.shape[:2] == (B, self.Hkv) and t.is_contiguous() and t.device == self.device, \
+                "weight, pos: fp32, int32 [B][H_kv][slots]"
+            assert c.track_stride in (0, t.shape[2]), "weight and pos: as many slots"
+            c.track_stride = t.shape[2]
+            if dt is torch.float32:
+                c.dev_weight = t.data_ptr()
+            else:
+                c.dev_pos = t.data_ptr()
+        c.dev_seen = None if seen is None else self._ints(seen, B, "seen")
+        c.dev_starts = None
+        return c
+
+    def _lse(self, lse, rows: int):
+        if lse is None:
+            return None
+        assert lse.dtype is torch.float32 and lse.shape == (rows, self.H) and lse.is_contiguous() and lse.device == self.device, "lse: fp32 [tokens][H]"
+        return lse.data_ptr()
+
+    def _tensors(self, c: glide_paged_call, q, k, v, out, rows: int):
+        """Addresses of the call's tensors of `rows` tokens; their strides go to the call."""
+        pq = pk = pv = po = None
+        if q is not None:
+            pq, c.q_stride = self._rows(q, self.H, "q")
+            assert q.shape[0] == rows
+        assert (k is None) == (v is None)
+        if k is not None:
+            pk, c.kv_stride = self._rows(k, self.Hkv, "k")
+            pv, stride = self._rows(v, self.Hkv, "v")
+            assert k.shape[0] == rows and v.shape[0] == rows and stride == c.kv_stride, "k and v: equal strides"
+        if out is not None:
+            po, c.out_stride = self._rows(out, self.H, "out")
+            assert out.shape[0] == rows
+        return pq, pk, pv, po
+
+    def _launch(self, where: str, stream, fn, *args) -> None:
+        if self.device.index == _current_device():
+            rc = fn(self._h, *args, _stream(stream))
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(self._h, *args, _stream(stream))
+        if rc:
+            _check(rc, where)
+
+    def glide_paged_prefill(self, table, lens, starts, q, k, v, out=None, lse=None, window: int = -1, n_sink: int = 0, weight=None,
+                            pos=None, seen=None, layer: int = 0, stream=None) -> None:
+        """Stores the new tokens (rows starts[b] .. starts[b + 1] - 1 of k, v; None: they are in the cache) and, with out, attends."""
+        c = self._begin(layer, table, lens, window, n_sink, weight, pos, seen)
+        c.dev_starts = self._ints(starts, c.batch + 1, "starts")
+        c.n_tokens = (k if k is not None else q).shape[0]
+        pq, pk, pv, po = self._tensors(c, q, k, v, out, c.n_tokens)
+        self._launch("glide_paged_prefill", stream, self.lib.glide_paged_prefill, self._callp, pq, pk, pv, po, self._lse(lse, c.n_tokens))
+
+    def glide_paged_decode(self, table, lens, q, k, v, out, lse=None, window: int = -1, n_sink: int = 0, weight=None, pos=None,
+                           seen=None, layer: int = 0, stream=None) -> None:
+        """One new token per sequence: stored at slot lens[b] - 1 (k, v None: it is in the cache), attends; weight: the account."""
+        c = self._begin(layer, table, lens, window, n_sink, weight, pos, seen)
+        pq, pk, pv, po = self._tensors(c, q, k, v, out, c.batch)
+        self._launch("glide_paged_decode", stream, self.lib.glide_paged_decode, self._callp, pq, pk, pv, po, self._lse(lse, c.batch))
+
+    def glide_paged_weights(self, table, lens, starts, q, lse, weight, window: int = -1, n_sink: int = 0, layer: int = 0, stream=None) -> None:
+        """Adds the weights that the tokens q with the row sums lse (of glide_paged_prefill) give every slot to the account."""
+        c = self._begin(layer, table, lens, window, n_sink, weight, None, None)
+        c.dev_starts = self._ints(starts, c.batch + 1, "starts")
+        c.n_tokens = q.shape[0]
+        pq = self._tensors(c, q, None, None, None, c.n_tokens)[0]
+        self._launch("glide_paged_weights", stream, self.lib.glide_paged_weights, self._callp, pq, self._lse(lse, c.n_tokens))
+
+    def glide_paged_evict(self, table, lens, seen, weight, pos, budget: int, new_lens, recent: int = 0, n_sink: int = 0, weight_out=None,
+                          pos_out=None, layer: int = 0, stream=None) -> None:
+        """Every (sequence, KV head) keeps min(lens[b], budget) slots; weight_out, pos_out None: the account changes in place."""
+        c = self._begin(layer, table, lens, -1, n_sink, weight, pos, seen)
+        weight_out, pos_out = weight if weight_out is None else weight_out, pos if pos_out is None else pos_out
+        for t, like in ((weight_out, weight), (pos_out, pos)):
+            assert t.dtype is like.dtype and t.shape == like.shape and t.is_contiguous() and t.device == self.device
+        self._launch("glide_paged_evict", stream, self.lib.glide_paged_evict, self._callp, int(budget), int(recent), weight_out.data_ptr(),
+                     pos_out.data_ptr(), self._ints(new_lens, c.batch, "new_lens"))
+
+    def glide_paged_device_status(self) -> int:
+        """The status word of the device-side checks, read and cleared (0: nothing was recorded)."""
+        out = ctypes.c_int32(0)
+        with torch.cuda.device(self.device):
+            _check(self.lib.glide_paged_device_status(self._h, _stream(None), ctypes.byref(out)), "glide_paged_device_status")
+        return int(out.value)
+
+    def glide_paged_destroy(self) -> None:
+        if getattr(self, "_h", None):
+            self.lib.glide_paged_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.glide_paged_destroy()
+        except Exception:
+            pass
