@@ -93,75 +93,6 @@ __global__ void __launch_bounds__(kWarps * 32) paged_weights_row_kernel(const __
   }
 }
 
-// One block per (sequence, KV head): the new token is stored, the warps take the slots in turns and join.
-template <typename T, int D, int G>
-__global__ void __launch_bounds__(kWarps * 32) paged_decode_unit_kernel(const __grid_constant__ PagedParams p) {
-  constexpr int E = D / 32;
-  __shared__ float sm_m[kWarps][G], sm_l[kWarps][G], sm_acc[kWarps][G][D];
-  __shared__ float sm_lse[G];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;
-  const int len = paged_len(p, b), i = len - 1;
-  PagedRow<T, D, G> row;
-  row.load_q(p, size_t(b), g);
-  float *scores = p.weight ? p.logits + size_t(blockIdx.x) * size_t(p.most) * G : nullptr;
-  int first = 0, second = 0;
-  if (len > 0) {
-    if (p.new_k && warp == 0) {
-      const int page = paged_page(p, b, i);
-      const size_t to = paged_row(p, page, i, g) + lane * E, from = size_t(b) * size_t(p.kv_stride) + size_t(g) * D + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (page < 0) break;
-        reinterpret_cast<T *>(p.k)[to + e] = reinterpret_cast<const T *>(p.new_k)[from + e];
-        reinterpret_cast<T *>(p.v)[to + e] = reinterpret_cast<const T *>(p.new_v)[from + e];
-      }
-    }
-    __syncthreads();
-    paged_ranges(p, i, first, second);
-    for_slots(0, first, warp, kWarps, [&](int j) { row.slot(p, b, g, j, scores ? scores + size_t(j) * G : nullptr); });
-    for_slots(second, len, warp, kWarps, [&](int j) { row.slot(p, b, g, j, scores ? scores + size_t(j) * G : nullptr); });
-  }
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-    if (lane == 0) sm_m[warp][h] = row.m[h], sm_l[warp][h] = row.l[h];
-#pragma unroll
-    for (int e = 0; e < E; ++e) sm_acc[warp][h][lane * E + e] = row.acc[h][e];
-  }
-  __syncthreads();
-  if (warp == 0) {
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      float m = -CUDART_INF_F, l = 0.f;
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm_m[w][h]);
-      const float ref = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll
-      for (int e = 0; e < E; ++e) row.acc[h][e] = 0.f;
-      for (int w = 0; w < kWarps; ++w) {
-        const float c = exp2f(sm_m[w][h] - ref);
-        l = fmaf(sm_l[w][h], c, l);
-#pragma unroll
-        for (int e = 0; e < E; ++e) row.acc[h][e] = fmaf(sm_acc[w][h][lane * E + e], c, row.acc[h][e]);
-      }
-      row.m[h] = m, row.l[h] = l;
-      if (lane == 0) sm_lse[h] = ref + (l == 0.f ? 0.f : log2f(l));
-    }
-    row.store(p, size_t(b), g);
-  }
-  __syncthreads();
-  const size_t at = (size_t(b) * p.Hkv + g) * size_t(p.track_stride);
-  if (scores) {
-    for (int j = threadIdx.x; j < len; j += kWarps * 32) {
-      if (!paged_sees(p, i, j)) continue;
-      float sum = 0.f;   // (the step's weights first: the account is rounded once)
-#pragma unroll
-      for (int h = 0; h < G; ++h) sum += exp2f(scores[size_t(j) * G + h] - sm_lse[h]);
-      p.weight[at + j] = p.new_k && j == i ? sum : p.weight[at + j] + sum;
-    }
-    if (threadIdx.x == 0 && len > 0 && p.new_k && !paged_sees(p, i, i)) p.weight[at + i] = 0.f;
-  }
-  if (p.pos && threadIdx.x == 0 && len > 0 && p.new_k) p.pos[at + i] = p.seen[b] - 1;
-}
-
 unsigned blocks_of(int64_t items) { return unsigned((items + kWarps - 1) / kWarps); }
 int launched() {
   if (cudaGetLastError() == cudaSuccess) return GLIDE_OK;
@@ -169,9 +100,6 @@ int launched() {
 }
 
 }  // namespace
-
-size_t paged_record_bytes(const glide_paged_config &) { return 0; }
-int setup_paged_decode(const glide_paged *) { return GLIDE_OK; }
 
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
@@ -192,14 +120,6 @@ int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
     const dim3 grid(unsigned(std::min<int64_t>(blocks_of(p.most), 1024)), unsigned(p.batch * p.Hkv));
     paged_weights_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value><<<grid, kWarps * 32, 0, st>>>(p);
-    return launched();
-  });
-}
-
-int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
-  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
-    paged_decode_unit_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>
-        <<<unsigned(p.batch * p.Hkv), kWarps * 32, 0, st>>>(p);
     return launched();
   });
 }

@@ -48,6 +48,7 @@ struct PagedParams {
   int32_t *pos;
   int64_t track_stride;
   int32_t *status;
+  int32_t *tickets;                   // [max_batch * Hkv] records left for a unit so far; 0 between calls
   float *records;                     // partial records of units that several blocks share
   float *logits;                      // [batch][Hkv][most][G]: scores of a decode step whose weights are kept
   int32_t *moves;                     // (the same memory) evict: [batch][Hkv] counts, then [batch][Hkv][most / 2] pairs of slots

@@ -52,7 +52,7 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   h->group = G;
   h->page_shift = shift;
   h->layer_pages = layer_pages;
-  size_t at = kControlBytes;
+  size_t at = kControlBytes + up256(size_t(c.max_batch) * size_t(c.n_kv_heads) * sizeof(int32_t));   // (tickets behind the status word)
   h->off_records = at;
   at += up256(paged_record_bytes(c));
   h->off_track = at;   // a step's scores (H floats a slot), or an eviction's counts and moves (8 bytes for every second slot of a KV head)
@@ -125,6 +125,7 @@ int params_of(const glide_paged *h, const glide_paged_call *a, int need, PagedPa
   p.pos = a->dev_pos;
   p.track_stride = a->track_stride;
   p.status = reinterpret_cast<int32_t *>(h->ws);
+  p.tickets = reinterpret_cast<int32_t *>(h->ws + kControlBytes);
   p.records = reinterpret_cast<float *>(h->ws + h->off_records);
   p.logits = reinterpret_cast<float *>(h->ws + h->off_track);
   p.moves = reinterpret_cast<int32_t *>(h->ws + h->off_track);
@@ -179,7 +180,7 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
       h->maps = ok;
     }
   }
-  ok = ok && cudaMemsetAsync(h->ws, 0, kControlBytes, as_stream(stream)) == cudaSuccess;
+  ok = ok && setup_paged_decode(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
     delete h;
