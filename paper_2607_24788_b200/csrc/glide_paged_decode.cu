@@ -201,7 +201,7 @@ struct WarpUnit {
       for (int i = 0; i < 2; ++i) {
         float top = fmaxf(s[i], s[i + 2]);
 #pragma unroll
-        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
         top = fmaxf(top, m[i]);
         const float f = m[i] == -CUDART_INF_F ? 0.f : ex2(m[i] - top);
         m[i] = top;
@@ -237,6 +237,15 @@ struct WarpUnit {
       for (int w = 4; w < 32; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w), x[i] += __shfl_xor_sync(0xffffffffu, x[i], w);
       const int h = (lane & 3) * 2 + i;
       if (lane < 4 && h < G) sm.m[warp][h] = m[i], sm.l[warp][h] = l[i], sm.e[warp][h] = x[i];
+    }
+  }
+  // O times the factor of its head, which lane h holds
+  __device__ __forceinline__ void scale(float factor) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = __shfl_sync(0xffffffffu, factor, (threadIdx.x & 3) * 2 + i);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) o[k][i] *= f, o[k][i + 2] *= f;
     }
   }
   // f(head, column, value) for this thread's part of O
@@ -338,6 +347,14 @@ struct WarpUnit<float, D, G> {
       if ((threadIdx.x & 31) == 0) sm.m[warp][h] = m[h], sm.l[warp][h] = sm.e[warp][h] = l[h];
     }
   }
+  __device__ __forceinline__ void scale(float factor) {
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      const float f = __shfl_sync(0xffffffffu, factor, h);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[h][e] *= f;
+    }
+  }
   template <typename F>
   __device__ __forceinline__ void each(F &&f) {
     const int lane = threadIdx.x & 31;
@@ -350,6 +367,10 @@ struct WarpUnit<float, D, G> {
 
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
 // What tile i of a warp is; a lane holds it for every 32nd.
 struct TileInfo {
@@ -369,37 +390,46 @@ template <typename T, int D, int G>
 __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, int c0, int c1, int t0, int share, bool keep) {
   const int tid = threadIdx.x, lane = tid & 31;
   auto rec_of = [&](int c) { return record<D, G>(p, c, int64_t(c) * share >= t0 ? 0 : 1); };
+  constexpr int kEach = (G * D + kThreads - 1) / kThreads;   // outputs of a thread
+  constexpr int kBatch = 32 / kEach;                         // records whose values are on their way at a time
+  float M[kEach], L[kEach], X[kEach], sum[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) M[e] = -CUDART_INF_F, L[e] = X[e] = sum[e] = 0.f;
 #pragma unroll 1
-  for (int i = tid; i < G * D; i += kThreads) {
-    const int h = i / D;   // (the same in all lanes)
-    float M = -CUDART_INF_F, L = 0.f, X = 0.f, sum = 0.f;
-#pragma unroll 1
-    for (int c = c0; c <= c1; c += 32) {
-      const int some = min(32, c1 + 1 - c);
-      float m = -CUDART_INF_F, l = 0.f, x = 0.f;   // of record c + lane
-      if (lane < some) {
+  for (int c = c0; c <= c1; c += kBatch) {
+    const int some = min(kBatch, c1 + 1 - c);
+    float v[kEach][kBatch], m[kEach], l[kEach], x[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = tid + e * kThreads, h = i / D;   // (h is the same in all lanes)
+      m[e] = -CUDART_INF_F, l[e] = x[e] = 0.f;       // of record c + lane
+      if (lane < some && i < G * D) {
         const float *r = rec_of(c + lane) + G * D + h;
-        m = __ldcg(r), l = __ldcg(r + G), x = __ldcg(r + 2 * G);
+        m[e] = __ldcg(r), l[e] = __ldcg(r + G), x[e] = __ldcg(r + 2 * G);
       }
-      float part = 0.f;
-      const float top = warp_max(m), f = part_factor(m, top);
 #pragma unroll
-      for (int k0 = 0; k0 < 32; k0 += 16) {
-        float v[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = k0 + k < some ? __ldcg(rec_of(c + k0 + k) + i) : 0.f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) part = fmaf(v[k], __shfl_sync(0xffffffffu, f, k0 + k), part);
-      }
-      l = warp_sum(l * f), x = warp_sum(x * f);
-      const float now = fmaxf(M, top), fa = part_factor(M, now), fb = part_factor(top, now);
-      sum = sum * fa + part * fb, L = L * fa + l * fb, X = X * fa + x * fb, M = now;
+      for (int k = 0; k < kBatch; ++k) v[e][k] = k < some && i < G * D ? __ldcg(rec_of(c + k) + i) : 0.f;
     }
-    from_f32(reinterpret_cast<T *>(p.out) + size_t(b) * size_t(p.out_stride) + size_t(g) * G * D + i, L == 0.f ? 0.f : sum / L);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const float top = warp_max(m[e]), f = part_factor(m[e], top);
+      float part = 0.f;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) part = fmaf(v[e][k], __shfl_sync(0xffffffffu, f, k), part);
+      const float ls = warp_sum(l[e] * f), xs = warp_sum(x[e] * f);
+      const float now = fmaxf(M[e], top), fa = part_factor(M[e], now), fb = part_factor(top, now);
+      sum[e] = sum[e] * fa + part * fb, L[e] = L[e] * fa + ls * fb, X[e] = X[e] * fa + xs * fb, M[e] = now;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int i = tid + e * kThreads, h = i / D;
+    if (i >= G * D) continue;
+    from_f32(reinterpret_cast<T *>(p.out) + size_t(b) * size_t(p.out_stride) + size_t(g) * G * D + i, L[e] == 0.f ? 0.f : sum[e] / L[e]);
     if (i % D == 0) {
       const size_t row = size_t(b) * p.H + g * G + h;
-      if (p.lse) p.lse[row] = PagedRow<T, D, G>::paged_lse(M, X);
-      if (keep) unit_lse(p, D, row) = X == 0.f ? 0.f : M + log2f(X);
+      if (p.lse) p.lse[row] = PagedRow<T, D, G>::paged_lse(M[e], X[e]);
+      if (keep) unit_lse(p, D, row) = X[e] == 0.f ? 0.f : M[e] + log2f(X[e]);
     }
   }
 }
@@ -429,13 +459,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     const int page = paged_page(p, b, t.slot);
     if (page < 0) return t;
     t.at = int64_t(paged_row(p, page, t.slot, g));
-#pragma unroll
-    for (int r = 0; r < Sh::kTile; ++r)
-      t.rows |= uint32_t(t.slot + r < len && (t.slot + r >= st.vis_begin || t.slot + r < st.vis_end)) << r;
+    auto below = [](int n) { return n <= 0 ? 0u : n >= Sh::kTile ? (1u << Sh::kTile) - 1u : (1u << n) - 1u; };
+    t.rows = (below(len - t.slot) & ~below(st.vis_begin - t.slot)) | below(st.vis_end - t.slot);
     if (p.new_k && len - 1 - t.slot < Sh::kTile) t.rows |= kFresh | uint32_t(len - 1 - t.slot) << 16;
     return t;
   };
-  TileInfo now = look_up(lane), next = look_up(32 + lane);
+  TileInfo now = look_up(lane), next;
+  if (mine > 32) next = look_up(32 + lane);
   uint32_t rows[S];   // of the tiles under way, the oldest first
   int slots[S];
   auto ask = [&](int i) {   // ask for this warp's tile i
@@ -453,18 +483,29 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       const T *k = reinterpret_cast<const T *>(p.k) + at + c * (16 / int(sizeof(T)));
       const int64_t to_v = reinterpret_cast<const T *>(p.v) - reinterpret_cast<const T *>(p.k);
       const uint32_t dst = smem_u32(sm.ring[warp][i % S]);
+      if (mask == (1u << Sh::kTile) - 1u) {   // a whole tile of the pages
+        const T *ks = k + int64_t(r0) * p.row_stride;
+        const int64_t step = int64_t(kAtOnce) * p.row_stride;
 #pragma unroll
-      for (int r = 0; r < Sh::kTile; r += kAtOnce) {
-        const int row = r + r0;
-        const bool seen = (mask >> row) & 1u;
-        const T *ks = seen ? k + int64_t(row) * p.row_stride : reinterpret_cast<const T *>(p.k), *vs = ks + to_v;
-        if ((mask & kFresh) && row == int((mask >> 16) & 15u)) {
-          const int b = unit / p.Hkv;
-          const int64_t from = int64_t(b) * p.kv_stride + (unit - b * p.Hkv) * D + c * (16 / int(sizeof(T)));
-          ks = reinterpret_cast<const T *>(p.new_k) + from, vs = reinterpret_cast<const T *>(p.new_v) + from;
+        for (int r = 0; r < Sh::kTile; r += kAtOnce) {
+          cp_async16(dst + Sh::at(r + r0, c), ks);
+          cp_async16(dst + Sh::kTile * Sh::kRowBytes + Sh::at(r + r0, c), ks + to_v);
+          ks += step;
         }
-        cp_async16(dst + Sh::at(row, c), ks, seen);
-        cp_async16(dst + Sh::kTile * Sh::kRowBytes + Sh::at(row, c), vs, seen);
+      } else {
+#pragma unroll 1
+        for (int r = 0; r < Sh::kTile; r += kAtOnce) {
+          const int row = r + r0;
+          const bool seen = (mask >> row) & 1u;
+          const T *ks = seen ? k + int64_t(row) * p.row_stride : reinterpret_cast<const T *>(p.k), *vs = ks + to_v;
+          if ((mask & kFresh) && row == int((mask >> 16) & 15u)) {
+            const int b = unit / p.Hkv;
+            const int64_t from = int64_t(b) * p.kv_stride + (unit - b * p.Hkv) * D + c * (16 / int(sizeof(T)));
+            ks = reinterpret_cast<const T *>(p.new_k) + from, vs = reinterpret_cast<const T *>(p.new_v) + from;
+          }
+          cp_async16(dst + Sh::at(row, c), ks, seen);
+          cp_async16(dst + Sh::kTile * Sh::kRowBytes + Sh::at(row, c), vs, seen);
+        }
       }
     }
     cp_async_commit();
@@ -525,18 +566,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       }
       factor = part_factor(sm.m[warp][lane], M);
     }
-    float fh[G];
-#pragma unroll
-    for (int h = 0; h < G; ++h) fh[h] = __shfl_sync(0xffffffffu, factor, h);
-    auto factor_of = [&](int h) {
-      float f = fh[0];
-#pragma unroll
-      for (int i = 1; i < G; ++i) f = h == i ? fh[i] : f;
-      return f;
-    };
-    if (warp >= kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - kSlots][h][c] = x * factor_of(h); });
+    unit.scale(factor);
+    if (warp >= kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - kSlots][h][c] = x; });
     __syncthreads();
-    if (warp < kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][c] = fmaf(x, factor_of(h), sm.o[warp][h][c]); });
+    if (warp < kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][c] += x; });
     __syncthreads();
     const bool whole = at == t0 && end == t0 + n;
     const int which = at == lo ? 0 : 1;
