@@ -55,12 +55,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_prefill_row_kernel(const __
   int b, i;
   if (r >= p.n_tokens || !row_of(p, r, b, i)) return;
   PagedRow<T, D, G> row;
-  row.load_q(p, size_t(r), g);
-  int first, second;
-  paged_ranges(p, i, first, second);
-  for_slots(0, first, 0, 1, [&](int j) { row.slot(p, b, g, j, nullptr); });
-  for_slots(second, i + 1, 0, 1, [&](int j) { row.slot(p, b, g, j, nullptr); });
-  row.store(p, size_t(r), g);
+  row.attend(p, size_t(r), b, i, g, g * G, p.lse != nullptr);
 }
 
 // One warp per (sequence, KV head, slot): the weights of all queries that see the slot.
@@ -109,6 +104,7 @@ int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t 
 }
 
 int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  if (h->cfg.io_dtype == GLIDE_BF16) return launch_paged_prefill_tc(h, p, st);
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
     paged_prefill_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>
         <<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);

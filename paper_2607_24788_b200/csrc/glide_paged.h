@@ -5,6 +5,10 @@
 
 #include "glide_internal.h"
 
+typedef CUresult (*TensorMapEncoder)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                     const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                     CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct glide_paged {
   glide_paged_config cfg;
   int device = 0;
@@ -15,9 +19,10 @@ struct glide_paged {
   unsigned char *ws = nullptr;
   unsigned char *k = nullptr, *v = nullptr;
   size_t off_records = 0, off_track = 0, total = 0;   // byte offsets in the workspace
-  CUtensorMap k16, v16;             // pages as {64 columns, halves, slots, KV heads, pages}: boxes of 16 slots x all columns
-  CUtensorMap kpage, vpage;         // boxes of min(page_size, 128) slots x 64 columns
-  bool maps = false;                // bf16 only
+  CUtensorMap kpage, vpage;         // bf16: pages as {64 columns, halves of a row, slots, KV heads, pages}, boxes of min(page_size, 128)
+                                    // slots x 64 columns
+  int32_t map_pages = 0;            // pages in the maps: of all layers
+  void *encode = nullptr;           // cuTensorMapEncodeTiled
 };
 
 namespace glide {
@@ -101,5 +106,7 @@ int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, i
                        int32_t *new_lens, cudaStream_t st);
 size_t paged_record_bytes(const glide_paged_config &cfg);
 int setup_paged_decode(const glide_paged *h);
+int setup_paged_tc(const glide_paged *h);
+int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 
 }  // namespace glide

@@ -52,6 +52,7 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   h->group = G;
   h->page_shift = shift;
   h->layer_pages = layer_pages;
+  h->map_pages = int32_t(layer_pages * (c.n_layers - 1) + c.n_pages);
   size_t at = kControlBytes + up256(size_t(c.max_batch) * size_t(c.n_kv_heads) * sizeof(int32_t));   // (tickets behind the status word)
   h->off_records = at;
   at += up256(paged_record_bytes(c));
@@ -62,17 +63,13 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   return GLIDE_OK;
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // The pages as a tensor {64 columns, halves of a row, slots, KV heads, pages}.
-bool encode_pages(EncodeFn fn, CUtensorMap *map, const glide_paged *h, void *base, unsigned halves, unsigned rows) {
+bool encode_pages(TensorMapEncoder fn, CUtensorMap *map, const glide_paged *h, void *base) {
   const glide_paged_config &c = h->cfg;
   const cuuint64_t dims[5] = {64, cuuint64_t(c.head_dim / 64), cuuint64_t(c.page_size), cuuint64_t(c.n_kv_heads),
-                              cuuint64_t(h->layer_pages * (c.n_layers - 1) + c.n_pages)};
+                              cuuint64_t(h->map_pages)};
   const cuuint64_t strides[4] = {128, cuuint64_t(c.row_stride) * 2, cuuint64_t(c.head_stride) * 2, cuuint64_t(c.page_stride) * 2};
-  const cuuint32_t box[5] = {64, halves, rows, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+  const cuuint32_t box[5] = {64, 1, cuuint32_t(std::min(c.page_size, 128)), 1, 1}, ones[5] = {1, 1, 1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -173,11 +170,9 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
     ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) == cudaSuccess && f &&
          found == cudaDriverEntryPointSuccess;
     if (ok) {
-      const EncodeFn fn = reinterpret_cast<EncodeFn>(f);
-      const unsigned halves = unsigned(h->cfg.head_dim / 64), rows = unsigned(std::min(h->cfg.page_size, 128));
-      ok = encode_pages(fn, &h->k16, h, h->k, halves, kPagedTile) && encode_pages(fn, &h->v16, h, h->v, halves, kPagedTile) &&
-           encode_pages(fn, &h->kpage, h, h->k, 1, rows) && encode_pages(fn, &h->vpage, h, h->v, 1, rows);
-      h->maps = ok;
+      h->encode = f;
+      const auto fn = reinterpret_cast<TensorMapEncoder>(f);
+      ok = encode_pages(fn, &h->kpage, h, h->k) && encode_pages(fn, &h->vpage, h, h->v) && setup_paged_tc(h) == GLIDE_OK;
     }
   }
   ok = ok && setup_paged_decode(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;

@@ -6,32 +6,28 @@
 
 namespace glide {
 
-// f(slot) for the slots of [begin, end) that this warp of `warps` takes
-template <typename F>
-__device__ __forceinline__ void for_slots(int begin, int end, int warp, int warps, F &&f) {
-  for (int j = begin + warp; j < end; j += warps) f(j);
-}
 // The slots that query slot i sees are [0, first) and [second, i]
 __device__ __forceinline__ void paged_ranges(const PagedParams &p, int i, int &first, int &second) {
   second = p.window < 0 ? 0 : max(0, i - p.window + 1);
   first = min(min(p.n_sink, second), i + 1);
 }
 
+// G query heads from head0 on, which read KV head g
 template <typename T, int D, int G>
 struct PagedRow {
   static constexpr int E = D / 32;
   float q[G][E], m[G], l[G], acc[G][E];
-  __device__ __forceinline__ void load_q(const PagedParams &p, size_t row, int g) {
+  __device__ __forceinline__ void load_q(const PagedParams &p, size_t row, int head0) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int h = 0; h < G; ++h) {
-      load_elems<T, E>(reinterpret_cast<const T *>(p.q) + row * size_t(p.q_stride) + size_t(g * G + h) * D + lane * E, q[h]);
+      load_elems<T, E>(reinterpret_cast<const T *>(p.q) + row * size_t(p.q_stride) + size_t(head0 + h) * D + lane * E, q[h]);
 #pragma unroll
       for (int e = 0; e < E; ++e) q[h][e] *= p.scale_log2, acc[h][e] = 0.f;
       m[h] = -CUDART_INF_F, l[h] = 0.f;
     }
   }
-  __device__ __forceinline__ void slot(const PagedParams &p, int b, int g, int j, float *scores) {
+  __device__ __forceinline__ void slot(const PagedParams &p, int b, int g, int j) {
     const int lane = threadIdx.x & 31;
     const size_t at = paged_row(p, paged_page(p, b, j), j, g) + lane * E;
     float k[E], v[E];
@@ -43,7 +39,6 @@ struct PagedRow {
 #pragma unroll
       for (int e = 0; e < E; ++e) part = fmaf(q[h][e], k[e], part);
       const float s = warp_sum(part);
-      if (scores && lane == 0) scores[h] = s;
       const float mn = fmaxf(m[h], s), ref = mn == -CUDART_INF_F ? 0.f : mn;
       const float c = exp2f(m[h] - ref), w = exp2f(s - ref);
       l[h] = fmaf(l[h], c, w);
@@ -52,16 +47,25 @@ struct PagedRow {
       m[h] = mn;
     }
   }
-  __device__ __forceinline__ void store(const PagedParams &p, size_t row, int g) {
+  __device__ __forceinline__ void store(const PagedParams &p, size_t row, int head0, bool with_lse) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int h = 0; h < G; ++h) {
       const float inv = l[h] == 0.f ? 0.f : 1.0f / l[h];
-      T *o = reinterpret_cast<T *>(p.out) + row * size_t(p.out_stride) + size_t(g * G + h) * D + lane * E;
+      T *o = reinterpret_cast<T *>(p.out) + row * size_t(p.out_stride) + size_t(head0 + h) * D + lane * E;
 #pragma unroll
       for (int e = 0; e < E; ++e) from_f32(o + e, l[h] == 0.f ? 0.f : acc[h][e] * inv);
-      if (p.lse && lane == 0) p.lse[row * size_t(p.H) + g * G + h] = paged_lse(m[h], l[h]);
+      if (with_lse && lane == 0) p.lse[row * size_t(p.H) + head0 + h] = paged_lse(m[h], l[h]);
     }
+  }
+  // all of it: the call's row `row`, slot i of sequence b
+  __device__ __forceinline__ void attend(const PagedParams &p, size_t row, int b, int i, int g, int head0, bool with_lse) {
+    load_q(p, row, head0);
+    int first, second;
+    paged_ranges(p, i, first, second);
+    for (int j = 0; j < first; ++j) slot(p, b, g, j);
+    for (int j = second; j <= i; ++j) slot(p, b, g, j);
+    store(p, row, head0, with_lse);
   }
   // natural logarithm of a row sum l taken against 2^m
   static __device__ __forceinline__ float paged_lse(float m, float l) {

@@ -1,0 +1,615 @@
+// Paged attention of prompts on the 5th-generation tensor cores (tcgen05 + TMEM + TMA), bf16.
+//
+// One CTA (19 warps) owns 256 query rows of one (sequence, KV head): two row tiles X = A, B of 128 rows, a row being (new token, query
+// head of the group), row = token * G + head.
+//   warps 0-3, 8-11    softmax of tile A: two threads per row (TMEM lane), 64 columns each
+//   warps 4-7, 12-15   softmax of tile B
+//   warps 16, 17       issue the tcgen05.mma of A and of B (one elected lane), in turns
+//   warp 18            finds the CTA's rows, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
+// Keys come in tiles of 128 slots (multiples of 128): those that hold a visible first token, then those of the window.  Per tile and
+// row tile S = Q K^T into TMEM, the weights P = 2^(s - m) as bf16 over the consumed S columns against a reference m that moves (and O
+// with it) only when the row's maximum grows by more than 2^8, O += P V with V as the MN-major B operand.
+// TMEM columns: S_A [0,128) S_B [128,256) O_A [256,256+d) O_B behind it.
+// Nothing that a row does not see reaches it: scores are selected, not added to; slots behind the CTA's last token are zeros in V's
+// buffer; and a row whose output is not finite all the same (0 times an infinity or a NaN of a masked slot before them) is computed
+// once more by itself, from the slots that it sees.
+// Every mbarrier wait is bounded; on a time-out the CTA records kDevWaitTimeout, leaves its loops, frees its TMEM columns and returns.
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+#include "glide_paged_rows.cuh"
+#include "glide_tc.cuh"
+
+namespace glide {
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kRows = 128;            // rows per row tile
+constexpr int kKT = 128;              // slots per key tile
+constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
+constexpr int kSoftmaxThreads = 512;
+constexpr int kThreads = 608;
+constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
+constexpr float kLazy = 8.0f;
+constexpr int kMostSlots = 1 << 30;
+
+struct PagedMaps {
+  CUtensorMap k, v, q;   // q: {d, H, tokens}, boxes of 64 columns x the G heads of a group x 128 / G tokens
+};
+
+template <int D>
+struct PrefillSmem {
+  static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
+  unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
+  uint64_t bar_full[kStages];            // the buffer's K or V tile has landed
+  uint64_t bar_free[kStages];            // the MMAs that read the buffer have completed (one arrival per row tile)
+  uint64_t bar_q[2];                     // Q_X staged
+  uint64_t bar_s[2];                     // MMA -> softmax threads of X: the products issued for X so far have completed
+  uint64_t bar_p[2];                     // softmax threads of X -> MMA: P is ready (one arrival per warp)
+  uint64_t bar_turn[2];                  // the other row tile's batch of products has been issued
+  uint64_t bar_tail;                     // V of the last tile has landed (its last rows are zeroed behind that)
+  uint32_t tmem_base;
+  int failed;
+  int seq, tok0;                         // the CTA's sequence and first new token; seq < 0: no work
+  float exch[kSoftmaxThreads / 2];       // a value of each row on its way between the row's two threads
+};
+
+// byte offset of 16-byte chunk c16 of row `row` in a tile with 128-byte swizzle
+__device__ __forceinline__ uint32_t sw128(int row, int c16) {
+  return uint32_t((c16 >> 3) * kBoxBytes + row * 128 + (((c16 & 7) ^ (row & 7)) << 4));
+}
+// instruction descriptor: fp32 accumulate, bf16 A and B, M = 128; b_mn: B is MN-major
+__device__ __forceinline__ uint32_t make_idesc(int n, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? (1u << 16) : 0u) | (uint32_t(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// S = A B^T, 128 x 128 x D, both K-major tiles; called by the whole warp with uniform operands, one lane issues
+template <int D>
+__device__ __forceinline__ void issue_scores(bool leader, uint32_t tmem_d, uint32_t a_tile, uint32_t b_tile) {
+  const uint32_t idesc = make_idesc(128, false), a0 = desc_lo(a_tile, 16), b0 = desc_lo(b_tile, 16);
+  if (leader) {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const uint32_t step = uint32_t(((ks >> 2) * kBoxBytes + (ks & 3) * 32) >> 4);
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+          "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(tmem_d),
+          "r"(a0 + step), "r"(b0 + step), "r"(idesc), "r"(ks > 0 ? 1u : 0u), "r"(kDescHi)
+          : "memory");
+    }
+  }
+}
+// O (+)= P V, 128 x D x 128: P in TMEM (32-bit column c = elements 2c, 2c + 1; elements 64 .. from column 64 on), V MN-major
+template <int D>
+__device__ __forceinline__ void issue_values(bool leader, uint32_t tmem_d, uint32_t tmem_a, uint32_t b_tile, bool accumulate) {
+  const uint32_t idesc = make_idesc(D, true), b0 = desc_lo(b_tile, kBoxBytes);
+  if (leader) {
+#pragma unroll
+    for (int ks = 0; ks < kKT / 16; ++ks)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+          "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(tmem_d),
+          "r"(tmem_a + (ks >> 2) * 64 + (ks & 3) * 8), "r"(b0 + uint32_t(ks * 2048 >> 4)), "r"(idesc), "r"((accumulate || ks > 0) ? 1u : 0u),
+          "r"(kDescHi)
+          : "memory");
+  }
+}
+
+// The key tiles of 128 slots that queries of slots [q0, q1] see: [0, sinks) and [first, end)
+struct KeyTiles {
+  int sinks, first, n;
+  __device__ __forceinline__ int slot(int k) const { return (k < sinks ? k : first + k - sinks) * kKT; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const PagedParams &p, int q0, int q1) {
+  KeyTiles t{0, 0, 0};
+  const int end = q1 / kKT + 1;
+  if (p.window != 0) t.first = p.window < 0 ? 0 : max(0, q0 - p.window + 1) / kKT;
+  else t.first = end;
+  t.sinks = (min(p.n_sink, q1 + 1) + kKT - 1) / kKT;
+  if (t.sinks >= t.first) t.sinks = 0, t.first = t.first == end && p.n_sink == 0 ? end : 0;
+  t.n = t.sinks + end - t.first;
+  return t;
+}
+// Whether some query of slots [q0, q1] sees a slot of the tile that starts at j0
+__device__ __forceinline__ bool tile_seen(const PagedParams &p, int q0, int q1, int j0) {
+  if (j0 > q1) return false;
+  return p.window < 0 || (p.window > 0 && j0 + kKT - 1 > q0 - p.window) || j0 < p.n_sink;
+}
+// Lane i of a warp: page number of piece i of a key tile, one past the last page (zeros) where nothing of the piece is seen
+__device__ __forceinline__ int piece_page(const PagedParams &p, int b, int q0, int q1, int j0, int pieces, int rows, int none) {
+  const int lane = threadIdx.x & 31, s = j0 + lane * rows;
+  if (lane >= pieces || s > q1) return none;
+  if (p.window >= 0 && s >= p.n_sink && (p.window == 0 || s + rows - 1 <= q0 - p.window)) return none;
+  const int page = paged_page(p, b, s);
+  return page < 0 ? none : p.page0 + page;
+}
+// The tile of K or V: lane i asks for piece i, a box per 64 columns
+template <int D>
+__device__ __forceinline__ void load_tile(const CUtensorMap *map, const PagedParams &p, uint32_t dst, int page, int j0, int g, int pieces, int rows,
+                                          uint32_t bar) {
+  const int lane = threadIdx.x & 31;
+  if (lane < pieces) {
+    const int off = (j0 + lane * rows) & ((1 << p.page_shift) - 1);
+#pragma unroll
+    for (int hf = 0; hf < D / 64; ++hf) tma_load_5d(dst + hf * kBoxBytes + lane * rows * 128, map, 0, hf, off, g, page, bar);
+  }
+}
+
+template <int D, int G, bool LSE>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none) {
+  using Sm = PrefillSmem<D>;
+  constexpr int TOKT = kRows / G, TOKC = 2 * TOKT, S = Sm::kStages, kHalf = D / 2;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int *failed = &sm.failed;
+  const int g = int(blockIdx.x % unsigned(p.Hkv));
+  const bool aligned = (smem_u32(smem_raw) & 1023u) == 0;   // (the swizzled tiles have to start on a multiple of 1024)
+  if (warp == kLoadWarp) {
+    // the CTA's rows: tiles of TOKC new tokens, counted through the sequences; the last ones, whose windows are the longest, first
+    int want = int(gridDim.x / unsigned(p.Hkv)) - 1 - int(blockIdx.x / unsigned(p.Hkv));
+    int seq = -1, tok0 = 0;
+    for (int b0 = 0; b0 < p.batch && seq < 0; b0 += 32) {
+      const int b = b0 + lane;
+      int row0, n = 0;
+      if (b < p.batch) n = paged_new(p, b, paged_len(p, b), row0);
+      const int tiles = (n + TOKC - 1) / TOKC;
+      int inc = tiles;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      const unsigned here = __ballot_sync(0xffffffffu, want < inc);
+      if (here) {
+        const int l = __ffs(int(here)) - 1;
+        seq = b0 + l;
+        tok0 = (want - __shfl_sync(0xffffffffu, inc - tiles, l)) * TOKC;
+      } else {
+        want -= __shfl_sync(0xffffffffu, inc, 31);
+      }
+    }
+    if (lane == 0) sm.seq = seq, sm.tok0 = tok0;
+  } else if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem_base;
+  const int b = sm.seq, tok0 = sm.tok0;
+  if (b < 0) {
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    return;
+  }
+  int row0;
+  const int len = paged_len(p, b), n_new = paged_new(p, b, len, row0);
+  const int ntok = min(TOKC, n_new - tok0), ntokA = min(TOKT, ntok), ntokB = ntok - ntokA;
+  const bool hasB = ntokB > 0;
+  const int tq0 = len - n_new + tok0, tq_last = tq0 + ntok - 1;   // slots of the CTA's queries
+  const KeyTiles kt = key_tiles(p, tq0, tq_last);
+  const int n_tiles = kt.n;
+  if (tid == 0) {
+    const int n_rows = hasB ? 2 : 1;
+    for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), 1), mbar_init(smem_u32(&sm.bar_free[s]), n_rows);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(smem_u32(&sm.bar_q[x]), 1);
+      mbar_init(smem_u32(&sm.bar_s[x]), 1);
+      mbar_init(smem_u32(&sm.bar_turn[x]), 1);
+      mbar_init(smem_u32(&sm.bar_p[x]), kSoftmaxThreads / 32 / 2);
+    }
+    mbar_init(smem_u32(&sm.bar_tail), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sm.failed = aligned ? 0 : 1;
+  }
+  __syncthreads();
+  const uint32_t sQ0 = smem_u32(sm.q[0]), sKV0 = smem_u32(sm.kv[0]);
+  auto q_addr = [&](int x) { return sQ0 + uint32_t(x) * Sm::kTileBytes; };
+  auto kv_addr = [&](int slot) { return sKV0 + uint32_t(slot) * Sm::kTileBytes; };
+  // slots of row tile x's queries; whether it has key tile k
+  auto x_q0 = [&](int x) { return tq0 + x * TOKT; };
+  auto x_q1 = [&](int x) { return tq0 + x * TOKT + (x ? ntokB : ntokA) - 1; };
+  auto has = [&](int x, int k) { return k >= 0 && k < n_tiles && tile_seen(p, x_q0(x), x_q1(x), kt.slot(k)); };
+  auto last_of = [&](int x) {   // its last key tile; -1: none
+    int k = n_tiles - 1;
+    while (k >= 0 && !has(x, k)) --k;
+    return k;
+  };
+
+  if (!aligned) {
+    // (nothing is in flight; the status word tells)
+  } else if (tid < kSoftmaxThreads) {
+    // =========================== softmax threads: half a row each ===========================
+    // What the row's two threads have in common goes through sm.exch behind barriers of the two warps, which every thread of a pair
+    // passes equally often: after a time-out the waits return at once and the loops run on, storing nothing.
+    const int X = (warp >> 2) & 1, H = warp >> 3, row = tid & 127;
+    const int ntokX = X ? ntokB : ntokA;
+    const int tok_r = row / G;
+    const int mine = x_q0(X) + tok_r;               // this row's slot
+    const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + uint32_t(X) * 128u + uint32_t(H) * 64u;
+    const uint32_t tO = tmem + (uint32_t((warp & 3) * 32) << 16) + 256u + uint32_t(X) * D + uint32_t(H) * kHalf;
+    float m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f;   // of this thread's columns: weights as O has them; exact ones
+    uint32_t n_s = 0;                               // batches of products waited for
+    bool ok = true;
+    auto wait_s = [&]() {
+      if (ok) ok = mbar_wait(smem_u32(&sm.bar_s[X]), n_s & 1u, failed);
+      ++n_s;
+      tc_fence_after();
+      ok = __all_sync(0xffffffffu, ok);             // warp-uniform
+    };
+    auto hand_over = [&]() {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.bar_p[X]));
+    };
+    const int pair_bar = 1 + (warp & 7);            // named barrier of warps w and w + 8
+    auto pair_sync = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair_bar) : "memory"); };
+    auto pair_any = [&](bool x) {
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, %2, 64, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(r)
+          : "r"(uint32_t(x)), "r"(pair_bar)
+          : "memory");
+      return r != 0;
+    };
+    auto combine = [&](float v, auto &&f) {         // f(first thread's value, second thread's value) in both threads of a row
+      float *slot = &sm.exch[tid & (kSoftmaxThreads / 2 - 1)];
+      if (H == 0) *slot = v;
+      pair_sync();
+      if (H == 1) *slot = v = f(*slot, v);
+      pair_sync();
+      return H == 0 ? *slot : v;
+    };
+    auto row_sum_of = [&](float v) { return combine(v, [](float a, float c) { return a + c; }); };
+    auto row_max_of = [&](float v) { return combine(v, [](float a, float c) { return fmaxf(a, c); }); };
+    auto scale_o = [&](float f) {
+#pragma unroll 1
+      for (int c0 = 0; c0 < kHalf; c0 += 32) {
+        uint32_t r[32];
+        tmem_ld32(tO + c0, r);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+        tmem_st32(tO + c0, r);
+      }
+    };
+    // the lazy reference for a tile whose largest score over this thread's columns is mx; returns what the weights are taken against
+    auto move_ref = [&](float mx, bool first) {
+      auto grows = [&]() {
+        const float ms = mx * p.scale_log2;
+        return ms > m_ref + kLazy || (m_ref == -CUDART_INF_F && ms > -CUDART_INF_F);
+      };
+      if (pair_any(grows())) {
+        mx = row_max_of(mx);
+        float f = 1.f;
+        if (grows()) {
+          mx *= p.scale_log2;
+          f = m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
+          m_ref = mx;
+        }
+        if (!first && __any_sync(0xffffffffu, f != 1.f)) scale_o(f);
+        l_sum *= f, x_sum *= f;
+      }
+      return m_ref == -CUDART_INF_F ? 0.f : m_ref;
+    };
+    struct Bounds {
+      int lo, hi, sink;   // of this thread's 64 columns, those lo .. hi and 0 .. sink are seen
+    };
+    auto seen_of = [](const Bounds &v, int c) { return column_mask(c, v.lo, v.hi) | column_mask(c, -1, v.sink); };
+    // A later key tile against the reference as it is, in one pass; the largest weight says afterwards whether that was right.
+    // Otherwise (false, to both threads of all rows of the pair) nothing has happened and the tile goes through soft_tile_masked.
+    auto soft_tile = [&](auto masked, const Bounds &v) {
+      float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
+      const float mr = m_ref;
+      uint32_t pk[32], mx2 = 0u;
+#pragma unroll
+      for (int c = 0; c < 64; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(tS + c, x);
+        if (decltype(masked)::value) {
+          const uint32_t m = seen_of(v, c);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = (m >> i) & 1u ? x[i] : 0xff800000u;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a0, a1;
+          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
+          a0 = ex2(a0), a1 = ex2(a1);
+          if (LSE) add2(ex0, ex1, a0, a1);
+          const uint32_t w2 = pack_bf16x2(a0, a1);
+          mx2 = max_bf16x2(mx2, w2);
+          add2(sum0, sum1, bf16_lo(w2), bf16_hi(w2));   // the sum uses the weights as the tensor core sees them
+          pk[(c >> 1) + e] = w2;
+        }
+      }
+      const float mx = fmaxf(bf16_lo(mx2), bf16_hi(mx2));
+      if (pair_any(!(mx < 0x1p8f))) return false;
+      tmem_st32(tS, pk);
+      l_sum += sum0 + sum1;
+      if (LSE) x_sum += ex0 + ex1;
+      return true;
+    };
+    // ... against a reference that moves first; for rows that have none yet, and tiles that soft_tile leaves alone
+    auto soft_tile_masked = [&](const Bounds &v, bool first) {
+      float mx = -CUDART_INF_F, sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < 64; c += 32) {
+        const uint32_t m = seen_of(v, c);
+        if (!__any_sync(0xffffffffu, m)) continue;
+        uint32_t x[32];
+        tmem_ld32(tS + c, x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = (m >> i) & 1u ? x[i] : 0xff800000u;
+        float m4[4] = {mx, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+        mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
+      }
+      const float mr = move_ref(mx, first);
+#pragma unroll 1
+      for (int c = 0; c < 64; c += 32) {
+        const uint32_t m = seen_of(v, c);
+        uint32_t x[32], pk[16];
+        if (!__any_sync(0xffffffffu, m)) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) pk[e] = 0u;
+          tmem_st16(tS + (c >> 1), pk);
+          continue;
+        }
+        tmem_ld32(tS + c, x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = (m >> i) & 1u ? x[i] : 0xff800000u;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a0, a1;
+          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
+          a0 = ex2(a0), a1 = ex2(a1);
+          if (LSE) add2(ex0, ex1, a0, a1);
+          pk[e] = pack_bf16x2(a0, a1);
+          add2(sum0, sum1, bf16_lo(pk[e]), bf16_hi(pk[e]));
+        }
+        tmem_st16(tS + (c >> 1), pk);
+      }
+      tmem_wait_st();
+      l_sum += sum0 + sum1;
+      if (LSE) x_sum += ex0 + ex1;
+    };
+    if (ntokX > 0) {
+      const int w = p.window < 0 ? kMostSlots : p.window;
+      int before = -1;                              // the key tile that this row tile had before
+      for (int k = 0; k < n_tiles; ++k) {
+        if (!has(X, k)) continue;
+        wait_s();
+        if (tid == X * kRows) {                     // S of the tile and P V of the tile before have completed
+          mbar_arrive(smem_u32(&sm.bar_free[2 * k % S]));
+          if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(2 * before + 1) % S]));
+        }
+        const int j0 = kt.slot(k);
+        const bool whole = j0 + kKT - 1 <= x_q0(X) && (j0 > x_q1(X) - w || j0 + kKT <= p.n_sink);
+        const int c0 = j0 + H * 64;
+        const Bounds v{mine - w + 1 - c0, mine - c0, min(p.n_sink - 1, mine) - c0};
+        bool done = false;
+        // (what is asked here is the same in both warps of a pair: their threads share the rows)
+        if (before >= 0 && !__any_sync(0xffffffffu, m_ref == -CUDART_INF_F)) {
+          if (whole) done = soft_tile(std::false_type{}, v);
+          else done = soft_tile(std::true_type{}, v);
+        }
+        if (!done) soft_tile_masked(v, before < 0);
+        hand_over();                                // this thread's TMEM accesses precede the MMAs that read P and overwrite S
+        before = k;
+      }
+      const float l_row = row_sum_of(l_sum);
+      const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
+      if (before >= 0) wait_s();                    // every product of X has completed
+      const bool live = tok_r < ntokX;
+      const float inv = live && before >= 0 && l_row != 0.f ? 1.0f / l_row : 0.f;
+      float chk0 = 0.f, chk1 = 0.f;                 // finite if all values of the row are
+#pragma unroll 1
+      for (int c0 = 0; c0 < kHalf; c0 += 32) {
+        uint32_t r[32];
+        if (before >= 0) {
+          tmem_ld32(tO + c0, r);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) add2(chk0, chk1, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          uint32_t pk[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            pk[e] = pack_bf16x2(__uint_as_float(r[q4 * 8 + e * 2]) * inv, __uint_as_float(r[q4 * 8 + e * 2 + 1]) * inv);
+          *reinterpret_cast<uint4 *>(sm.q[X] + sw128(row, H * (kHalf / 8) + (c0 >> 3) + q4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        }
+      }
+      // a warp stores the 32 half rows that its own threads have written, some lanes to each
+      __syncwarp();
+      constexpr int kLanes = kHalf / 8, kAtOnce = 32 / kLanes;   // lanes of a half row; half rows at once
+      const int c = H * kLanes + lane % kLanes, r0 = (row & ~31) + lane / kLanes;
+      bf16 *obase = reinterpret_cast<bf16 *>(p.out) + size_t(row0 + tok0 + X * TOKT) * size_t(p.out_stride) + size_t(g * G) * D + c * 8;
+#pragma unroll 4
+      for (int i = 0; i < 32 / kAtOnce; ++i) {
+        const int rr = r0 + kAtOnce * i, tk = rr / G;
+        const uint4 val = *reinterpret_cast<const uint4 *>(sm.q[X] + sw128(rr, c));
+        if (ok && tk < ntokX) *reinterpret_cast<uint4 *>(obase + size_t(tk) * size_t(p.out_stride) + (rr - tk * G) * D) = val;
+      }
+      const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
+      if (LSE && H == 0 && live && ok) p.lse[out_row * p.H + g * G + row % G] = PagedRow<bf16, D, 1>::paged_lse(m_ref, x_row);
+      // rows of which either half is not finite, by the first warp of the pair when both have stored
+      const bool bad = live && (!isfinite((chk0 + chk1) * inv) || !isfinite(inv));
+      unsigned again = __ballot_sync(0xffffffffu, row_sum_of(bad ? 1.f : 0.f) > 0.f);
+      if (H == 0 && ok) {
+        for (; again; again &= again - 1) {
+          const int rr = (row & ~31) + __ffs(int(again)) - 1;
+          PagedRow<bf16, D, 1> one;
+          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, false);   // (the sums of the scores were right)
+        }
+      }
+    }
+  } else if (warp < kLoadWarp) {
+    // =========================== MMA warps ===========================
+    // A warp stays together (every wait ends in a vote), one elected lane issues.
+    const bool leader = elect_one();
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const int x = __shfl_sync(0xffffffffu, warp, 0) - kMmaWarp;   // the row tile
+    const uint32_t tS = tm + uint32_t(x) * 128u, tO = tm + 256u + uint32_t(x) * D;
+    const int last = x == 0 || hasB ? last_of(x) : -1;
+    uint32_t p_phase = 0;                          // parity of the next P
+    bool ok = x == 0 || hasB, first_s = true, first_o = true;
+    auto wait = [&](uint64_t &bar, uint32_t parity) {
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, failed));
+      return ok;
+    };
+    auto commit = [&](uint64_t &bar) {
+      if (leader) mma_commit(smem_u32(&bar));
+    };
+    // k = -1: the first S product; then per key tile P V of the tile and S of the next one, the two row tiles in turns
+    for (int k = -1; k < n_tiles && ok; ++k) {
+      const int seqV = 2 * k + 1, seqK = 2 * k + 2;
+      const bool more = k + 1 < n_tiles, pv = has(x, k), qk = has(x, k + 1);
+      if (k >= 0) wait(sm.bar_full[seqV % S], uint32_t(seqV / S) & 1u);
+      if (ok && more) wait(sm.bar_full[seqK % S], uint32_t(seqK / S) & 1u);
+      if (ok && qk && first_s) wait(sm.bar_q[x], 0u);
+      if (ok && hasB && (x == 1 || k >= 0)) wait(sm.bar_turn[x], uint32_t(x == 1 ? k + 1 : k) & 1u);
+      if (ok && pv) {
+        wait(sm.bar_p[x], p_phase);
+        p_phase ^= 1u;
+        tc_fence_after();
+      }
+      if (!ok) break;
+      if (pv) {
+        issue_values<D>(leader, tO, tS, kv_addr(seqV % S), !first_o);
+        first_o = false;
+        if (k == last) commit(sm.bar_s[x]);        // O is complete
+      }
+      if (qk) {
+        issue_scores<D>(leader, tS, q_addr(x), kv_addr(seqK % S));
+        first_s = false;
+        commit(sm.bar_s[x]);
+      }
+      if (leader) {
+        if (hasB) mbar_arrive(smem_u32(&sm.bar_turn[x ^ 1]));
+        if (pv && k == last) mma_commit(smem_u32(&sm.bar_free[seqV % S]));
+        if (!pv && k >= 0) mbar_arrive(smem_u32(&sm.bar_free[seqV % S]));   // (a tile of which this row tile sees nothing)
+        if (!qk && more) mbar_arrive(smem_u32(&sm.bar_free[seqK % S]));
+      }
+    }
+  } else {
+    // =========================== loader warp ===========================
+    const int rows = min(1 << p.page_shift, kKT), pieces = kKT / rows;
+    bool ok = true;
+    int asked = 0;                                 // K and V tiles
+    if (lane == 0) {
+      for (int x = 0; x < (hasB && n_tiles ? 2 : n_tiles ? 1 : 0); ++x) {
+        const uint32_t bar = smem_u32(&sm.bar_q[x]);
+        mbar_expect_tx(bar, Sm::kTileBytes);
+        for (int hf = 0; hf < D / 64; ++hf) tma_load_3d(q_addr(x) + hf * kBoxBytes, &maps.q, hf * 64, g * G, row0 + tok0 + x * TOKT, bar);
+      }
+    }
+    int next = n_tiles ? piece_page(p, b, tq0, tq_last, kt.slot(0), pieces, rows, none) : 0;
+#pragma unroll 1
+    for (int k = 0; k < n_tiles && ok; ++k) {
+      const int j0 = kt.slot(k), page = next;
+      if (k + 1 < n_tiles) next = piece_page(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows, none);
+#pragma unroll 1
+      for (int is_v = 0; is_v < 2; ++is_v) {
+        const int job = 2 * k + is_v, slot = job % S;
+        const uint32_t bar = smem_u32(&sm.bar_full[slot]);
+        if (job >= S) ok = mbar_wait(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        // V rows behind the CTA's last token: whatever they hold, their weights are 0 and they have to be finite
+        const bool tail = is_v && j0 + kKT - 1 > tq_last;
+        const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
+        if (lane == 0) mbar_expect_tx(to, Sm::kTileBytes);
+        __syncwarp();
+        load_tile<D>(is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
+        ++asked;
+        if (tail) {
+          ok = __all_sync(0xffffffffu, mbar_wait(to, 0u, failed));
+          if (!ok) break;
+          for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
+#pragma unroll
+            for (int hf = 0; hf < D / 64; ++hf)
+              *reinterpret_cast<uint4 *>(sm.kv[slot] + hf * kBoxBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar);
+        }
+      }
+    }
+    if (!ok) {   // after a time-out: no copy outlives the CTA
+      int alone = 0;
+      for (int x = 0; x < (hasB ? 2 : 1); ++x) mbar_wait(smem_u32(&sm.bar_q[x]), 0u, &alone);
+      for (int job = max(0, asked - S); job < asked; ++job) {
+        const bool tail = (job & 1) && kt.slot(job >> 1) + kKT - 1 > tq_last;
+        alone = 0;
+        if (tail) mbar_wait(smem_u32(&sm.bar_tail), 0u, &alone);
+        else mbar_wait(smem_u32(&sm.bar_full[job % S]), uint32_t(job / S) & 1u, &alone);
+      }
+    }
+  }
+  // after a time-out the waits return at once and nothing is stored; the CTA meets here either way
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0 && sm.failed) atomicExch(p.status, kDevWaitTimeout);
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+bool encode_queries(const glide_paged *h, const PagedParams &p, CUtensorMap *map) {
+  const cuuint64_t dims[3] = {cuuint64_t(h->cfg.head_dim), cuuint64_t(p.H), cuuint64_t(p.n_tokens)};
+  const cuuint64_t strides[2] = {cuuint64_t(h->cfg.head_dim) * 2, cuuint64_t(p.q_stride) * 2};
+  const cuuint32_t box[3] = {64, cuuint32_t(h->group), cuuint32_t(kRows / h->group)}, ones[3] = {1, 1, 1};
+  return reinterpret_cast<TensorMapEncoder>(h->encode)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p.q), dims, strides, box, ones,
+                                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename F>
+int dispatch_tc(const glide_paged *h, F &&f) {
+  return dispatch_config(GLIDE_BF16, h->cfg.head_dim, h->group, [&](auto, auto d, auto g) { return f(d, g); });
+}
+
+}  // namespace
+
+int setup_paged_tc(const glide_paged *h) {
+  return dispatch_tc(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value, kBytes = int(sizeof(PrefillSmem<D>));
+    static_assert(kBytes <= 232448, "shared memory of one CTA");
+    return cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
+                   cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess
+               ? int(GLIDE_OK)
+               : int(GLIDE_ERR_CUDA);
+  });
+}
+
+int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  PagedMaps maps;
+  maps.k = h->kpage;
+  maps.v = h->vpage;
+  if (!encode_queries(h, p, &maps.q)) return GLIDE_ERR_CUDA;
+  return dispatch_tc(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    const int64_t tiles = p.n_tokens / (2 * kRows / G) + p.batch;   // at most: each sequence's last one may be short
+    const int64_t grid = tiles * p.Hkv;
+    if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
+    const size_t bytes = sizeof(PrefillSmem<D>);
+    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
+    else paged_prefill_tc_kernel<D, G, false><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
+    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+  });
+}
+
+}  // namespace glide
