@@ -113,6 +113,7 @@ int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_
 }
 
 int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  if (h->cfg.io_dtype == GLIDE_BF16) return launch_paged_weights_tc(h, p, st);
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
     const dim3 grid(unsigned(std::min<int64_t>(blocks_of(p.most), 1024)), unsigned(p.batch * p.Hkv));
     paged_weights_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value><<<grid, kWarps * 32, 0, st>>>(p);

@@ -107,6 +107,7 @@ int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, i
 size_t paged_record_bytes(const glide_paged_config &cfg);
 int setup_paged_decode(const glide_paged *h);
 int setup_paged_tc(const glide_paged *h);
+int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 
 }  // namespace glide

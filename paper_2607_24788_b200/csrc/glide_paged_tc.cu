@@ -568,6 +568,266 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   }
 }
 
+// ---- the account of a prompt's weights ----------------------------------------------------------------------------------
+//
+// A CTA takes key tiles of 128 slots of one (sequence, KV head) in turns.  Per tile of 128 query rows (token * G + head) that may see the
+// slots, S^T = K Q^T with the slots on the TMEM lanes, so that a slot's weights 2^(s - lse) lie in one lane: each of its threads adds up
+// its own columns, and the four threads of a lane meet once per key tile.  No sum crosses a CTA, so nothing is added by atomics.
+//   warps 0-15   weights: warps 0-7 of the even query tiles, 8-15 of the odd ones, two threads per slot, 64 columns each
+//   warp 16      issues the products (four S buffers of 128 columns: all of TMEM)
+//   warp 17      loads the K tile and, four ahead, Q tiles with their row sums
+// Bound: the exponentials (16 per cycle and SM), of which a product tile has 16384 for 512 cycles of tensor core time (d = 128).
+
+constexpr int kAccThreads = 576;
+constexpr int kAccMmaWarp = 16, kAccLoadWarp = 17;
+constexpr int kAccStages = 4;
+
+template <int D>
+struct AccountSmem {
+  static constexpr int kTileBytes = D * 256;
+  unsigned char k[2][kTileBytes];
+  unsigned char q[kAccStages][kTileBytes];
+  float lse[kAccStages][kRows];          // row sums, log2
+  float part[4][kKT];                    // sums of a slot's four threads
+  uint64_t bar_k[2], bar_kfree[2];       // K tile landed; every product that reads it has completed
+  uint64_t bar_full[kAccStages];         // Q tile and row sums are there
+  uint64_t bar_s[kAccStages];            // the product has completed
+  uint64_t bar_sfree[kAccStages];        // S and the row sums have been read (one arrival per warp of the eight)
+  uint32_t tmem_base;
+  int failed, total;
+  int prefix[kMaxPagedBatch + 1];        // key tiles of the sequences before
+};
+
+// x - c for two values with a constant each
+__device__ __forceinline__ void fma2v(float &a0, float &a1, float x0, float x1, float s, float c0, float c1) {
+  asm("{\n\t.reg .b64 x, s, c, d;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmov.b64 c, {%5, %6};\n\t"
+      "fma.rn.f32x2 d, x, s, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(a0), "=f"(a1)
+      : "f"(x0), "f"(x1), "f"(s), "f"(c0), "f"(c1));
+}
+
+// One key tile of a CTA: its sequence, and the new tokens t0 .. t1 - 1 that may see it
+struct KeyTile {
+  int b, g, j0, len, n_new, row0, t0, t1;
+};
+template <int G>
+__device__ __forceinline__ KeyTile key_tile(const PagedParams &p, const int *prefix, int item) {
+  KeyTile k;
+  const int f = item / p.Hkv;
+  k.g = item - f * p.Hkv;
+  int lo = 0, hi = p.batch;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] <= f) lo = mid; else hi = mid;
+  }
+  k.b = lo;
+  k.j0 = (f - prefix[lo]) * kKT;
+  k.len = paged_len(p, lo);
+  k.n_new = paged_new(p, lo, k.len, k.row0);
+  const int q0 = k.len - k.n_new;        // slot of the first new token
+  k.t0 = max(0, k.j0 - q0);
+  k.t1 = k.n_new;
+  if (p.window >= 0 && k.j0 >= p.n_sink) k.t1 = min(k.t1, p.window == 0 ? 0 : k.j0 + kKT - 1 + p.window - q0);
+  if (k.t1 < k.t0) k.t1 = k.t0;
+  return k;
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(kAccThreads, 1)
+paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none) {
+  using Sm = AccountSmem<D>;
+  constexpr int TOKT = kRows / G;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int *failed = &sm.failed;
+  const bool aligned = (smem_u32(smem_raw) & 1023u) == 0;
+  if (warp == kAccLoadWarp) {
+    int base = 0;   // key tiles that hold a slot of the sequence; none where it has no new token
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+      const int b = b0 + lane;
+      int n = 0, row0;
+      if (b < p.batch) {
+        const int len = paged_len(p, b);
+        n = paged_new(p, b, len, row0) > 0 ? (len + kKT - 1) / kKT : 0;
+      }
+      int inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (b < p.batch) sm.prefix[b] = base + inc - n;
+      base += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) {
+      sm.prefix[p.batch] = base;
+      sm.total = base * p.Hkv;
+      sm.failed = aligned ? 0 : 1;
+      for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sm.bar_k[i]), 1), mbar_init(smem_u32(&sm.bar_kfree[i]), 1);
+      for (int i = 0; i < kAccStages; ++i) {
+        mbar_init(smem_u32(&sm.bar_full[i]), 1);
+        mbar_init(smem_u32(&sm.bar_s[i]), 1);
+        mbar_init(smem_u32(&sm.bar_sfree[i]), 8);
+      }
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+  } else if (warp == kAccMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem_base;
+  const int total = sm.total;
+
+  if (!aligned) {
+    // (the status word tells)
+  } else if (tid < 512) {
+    const int par = warp >> 3, H = (warp >> 2) & 1, slot = (warp & 3) * 32 + lane;
+    const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + uint32_t(H) * 64u;
+    bool ok = true;
+    int done = 0;   // query tiles of the CTA's earlier key tiles
+    for (int item = int(blockIdx.x); item < total; item += int(gridDim.x)) {
+      const KeyTile kt = key_tile<G>(p, sm.prefix, item);
+      const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT, q0 = kt.len - kt.n_new, j = kt.j0 + slot;
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        const int t = done + i;
+        if ((t & 1) != par) continue;
+        const int st = t % kAccStages;
+        const uint32_t ph = uint32_t(t / kAccStages) & 1u;
+        if (ok) ok = mbar_wait(smem_u32(&sm.bar_full[st]), ph, failed);
+        if (ok) ok = mbar_wait(smem_u32(&sm.bar_s[st]), ph, failed);
+        tc_fence_after();
+        ok = __all_sync(0xffffffffu, ok);
+        const int tok = kt.t0 + i * TOKT, i0 = q0 + tok, ntok = min(TOKT, kt.n_new - tok);
+        // columns lo .. hi of this thread's half see the slot
+        const int lo = max(0, min(j - i0, TOKT)) * G;
+        const int until = p.window < 0 || j < p.n_sink ? TOKT : max(0, min(j - i0 + p.window, TOKT));
+        const int hi = min(until, ntok) * G - 1;
+        const bool whole = kt.j0 + kKT - 1 <= i0 && ntok == TOKT && (p.window < 0 || kt.j0 + kKT <= p.n_sink || i0 + TOKT - 1 < kt.j0 + p.window);
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t x[32];
+          tmem_ld32(tS + uint32_t(st) * 128u + c, x);
+          const float4 *lse = reinterpret_cast<const float4 *>(&sm.lse[st][H * 64 + c]);
+          const uint32_t m = whole ? ~0u : column_mask(H * 64 + c, lo, hi);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float4 l4 = lse[e];
+            float a0, a1, a2, a3;
+            fma2v(a0, a1, __uint_as_float(x[e * 4]), __uint_as_float(x[e * 4 + 1]), p.scale_log2, l4.x, l4.y);
+            fma2v(a2, a3, __uint_as_float(x[e * 4 + 2]), __uint_as_float(x[e * 4 + 3]), p.scale_log2, l4.z, l4.w);
+            if (!whole) {
+              a0 = (m >> (e * 4)) & 1u ? a0 : -CUDART_INF_F, a1 = (m >> (e * 4 + 1)) & 1u ? a1 : -CUDART_INF_F;
+              a2 = (m >> (e * 4 + 2)) & 1u ? a2 : -CUDART_INF_F, a3 = (m >> (e * 4 + 3)) & 1u ? a3 : -CUDART_INF_F;
+            }
+            add2(sum0, sum1, ex2(a0), ex2(a1));
+            add2(sum0, sum1, ex2(a2), ex2(a3));
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.bar_sfree[st]));
+      }
+      done += n;
+      if (n == 0) continue;   // (the same for all)
+      sm.part[par * 2 + H][slot] = sum0 + sum1;
+      asm volatile("barrier.cta.sync 1, 512;" ::: "memory");
+      if (tid < kKT && j < kt.len && ok) {
+        const float sum = (sm.part[0][slot] + sm.part[1][slot]) + (sm.part[2][slot] + sm.part[3][slot]);
+        float *w = p.weight + (size_t(kt.b) * p.Hkv + kt.g) * size_t(p.track_stride) + j;
+        if (sum != 0.f) *w += sum;   // (a NaN is not 0)
+      }
+      asm volatile("barrier.cta.sync 1, 512;" ::: "memory");
+    }
+  } else if (warp == kAccMmaWarp) {
+    const bool leader = elect_one();
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint32_t sK = smem_u32(sm.k[0]), sQ = smem_u32(sm.q[0]);
+    bool ok = true;
+    auto wait = [&](uint64_t &bar, uint32_t parity) {
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, failed));
+      return ok;
+    };
+    int done = 0, kn = 0;   // query tiles, key tiles so far
+    for (int item = int(blockIdx.x); item < total && ok; item += int(gridDim.x)) {
+      const KeyTile kt = key_tile<G>(p, sm.prefix, item);
+      const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT;
+      if (n == 0) continue;
+      if (!wait(sm.bar_k[kn & 1], uint32_t(kn >> 1) & 1u)) break;
+      for (int i = 0; i < n && ok; ++i) {
+        const int t = done + i, st = t % kAccStages;
+        if (t >= kAccStages) wait(sm.bar_sfree[st], uint32_t(t / kAccStages - 1) & 1u);
+        if (ok) wait(sm.bar_full[st], uint32_t(t / kAccStages) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        issue_scores<D>(leader, tm + uint32_t(st) * 128u, sK + uint32_t(kn & 1) * Sm::kTileBytes, sQ + uint32_t(st) * Sm::kTileBytes);
+        if (leader) {
+          mma_commit(smem_u32(&sm.bar_s[st]));
+          if (i + 1 == n) mma_commit(smem_u32(&sm.bar_kfree[kn & 1]));
+        }
+      }
+      done += n;
+      ++kn;
+    }
+  } else {
+    const int rows = min(1 << p.page_shift, kKT), pieces = kKT / rows;
+    bool ok = true;
+    int done = 0, kn = 0;
+    for (int item = int(blockIdx.x); item < total && ok; item += int(gridDim.x)) {
+      const KeyTile kt = key_tile<G>(p, sm.prefix, item);
+      const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT, q0 = kt.len - kt.n_new;
+      if (n == 0) continue;
+      const int page = piece_page(p, kt.b, q0 + kt.t0, q0 + kt.t1 - 1, kt.j0, pieces, rows, none);
+      if (kn >= 2) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_kfree[kn & 1]), uint32_t((kn >> 1) - 1) & 1u, failed));
+      if (!ok) break;
+      const uint32_t bar_k = smem_u32(&sm.bar_k[kn & 1]);
+      if (lane == 0) mbar_expect_tx(bar_k, Sm::kTileBytes);
+      __syncwarp();
+      load_tile<D>(&maps.k, p, smem_u32(sm.k[kn & 1]), page, kt.j0, kt.g, pieces, rows, bar_k);
+      ++kn;
+      for (int i = 0; i < n; ++i) {
+        const int t = done + i, st = t % kAccStages, tok = kt.t0 + i * TOKT;
+        // (the row sums before the wait, so that they are on their way during it; rows of no token: their weights are masked)
+        float lse[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = lane * 4 + e, tk = tok + r / G;
+          const float x = tk < kt.n_new ? p.lse[size_t(kt.row0 + tk) * p.H + kt.g * G + r % G] : 0.f;
+          lse[e] = x == -CUDART_INF_F ? 0.f : -x * kLog2e;   // (a row that sees nothing has no column here that counts)
+        }
+        if (t >= kAccStages) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_sfree[st]), uint32_t(t / kAccStages - 1) & 1u, failed));
+        if (!ok) break;
+        *reinterpret_cast<float4 *>(&sm.lse[st][lane * 4]) = make_float4(lse[0], lse[1], lse[2], lse[3]);
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&sm.bar_full[st]);
+          mbar_expect_tx(bar, Sm::kTileBytes);
+          for (int hf = 0; hf < D / 64; ++hf)
+            tma_load_3d(smem_u32(sm.q[st]) + hf * kBoxBytes, &maps.q, hf * 64, kt.g * G, kt.row0 + tok, bar);
+        }
+      }
+      done += n;
+    }
+    if (!ok) {   // after a time-out: no copy outlives the CTA (each barrier's last phase ends, or has ended)
+      int alone = 0;
+      for (int i = 0; i < 2 && i < kn; ++i) mbar_wait(smem_u32(&sm.bar_k[(kn - 1 - i) & 1]), uint32_t((kn - 1 - i) >> 1) & 1u, &alone);
+      for (int i = 0; i < kAccStages; ++i) alone = 0, mbar_wait(smem_u32(&sm.bar_full[i]), 0u, &alone), alone = 0, mbar_wait(smem_u32(&sm.bar_full[i]), 1u, &alone);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0 && sm.failed) atomicExch(p.status, kDevWaitTimeout);
+  if (warp == kAccMmaWarp) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
 bool encode_queries(const glide_paged *h, const PagedParams &p, CUtensorMap *map) {
   const cuuint64_t dims[3] = {cuuint64_t(h->cfg.head_dim), cuuint64_t(p.H), cuuint64_t(p.n_tokens)};
   const cuuint64_t strides[2] = {cuuint64_t(h->cfg.head_dim) * 2, cuuint64_t(p.q_stride) * 2};
@@ -589,7 +849,9 @@ int setup_paged_tc(const glide_paged *h) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value, kBytes = int(sizeof(PrefillSmem<D>));
     static_assert(kBytes <= 232448, "shared memory of one CTA");
     return cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
-                   cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess
+                   cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
+                   cudaFuncSetAttribute(paged_weights_tc_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(AccountSmem<D>))) ==
+                       cudaSuccess
                ? int(GLIDE_OK)
                : int(GLIDE_ERR_CUDA);
   });
@@ -608,6 +870,21 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const size_t bytes = sizeof(PrefillSmem<D>);
     if (p.lse) paged_prefill_tc_kernel<D, G, true><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
     else paged_prefill_tc_kernel<D, G, false><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
+    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+  });
+}
+
+int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  PagedMaps maps;
+  maps.k = h->kpage;
+  maps.v = h->vpage;
+  if (!encode_queries(h, p, &maps.q)) return GLIDE_ERR_CUDA;
+  return dispatch_tc(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    static_assert(sizeof(AccountSmem<D>) <= 232448, "shared memory of one CTA");
+    const int64_t most = (int64_t(p.most) / kKT + 1) * p.batch * p.Hkv;
+    const unsigned grid = unsigned(std::min<int64_t>(most, p.sm_count));
+    paged_weights_tc_kernel<D, G><<<grid, kAccThreads, sizeof(AccountSmem<D>), st>>>(p, maps, h->map_pages);
     return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
