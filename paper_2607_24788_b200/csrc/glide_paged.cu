@@ -1,7 +1,6 @@
-// Paged attention: storing new tokens, and the forms that take one query token, or one slot, at a time.
-#include <algorithm>
-
-#include "glide_paged_rows.cuh"
+// Paged attention: storing new tokens.
+#include "glide_device.cuh"
+#include "glide_paged.h"
 
 namespace glide {
 
@@ -46,48 +45,6 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
   if (lane == 0 && p.pos) p.pos[at] = p.seen[b] - paged_len(p, b) + slot;
 }
 
-// One warp per (new token, KV head).
-template <typename T, int D, int G>
-__global__ void __launch_bounds__(kWarps * 32) paged_prefill_row_kernel(const __grid_constant__ PagedParams p) {
-  const int64_t item = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int64_t r = item / p.Hkv;
-  const int g = int(item - r * p.Hkv);
-  int b, i;
-  if (r >= p.n_tokens || !row_of(p, r, b, i)) return;
-  PagedRow<T, D, G> row;
-  row.attend(p, size_t(r), b, i, g, g * G, p.lse != nullptr);
-}
-
-// One warp per (sequence, KV head, slot): the weights of all queries that see the slot.
-template <typename T, int D, int G>
-__global__ void __launch_bounds__(kWarps * 32) paged_weights_row_kernel(const __grid_constant__ PagedParams p) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31, b = blockIdx.y / p.Hkv, g = blockIdx.y % p.Hkv;
-  const int len = paged_len(p, b);
-  int row0;
-  const int n = paged_new(p, b, len, row0);
-  for (int j = blockIdx.x * kWarps + (threadIdx.x >> 5); j < len; j += gridDim.x * kWarps) {
-    float k[E], sum = 0.f;
-    bool seen = false;
-    for (int t = 0; t < n; ++t) {
-      const int i = len - n + t;
-      if (!paged_sees(p, i, j)) continue;
-      if (!seen) load_elems<T, E>(reinterpret_cast<const T *>(p.k) + paged_row(p, paged_page(p, b, j), j, g) + lane * E, k);
-      seen = true;
-#pragma unroll
-      for (int h = 0; h < G; ++h) {
-        float q[E], part = 0.f;
-        load_elems<T, E>(reinterpret_cast<const T *>(p.q) + size_t(row0 + t) * size_t(p.q_stride) + size_t(g * G + h) * D + lane * E, q);
-#pragma unroll
-        for (int e = 0; e < E; ++e) part = fmaf(q[e] * p.scale_log2, k[e], part);
-        const float lse = p.lse[size_t(row0 + t) * size_t(p.H) + g * G + h];
-        sum += exp2f(warp_sum(part) - lse * kLog2e);
-      }
-    }
-    if (seen && lane == 0) p.weight[(size_t(b) * p.Hkv + g) * size_t(p.track_stride) + j] += sum;
-  }
-}
-
 unsigned blocks_of(int64_t items) { return unsigned((items + kWarps - 1) / kWarps); }
 int launched() {
   if (cudaGetLastError() == cudaSuccess) return GLIDE_OK;
@@ -99,24 +56,6 @@ int launched() {
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
     paged_store_kernel<typename decltype(t)::type, decltype(d)::value><<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);
-    return launched();
-  });
-}
-
-int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
-  if (h->cfg.io_dtype == GLIDE_BF16) return launch_paged_prefill_tc(h, p, st);
-  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
-    paged_prefill_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>
-        <<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);
-    return launched();
-  });
-}
-
-int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
-  if (h->cfg.io_dtype == GLIDE_BF16) return launch_paged_weights_tc(h, p, st);
-  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
-    const dim3 grid(unsigned(std::min<int64_t>(blocks_of(p.most), 1024)), unsigned(p.batch * p.Hkv));
-    paged_weights_row_kernel<typename decltype(t)::type, decltype(d)::value, decltype(g)::value><<<grid, kWarps * 32, 0, st>>>(p);
     return launched();
   });
 }

@@ -99,15 +99,16 @@ __device__ __forceinline__ bool paged_sees(const PagedParams &p, int i, int j) {
 }
 
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st);
-int launch_paged_prefill(const glide_paged *h, const PagedParams &p, cudaStream_t st);
-int launch_paged_weights(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);    // bf16
+int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st);   // fp32
+int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, int recent, float *weight_out, int32_t *pos_out,
                        int32_t *new_lens, cudaStream_t st);
 size_t paged_record_bytes(const glide_paged_config &cfg);
-int setup_paged_decode(const glide_paged *h);
+int setup_paged_decode(const glide_paged *h);   // what the device's context has to know of the kernels, once per handle
 int setup_paged_tc(const glide_paged *h);
-int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
-int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);
+int setup_paged_fma(const glide_paged *h);
 
 }  // namespace glide

@@ -1,0 +1,348 @@
+// Paged attention of prompts on the CUDA cores, fp32.
+//
+// A CTA of 256 threads owns 64 query rows (token * G + head) of one (sequence, KV head) and goes through tiles of 64 slots; a thread
+// (ty, tx) of 16 x 16 has rows 4 ty .. 4 ty + 3 and slots 4 tx .. 4 tx + 3 of the scores and columns 4 tx .. (and 64 + 4 tx ..) of the
+// output.  Q and K lie in shared memory by feature, so that a step of the product takes two 16-byte reads for 16 multiply-adds; the
+// next tile's rows are on their way in registers meanwhile.  Weights are taken against a reference that moves when a score exceeds
+// it by more than 8 in the exponent.  Bound: the multiply-adds.
+// What a row does not see does not reach it: scores are selected; rows of V that no row of the CTA sees are zeros; a row whose output
+// is not finite all the same is computed once more by itself.
+#include <algorithm>
+
+#include "glide_paged_rows.cuh"
+#include "glide_tc.cuh"
+
+namespace glide {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRows = 64, kSlots = 64;   // of a tile
+constexpr int kPad = kSlots + 4;
+constexpr float kLazy = 8.0f;
+
+template <int D>
+struct Smem {
+  float q[D][kRows], k[D][kPad], v[kSlots][D], p[kSlots][kPad];
+};
+
+// Rows of 64 slots (or queries) on their way from memory: thread (r = tid & 63, c = tid >> 6) has 16-byte chunks c, c + 4, ... of row r
+template <int D>
+struct Staged {
+  static constexpr int kEach = D / 16;
+  float4 x[kEach];
+  __device__ __forceinline__ void load(const float *row) {   // nullptr: zeros
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      x[i] = row ? reinterpret_cast<const float4 *>(row)[(threadIdx.x >> 6) + 4 * i] : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  template <int W>
+  __device__ __forceinline__ void store_by_feature(float (&to)[D][W], float scale) {
+    const int r = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int c = ((threadIdx.x >> 6) + 4 * i) * 4;
+      to[c][r] = x[i].x * scale, to[c + 1][r] = x[i].y * scale, to[c + 2][r] = x[i].z * scale, to[c + 3][r] = x[i].w * scale;
+    }
+  }
+  __device__ __forceinline__ void store(float (&to)[kSlots][D]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) *reinterpret_cast<float4 *>(&to[threadIdx.x & 63][((threadIdx.x >> 6) + 4 * i) * 4]) = x[i];
+  }
+};
+
+// s[a][c] = row 4 ty + a of q times row 4 tx + c of k
+template <int D>
+__device__ __forceinline__ void scores(const float (&q)[D][kRows], const float (&k)[D][kPad], float (&s)[4][4]) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
+#pragma unroll 8
+  for (int d = 0; d < D; ++d) {
+    const float4 x = *reinterpret_cast<const float4 *>(&q[d][ty * 4]), y = *reinterpret_cast<const float4 *>(&k[d][tx * 4]);
+    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[a][c] = fmaf(xs[a], ys[c], s[a][c]);
+  }
+}
+
+// Tiles of 64 slots that queries of slots [q0, q1] see: [0, sinks) and [first, end)
+struct SlotTiles {
+  int sinks, first, n;
+  __device__ __forceinline__ int slot(int k) const { return (k < sinks ? k : first + k - sinks) * kSlots; }
+};
+__device__ __forceinline__ SlotTiles slot_tiles(const PagedParams &p, int q0, int q1) {
+  const int end = q1 / kSlots + 1;
+  SlotTiles t{(min(p.n_sink, q1 + 1) + kSlots - 1) / kSlots, p.window < 0 ? 0 : p.window == 0 ? end : max(0, q0 - p.window + 1) / kSlots, 0};
+  if (t.sinks > t.first) t.sinks = t.first = 0;
+  t.n = t.sinks + end - t.first;
+  return t;
+}
+
+// The sequence and first new token of a CTA that is number `want` of those that hold `tokens` new tokens each; seq < 0: none.  Every
+// warp finds it for itself.
+struct Place {
+  int seq, tok0, len, n_new, row0;
+};
+__device__ __forceinline__ Place place_of(const PagedParams &p, int want, int tokens) {
+  const int lane = threadIdx.x & 31;
+  Place at{-1, 0, 0, 0, 0};
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int b = b0 + lane;
+    int row0 = 0, n = 0, len = 0;
+    if (b < p.batch) len = paged_len(p, b), n = paged_new(p, b, len, row0);
+    const int tiles = (n + tokens - 1) / tokens;
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    const unsigned here = __ballot_sync(0xffffffffu, want < inc);
+    if (here) {
+      const int l = __ffs(int(here)) - 1;
+      at.seq = b0 + l;
+      at.tok0 = (want - __shfl_sync(0xffffffffu, inc - tiles, l)) * tokens;
+      at.len = __shfl_sync(0xffffffffu, len, l);
+      at.n_new = __shfl_sync(0xffffffffu, n, l);
+      at.row0 = __shfl_sync(0xffffffffu, row0, l);
+      return at;
+    }
+    want -= __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return at;
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int TOK = kRows / G, N = D / 64;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  auto &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+  const int g = int(blockIdx.x % unsigned(p.Hkv));
+  // (the last tokens, whose windows are the longest, first)
+  const Place at = place_of(p, int(gridDim.x / unsigned(p.Hkv)) - 1 - int(blockIdx.x / unsigned(p.Hkv)), TOK);
+  if (at.seq < 0) return;
+  const int ntok = min(TOK, at.n_new - at.tok0), q0 = at.len - at.n_new + at.tok0, q1 = q0 + ntok - 1;
+  const SlotTiles st = slot_tiles(p, q0, q1);
+  const int r_mine = tid & 63;   // the row of Q, K, V that this thread brings
+  auto row_of = [&](const void *pages, int j) -> const float * {
+    if (j > q1 || (p.window >= 0 && j <= q0 - p.window && j >= p.n_sink)) return nullptr;
+    const int page = paged_page(p, at.seq, j);
+    return page < 0 ? nullptr : reinterpret_cast<const float *>(pages) + paged_row(p, page, j, g);
+  };
+  Staged<D> a, b;
+  a.load(r_mine < ntok * G ? reinterpret_cast<const float *>(p.q) + size_t(at.row0 + at.tok0 + r_mine / G) * size_t(p.q_stride) +
+                                 size_t(g * G + r_mine % G) * D
+                           : nullptr);
+  a.store_by_feature(sm.q, p.scale_log2);
+  float o[4][4 * N], m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -CUDART_INF_F, l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4 * N; ++c) o[i][c] = 0.f;
+  }
+  if (st.n) a.load(row_of(p.k, st.slot(0) + r_mine)), b.load(row_of(p.v, st.slot(0) + r_mine));
+#pragma unroll 1
+  for (int t = 0; t < st.n; ++t) {
+    const int j0 = st.slot(t);
+    __syncthreads();   // the tile before has been read
+    a.store_by_feature(sm.k, 1.f);
+    b.store(sm.v);
+    __syncthreads();
+    if (t + 1 < st.n) a.load(row_of(p.k, st.slot(t + 1) + r_mine)), b.load(row_of(p.v, st.slot(t + 1) + r_mine));
+    float s[4][4];
+    scores<D>(sm.q, sm.k, s);
+    const bool whole = j0 + kSlots - 1 <= q0 && (p.window < 0 || j0 > q1 - p.window || j0 + kSlots <= p.n_sink);
+    bool grows = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int mine = q0 + (ty * 4 + i) / G;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (!whole && !paged_sees(p, mine, j0 + tx * 4 + c)) s[i][c] = -CUDART_INF_F;
+      const float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+      grows |= top > m[i] + kLazy || (m[i] == -CUDART_INF_F && top > -CUDART_INF_F);
+    }
+    if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+#pragma unroll
+        for (int w = 1; w < 16; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        top = fmaxf(top, m[i]);
+        const float f = m[i] == -CUDART_INF_F ? 0.f : ex2(m[i] - top);
+        m[i] = top;
+        l[i] *= f;
+#pragma unroll
+        for (int c = 0; c < 4 * N; ++c) o[i][c] *= f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float ref = m[i] == -CUDART_INF_F ? 0.f : m[i];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[i][c] = ex2(s[i][c] - ref), l[i] += s[i][c];
+    }
+    // (the rows of a warp's weights are read by that warp alone)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) *reinterpret_cast<float4 *>(&sm.p[tx * 4 + c][ty * 4]) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+    __syncwarp();
+#pragma unroll 8
+    for (int j = 0; j < kSlots; ++j) {
+      const float4 w = *reinterpret_cast<const float4 *>(&sm.p[j][ty * 4]);
+      const float ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float4 v = *reinterpret_cast<const float4 *>(&sm.v[j][n * 64 + tx * 4]);
+        const float vs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[i][n * 4 + c] = fmaf(ws[i], vs[c], o[i][n * 4 + c]);
+      }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int w = 1; w < 16; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+  }
+  unsigned again = 0;   // rows of this thread's four that are not finite
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    if (r >= ntok * G) continue;
+    const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+    float chk = inv;
+    float *out = reinterpret_cast<float *>(p.out) + size_t(at.row0 + at.tok0 + r / G) * size_t(p.out_stride) + size_t(g * G + r % G) * D;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float4 x = make_float4(o[i][n * 4] * inv, o[i][n * 4 + 1] * inv, o[i][n * 4 + 2] * inv, o[i][n * 4 + 3] * inv);
+      chk += x.x + x.y + x.z + x.w;
+      *reinterpret_cast<float4 *>(out + n * 64 + tx * 4) = x;
+    }
+    if (p.lse && tx == 0) p.lse[size_t(at.row0 + at.tok0 + r / G) * p.H + g * G + r % G] = PagedRow<float, D, 1>::paged_lse(m[i], l[i]);
+    again |= (!isfinite(chk) ? 1u : 0u) << i;
+  }
+  __syncwarp();
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half)   // the warp's two values of ty
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      if (!__any_sync(0xffffffffu, ((tid >> 4) & 1) == half && ((again >> i) & 1u))) continue;
+      const int r = ((tid >> 5) * 2 + half) * 4 + i;
+      PagedRow<float, D, 1> one;
+      one.attend(p, size_t(at.row0 + at.tok0 + r / G), at.seq, q0 + r / G, g, g * G + r % G, false);   // (the sums of the scores were right)
+    }
+}
+
+// A CTA takes tiles of 64 slots of one (sequence, KV head) in turns: the weights of all new tokens' rows, 64 at a time.  A thread adds up
+// its own rows' weights for its four slots; the 16 threads of a slot meet once per tile.
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int TOK = kRows / G;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  auto &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r_mine = tid & 63;
+  int base = 0;   // tiles of the sequences before
+  int64_t item = blockIdx.x;
+  for (int b = 0; b < p.batch; ++b) {
+    const int len = paged_len(p, b);
+    int row0;
+    const int n_new = paged_new(p, b, len, row0), tiles = n_new ? (len + kSlots - 1) / kSlots : 0, q0 = len - n_new;
+    for (; item < int64_t(base + tiles) * p.Hkv; item += gridDim.x) {
+      const int f = int(item / p.Hkv), g = int(item - int64_t(f) * p.Hkv), j0 = (f - base) * kSlots;
+      const int t0 = max(0, j0 - q0);
+      const int t1 = p.window >= 0 && j0 >= p.n_sink ? min(n_new, p.window == 0 ? 0 : j0 + kSlots - 1 + p.window - q0) : n_new;
+      if (t0 >= t1) continue;
+      auto load_q = [&](int tok, Staged<D> &x) {
+        const int tk = tok + r_mine / G;
+        x.load(tk < t1 ? reinterpret_cast<const float *>(p.q) + size_t(row0 + tk) * size_t(p.q_stride) + size_t(g * G + r_mine % G) * D : nullptr);
+      };
+      Staged<D> a;
+      {
+        const int j = j0 + r_mine, page = j < len ? paged_page(p, b, j) : -1;
+        a.load(page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g));
+      }
+      __syncthreads();   // the tile before has been read
+      a.store_by_feature(sm.k, 1.f);
+      load_q(t0, a);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int tok = t0; tok < t1; tok += TOK) {
+        __syncthreads();
+        a.store_by_feature(sm.q, p.scale_log2);
+        __syncthreads();
+        if (tok + TOK < t1) load_q(tok + TOK, a);
+        float s[4][4];
+        scores<D>(sm.q, sm.k, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = ty * 4 + i, tk = tok + r / G;
+          if (tk >= t1) continue;
+          const float lse = p.lse[size_t(row0 + tk) * p.H + g * G + r % G] * kLog2e;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (paged_sees(p, q0 + tk, j0 + tx * 4 + c)) sum[c] += ex2(s[i][c] - (lse == -CUDART_INF_F ? 0.f : lse));
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sm.p[tx * 4 + c][ty] = sum[c];
+      __syncthreads();
+      if (tid < kSlots && j0 + tid < len) {
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) total += sm.p[tid][i];
+        float *w = p.weight + (size_t(b) * p.Hkv + g) * size_t(p.track_stride) + j0 + tid;
+        if (total != 0.f) *w += total;   // (a NaN is not 0)
+      }
+    }
+    base += tiles;
+  }
+}
+
+template <typename F>
+int dispatch_fma(const glide_paged *h, F &&f) {
+  return dispatch_config(GLIDE_F32, h->cfg.head_dim, h->group, [&](auto, auto d, auto g) { return f(d, g); });
+}
+
+}  // namespace
+
+int setup_paged_fma(const glide_paged *h) {
+  return dispatch_fma(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value, kBytes = int(sizeof(Smem<D>));
+    return cudaFuncSetAttribute(paged_prefill_fma_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
+                   cudaFuncSetAttribute(paged_weights_fma_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess
+               ? int(GLIDE_OK)
+               : int(GLIDE_ERR_CUDA);
+  });
+}
+
+int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_fma(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    const int64_t grid = (p.n_tokens / (kRows / G) + p.batch) * p.Hkv;   // at most: each sequence's last tile may be short
+    if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
+    paged_prefill_fma_kernel<D, G><<<unsigned(grid), kThreads, sizeof(Smem<D>), st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+  });
+}
+
+int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
+  return dispatch_fma(h, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    const int64_t most = (int64_t(p.most) / kSlots + 1) * p.batch * p.Hkv;
+    const unsigned grid = unsigned(std::min<int64_t>(most, int64_t(p.sm_count) * (D == 64 ? 3 : 1)));
+    paged_weights_fma_kernel<D, G><<<grid, kThreads, sizeof(Smem<D>), st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+  });
+}
+
+}  // namespace glide

@@ -175,6 +175,7 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
       ok = encode_pages(fn, &h->kpage, h, h->k) && encode_pages(fn, &h->vpage, h, h->v) && setup_paged_tc(h) == GLIDE_OK;
     }
   }
+  if (ok && h->cfg.io_dtype == GLIDE_F32) ok = setup_paged_fma(h) == GLIDE_OK;
   ok = ok && setup_paged_decode(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
@@ -205,7 +206,8 @@ int glide_paged_prefill(glide_paged *h, const glide_paged_call *call, const void
     const int r = launch_paged_store(h, p, as_stream(stream));
     if (r) return r;
   }
-  return dev_out ? launch_paged_prefill(h, p, as_stream(stream)) : int(GLIDE_OK);
+  if (!dev_out) return GLIDE_OK;
+  return h->cfg.io_dtype == GLIDE_BF16 ? launch_paged_prefill_tc(h, p, as_stream(stream)) : launch_paged_prefill_fma(h, p, as_stream(stream));
 }
 
 int glide_paged_decode(glide_paged *h, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
@@ -228,7 +230,7 @@ int glide_paged_weights(glide_paged *h, const glide_paged_call *call, const void
   if (!dev_q || misaligned(dev_q) || !dev_lse || (reinterpret_cast<uintptr_t>(dev_lse) & 3u) || !p.weight) return GLIDE_ERR_INVALID_ARG;
   if (p.n_tokens == 0) return GLIDE_OK;
   p.q = dev_q, p.lse = const_cast<float *>(dev_lse);
-  return launch_paged_weights(h, p, as_stream(stream));
+  return h->cfg.io_dtype == GLIDE_BF16 ? launch_paged_weights_tc(h, p, as_stream(stream)) : launch_paged_weights_fma(h, p, as_stream(stream));
 }
 
 int glide_paged_evict(glide_paged *h, const glide_paged_call *call, int64_t budget, int64_t recent, float *dev_weight_out,
