@@ -56,7 +56,7 @@ struct PagedParams {
   int32_t *tickets;                   // [max_batch * Hkv] records left for a unit so far; 0 between calls
   float *records;                     // partial records of units that several blocks share
   float *logits;                      // [batch][Hkv][most][G]: scores of a decode step whose weights are kept
-  int32_t *moves;                     // (the same memory) evict: [batch][Hkv] counts, then [batch][Hkv][most / 2] pairs of slots
+  int32_t *moves;                     // (the same memory) evict: [batch][Hkv][most / 2] pairs of slots
   int32_t sm_count;
 };
 
@@ -110,5 +110,6 @@ size_t paged_record_bytes(const glide_paged_config &cfg);
 int setup_paged_decode(const glide_paged *h);   // what the device's context has to know of the kernels, once per handle
 int setup_paged_tc(const glide_paged *h);
 int setup_paged_fma(const glide_paged *h);
+int setup_paged_evict(const glide_paged *h);
 
 }  // namespace glide

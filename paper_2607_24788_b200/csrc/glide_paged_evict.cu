@@ -1,28 +1,47 @@
-// Eviction by accumulated attention weight: which slots leave (one block per sequence and KV head), and the moves of the kept ones.
+// Eviction by accumulated attention weight: which slots leave, and the moves of the kept ones (glide_paged_evict).
 //
-// The weights as unsigned numbers in the floats' order, protected slots above all others; e = len - kept slots leave: those
-// below the e-th least number T, and of those equal to T the lowest slots.  T is found digit by digit (four histograms of 8
-// bits).  One more pass in slot order lists the freed slots below the new length and the kept ones behind it, which are equally
-// many; the i-th of one moves into the i-th of the other.  Sources lie behind the new length and targets before it: no
-// move waits for another.
+// A cluster of up to 8 CTAs owns one (sequence, KV head), each CTA a run of its slots.  The weights become unsigned numbers in the floats'
+// order (protected slots above all others) and stay in shared memory; e = len - kept slots leave: those below the e-th least number T,
+// and of those equal to T the lowest slots.  T is found by digits of 11, 11 and 10 bits: a histogram per CTA, added up over the cluster
+// through distributed shared memory by every CTA for itself (one slot that leaves, as in the steady state of a decode loop, is found as
+// a minimum instead).  The freed slots below the new length and the kept ones behind it are listed in slot order; the i-th of one moves
+// into the i-th of the other: sources lie behind the new length and targets before it, so no move waits for another.
+// Bound: the chain of small steps (a meeting of the cluster per digit); the rows of many moves by memory.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
 #include "glide_device.cuh"
 #include "glide_paged.h"
+
+namespace cg = cooperative_groups;
 
 namespace glide {
 
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kItems = 4;             // consecutive slots of a thread
-constexpr int kMoveWarps = 8;
+constexpr int kBins = 2048;
+constexpr int kMostCluster = 8;
 
 struct EvictParams {
   int budget, recent;
   float *weight_out;
   int32_t *pos_out, *new_lens;
+  int keys;   // keys that fit in a CTA's shared memory
 };
 
-// exclusive sum over the block; total in `total`
+struct Smem {
+  int hist[2][kBins];     // (two: the next digit's counts while other CTAs still read this one's)
+  int warp_sums[32];
+  uint32_t digit;
+  int before;
+  int counts[2][3];       // this CTA's ties; then holes and movers
+  unsigned long long least[32];
+  unsigned long long cta_least;
+};
+
+// exclusive sum over the block; the whole in `total`
 __device__ __forceinline__ int block_scan(int x, int *warp_sums, int &total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int inc = x;
@@ -45,126 +64,216 @@ __device__ __forceinline__ int block_scan(int x, int *warp_sums, int &total) {
   return inc - x + __shfl_sync(0xffffffffu, w - s, warp);
 }
 
-__global__ void __launch_bounds__(kThreads) paged_evict_select_kernel(const __grid_constant__ PagedParams p, EvictParams e) {
-  __shared__ int hist[256];
-  __shared__ int warp_sums[32];
-  __shared__ uint32_t found_digit;
-  __shared__ int found_before;
-  const int unit = blockIdx.x, b = unit / p.Hkv;
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ EvictParams e) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
+  uint32_t *keys = reinterpret_cast<uint32_t *>(smem_raw + sizeof(Smem));
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ranks = int(cluster.num_blocks()), rank = int(cluster.block_rank()), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int unit = int(blockIdx.x) / ranks, b = unit / p.Hkv, g = unit - b * p.Hkv;
+  wait_for_predecessor();
   const int len = paged_len(p, b), kept = min(len, e.budget), leave = len - kept;
-  const float *weight = p.weight + size_t(unit) * size_t(p.track_stride);
-  const int32_t *pos = p.pos + size_t(unit) * size_t(p.track_stride);
-  float *weight_out = e.weight_out + size_t(unit) * size_t(p.track_stride);
-  int32_t *pos_out = e.pos_out + size_t(unit) * size_t(p.track_stride);
+  const size_t row = size_t(unit) * size_t(p.track_stride);
+  const float *weight = p.weight + row;
+  const int32_t *pos = p.pos + row;
+  float *weight_out = e.weight_out + row;
+  int32_t *pos_out = e.pos_out + row;
   const bool apart = weight_out != weight;
-  int32_t *pairs = p.moves + p.batch * p.Hkv + size_t(unit) * size_t(p.most);
+  int32_t *pairs = p.moves + size_t(unit) * size_t(p.most);   // (target, source)
   const int newest = p.seen[b] - e.recent;
   auto key_of = [&](int j) {
     const int at = pos[j];
-    if (at < p.n_sink || at >= newest) return 0xffffffffu;
     const float w = weight[j];
-    if (w != w) return 0xfffffffeu;
     const uint32_t x = __float_as_uint(w == 0.f ? 0.f : w);
-    return x & 0x80000000u ? ~x : x | 0x80000000u;
+    const uint32_t k = w != w ? 0xfffffffeu : x & 0x80000000u ? ~x : x | 0x80000000u;
+    return at < p.n_sink || at >= newest ? 0xffffffffu : k;
   };
-  uint32_t prefix = 0;
-  int rank = leave;   // the rank (from 1) of T among the slots that share the prefix
-  if (leave > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (threadIdx.x < 256) hist[threadIdx.x] = 0;
-      __syncthreads();
-      for (int j = threadIdx.x; j < len; j += kThreads) {
-        const uint32_t k = key_of(j);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+  // this CTA's slots: begin .. begin + n - 1; a thread's: `per` in a row, an odd number (the keys' banks)
+  const int share = (len + ranks - 1) / ranks, begin = min(len, rank * share), n = min(len, begin + share) - begin;
+  const int per = ((n + kThreads - 1) / kThreads) | 1;
+  const bool resident = n <= e.keys;
+  auto key = [&](int i) { return resident ? keys[i] : key_of(begin + i); };
+  if (resident && leave > 0) {
+#pragma unroll 4
+    for (int i = tid; i < n; i += kThreads) keys[i] = key_of(begin + i);
+  }
+  for (int i = tid; i < 2 * kBins; i += kThreads) (&sm.hist[0][0])[i] = 0;
+  cluster.sync();
+  // Every CTA of the unit has read the length: the new one may take its place once all units of the sequence have come here.
+  if (rank == 0 && tid == 0 && atomicAdd(&p.tickets[b], 1) == p.Hkv - 1) {
+    p.tickets[b] = 0;   // as the next call wants it
+    e.new_lens[b] = kept;
+  }
+  uint32_t least = 0;   // T
+  int quota = leave;    // slots equal to T that leave: the rank (from 1) of T among the slots that share the digits so far
+  if (leave == 1) {
+    unsigned long long best = ~0ull;
+    for (int i = tid; i < n; i += kThreads) {
+      const unsigned long long x = (static_cast<unsigned long long>(key(i)) << 32) | unsigned(begin + i);
+      best = x < best ? x : best;
+    }
+    auto warp_least = [](unsigned long long x) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long y = __shfl_xor_sync(0xffffffffu, x, o);
+        x = y < x ? y : x;
+      }
+      return x;
+    };
+    best = warp_least(best);
+    if (lane == 0) sm.least[warp] = best;
+    __syncthreads();
+    if (warp == 0) {
+      best = warp_least(sm.least[lane]);
+      if (lane == 0) sm.cta_least = best;
+    }
+    cluster.sync();
+    best = ~0ull;
+    for (int r = 0; r < ranks; ++r) {
+      const unsigned long long x = *cluster.map_shared_rank(&sm.cta_least, r);
+      best = x < best ? x : best;
+    }
+    least = uint32_t(best >> 32);
+  } else if (leave > 0) {
+#pragma unroll 1
+    for (int step = 0; step < 3; ++step) {
+      const int shift = step == 0 ? 21 : step == 1 ? 10 : 0, bits = step == 2 ? 10 : 11;
+      int *hist = sm.hist[step & 1];
+      if (step == 2) {   // (its first counts have been read by all: they met at the second step's)
+        for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+        __syncthreads();
+      }
+      for (int i = tid; i < n; i += kThreads) {
+        const uint32_t k = key(i);
+        if (step == 0 || (k >> (shift + bits)) == (least >> (shift + bits))) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1);
+      }
+      cluster.sync();
+      int c[2] = {0, 0};   // of bins 2 tid and 2 tid + 1
+      for (int r = 0; r < ranks; ++r) {
+        const int2 x = reinterpret_cast<const int2 *>(cluster.map_shared_rank(hist, r))[tid];
+        c[0] += x.x, c[1] += x.y;
+      }
+      int total;
+      int before = block_scan(c[0] + c[1], sm.warp_sums, total);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (before < quota && quota <= before + c[i]) sm.digit = uint32_t(2 * tid + i), sm.before = before;
+        before += c[i];
       }
       __syncthreads();
-      int total;
-      const int mine = threadIdx.x < 256 ? hist[threadIdx.x] : 0;
-      const int before = block_scan(mine, warp_sums, total);
-      if (before < rank && rank <= before + mine) found_digit = threadIdx.x, found_before = before;
-      __syncthreads();
-      prefix |= found_digit << shift;
-      rank -= found_before;
+      least |= sm.digit << shift;
+      quota -= sm.before;
     }
   }
-  int ties = 0, holes = 0, movers = 0;   // so far
-  const int slots = leave > 0 ? len : (apart ? kept : 0);
-  for (int base = 0; base < slots; base += kThreads * kItems) {
-    const int j0 = base + threadIdx.x * kItems;
-    uint32_t k[kItems];
-    int my_ties = 0;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      k[i] = j0 + i < len && leave > 0 ? key_of(j0 + i) : 0xffffffffu;
-      my_ties += j0 + i < len && leave > 0 && k[i] == prefix;
+  int moves = 0;
+  if (leave > 0) {
+    // ties of this thread, of the CTAs before
+    const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+    int ties = 0, total;
+    for (int i = i0; i < i1; ++i) ties += key(i) == least;
+    int tie = block_scan(ties, sm.warp_sums, total);
+    if (tid == 0) sm.counts[0][0] = total;
+    cluster.sync();
+    for (int r = 0; r < rank; ++r) tie += *cluster.map_shared_rank(&sm.counts[0][0], r);
+    auto gone = [&](uint32_t k, int &at) { return k < least || (k == least && at++ < quota); };
+    int holes = 0, movers = 0, at = tie;
+    for (int i = i0; i < i1; ++i) {
+      const bool out = gone(key(i), at);
+      holes += out && begin + i < kept;
+      movers += !out && begin + i >= kept;
     }
-    int total;
-    int tie = ties + block_scan(my_ties, warp_sums, total);
-    ties += total;
-    uint32_t gone = 0;
-    int my_holes = 0, my_movers = 0;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int j = j0 + i;
-      if (j >= len || leave == 0) continue;
-      const bool out = k[i] < prefix || (k[i] == prefix && tie++ < rank);
-      gone |= uint32_t(out) << i;
-      my_holes += out && j < kept;
-      my_movers += !out && j >= kept;
+    // (a CTA has both only where the new length lies inside its run)
+    int hole = block_scan(holes, sm.warp_sums, total);
+    if (tid == 0) sm.counts[1][0] = total;
+    int mover = block_scan(movers, sm.warp_sums, total);
+    if (tid == 0) sm.counts[1][1] = total;
+    cluster.sync();
+    for (int r = 0; r < ranks; ++r) {
+      const int *c = cluster.map_shared_rank(&sm.counts[1][0], r);
+      const int h = c[0];
+      if (r < rank) hole += h, mover += c[1];
+      moves += h;
     }
-    int hole = holes + block_scan(my_holes, warp_sums, total);
-    holes += total;
-    int mover = movers + block_scan(my_movers, warp_sums, total);
-    movers += total;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int j = j0 + i;
-      if (j >= len) continue;
-      const bool out = (gone >> i) & 1u;
+    at = tie;
+    for (int i = i0; i < i1; ++i) {
+      const int j = begin + i;
+      const bool out = gone(key(i), at);
       if (out && j < kept) pairs[2 * hole++] = j;
       if (!out && j >= kept) pairs[2 * mover++ + 1] = j;
-      if (apart && !out && j < kept) weight_out[j] = weight[j], pos_out[j] = pos[j];
     }
   }
-  if (threadIdx.x == 0) p.moves[unit] = holes;
+  if (apart) {
+    for (int j = begin + tid; j < min(begin + n, kept); j += kThreads) weight_out[j] = weight[j], pos_out[j] = pos[j];   // (holes: below)
+  }
+  cluster.sync();   // the lists are complete, and so is what the moves write over
+  // The moves: a lane looks one up, the warp copies them.
+  constexpr int kChunks = D * int(sizeof(T)) / 16;   // of a row
+  constexpr int kAtOnce = 32 / kChunks;              // rows that a warp copies at once
+  const T *k_pages = reinterpret_cast<const T *>(p.k);
+  const int64_t to_v = reinterpret_cast<const T *>(p.v) - k_pages;
+#pragma unroll 1
+  for (int m0 = (warp * ranks + rank) * 32; m0 < moves; m0 += ranks * kThreads) {
+    int64_t from = -1, to = 0;
+    if (m0 + lane < moves) {
+      const int dst = pairs[2 * (m0 + lane)], src = pairs[2 * (m0 + lane) + 1];
+      const int page_to = paged_page(p, b, dst), page_from = paged_page(p, b, src);
+      weight_out[dst] = weight[src], pos_out[dst] = pos[src];
+      if (page_to >= 0 && page_from >= 0) from = int64_t(paged_row(p, page_from, src, g)), to = int64_t(paged_row(p, page_to, dst, g));
+    }
+    const int some = min(32, moves - m0);
+#pragma unroll 4
+    for (int i = 0; i < some; i += kAtOnce) {
+      const int l = i + lane / kChunks;
+      const int64_t f = __shfl_sync(0xffffffffu, from, l), t = __shfl_sync(0xffffffffu, to, l);
+      if (l >= some || f < 0) continue;
+      const int c = (lane % kChunks) * (16 / int(sizeof(T)));
+      const uint4 x = *reinterpret_cast<const uint4 *>(k_pages + f + c), y = *reinterpret_cast<const uint4 *>(k_pages + to_v + f + c);
+      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + t + c) = x;
+      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + to_v + t + c) = y;
+    }
+  }
+  dependents_may_start();
 }
 
-// A warp per move.
 template <typename T, int D>
-__global__ void __launch_bounds__(kMoveWarps * 32) paged_evict_move_kernel(const __grid_constant__ PagedParams p, EvictParams e, int parts) {
-  constexpr int kChunks = D * int(sizeof(T)) / 16;
-  const int unit = blockIdx.x / parts, part = blockIdx.x - unit * parts, b = unit / p.Hkv, g = unit - b * p.Hkv;
-  const int lane = threadIdx.x & 31;
-  const int n = p.moves[unit];
-  const int32_t *pairs = p.moves + p.batch * p.Hkv + size_t(unit) * size_t(p.most);
-  const size_t at = size_t(unit) * size_t(p.track_stride);
-  for (int m = part * kMoveWarps + (threadIdx.x >> 5); m < n; m += parts * kMoveWarps) {
-    const int to = pairs[2 * m], from = pairs[2 * m + 1];
-    const int page_to = paged_page(p, b, to), page_from = paged_page(p, b, from);
-    if (lane == 0) e.weight_out[at + to] = p.weight[at + from], e.pos_out[at + to] = p.pos[at + from];
-    if (page_to < 0 || page_from < 0 || lane >= kChunks) continue;
-    const size_t row_to = paged_row(p, page_to, to, g), row_from = paged_row(p, page_from, from, g);
-    T *k = reinterpret_cast<T *>(p.k), *v = reinterpret_cast<T *>(p.v);
-    const uint4 a = reinterpret_cast<const uint4 *>(k + row_from)[lane], c = reinterpret_cast<const uint4 *>(v + row_from)[lane];
-    reinterpret_cast<uint4 *>(k + row_to)[lane] = a;
-    reinterpret_cast<uint4 *>(v + row_to)[lane] = c;
-  }
-  // (this thread alone reads and writes the sequence's length here: the two may be the same array)
-  if (part == 0 && g == 0 && threadIdx.x == 0) e.new_lens[b] = min(paged_len(p, b), e.budget);
+int launch(const PagedParams &p, EvictParams e, cudaStream_t st) {
+  const int units = p.batch * p.Hkv;
+  // CTAs of a unit: so many that each has some 4096 slots, no more than the chip has room for
+  int ranks = 1;
+  while (ranks < kMostCluster && int64_t(ranks) * 4096 < p.most && units * ranks * 2 <= p.sm_count) ranks *= 2;
+  e.keys = int(std::min<int64_t>((int64_t(p.most) + ranks - 1) / ranks, (200 * 1024 - int(sizeof(Smem))) / 4));
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(ranks), attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(units * ranks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem) + size_t(e.keys) * 4;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, paged_evict_kernel<T, D>, p, e) == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
 }
 
 }  // namespace
 
+int setup_paged_evict(const glide_paged *h) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
+    return cudaFuncSetAttribute(paged_evict_kernel<typename decltype(t)::type, decltype(d)::value>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                200 * 1024) == cudaSuccess
+               ? int(GLIDE_OK)
+               : int(GLIDE_ERR_CUDA);
+  });
+}
+
 int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, int recent, float *weight_out, int32_t *pos_out,
                        int32_t *new_lens, cudaStream_t st) {
-  const EvictParams e{budget, recent, weight_out, pos_out, new_lens};
-  const int units = p.batch * p.Hkv;
-  paged_evict_select_kernel<<<units, kThreads, 0, st>>>(p, e);
-  if (cudaGetLastError() != cudaSuccess) return GLIDE_ERR_CUDA;
-  const int parts = 16;
+  const EvictParams e{budget, recent, weight_out, pos_out, new_lens, 0};
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
-    paged_evict_move_kernel<typename decltype(t)::type, decltype(d)::value><<<units * parts, kMoveWarps * 32, 0, st>>>(p, e, parts);
-    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    return launch<typename decltype(t)::type, decltype(d)::value>(p, e, st);
   });
 }
 

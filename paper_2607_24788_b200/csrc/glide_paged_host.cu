@@ -56,9 +56,8 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   size_t at = kControlBytes + up256(size_t(c.max_batch) * size_t(c.n_kv_heads) * sizeof(int32_t));   // (tickets behind the status word)
   h->off_records = at;
   at += up256(paged_record_bytes(c));
-  h->off_track = at;   // a step's scores (H floats a slot), or an eviction's counts and moves (8 bytes for every second slot of a KV head)
-  if (c.weights)
-    at += up256(size_t(c.max_batch) * (size_t(c.n_q_heads) * size_t(c.max_tokens) + size_t(c.n_kv_heads)) * sizeof(float));
+  h->off_track = at;   // a step's scores (H floats a slot), or an eviction's moves (8 bytes for every second slot of a KV head)
+  if (c.weights) at += up256(size_t(c.max_batch) * size_t(c.n_q_heads) * size_t(c.max_tokens) * sizeof(float));
   h->total = at;
   return GLIDE_OK;
 }
@@ -176,7 +175,7 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
     }
   }
   if (ok && h->cfg.io_dtype == GLIDE_F32) ok = setup_paged_fma(h) == GLIDE_OK;
-  ok = ok && setup_paged_decode(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;
+  ok = ok && setup_paged_decode(h) == GLIDE_OK && setup_paged_evict(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
     delete h;
