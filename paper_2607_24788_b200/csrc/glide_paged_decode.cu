@@ -26,7 +26,6 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxGrid = 256;          // CTAs that the records are laid out for
-constexpr int kSlots = kWarps / 2;     // warps whose O is in shared memory at a time when a CTA's warps meet
 constexpr float kLazy = 8.0f;
 
 template <typename T, int D>
@@ -46,12 +45,13 @@ struct Shape {
 template <typename T, int D, int G>
 struct Smem {
   unsigned char ring[kWarps][Shape<T, D>::kStages][Shape<T, D>::kTileBytes];
+  static constexpr int kSlots = G == 8 ? kWarps / 2 : kWarps;         // warps whose O is here at a time when a CTA's warps meet
   float o[kSlots][G][D + 4];
   float m[kWarps][G], l[kWarps][G], e[kWarps][G];                     // maximum; sum of the weights as O has them; exact sum
   float q[sizeof(T) == 4 ? G : 1][D];                                 // fp32: the unit's queries, scaled
   float p[sizeof(T) == 4 ? kWarps : 1][Shape<T, D>::kTile][G];        // fp32: a tile's weights
   int len[kMaxPagedBatch], prefix[kMaxPagedBatch + 1];                // slots; tiles of the sequences before
-  int warp_sums[kWarps];
+  int warp_sums[kWarps], warp_most[kWarps];
   int last[2];   // whether this CTA left the last record of the units of its slots 0 and 1
 };
 
@@ -73,19 +73,21 @@ __device__ __forceinline__ SeqTiles tiles_of(const PagedParams &p, int len) {
   return s;
 }
 
-// Tiles of the sequences before each one, times the KV heads; every thread of the block.
+// Tiles of the sequences before each one, times the KV heads; every thread of the block.  Returns the most tiles of a unit.
 template <int TILE, int THREADS>
-__device__ __forceinline__ void prefix_of(const PagedParams &p, int *len, int *prefix, int *warp_sums) {
+__device__ __forceinline__ int prefix_of(const PagedParams &p, int *len, int *prefix, int *warp_sums, int *warp_most) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int base = 0;
+  int base = 0, most = 0;
   for (int b0 = 0; b0 < p.batch; b0 += THREADS) {
     const int b = b0 + int(threadIdx.x);
     int n = 0;
     if (b < p.batch) {
       const int l = paged_len(p, b);
       len[b] = l;
-      n = tiles_of<TILE>(p, l).n * p.Hkv;
+      n = tiles_of<TILE>(p, l).n;
     }
+    most = max(most, n);
+    n *= p.Hkv;
     int inc = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -102,8 +104,13 @@ __device__ __forceinline__ void prefix_of(const PagedParams &p, int *len, int *p
     }
     if (b < p.batch) prefix[b] = before + inc - n;
   }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) warp_most[warp] = most;
   if (threadIdx.x == 0) prefix[p.batch] = base;
   __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) most = max(most, warp_most[w]);
+  return most;
 }
 __device__ __forceinline__ int seq_of(const int *prefix, int batch, int f) {   // the sequence that tile f belongs to
   int lo = 0, hi = batch;
@@ -113,6 +120,8 @@ __device__ __forceinline__ int seq_of(const int *prefix, int batch, int f) {   /
   }
   return lo;
 }
+// What it costs to cut units, in tiles of a CTA: records, a ticket and the last CTA's additions.
+constexpr int kCutCost = 40;
 // Tiles of a CTA: at least one for each warp.
 __device__ __forceinline__ int share_of(int total, int grid) { return max((total + grid - 1) / grid, kWarps); }
 template <int D, int G>
@@ -389,37 +398,43 @@ __device__ __forceinline__ float part_factor(float m, float M) { return m == -CU
 template <typename T, int D, int G>
 __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, int c0, int c1, int t0, int share, bool keep) {
   const int tid = threadIdx.x, lane = tid & 31;
-  auto rec_of = [&](int c) { return record<D, G>(p, c, int64_t(c) * share >= t0 ? 0 : 1); };
-  constexpr int kEach = (G * D + kThreads - 1) / kThreads;   // outputs of a thread
-  constexpr int kBatch = 32 / kEach;                         // records whose values are on their way at a time
+  constexpr int kEach = (G * D + kThreads - 1) / kThreads;   // outputs of a thread; those of a warp are of one head each
+  constexpr int kRecord = G * (D + 3);
+  // (the code is kept short: few CTAs come here, and each fetches it anew)
   float M[kEach], L[kEach], X[kEach], sum[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) M[e] = -CUDART_INF_F, L[e] = X[e] = sum[e] = 0.f;
+  const int first = int64_t(c0) * share >= t0 ? 0 : 1;       // (the first CTA's other record where the unit begins inside its run)
 #pragma unroll 1
-  for (int c = c0; c <= c1; c += kBatch) {
-    const int some = min(kBatch, c1 + 1 - c);
-    float v[kEach][kBatch], m[kEach], l[kEach], x[kEach];
+  for (int c = c0; c <= c1; c += 32) {
+    const int some = min(32, c1 + 1 - c);
+    const float *rec = record<D, G>(p, c, 0), *rec0 = rec + (c == c0 ? first * kRecord : 0);
+    float f[kEach], part[kEach], top[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const int i = tid + e * kThreads, h = i / D;   // (h is the same in all lanes)
-      m[e] = -CUDART_INF_F, l[e] = x[e] = 0.f;       // of record c + lane
-      if (lane < some && i < G * D) {
-        const float *r = rec_of(c + lane) + G * D + h;
-        m[e] = __ldcg(r), l[e] = __ldcg(r + G), x[e] = __ldcg(r + 2 * G);
+      const int h = min((tid + e * kThreads) / D, G - 1);
+      float m = -CUDART_INF_F, l = 0.f, x = 0.f;             // of record c + lane
+      if (lane < some) {
+        const float *r = (lane ? rec + lane * 2 * kRecord : rec0) + G * D + h;
+        m = __ldcg(r), l = __ldcg(r + G), x = __ldcg(r + 2 * G);
       }
+      top[e] = warp_max(m);
+      f[e] = part_factor(m, top[e]);
+      const float ls = warp_sum(l * f[e]), xs = warp_sum(x * f[e]), now = fmaxf(M[e], top[e]), fa = part_factor(M[e], now);
+      L[e] = fmaf(L[e], fa, ls * part_factor(top[e], now)), X[e] = fmaf(X[e], fa, xs * part_factor(top[e], now));
+      sum[e] *= fa, part[e] = 0.f, M[e] = now;
+    }
+#pragma unroll 8
+    for (int k = 0; k < some; ++k) {
+      const float *r = (k ? rec + k * 2 * kRecord : rec0) + tid;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) v[e][k] = k < some && i < G * D ? __ldcg(rec_of(c + k) + i) : 0.f;
+      for (int e = 0; e < kEach; ++e) {
+        const float v = tid + e * kThreads < G * D ? __ldcg(r + e * kThreads) : 0.f;
+        part[e] = fmaf(v, __shfl_sync(0xffffffffu, f[e], k), part[e]);
+      }
     }
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const float top = warp_max(m[e]), f = part_factor(m[e], top);
-      float part = 0.f;
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) part = fmaf(v[e][k], __shfl_sync(0xffffffffu, f, k), part);
-      const float ls = warp_sum(l[e] * f), xs = warp_sum(x[e] * f);
-      const float now = fmaxf(M[e], top), fa = part_factor(M[e], now), fb = part_factor(top, now);
-      sum[e] = sum[e] * fa + part * fb, L[e] = L[e] * fa + ls * fb, X[e] = X[e] * fa + xs * fb, M[e] = now;
-    }
+    for (int e = 0; e < kEach; ++e) sum[e] = fmaf(part[e], part_factor(top[e], M[e]), sum[e]);
   }
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
@@ -442,9 +457,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
   auto &sm = *reinterpret_cast<Smem<T, D, G> *>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_for_predecessor();
-  prefix_of<Sh::kTile, kThreads>(p, sm.len, sm.prefix, sm.warp_sums);
-  const int total = sm.prefix[p.batch], share = share_of(total, int(gridDim.x));
-  const int lo = int(min(int64_t(total), int64_t(blockIdx.x) * share)), hi = min(total, lo + share);
+  const int most = prefix_of<Sh::kTile, kThreads>(p, sm.len, sm.prefix, sm.warp_sums, sm.warp_most);
+  const int total = sm.prefix[p.batch], share = share_of(total, int(gridDim.x)), units = p.batch * p.Hkv;
+  int lo = int(min(int64_t(total), int64_t(blockIdx.x) * share)), hi = min(total, lo + share);
+  if (units <= int(gridDim.x) && most <= share + kCutCost) {   // a unit for each CTA
+    const int u = min(int(blockIdx.x), units), b = u / p.Hkv, n = u < units ? (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv : 0;
+    lo = u < units ? sm.prefix[b] + (u - b * p.Hkv) * n : total;
+    hi = lo + n;
+  }
   const bool keep = p.weight != nullptr;
   const int mine = lo + warp < hi ? (hi - lo - warp - 1) / kWarps + 1 : 0;   // tiles of this warp: lo + warp + 8 i
 
@@ -464,15 +484,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     if (p.new_k && len - 1 - t.slot < Sh::kTile) t.rows |= kFresh | uint32_t(len - 1 - t.slot) << 16;
     return t;
   };
-  TileInfo now = look_up(lane), next;
-  if (mine > 32) next = look_up(32 + lane);
+  TileInfo now;
   uint32_t rows[S];   // of the tiles under way, the oldest first
   int slots[S];
   auto ask = [&](int i) {   // ask for this warp's tile i
 #pragma unroll
     for (int s = 0; s + 1 < S; ++s) rows[s] = rows[s + 1], slots[s] = slots[s + 1];
     if (i < mine) {
-      if (i && !(i & 31)) now = next, next = look_up(i + 32 + lane);
+      if (!(i & 31)) now = look_up(i + lane);
       const int64_t at = __shfl_sync(0xffffffffu, now.at, i & 31);
       const uint32_t mask = __shfl_sync(0xffffffffu, now.rows, i & 31);
       rows[S - 1] = mask;
@@ -510,6 +529,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     }
     cp_async_commit();
   };
+
+  // the first unit's queries, before the tiles that they would wait behind
+  if (lo < hi && warp == 0) {
+    const int b = seq_of(sm.prefix, p.batch, lo), g = (lo - sm.prefix[b]) / ((sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv);
+    if (lane < G * Sh::kRowBytes / 128)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char *>(reinterpret_cast<const T *>(p.q) + size_t(b) * size_t(p.q_stride) + size_t(g) * G * D) + lane * 128));
+  }
 #pragma unroll 1
   for (int s = 0; s < S; ++s) ask(s);
 
@@ -537,6 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
   }
 
   int cur = 0, cut[2] = {-1, -1};   // tiles done; the first tiles here of units that other CTAs share
+#pragma unroll 1
   for (int at = lo; at < hi;) {
     const int b = seq_of(sm.prefix, p.batch, at), n = (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv, g = (at - sm.prefix[b]) / n;
     const int t0 = sm.prefix[b] + g * n, end = min(hi, t0 + n);
@@ -567,10 +594,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       factor = part_factor(sm.m[warp][lane], M);
     }
     unit.scale(factor);
-    if (warp >= kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - kSlots][h][c] = x; });
+    constexpr int kSlots = Smem<T, D, G>::kSlots;
+    if (warp >= kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - (kWarps - kSlots)][h][c] = x; });
     __syncthreads();
-    if (warp < kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][c] += x; });
-    __syncthreads();
+    if (kSlots < kWarps) {
+      if (warp < kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][c] += x; });
+      __syncthreads();
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
     const bool whole = at == t0 && end == t0 + n;
     const int which = at == lo ? 0 : 1;
     float *rec = record<D, G>(p, int(blockIdx.x), which);
@@ -579,9 +610,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       float x = 0.f;
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) x += sm.o[s][h][c];
-      const float l = __shfl_sync(0xffffffffu, L, h);
+      const float f = __shfl_sync(0xffffffffu, inv, h);
       if (whole)
-        from_f32(reinterpret_cast<T *>(p.out) + size_t(b) * size_t(p.out_stride) + size_t(g * G + h) * D + c, l == 0.f ? 0.f : x / l);
+        from_f32(reinterpret_cast<T *>(p.out) + size_t(b) * size_t(p.out_stride) + size_t(g * G + h) * D + c, x * f);
       else
         rec[i] = x;
     }
@@ -653,10 +684,11 @@ int launch(const PagedParams &p, cudaStream_t st) {
   // tiles that the sequences can have at most: no more CTAs than their warps can have
   const int64_t longest = p.window < 0 ? p.most : std::min<int64_t>(p.most, int64_t(p.window) + p.n_sink + 2 * Sh::kTile);
   const int64_t tiles = (longest / Sh::kTile + 2) * p.Hkv * p.batch;
-  const int grid = int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kWarps - 1) / kWarps, p.sm_count, kMaxGrid})));
+  const int units = p.batch * p.Hkv;
+  int grid = int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kWarps - 1) / kWarps, p.sm_count, kMaxGrid})));
+  if (units <= std::min(p.sm_count, kMaxGrid)) grid = std::max(grid, units);
   if (launch_chained(paged_decode_kernel<T, D, G>, unsigned(grid), kThreads, sizeof(Smem<T, D, G>), st, p) != cudaSuccess) return GLIDE_ERR_CUDA;
   if (!p.weight) return GLIDE_OK;
-  const int units = p.batch * p.Hkv;
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(longest / (2 * kAccountThreads), p.sm_count * 8 / units)));
   if (launch_chained(paged_account_kernel<G, Sh::kTile>, unsigned(units * parts), kAccountThreads, 0, st, p, parts, D) != cudaSuccess)
     return GLIDE_ERR_CUDA;

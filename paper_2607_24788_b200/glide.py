@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -109,10 +110,10 @@ def load_library() -> ctypes.CDLL:
     lib.glide_paged_workspace_bytes.argtypes = [pagedp, ctypes.POINTER(ctypes.c_size_t)]
     lib.glide_paged_create.argtypes = [pagedp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
     lib.glide_paged_destroy.argtypes = [vp]
-    lib.glide_paged_prefill.argtypes = [vp, callp, vp, vp, vp, vp, vp, vp]
-    lib.glide_paged_decode.argtypes = [vp, callp, vp, vp, vp, vp, vp, vp]
-    lib.glide_paged_weights.argtypes = [vp, callp, vp, vp, vp]
-    lib.glide_paged_evict.argtypes = [vp, callp, i64, i64, vp, vp, vp, vp]
+    lib.glide_paged_prefill.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.glide_paged_decode.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.glide_paged_weights.argtypes = [vp, vp, vp, vp, vp]
+    lib.glide_paged_evict.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp]
     lib.glide_paged_check_call.argtypes = [pagedp, callp]
     lib.glide_paged_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.glide_strerror.argtypes = [ctypes.c_int]
@@ -436,107 +437,112 @@ class GlidePaged:
             _check(self.lib.glide_paged_create(ctypes.byref(self.cfg), k_pages.data_ptr(), v_pages.data_ptr(), base, self.workspace_bytes,
                                                _stream(None), ctypes.byref(handle)), "glide_paged_create")
         self._h = handle
-        self._call = glide_paged_call()
-        self._callp = ctypes.byref(self._call)
+        self._index = self.device.index
+        # the call's fields, written anew by every call (one pack instead of a store per field: a step's host time is what counts
+        # where the cache is short)
+        self._call = ctypes.create_string_buffer(ctypes.sizeof(glide_paged_call))
+        self._callp = ctypes.addressof(self._call)
+        self._pack = struct.Struct("@iiPiiqPPqqqqqPPPq").pack_into
+        assert struct.calcsize("@iiPiiqPPqqqqqPPPq") == ctypes.sizeof(glide_paged_call)
 
     def _ints(self, t: torch.Tensor, n: int, what: str) -> int:
-        assert t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous() and t.device == self.device, f"{what}: int32 [{n}] on {self.device}"
+        assert t.dtype is torch.int32 and t.dim() == 1 and t.size(0) == n and t.is_contiguous() and t.get_device() == self._index, \
+            f"{what}: int32 [{n}] on {self.device}"
         return t.data_ptr()
 
-    def _rows(self, t: torch.Tensor, heads: int, what: str):
-        """Address and token stride of [tokens][heads][d] whose heads lie side by side."""
-        assert t.dtype is self.dtype and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.d and t.device == self.device, what
+    def _rows(self, t: torch.Tensor, rows: int, heads: int, what: str):
+        """Address and token stride (0: side by side) of [rows][heads][d] whose heads lie side by side."""
+        assert (t.dtype is self.dtype and t.dim() == 3 and t.size(0) == rows and t.size(1) == heads and t.size(2) == self.d
+                and t.get_device() == self._index), f"{what}: {self.dtype} [{rows}][{heads}][{self.d}] on {self.device}"
+        if t.is_contiguous():
+            return t.data_ptr(), 0
         assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.d), f"{what}: a token's heads have to lie side by side"
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+        return t.data_ptr(), t.stride(0) if rows > 1 else 0
 
-    def _begin(self, layer: int, table: torch.Tensor, lens: torch.Tensor, window: int, n_sink: int, weight, pos, seen) -> glide_paged_call:
-        c = self._call
-        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.device == self.device, "table: int32 [B][cols]"
-        B, cols = table.shape
-        c.layer, c.batch, c.dev_table, c.table_cols = layer, B, table.data_ptr(), cols
-        c.table_stride = table.stride(0) if B > 1 else cols
-        c.dev_lens = self._ints(lens, B, "lens")
-        c.window, c.n_sink = window, n_sink
-        c.track_stride, c.dev_weight, c.dev_pos = 0, None, None
-        for t, dt in ((weight, torch.float32), (pos, torch.int32)):
-            if t is None:
-                continue
-            assert t.dtype is dt and t.dim() == 3 and t.shape[:2] == (B, self.Hkv) and t.is_contiguous() and t.device == self.device, \
-                "weight, pos: fp32, int32 [B][H_kv][slots]"
-            assert c.track_stride in (0, t.shape[2]), "weight and pos: as many slots"
-            c.track_stride = t.shape[2]
-            if dt is torch.float32:
-                c.dev_weight = t.data_ptr()
-            else:
-                c.dev_pos = t.data_ptr()
-        c.dev_seen = None if seen is None else self._ints(seen, B, "seen")
-        c.dev_starts = None
-        return c
+    def _track(self, t: torch.Tensor, B: int, dtype, what: str):
+        assert (t.dtype is dtype and t.dim() == 3 and t.size(0) == B and t.size(1) == self.Hkv and t.is_contiguous()
+                and t.get_device() == self._index), f"{what}: {dtype} [{B}][{self.Hkv}][slots] on {self.device}"
+        return t.data_ptr(), t.size(2)
 
     def _lse(self, lse, rows: int):
         if lse is None:
             return None
-        assert lse.dtype is torch.float32 and lse.shape == (rows, self.H) and lse.is_contiguous() and lse.device == self.device, "lse: fp32 [tokens][H]"
+        assert (lse.dtype is torch.float32 and lse.dim() == 2 and lse.size(0) == rows and lse.size(1) == self.H and lse.is_contiguous()
+                and lse.get_device() == self._index), f"lse: fp32 [{rows}][{self.H}] on {self.device}"
         return lse.data_ptr()
 
-    def _tensors(self, c: glide_paged_call, q, k, v, out, rows: int):
-        """Addresses of the call's tensors of `rows` tokens; their strides go to the call."""
-        pq = pk = pv = po = None
-        if q is not None:
-            pq, c.q_stride = self._rows(q, self.H, "q")
-            assert q.shape[0] == rows
-        assert (k is None) == (v is None)
-        if k is not None:
-            pk, c.kv_stride = self._rows(k, self.Hkv, "k")
-            pv, stride = self._rows(v, self.Hkv, "v")
-            assert k.shape[0] == rows and v.shape[0] == rows and stride == c.kv_stride, "k and v: equal strides"
-        if out is not None:
-            po, c.out_stride = self._rows(out, self.H, "out")
-            assert out.shape[0] == rows
-        return pq, pk, pv, po
-
-    def _launch(self, where: str, stream, fn, *args) -> None:
-        if self.device.index == _current_device():
-            rc = fn(self._h, *args, _stream(stream))
+    def _run(self, where: str, stream, fn, layer: int, table, lens, starts, rows, q, k, v, out, window: int, n_sink: int, weight, pos, seen, *args):
+        """Checks the tensors, writes the call and makes it: fn(handle, call, addresses of q, k, v, out as far as there are, *args)."""
+        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.get_device() == self._index, \
+            f"table: int32 [B][cols] on {self.device}"
+        B, cols = table.size(0), table.size(1)
+        if rows is None:
+            rows = B
+        p_starts = 0 if starts is None else self._ints(starts, B + 1, "starts")
+        q_stride = kv_stride = out_stride = p_weight = p_pos = track = 0
+        addresses = []
+        if q is not False:   # (False: this call has no such argument)
+            p_q = None
+            if q is not None:
+                p_q, q_stride = self._rows(q, rows, self.H, "q")
+            addresses.append(p_q)
+        if k is not False:
+            assert (k is None) == (v is None), "k and v: both or neither"
+            p_k = p_v = None
+            if k is not None:
+                p_k, kv_stride = self._rows(k, rows, self.Hkv, "k")
+                p_v, stride = self._rows(v, rows, self.Hkv, "v")
+                assert stride == kv_stride, "k and v: equal strides"
+            addresses += (p_k, p_v)
+        if out is not False:
+            p_out = None
+            if out is not None:
+                p_out, out_stride = self._rows(out, rows, self.H, "out")
+            addresses.append(p_out)
+        if weight is not None:
+            p_weight, track = self._track(weight, B, torch.float32, "weight")
+        if pos is not None:
+            p_pos, slots = self._track(pos, B, torch.int32, "pos")
+            assert track in (0, slots), "weight and pos: as many slots"
+            track = slots
+        self._pack(self._call, 0, layer, B, table.data_ptr(), cols, n_sink, table.stride(0) if B > 1 else cols, self._ints(lens, B, "lens"), p_starts,
+                   rows, q_stride, kv_stride, out_stride, window, p_weight, p_pos, 0 if seen is None else self._ints(seen, B, "seen"), track)
+        if self._index == _current_device():
+            rc = fn(self._h, self._callp, *addresses, *args, _stream(stream))
         else:
             with torch.cuda.device(self.device):
-                rc = fn(self._h, *args, _stream(stream))
+                rc = fn(self._h, self._callp, *addresses, *args, _stream(stream))
         if rc:
             _check(rc, where)
 
     def glide_paged_prefill(self, table, lens, starts, q, k, v, out=None, lse=None, window: int = -1, n_sink: int = 0, weight=None,
                             pos=None, seen=None, layer: int = 0, stream=None) -> None:
         """Stores the new tokens (rows starts[b] .. starts[b + 1] - 1 of k, v; None: they are in the cache) and, with out, attends."""
-        c = self._begin(layer, table, lens, window, n_sink, weight, pos, seen)
-        c.dev_starts = self._ints(starts, c.batch + 1, "starts")
-        c.n_tokens = (k if k is not None else q).shape[0]
-        pq, pk, pv, po = self._tensors(c, q, k, v, out, c.n_tokens)
-        self._launch("glide_paged_prefill", stream, self.lib.glide_paged_prefill, self._callp, pq, pk, pv, po, self._lse(lse, c.n_tokens))
+        rows = (k if k is not None else q).size(0)
+        self._run("glide_paged_prefill", stream, self.lib.glide_paged_prefill, layer, table, lens, starts, rows, q, k, v, out, window, n_sink,
+                  weight, pos, seen, self._lse(lse, rows))
 
     def glide_paged_decode(self, table, lens, q, k, v, out, lse=None, window: int = -1, n_sink: int = 0, weight=None, pos=None,
                            seen=None, layer: int = 0, stream=None) -> None:
         """One new token per sequence: stored at slot lens[b] - 1 (k, v None: it is in the cache), attends; weight: the account."""
-        c = self._begin(layer, table, lens, window, n_sink, weight, pos, seen)
-        pq, pk, pv, po = self._tensors(c, q, k, v, out, c.batch)
-        self._launch("glide_paged_decode", stream, self.lib.glide_paged_decode, self._callp, pq, pk, pv, po, self._lse(lse, c.batch))
+        self._run("glide_paged_decode", stream, self.lib.glide_paged_decode, layer, table, lens, None, None, q, k, v, out, window, n_sink,
+                  weight, pos, seen, self._lse(lse, table.size(0)))
 
     def glide_paged_weights(self, table, lens, starts, q, lse, weight, window: int = -1, n_sink: int = 0, layer: int = 0, stream=None) -> None:
         """Adds the weights that the tokens q with the row sums lse (of glide_paged_prefill) give every slot to the account."""
-        c = self._begin(layer, table, lens, window, n_sink, weight, None, None)
-        c.dev_starts = self._ints(starts, c.batch + 1, "starts")
-        c.n_tokens = q.shape[0]
-        pq = self._tensors(c, q, None, None, None, c.n_tokens)[0]
-        self._launch("glide_paged_weights", stream, self.lib.glide_paged_weights, self._callp, pq, self._lse(lse, c.n_tokens))
+        rows = q.size(0)
+        self._run("glide_paged_weights", stream, self.lib.glide_paged_weights, layer, table, lens, starts, rows, q, False, False, False, window,
+                  n_sink, weight, None, None, self._lse(lse, rows))
 
     def glide_paged_evict(self, table, lens, seen, weight, pos, budget: int, new_lens, recent: int = 0, n_sink: int = 0, weight_out=None,
                           pos_out=None, layer: int = 0, stream=None) -> None:
         """Every (sequence, KV head) keeps min(lens[b], budget) slots; weight_out, pos_out None: the account changes in place."""
-        c = self._begin(layer, table, lens, -1, n_sink, weight, pos, seen)
-        weight_out, pos_out = weight if weight_out is None else weight_out, pos if pos_out is None else pos_out
-        for t, like in ((weight_out, weight), (pos_out, pos)):
-            assert t.dtype is like.dtype and t.shape == like.shape and t.is_contiguous() and t.device == self.device
-        self._launch("glide_paged_evict", stream, self.lib.glide_paged_evict, self._callp, int(budget), int(recent), weight_out.data_ptr(),
-                     pos_out.data_ptr(), self._ints(new_lens, c.batch, "new_lens"))
+        B = table.size(0)
+        p_weight, slots = self._track(weight if weight_out is None else weight_out, B, torch.float32, "weight_out")
+        p_pos, pos_slots = self._track(pos if pos_out is None else pos_out, B, torch.int32, "pos_out")
+        assert slots == pos_slots == weight.size(2), "the accounts: as many slots"
+        self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, layer, table, lens, None, None, False, False, False, False, -1,
+                  n_sink, weight, pos, seen, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
 
     def glide_paged_device_status(self) -> int:
         """The status word of the device-side checks, read and cleared (0: nothing was recorded)."""
