@@ -34,6 +34,10 @@ constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
 constexpr float kLazy = 8.0f;
+// Of 16 pairs of weights, those that soft_tile makes by multiply-adds where their exact sum is not asked for (which would take the longer
+// polynomial).  8001 tokens, 32 / 8 heads: 487 us with 0, 474 with 4, 486 with 6, 506 with 8; 4 x 1000 tokens behind 131072 8.69, 8.52, 8.77,
+// 9.15 ms.  With exact sums 4 took 2 % longer than 0.
+constexpr int kByFma = 4;
 constexpr int kMostSlots = 1 << 30;
 
 struct PagedMaps {
@@ -119,23 +123,35 @@ __device__ __forceinline__ bool tile_seen(const PagedParams &p, int q0, int q1, 
   if (j0 > q1) return false;
   return p.window < 0 || (p.window > 0 && j0 + kKT - 1 > q0 - p.window) || j0 < p.n_sink;
 }
-// Lane i of a warp: page number of piece i of a key tile, one past the last page (zeros) where nothing of the piece is seen
-__device__ __forceinline__ int piece_page(const PagedParams &p, int b, int q0, int q1, int j0, int pieces, int rows, int none) {
+// Lane i of a warp: the table's entry for piece i of a key tile (looked at a tile later: nothing waits for it here), -1 where nothing
+// of the piece is seen
+__device__ __forceinline__ int piece_entry(const PagedParams &p, int b, int q0, int q1, int j0, int pieces, int rows) {
   const int lane = threadIdx.x & 31, s = j0 + lane * rows;
-  if (lane >= pieces || s > q1) return none;
-  if (p.window >= 0 && s >= p.n_sink && (p.window == 0 || s + rows - 1 <= q0 - p.window)) return none;
-  const int page = paged_page(p, b, s);
-  return page < 0 ? none : p.page0 + page;
+  if (lane >= pieces || s > q1) return -1;
+  if (p.window >= 0 && s >= p.n_sink && (p.window == 0 || s + rows - 1 <= q0 - p.window)) return -1;
+  return p.table[size_t(b) * size_t(p.table_stride) + size_t(s >> p.page_shift)];
 }
-// The tile of K or V: lane i asks for piece i, a box per 64 columns
+// ... its page number in the maps: `none` (one past the last page: zeros) where nothing is seen or the id is bad
+__device__ __forceinline__ int piece_page(const PagedParams &p, int entry, int q0, int q1, int j0, int pieces, int rows, int none) {
+  if (unsigned(entry) < unsigned(p.n_pages)) return p.page0 + entry;
+  const int lane = threadIdx.x & 31, s = j0 + lane * rows;
+  if (lane < pieces && s <= q1 && !(p.window >= 0 && s >= p.n_sink && (p.window == 0 || s + rows - 1 <= q0 - p.window)))
+    atomicExch(p.status, kDevBadPage);
+  return none;
+}
+// The tile of K or V, the whole warp: a box per piece and 64 columns.  (One lane with operands that are the same in all: lanes of
+// their own took 1000 cycles for four boxes.)
 template <int D>
-__device__ __forceinline__ void load_tile(const CUtensorMap *map, const PagedParams &p, uint32_t dst, int page, int j0, int g, int pieces, int rows,
-                                          uint32_t bar) {
-  const int lane = threadIdx.x & 31;
-  if (lane < pieces) {
-    const int off = (j0 + lane * rows) & ((1 << p.page_shift) - 1);
+__device__ __forceinline__ void load_tile(bool leader, const CUtensorMap *map, const PagedParams &p, uint32_t dst, int page, int j0, int g, int pieces,
+                                          int rows, uint32_t bar) {
+  const int mask = (1 << p.page_shift) - 1;
+#pragma unroll 1
+  for (int i = 0; i < pieces; ++i) {
+    const int pg = __shfl_sync(0xffffffffu, page, i);
+    if (leader) {
 #pragma unroll
-    for (int hf = 0; hf < D / 64; ++hf) tma_load_5d(dst + hf * kBoxBytes + lane * rows * 128, map, 0, hf, off, g, page, bar);
+      for (int hf = 0; hf < D / 64; ++hf) tma_load_5d(dst + hf * kBoxBytes + i * rows * 128, map, 0, hf, (j0 + i * rows) & mask, g, pg, bar);
+    }
   }
 }
 
@@ -321,7 +337,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int e = 0; e < 16; ++e) {
           float a0, a1;
           fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
-          a0 = ex2(a0), a1 = ex2(a1);
+          if (!LSE && !decltype(masked)::value && e < kByFma) exp2_fma<3>(a0, a1);
+          else a0 = ex2(a0), a1 = ex2(a1);
           if (LSE) add2(ex0, ex1, a0, a1);
           const uint32_t w2 = pack_bf16x2(a0, a1);
           mx2 = max_bf16x2(mx2, w2);
@@ -515,11 +532,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int hf = 0; hf < D / 64; ++hf) tma_load_3d(q_addr(x) + hf * kBoxBytes, &maps.q, hf * 64, g * G, row0 + tok0 + x * TOKT, bar);
       }
     }
-    int next = n_tiles ? piece_page(p, b, tq0, tq_last, kt.slot(0), pieces, rows, none) : 0;
+    const bool leader = elect_one();
+    int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
 #pragma unroll 1
     for (int k = 0; k < n_tiles && ok; ++k) {
-      const int j0 = kt.slot(k), page = next;
-      if (k + 1 < n_tiles) next = piece_page(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows, none);
+      const int j0 = kt.slot(k), page = piece_page(p, next, tq0, tq_last, j0, pieces, rows, none);
+      if (k + 1 < n_tiles) next = piece_entry(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows);
 #pragma unroll 1
       for (int is_v = 0; is_v < 2; ++is_v) {
         const int job = 2 * k + is_v, slot = job % S;
@@ -530,9 +548,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         // V rows behind the CTA's last token: whatever they hold, their weights are 0 and they have to be finite
         const bool tail = is_v && j0 + kKT - 1 > tq_last;
         const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
-        if (lane == 0) mbar_expect_tx(to, Sm::kTileBytes);
-        __syncwarp();
-        load_tile<D>(is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
+        if (leader) mbar_expect_tx(to, Sm::kTileBytes);
+        load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
         ++asked;
         if (tail) {
           ok = __all_sync(0xffffffffu, mbar_wait(to, 0u, failed));
@@ -776,19 +793,19 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     }
   } else {
     const int rows = min(1 << p.page_shift, kKT), pieces = kKT / rows;
+    const bool leader = elect_one();
     bool ok = true;
     int done = 0, kn = 0;
     for (int item = int(blockIdx.x); item < total && ok; item += int(gridDim.x)) {
       const KeyTile kt = key_tile<G>(p, sm.prefix, item);
       const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT, q0 = kt.len - kt.n_new;
       if (n == 0) continue;
-      const int page = piece_page(p, kt.b, q0 + kt.t0, q0 + kt.t1 - 1, kt.j0, pieces, rows, none);
+      const int page = piece_page(p, piece_entry(p, kt.b, q0 + kt.t0, q0 + kt.t1 - 1, kt.j0, pieces, rows), q0 + kt.t0, q0 + kt.t1 - 1, kt.j0, pieces, rows, none);
       if (kn >= 2) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_kfree[kn & 1]), uint32_t((kn >> 1) - 1) & 1u, failed));
       if (!ok) break;
       const uint32_t bar_k = smem_u32(&sm.bar_k[kn & 1]);
-      if (lane == 0) mbar_expect_tx(bar_k, Sm::kTileBytes);
-      __syncwarp();
-      load_tile<D>(&maps.k, p, smem_u32(sm.k[kn & 1]), page, kt.j0, kt.g, pieces, rows, bar_k);
+      if (leader) mbar_expect_tx(bar_k, Sm::kTileBytes);
+      load_tile<D>(leader, &maps.k, p, smem_u32(sm.k[kn & 1]), page, kt.j0, kt.g, pieces, rows, bar_k);
       ++kn;
       for (int i = 0; i < n; ++i) {
         const int t = done + i, st = t % kAccStages, tok = kt.t0 + i * TOKT;
@@ -804,7 +821,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (!ok) break;
         *reinterpret_cast<float4 *>(&sm.lse[st][lane * 4]) = make_float4(lse[0], lse[1], lse[2], lse[3]);
         __syncwarp();
-        if (lane == 0) {
+        if (leader) {
           const uint32_t bar = smem_u32(&sm.bar_full[st]);
           mbar_expect_tx(bar, Sm::kTileBytes);
           for (int hf = 0; hf < D / 64; ++hf)
