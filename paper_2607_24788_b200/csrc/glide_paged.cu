@@ -1,6 +1,7 @@
-// Paged attention: storing new tokens.
-#include "glide_device.cuh"
-#include "glide_paged.h"
+// Paged attention: storing new tokens; the parts of a prompt of few rows.
+#include <algorithm>
+
+#include "glide_paged_rows.cuh"
 
 namespace glide {
 
@@ -45,6 +46,48 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
   if (lane == 0 && p.pos) p.pos[at] = p.seen[b] - paged_len(p, b) + slot;
 }
 
+// One warp per (new token, query head): the records of the row's parts, added up in their order.
+template <typename T, int D>
+__global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_constant__ PagedParams p, int splits) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t item = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t r = item / p.H;
+  const int head = int(item - r * p.H);
+  wait_for_predecessor();
+  int b, i;
+  if (r >= p.n_tokens || !row_of(p, r, b, i)) return;
+  float M = -CUDART_INF_F, L = 0.f, X = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int s = 0; s < splits; ++s) M = fmaxf(M, split_record(p, D, s, size_t(r), head)[D]);
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float *rec = split_record(p, D, s, size_t(r), head);
+    const float4 tail = *reinterpret_cast<const float4 *>(rec + D);
+    if (tail.x == -CUDART_INF_F && tail.y == 0.f) continue;   // nothing seen there (and nothing of O written)
+    const float f = tail.x == -CUDART_INF_F ? 1.f : exp2f(tail.x - M);
+    float x[E];
+    load_elems<float, E>(rec + lane * E, x);
+    L = fmaf(tail.y, f, L), X = fmaf(tail.z, f, X);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(x[e], f, o[e]);
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  bool fine = true;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    o[e] *= inv;
+    fine &= isfinite(o[e]);
+    from_f32(reinterpret_cast<T *>(p.out) + size_t(r) * size_t(p.out_stride) + size_t(head) * D + lane * E + e, o[e]);
+  }
+  if (p.lse && lane == 0) p.lse[r * p.H + head] = PagedRow<T, D, 1>::paged_lse(M, X);
+  if (!__all_sync(0xffffffffu, fine)) {   // (0 times what a slot holds that the row does not see, for one)
+    PagedRow<T, D, 1> one;
+    one.attend(p, size_t(r), b, i, head / (p.H / p.Hkv), head, false);
+  }
+}
+
 unsigned blocks_of(int64_t items) { return unsigned((items + kWarps - 1) / kWarps); }
 int launched() {
   if (cudaGetLastError() == cudaSuccess) return GLIDE_OK;
@@ -57,6 +100,22 @@ int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t 
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
     paged_store_kernel<typename decltype(t)::type, decltype(d)::value><<<blocks_of(p.n_tokens * p.Hkv), kWarps * 32, 0, st>>>(p);
     return launched();
+  });
+}
+
+int paged_splits(const PagedParams &p, int64_t ctas, int tile) {
+  const int64_t longest = p.window < 0 ? p.most : std::min<int64_t>(p.most, int64_t(p.window) + p.n_sink + p.n_tokens);
+  const int64_t rows = p.n_tokens * p.H;
+  const int64_t most = std::min<int64_t>({p.sm_count / ctas, longest / (8 * tile), rows <= kSplitRows ? kSplitRows / rows : 1, 64});
+  return p.most <= 1024 || most < 2 ? 1 : int(most);
+}
+
+int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st) {
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
+    return launch_chained(paged_join_kernel<typename decltype(t)::type, decltype(d)::value>, blocks_of(p.n_tokens * p.H), kWarps * 32, 0, st, p,
+                          splits) == cudaSuccess
+               ? int(GLIDE_OK)
+               : int(GLIDE_ERR_CUDA);
   });
 }
 

@@ -98,6 +98,16 @@ __device__ __forceinline__ bool paged_sees(const PagedParams &p, int i, int j) {
   return j <= i && (p.window < 0 || j > i - p.window || j < p.n_sink);
 }
 
+// Prompts of few rows: the key tiles are cut into parts, each of which leaves a record per (token, query head): O [d] against 2^m, then m,
+// the sum that O goes with, the exact sum, 0.
+constexpr int kSplitRows = 16384;     // rows of all parts that the workspace has records for
+__device__ __forceinline__ float *split_record(const PagedParams &p, int head_dim, int part, size_t row, int head) {
+  return p.records + (size_t(part) * size_t(p.n_tokens) * size_t(p.H) + row * size_t(p.H) + size_t(head)) * size_t(head_dim + 4);
+}
+// (host) How many parts: so many that the CTAs fill the chip, of eight tiles at least, as far as the records reach.
+int paged_splits(const PagedParams &p, int64_t ctas, int tile);
+int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st);
+
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);    // bf16
 int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);

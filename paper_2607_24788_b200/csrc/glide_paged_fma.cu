@@ -72,12 +72,12 @@ __device__ __forceinline__ void scores(const float (&q)[D][kRows], const float (
 
 // Tiles of 64 slots that queries of slots [q0, q1] see: [0, sinks) and [first, end)
 struct SlotTiles {
-  int sinks, first, n;
-  __device__ __forceinline__ int slot(int k) const { return (k < sinks ? k : first + k - sinks) * kSlots; }
+  int sinks, first, n, t0;   // t0: the first one of this CTA's part
+  __device__ __forceinline__ int slot(int k) const { return (k + t0 < sinks ? k + t0 : first + k + t0 - sinks) * kSlots; }
 };
 __device__ __forceinline__ SlotTiles slot_tiles(const PagedParams &p, int q0, int q1) {
   const int end = q1 / kSlots + 1;
-  SlotTiles t{(min(p.n_sink, q1 + 1) + kSlots - 1) / kSlots, p.window < 0 ? 0 : p.window == 0 ? end : max(0, q0 - p.window + 1) / kSlots, 0};
+  SlotTiles t{(min(p.n_sink, q1 + 1) + kSlots - 1) / kSlots, p.window < 0 ? 0 : p.window == 0 ? end : max(0, q0 - p.window + 1) / kSlots, 0, 0};
   if (t.sinks > t.first) t.sinks = t.first = 0;
   t.n = t.sinks + end - t.first;
   return t;
@@ -128,7 +128,12 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
   const Place at = place_of(p, int(gridDim.x / unsigned(p.Hkv)) - 1 - int(blockIdx.x / unsigned(p.Hkv)), TOK);
   if (at.seq < 0) return;
   const int ntok = min(TOK, at.n_new - at.tok0), q0 = at.len - at.n_new + at.tok0, q1 = q0 + ntok - 1;
-  const SlotTiles st = slot_tiles(p, q0, q1);
+  SlotTiles st = slot_tiles(p, q0, q1);
+  if (gridDim.y > 1) {   // few rows behind long caches: each part of the tiles has a CTA, which leaves a record per row
+    const int all = st.n;
+    st.t0 = int(int64_t(all) * blockIdx.y / gridDim.y);
+    st.n = int(int64_t(all) * (blockIdx.y + 1) / gridDim.y) - st.t0;
+  }
   const int r_mine = tid & 63;   // the row of Q, K, V that this thread brings
   auto row_of = [&](const void *pages, int j) -> const float * {
     if (j > q1 || (p.window >= 0 && j <= q0 - p.window && j >= p.n_sink)) return nullptr;
@@ -213,6 +218,19 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int w = 1; w < 16; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+  }
+  if (gridDim.y > 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = ty * 4 + i;
+      if (r >= ntok * G) continue;
+      float *rec = split_record(p, D, blockIdx.y, size_t(at.row0 + at.tok0 + r / G), g * G + r % G);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        *reinterpret_cast<float4 *>(rec + n * 64 + tx * 4) = make_float4(o[i][n * 4], o[i][n * 4 + 1], o[i][n * 4 + 2], o[i][n * 4 + 3]);
+      if (tx == 0) *reinterpret_cast<float4 *>(rec + D) = make_float4(m[i], l[i], l[i], 0.f);
+    }
+    return;
   }
   unsigned again = 0;   // rows of this thread's four that are not finite
 #pragma unroll
@@ -330,8 +348,10 @@ int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStr
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     const int64_t grid = (p.n_tokens / (kRows / G) + p.batch) * p.Hkv;   // at most: each sequence's last tile may be short
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
-    paged_prefill_fma_kernel<D, G><<<unsigned(grid), kThreads, sizeof(Smem<D>), st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    const int splits = paged_splits(p, grid, kSlots);
+    paged_prefill_fma_kernel<D, G><<<dim3(unsigned(grid), unsigned(splits)), kThreads, sizeof(Smem<D>), st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
+    return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });
 }
 

@@ -55,7 +55,8 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   h->map_pages = int32_t(layer_pages * (c.n_layers - 1) + c.n_pages);
   size_t at = kControlBytes + up256(size_t(c.max_batch) * size_t(c.n_kv_heads) * sizeof(int32_t));   // (tickets behind the status word)
   h->off_records = at;
-  at += up256(paged_record_bytes(c));
+  // (a decode step's records, or those of a prompt of few rows behind a long cache)
+  at += up256(std::max(paged_record_bytes(c), c.max_tokens > 1024 ? size_t(kSplitRows) * size_t(c.head_dim + 4) * sizeof(float) : size_t(0)));
   h->off_track = at;   // a step's scores (H floats a slot), or an eviction's moves (8 bytes for every second slot of a KV head)
   if (c.weights) at += up256(size_t(c.max_batch) * size_t(c.n_q_heads) * size_t(c.max_tokens) * sizeof(float));
   h->total = at;

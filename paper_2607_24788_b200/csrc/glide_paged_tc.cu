@@ -105,11 +105,11 @@ __device__ __forceinline__ void issue_values(bool leader, uint32_t tmem_d, uint3
 
 // The key tiles of 128 slots that queries of slots [q0, q1] see: [0, sinks) and [first, end)
 struct KeyTiles {
-  int sinks, first, n;
-  __device__ __forceinline__ int slot(int k) const { return (k < sinks ? k : first + k - sinks) * kKT; }
+  int sinks, first, n, k0;   // k0: the first one of this CTA's part
+  __device__ __forceinline__ int slot(int k) const { return (k + k0 < sinks ? k + k0 : first + k + k0 - sinks) * kKT; }
 };
 __device__ __forceinline__ KeyTiles key_tiles(const PagedParams &p, int q0, int q1) {
-  KeyTiles t{0, 0, 0};
+  KeyTiles t{0, 0, 0, 0};
   const int end = q1 / kKT + 1;
   if (p.window != 0) t.first = p.window < 0 ? 0 : max(0, q0 - p.window + 1) / kKT;
   else t.first = end;
@@ -158,6 +158,7 @@ __device__ __forceinline__ void load_tile(bool leader, const CUtensorMap *map, c
 template <int D, int G, bool LSE>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none) {
+  // gridDim.y > 1: few rows behind long caches; each part of the key tiles has a CTA, which leaves a record per row
   using Sm = PrefillSmem<D>;
   constexpr int TOKT = kRows / G, TOKC = 2 * TOKT, S = Sm::kStages, kHalf = D / 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -209,7 +210,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   const int ntok = min(TOKC, n_new - tok0), ntokA = min(TOKT, ntok), ntokB = ntok - ntokA;
   const bool hasB = ntokB > 0;
   const int tq0 = len - n_new + tok0, tq_last = tq0 + ntok - 1;   // slots of the CTA's queries
-  const KeyTiles kt = key_tiles(p, tq0, tq_last);
+  KeyTiles kt = key_tiles(p, tq0, tq_last);
+  if (gridDim.y > 1) {
+    const int all = kt.n;
+    kt.k0 = int(int64_t(all) * blockIdx.y / gridDim.y);
+    kt.n = int(int64_t(all) * (blockIdx.y + 1) / gridDim.y) - kt.k0;
+  }
   const int n_tiles = kt.n;
   if (tid == 0) {
     const int n_rows = hasB ? 2 : 1;
@@ -426,6 +432,21 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
       const bool live = tok_r < ntokX;
+      const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
+      if (gridDim.y > 1) {
+        float *rec = split_record(p, D, blockIdx.y, out_row, g * G + row % G);
+#pragma unroll 1
+        for (int c0 = 0; c0 < kHalf && before >= 0; c0 += 32) {
+          uint32_t r[32];
+          tmem_ld32(tO + c0, r);
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            if (live && ok)
+              *reinterpret_cast<float4 *>(rec + H * kHalf + c0 + i) = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]),
+                                                                                  __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+        }
+        if (H == 0 && live && ok) *reinterpret_cast<float4 *>(rec + D) = make_float4(m_ref, l_row, x_row, 0.f);
+      } else {
       const float inv = live && before >= 0 && l_row != 0.f ? 1.0f / l_row : 0.f;
       float chk0 = 0.f, chk1 = 0.f;                 // finite if all values of the row are
 #pragma unroll 1
@@ -459,7 +480,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         const uint4 val = *reinterpret_cast<const uint4 *>(sm.q[X] + sw128(rr, c));
         if (ok && tk < ntokX) *reinterpret_cast<uint4 *>(obase + size_t(tk) * size_t(p.out_stride) + (rr - tk * G) * D) = val;
       }
-      const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
       if (LSE && H == 0 && live && ok) p.lse[out_row * p.H + g * G + row % G] = PagedRow<bf16, D, 1>::paged_lse(m_ref, x_row);
       // rows of which either half is not finite, by the first warp of the pair when both have stored
       const bool bad = live && (!isfinite((chk0 + chk1) * inv) || !isfinite(inv));
@@ -470,6 +490,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           PagedRow<bf16, D, 1> one;
           one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, false);   // (the sums of the scores were right)
         }
+      }
       }
     }
   } else if (warp < kLoadWarp) {
@@ -885,9 +906,12 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const int64_t grid = tiles * p.Hkv;
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
     const size_t bytes = sizeof(PrefillSmem<D>);
-    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
-    else paged_prefill_tc_kernel<D, G, false><<<unsigned(grid), kThreads, bytes, st>>>(p, maps, h->map_pages);
-    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    const int splits = paged_splits(p, grid, kKT);
+    dim3 blocks = dim3(unsigned(grid), unsigned(splits));
+    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);
+    else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);
+    if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
+    return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });
 }
 

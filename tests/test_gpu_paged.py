@@ -137,6 +137,23 @@ def test_prefill_a_few_tokens_behind_a_long_cache(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_few_tokens_behind_a_long_cache_that_is_not_finite_everywhere(dtype, value):
+    """Parts of the cache that some of the tokens do not see hold infinities and NaN."""
+    c = Cache([5000, 4000], [9, 3], 4, 2, 128, dtype, 64)
+    out, lse = run_prefill(c, 3000, 5)
+    want, tol, want_lse, lse_tol, _, _ = reference(c, 3000, 5)
+    check(out, want, tol, "out")
+    bad = 2004   # of sequence 0: seen by its queries 5000 .. 5003
+    page, off = c.place(0, torch.tensor(bad, device="cuda"))
+    c.v_pages[0][page, :, off] = value
+    got, got_lse = torch.empty_like(out), torch.empty_like(lse)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, None, None, got, lse=got_lse, window=3000, n_sink=5)
+    check(got[4:], want[4:], tol[4:], "out")
+    assert not got[:4].isfinite().any() and torch.equal(got_lse, lse)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_of_no_sequence_are_left_alone(dtype):
     c = Cache([20, 0], [30, 50], 4, 2, 64, dtype, 16)
     pad = lambda x: torch.cat([x, torch.full_like(x, math.nan)])  # noqa: E731
@@ -453,11 +470,12 @@ def test_two_handles_on_two_streams(dtype):
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     got = [[torch.empty_like(out) for _ in range(10)], [torch.empty_like(prompt) for _ in range(10)]]
+    lses = [torch.empty_like(lse) for _ in range(10)]
     for i in range(10):
         handles[0].glide_paged_decode(c.table, c.lens_dev, c.q, None, None, got[0][i], stream=streams[0])
-        handles[1].glide_paged_prefill(big.table, big.lens_dev, big.starts, big.q, None, None, got[1][i], stream=streams[1])
+        handles[1].glide_paged_prefill(big.table, big.lens_dev, big.starts, big.q, None, None, got[1][i], lse=lses[i], stream=streams[1])
     torch.cuda.synchronize()
-    assert all(torch.equal(x, out) for x in got[0]) and all(torch.equal(x, prompt) for x in got[1])
+    assert all(torch.equal(x, out) for x in got[0]) and all(torch.equal(x, prompt) for x in got[1]) and all(torch.equal(x, lse) for x in lses)
 
 
 def test_calls_back_to_back():
