@@ -52,7 +52,7 @@ struct PagedParams {
   float *weight;
   int32_t *pos;
   int64_t track_stride;
-  int32_t *status;
+  int32_t *status;                    // status word; behind it two counters, 0 between calls
   int32_t *tickets;                   // [max_batch * Hkv] records left for a unit so far; 0 between calls
   float *records;                     // partial records of units that several blocks share
   float *logits;                      // [batch][Hkv][most][G]: scores of a decode step whose weights are kept
@@ -104,8 +104,8 @@ constexpr int kSplitRows = 16384;     // rows of all parts that the workspace ha
 __device__ __forceinline__ float *split_record(const PagedParams &p, int head_dim, int part, size_t row, int head) {
   return p.records + (size_t(part) * size_t(p.n_tokens) * size_t(p.H) + row * size_t(p.H) + size_t(head)) * size_t(head_dim + 4);
 }
-// (host) How many parts: so many that the CTAs fill the chip, of eight tiles at least, as far as the records reach.
-int paged_splits(const PagedParams &p, int64_t ctas, int tile);
+// (host) How many parts: so many that the CTAs fill the chip, of `least` slots at least, as far as the records reach.
+int paged_splits(const PagedParams &p, int64_t ctas, int least);
 int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st);
 
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st);

@@ -348,7 +348,7 @@ int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStr
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     const int64_t grid = (p.n_tokens / (kRows / G) + p.batch) * p.Hkv;   // at most: each sequence's last tile may be short
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
-    const int splits = paged_splits(p, grid, kSlots);
+    const int splits = paged_splits(p, grid, 2 * kSlots);
     paged_prefill_fma_kernel<D, G><<<dim3(unsigned(grid), unsigned(splits)), kThreads, sizeof(Smem<D>), st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);

@@ -8,7 +8,7 @@
 //   warp 18            finds the CTA's rows, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
 // Keys come in tiles of 128 slots (multiples of 128): those that hold a visible first token, then those of the window.  Per tile and
 // row tile S = Q K^T into TMEM, the weights P = 2^(s - m) as bf16 over the consumed S columns against a reference m that moves (and O
-// with it) only when the row's maximum grows by more than 2^8, O += P V with V as the MN-major B operand.
+// with it) only when the row's maximum grows by more than 2^32, O += P V with V as the MN-major B operand.
 // TMEM columns: S_A [0,128) S_B [128,256) O_A [256,256+d) O_B behind it.
 // Nothing that a row does not see reaches it: scores are selected, not added to; slots behind the CTA's last token are zeros in V's
 // buffer; and a row whose output is not finite all the same (0 times an infinity or a NaN of a masked slot before them) is computed
@@ -33,7 +33,10 @@ constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
 constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
-constexpr float kLazy = 8.0f;
+// How far (in the exponent) scores may exceed a row's reference before it moves.  Weights, sums and O are floating numbers: the reference only
+// has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
+// pass over the tile: 8 sequences of up to 2048 tokens, windows of 256 with 4 first tokens 228 us with 8, 169 with 32, 171 with 64.
+constexpr float kLazy = 32.0f, kMostWeight = 0x1p32f;
 // Of 16 pairs of weights, those that soft_tile makes by multiply-adds where their exact sum is not asked for (which would take the longer
 // polynomial).  8001 tokens, 32 / 8 heads: 487 us with 0, 474 with 4, 486 with 6, 506 with 8; 4 x 1000 tokens behind 131072 8.69, 8.52, 8.77,
 // 9.15 ms.  With exact sums 4 took 2 % longer than 0.
@@ -329,6 +332,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     auto soft_tile = [&](auto masked, const Bounds &v) {
       float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
       const float mr = m_ref;
+      float odd0 = 0.f, odd1 = 0.f;                 // not finite if an argument of exp2_fma is not
       uint32_t pk[32], mx2 = 0u;
 #pragma unroll
       for (int c = 0; c < 64; c += 32) {
@@ -343,8 +347,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int e = 0; e < 16; ++e) {
           float a0, a1;
           fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
-          if (!LSE && !decltype(masked)::value && e < kByFma) exp2_fma<3>(a0, a1);
-          else a0 = ex2(a0), a1 = ex2(a1);
+          if (!LSE && !decltype(masked)::value && e < kByFma) {
+            add2(odd0, odd1, a0, a1);
+            exp2_fma<3>(a0, a1);
+          } else {
+            a0 = ex2(a0), a1 = ex2(a1);
+          }
           if (LSE) add2(ex0, ex1, a0, a1);
           const uint32_t w2 = pack_bf16x2(a0, a1);
           mx2 = max_bf16x2(mx2, w2);
@@ -353,7 +361,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         }
       }
       const float mx = fmaxf(bf16_lo(mx2), bf16_hi(mx2));
-      if (pair_any(!(mx < 0x1p8f))) return false;
+      if (pair_any(!(mx < kMostWeight) || !isfinite(odd0 + odd1))) return false;
       tmem_st32(tS, pk);
       l_sum += sum0 + sum1;
       if (LSE) x_sum += ex0 + ex1;
@@ -608,7 +616,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 
 // ---- the account of a prompt's weights ----------------------------------------------------------------------------------
 //
-// A CTA takes key tiles of 128 slots of one (sequence, KV head) in turns.  Per tile of 128 query rows (token * G + head) that may see the
+// A CTA takes key tiles of 128 slots of one (sequence, KV head) from a counter (the first ones have the most queries).  Per tile of 128 query rows (token * G + head) that may see the
 // slots, S^T = K Q^T with the slots on the TMEM lanes, so that a slot's weights 2^(s - lse) lie in one lane: each of its threads adds up
 // its own columns, and the four threads of a lane meet once per key tile.  No sum crosses a CTA, so nothing is added by atomics.
 //   warps 0-15   weights: warps 0-7 of the even query tiles, 8-15 of the odd ones, two threads per slot, 64 columns each
@@ -619,6 +627,9 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 constexpr int kAccThreads = 576;
 constexpr int kAccMmaWarp = 16, kAccLoadWarp = 17;
 constexpr int kAccStages = 4;
+// Of 8 pairs of a thread's weights, those made by multiply-adds (2 x 4096 tokens, prefill and account, 32 / 8 heads: 425 us with 0, 414 with 4
+// of the first pair of each four, 421 with 5, 442 with 8).
+constexpr int kAccByFma = 4;
 
 template <int D>
 struct AccountSmem {
@@ -632,6 +643,8 @@ struct AccountSmem {
   uint64_t bar_s[kAccStages];            // the product has completed
   uint64_t bar_sfree[kAccStages];        // S and the row sums have been read (one arrival per warp of the eight)
   uint32_t tmem_base;
+  uint64_t bar_item[2], bar_itemfree[2]; // the next key tile's number is there; all warps that go by it have read it
+  int item[2];
   int failed, total;
   int prefix[kMaxPagedBatch + 1];        // key tiles of the sequences before
 };
@@ -702,7 +715,10 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       sm.prefix[p.batch] = base;
       sm.total = base * p.Hkv;
       sm.failed = aligned ? 0 : 1;
-      for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sm.bar_k[i]), 1), mbar_init(smem_u32(&sm.bar_kfree[i]), 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&sm.bar_k[i]), 1), mbar_init(smem_u32(&sm.bar_kfree[i]), 1);
+        mbar_init(smem_u32(&sm.bar_item[i]), 1), mbar_init(smem_u32(&sm.bar_itemfree[i]), 17);
+      }
       for (int i = 0; i < kAccStages; ++i) {
         mbar_init(smem_u32(&sm.bar_full[i]), 1);
         mbar_init(smem_u32(&sm.bar_s[i]), 1);
@@ -719,6 +735,14 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   const int total = sm.total;
+  // The number of the CTA's i-th key tile, as the loader has drawn it; total or more: no further one.  (The whole warp; false: a time-out.)
+  auto next_item = [&](int i, int &item) {
+    const bool got = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_item[i & 1]), uint32_t(i >> 1) & 1u, failed));
+    item = got ? *reinterpret_cast<volatile int *>(&sm.item[i & 1]) : total;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.bar_itemfree[i & 1]));
+    return got && item < total;
+  };
 
   if (!aligned) {
     // (the status word tells)
@@ -727,7 +751,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + uint32_t(H) * 64u;
     bool ok = true;
     int done = 0;   // query tiles of the CTA's earlier key tiles
-    for (int item = int(blockIdx.x); item < total; item += int(gridDim.x)) {
+    for (int it = 0, item; next_item(it, item); ++it) {
       const KeyTile kt = key_tile<G>(p, sm.prefix, item);
       const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT, q0 = kt.len - kt.n_new, j = kt.j0 + slot;
       float sum0 = 0.f, sum1 = 0.f;
@@ -747,26 +771,41 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         const int until = p.window < 0 || j < p.n_sink ? TOKT : max(0, min(j - i0 + p.window, TOKT));
         const int hi = min(until, ntok) * G - 1;
         const bool whole = kt.j0 + kKT - 1 <= i0 && ntok == TOKT && (p.window < 0 || kt.j0 + kKT <= p.n_sink || i0 + TOKT - 1 < kt.j0 + p.window);
+        // false: an argument of exp2_fma was not finite, and nothing has been added
+        auto add_tile = [&](auto fast) {
+          float here0 = 0.f, here1 = 0.f, odd0 = 0.f, odd1 = 0.f;
 #pragma unroll
-        for (int c = 0; c < 64; c += 32) {
-          uint32_t x[32];
-          tmem_ld32(tS + uint32_t(st) * 128u + c, x);
-          const float4 *lse = reinterpret_cast<const float4 *>(&sm.lse[st][H * 64 + c]);
-          const uint32_t m = whole ? ~0u : column_mask(H * 64 + c, lo, hi);
+          for (int c = 0; c < 64; c += 32) {
+            uint32_t x[32];
+            tmem_ld32(tS + uint32_t(st) * 128u + c, x);
+            const float4 *lse = reinterpret_cast<const float4 *>(&sm.lse[st][H * 64 + c]);
+            const uint32_t m = column_mask(H * 64 + c, lo, hi);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float4 l4 = lse[e];
-            float a0, a1, a2, a3;
-            fma2v(a0, a1, __uint_as_float(x[e * 4]), __uint_as_float(x[e * 4 + 1]), p.scale_log2, l4.x, l4.y);
-            fma2v(a2, a3, __uint_as_float(x[e * 4 + 2]), __uint_as_float(x[e * 4 + 3]), p.scale_log2, l4.z, l4.w);
-            if (!whole) {
-              a0 = (m >> (e * 4)) & 1u ? a0 : -CUDART_INF_F, a1 = (m >> (e * 4 + 1)) & 1u ? a1 : -CUDART_INF_F;
-              a2 = (m >> (e * 4 + 2)) & 1u ? a2 : -CUDART_INF_F, a3 = (m >> (e * 4 + 3)) & 1u ? a3 : -CUDART_INF_F;
+            for (int e = 0; e < 8; ++e) {
+              const float4 l4 = lse[e];
+              float a0, a1, a2, a3;
+              fma2v(a0, a1, __uint_as_float(x[e * 4]), __uint_as_float(x[e * 4 + 1]), p.scale_log2, l4.x, l4.y);
+              fma2v(a2, a3, __uint_as_float(x[e * 4 + 2]), __uint_as_float(x[e * 4 + 3]), p.scale_log2, l4.z, l4.w);
+              if (decltype(fast)::value && e < kAccByFma) {
+                add2(odd0, odd1, a0, a1);
+                exp2_fma<5>(a0, a1);
+                a2 = ex2(a2), a3 = ex2(a3);
+              } else {
+                if (!decltype(fast)::value) {
+                  a0 = (m >> (e * 4)) & 1u ? a0 : -CUDART_INF_F, a1 = (m >> (e * 4 + 1)) & 1u ? a1 : -CUDART_INF_F;
+                  a2 = (m >> (e * 4 + 2)) & 1u ? a2 : -CUDART_INF_F, a3 = (m >> (e * 4 + 3)) & 1u ? a3 : -CUDART_INF_F;
+                }
+                a0 = ex2(a0), a1 = ex2(a1), a2 = ex2(a2), a3 = ex2(a3);
+              }
+              add2(here0, here1, a0, a1);
+              add2(here0, here1, a2, a3);
             }
-            add2(sum0, sum1, ex2(a0), ex2(a1));
-            add2(sum0, sum1, ex2(a2), ex2(a3));
           }
-        }
+          if (decltype(fast)::value && __any_sync(0xffffffffu, !isfinite(odd0 + odd1))) return false;
+          sum0 += here0, sum1 += here1;
+          return true;
+        };
+        if (!whole || !add_tile(std::true_type{})) add_tile(std::false_type{});
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.bar_sfree[st]));
@@ -792,7 +831,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       return ok;
     };
     int done = 0, kn = 0;   // query tiles, key tiles so far
-    for (int item = int(blockIdx.x); item < total && ok; item += int(gridDim.x)) {
+    for (int it = 0, item; ok && next_item(it, item); ++it) {
       const KeyTile kt = key_tile<G>(p, sm.prefix, item);
       const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT;
       if (n == 0) continue;
@@ -817,7 +856,18 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const bool leader = elect_one();
     bool ok = true;
     int done = 0, kn = 0;
-    for (int item = int(blockIdx.x); item < total && ok; item += int(gridDim.x)) {
+    int drawn = 0;
+    if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
+    for (int it = 0; ok; ++it) {
+      const int item = __shfl_sync(0xffffffffu, drawn, 0);
+      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_itemfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed));
+      if (!ok) break;
+      if (lane == 0) {
+        sm.item[it & 1] = item;
+        mbar_arrive(smem_u32(&sm.bar_item[it & 1]));
+        if (item < total) drawn = atomicAdd(p.status + 1, 1);
+      }
+      if (item >= total) break;
       const KeyTile kt = key_tile<G>(p, sm.prefix, item);
       const int n = (kt.t1 - kt.t0 + TOKT - 1) / TOKT, q0 = kt.len - kt.n_new;
       if (n == 0) continue;
@@ -859,7 +909,11 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   }
   tc_fence_before();
   __syncthreads();
-  if (tid == 0 && sm.failed) atomicExch(p.status, kDevWaitTimeout);
+  if (tid == 0) {
+    if (sm.failed) atomicExch(p.status, kDevWaitTimeout);
+    // the counters as the next call wants them: the last CTA has drawn its last number, and so have all
+    if (atomicAdd(p.status + 2, 1) == int(gridDim.x) - 1) p.status[1] = p.status[2] = 0;
+  }
   if (warp == kAccMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -906,7 +960,7 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const int64_t grid = tiles * p.Hkv;
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
     const size_t bytes = sizeof(PrefillSmem<D>);
-    const int splits = paged_splits(p, grid, kKT);
+    const int splits = paged_splits(p, grid, 4 * kKT);
     dim3 blocks = dim3(unsigned(grid), unsigned(splits));
     if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);
     else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);

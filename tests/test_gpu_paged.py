@@ -245,6 +245,26 @@ def test_values_that_are_not_finite_reach_who_sees_them_only(dtype, value):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_a_key_or_a_query_that_is_not_finite(dtype, value):
+    """... reaches every row, and the account of every slot, that it belongs to: one key at each place of a tile in turn."""
+    n = 700
+    c = Cache([0], [n], 2, 1, 64, dtype, 64)
+    weight = torch.zeros_like(c.weight)
+    for bad in range(0, 384, 13):
+        k, q = c.k.clone(), c.q.clone()
+        k[bad] = value          # (mixed signs of q: its scores are NaN)
+        out, lse = torch.empty_like(q), torch.empty(n, 2, device="cuda")
+        c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q, k, c.v, out)
+        assert out[bad:].isnan().all() and out[:bad].isfinite().all()
+        c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q, c.k, c.v, out, lse=lse)
+        q[bad + 300] = math.nan
+        weight.zero_()
+        c.handle.glide_paged_weights(c.table, c.lens_dev, c.starts, q, lse, weight)
+        assert weight[0, 0, :bad + 301].isnan().all() and weight[0, 0, bad + 301:n].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_scores_of_minus_infinity_and_large_ones(dtype):
     """A row whose scores are all -inf is 0; scores of a few thousand, of either sign, overflow nothing."""
     c = Cache([31, 31], [1, 1], 2, 1, 64, dtype, 16)
