@@ -2,8 +2,9 @@
 //
 // A cluster of up to 8 CTAs owns one (sequence, KV head), each CTA a run of its slots.  The weights become unsigned numbers in the floats'
 // order (protected slots above all others) and stay in shared memory; e = len - kept slots leave: those below the e-th least number T,
-// and of those equal to T the lowest slots.  T is found by digits of 11, 11 and 10 bits: a histogram per CTA, added up over the cluster
-// through distributed shared memory by every CTA for itself (one slot that leaves, as in the steady state of a decode loop, is found as
+// and of those equal to T the lowest slots.  T is found by four digits of 8 bits: a histogram per CTA, added up over the cluster
+// through distributed shared memory by every CTA for itself (three digits of 11, 11 and 10 bits took 22800 cycles for 32768 slots: 2048
+// counts of eight CTAs are read by each of them) (one slot that leaves, as in the steady state of a decode loop, is found as
 // a minimum instead).  The freed slots below the new length and the kept ones behind it are listed in slot order; the i-th of one moves
 // into the i-th of the other: sources lie behind the new length and targets before it, so no move waits for another.
 // Bound: the chain of small steps (a meeting of the cluster per digit); the rows of many moves by memory.
@@ -21,7 +22,7 @@ namespace glide {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kBins = 2048;
+constexpr int kBins = 256;
 constexpr int kMostCluster = 8;
 
 struct EvictParams {
@@ -35,8 +36,8 @@ struct Smem {
   int hist[2][kBins];     // (two: the next digit's counts while other CTAs still read this one's)
   int warp_sums[32];
   uint32_t digit;
-  int before;
-  int counts[2][3];       // this CTA's ties; then holes and movers
+  int before, ties_before;   // slots below the digit; slots of the digit in the CTAs before this one (of the last digit: equal to T)
+  int counts[2];          // this CTA's holes and movers
   unsigned long long least[32];
   unsigned long long cta_least;
 };
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     e.new_lens[b] = kept;
   }
   uint32_t least = 0;   // T
+  int least_before = 0; // (one slot that leaves) whether it lies in a CTA before this one
   int quota = leave;    // slots equal to T that leave: the rank (from 1) of T among the slots that share the digits so far
   if (leave == 1) {
     unsigned long long best = ~0ull;
@@ -135,32 +137,37 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
       best = x < best ? x : best;
     }
     least = uint32_t(best >> 32);
+    least_before = int(uint32_t(best)) < begin;   // (then no tie here leaves)
   } else if (leave > 0) {
 #pragma unroll 1
-    for (int step = 0; step < 3; ++step) {
-      const int shift = step == 0 ? 21 : step == 1 ? 10 : 0, bits = step == 2 ? 10 : 11;
+    for (int step = 0; step < 4; ++step) {
+      const int shift = 24 - 8 * step;
       int *hist = sm.hist[step & 1];
-      if (step == 2) {   // (its first counts have been read by all: they met at the second step's)
-        for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+      if (step >= 2) {   // (its first counts have been read by all: they have met since)
+        if (tid < kBins) hist[tid] = 0;
         __syncthreads();
       }
-      for (int i = tid; i < n; i += kThreads) {
-        const uint32_t k = key(i);
-        if (step == 0 || (k >> (shift + bits)) == (least >> (shift + bits))) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1);
+      for (int i0 = warp * 32; i0 < n; i0 += kThreads) {
+        const int i = i0 + lane;
+        const uint32_t k = i < n ? key(i) : 0u;
+        const bool in = i < n && (step == 0 || (k >> (shift + 8)) == (least >> (shift + 8)));
+        const uint32_t digit = in ? (k >> shift) & 255u : 256u;
+        const unsigned same = __match_any_sync(0xffffffffu, digit);   // (weights lie within a few octaves: lanes often share a bin)
+        if (in && lane == __ffs(int(same)) - 1) atomicAdd(&hist[digit], __popc(same));
       }
       cluster.sync();
-      int c[2] = {0, 0};   // of bins 2 tid and 2 tid + 1
-      for (int r = 0; r < ranks; ++r) {
-        const int2 x = reinterpret_cast<const int2 *>(cluster.map_shared_rank(hist, r))[tid];
-        c[0] += x.x, c[1] += x.y;
+      int c = 0, mine = 0;   // of bin tid: all CTAs', the ones before this CTA's
+      if (tid < kBins) {
+#pragma unroll
+        for (int r = 0; r < kMostCluster; ++r) {
+          const int x = r < ranks ? *cluster.map_shared_rank(hist + tid, r) : 0;
+          c += x;
+          mine += r < rank ? x : 0;
+        }
       }
       int total;
-      int before = block_scan(c[0] + c[1], sm.warp_sums, total);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (before < quota && quota <= before + c[i]) sm.digit = uint32_t(2 * tid + i), sm.before = before;
-        before += c[i];
-      }
+      const int before = block_scan(c, sm.warp_sums, total);
+      if (before < quota && quota <= before + c) sm.digit = uint32_t(tid), sm.before = before, sm.ties_before = mine;
       __syncthreads();
       least |= sm.digit << shift;
       quota -= sm.before;
@@ -168,14 +175,11 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
   }
   int moves = 0;
   if (leave > 0) {
-    // ties of this thread, of the CTAs before
+    // ties of the threads before (and the CTAs before: of one slot that leaves, the least of all, there is one)
     const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
     int ties = 0, total;
     for (int i = i0; i < i1; ++i) ties += key(i) == least;
-    int tie = block_scan(ties, sm.warp_sums, total);
-    if (tid == 0) sm.counts[0][0] = total;
-    cluster.sync();
-    for (int r = 0; r < rank; ++r) tie += *cluster.map_shared_rank(&sm.counts[0][0], r);
+    int tie = block_scan(ties, sm.warp_sums, total) + (leave > 1 ? sm.ties_before : least_before);
     auto gone = [&](uint32_t k, int &at) { return k < least || (k == least && at++ < quota); };
     int holes = 0, movers = 0, at = tie;
     for (int i = i0; i < i1; ++i) {
@@ -183,14 +187,13 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
       holes += out && begin + i < kept;
       movers += !out && begin + i >= kept;
     }
-    // (a CTA has both only where the new length lies inside its run)
-    int hole = block_scan(holes, sm.warp_sums, total);
-    if (tid == 0) sm.counts[1][0] = total;
-    int mover = block_scan(movers, sm.warp_sums, total);
-    if (tid == 0) sm.counts[1][1] = total;
+    int hole = block_scan(holes, sm.warp_sums, total), mover = 0, all_movers = 0;
+    const int all_holes = total;
+    if (begin + n > kept) mover = block_scan(movers, sm.warp_sums, all_movers);   // (the same for the CTA)
+    if (tid == 0) sm.counts[0] = all_holes, sm.counts[1] = all_movers;
     cluster.sync();
     for (int r = 0; r < ranks; ++r) {
-      const int *c = cluster.map_shared_rank(&sm.counts[1][0], r);
+      const int *c = cluster.map_shared_rank(&sm.counts[0], r);
       const int h = c[0];
       if (r < rank) hole += h, mover += c[1];
       moves += h;
@@ -210,27 +213,35 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
   // The moves: a lane looks one up, the warp copies them.
   constexpr int kChunks = D * int(sizeof(T)) / 16;   // of a row
   constexpr int kAtOnce = 32 / kChunks;              // rows that a warp copies at once
+  constexpr int kBatch = 4 * kAtOnce;                // moves of a warp at a time, all on their way together
   const T *k_pages = reinterpret_cast<const T *>(p.k);
   const int64_t to_v = reinterpret_cast<const T *>(p.v) - k_pages;
 #pragma unroll 1
-  for (int m0 = (warp * ranks + rank) * 32; m0 < moves; m0 += ranks * kThreads) {
+  for (int m0 = (warp * ranks + rank) * kBatch; m0 < moves; m0 += ranks * (kThreads / 32) * kBatch) {
     int64_t from = -1, to = 0;
-    if (m0 + lane < moves) {
+    if (lane < kBatch && m0 + lane < moves) {
       const int dst = pairs[2 * (m0 + lane)], src = pairs[2 * (m0 + lane) + 1];
       const int page_to = paged_page(p, b, dst), page_from = paged_page(p, b, src);
       weight_out[dst] = weight[src], pos_out[dst] = pos[src];
       if (page_to >= 0 && page_from >= 0) from = int64_t(paged_row(p, page_from, src, g)), to = int64_t(paged_row(p, page_to, dst, g));
     }
-    const int some = min(32, moves - m0);
-#pragma unroll 4
-    for (int i = 0; i < some; i += kAtOnce) {
-      const int l = i + lane / kChunks;
-      const int64_t f = __shfl_sync(0xffffffffu, from, l), t = __shfl_sync(0xffffffffu, to, l);
-      if (l >= some || f < 0) continue;
-      const int c = (lane % kChunks) * (16 / int(sizeof(T)));
-      const uint4 x = *reinterpret_cast<const uint4 *>(k_pages + f + c), y = *reinterpret_cast<const uint4 *>(k_pages + to_v + f + c);
-      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + t + c) = x;
-      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + to_v + t + c) = y;
+    const int some = min(kBatch, moves - m0);
+    const int c = (lane % kChunks) * (16 / int(sizeof(T)));
+    int64_t f[kBatch / kAtOnce], t[kBatch / kAtOnce];
+    uint4 x[kBatch / kAtOnce], y[kBatch / kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kBatch / kAtOnce; ++i) {
+      const int l = i * kAtOnce + lane / kChunks;
+      f[i] = __shfl_sync(0xffffffffu, from, l), t[i] = __shfl_sync(0xffffffffu, to, l);
+      if (l >= some) f[i] = -1;
+      if (f[i] < 0) continue;
+      x[i] = *reinterpret_cast<const uint4 *>(k_pages + f[i] + c), y[i] = *reinterpret_cast<const uint4 *>(k_pages + to_v + f[i] + c);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch / kAtOnce; ++i) {
+      if (f[i] < 0) continue;
+      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + t[i] + c) = x[i];
+      *reinterpret_cast<uint4 *>(const_cast<T *>(k_pages) + to_v + t[i] + c) = y[i];
     }
   }
   dependents_may_start();
