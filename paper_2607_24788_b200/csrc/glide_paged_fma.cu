@@ -2,7 +2,7 @@
 //
 // A CTA of 256 threads owns 64 query rows (token * G + head) of one (sequence, KV head) and goes through tiles of 64 slots; a thread
 // (ty, tx) of 16 x 16 has rows 4 ty .. 4 ty + 3 and slots 4 tx .. 4 tx + 3 of the scores and columns 4 tx .. (and 64 + 4 tx ..) of the
-// output.  Q and K lie in shared memory by feature, so that a step of the product takes two 16-byte reads for 16 multiply-adds; the
+// output.  Where that makes fewer CTAs than the GPU has SMs, a CTA owns 16 rows (the account: 16 slots), one per thread.  Q and K lie in shared memory by feature, so that a step of the product takes two 16-byte reads for 16 multiply-adds; the
 // next tile's rows are on their way in registers meanwhile.  Weights are taken against a reference that moves when a score exceeds
 // it by more than 8 in the exponent.  Bound: the multiply-adds.
 // What a row does not see does not reach it: scores are selected; rows of V that no row of the CTA sees are zeros; a row whose output
@@ -17,14 +17,30 @@ namespace glide {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 64, kSlots = 64;   // of a tile
-constexpr int kPad = kSlots + 4;
+constexpr int kSlots = 64;   // of a tile
 constexpr float kLazy = 8.0f;
 
-template <int D>
+// R rows per thread of the operand that the CTA keeps, 4 of the one that it goes through
+template <int D, int R>
 struct Smem {
-  float q[D][kRows], k[D][kPad], v[kSlots][D], p[kSlots][kPad];
+  static constexpr int kRows = 16 * R;
+  float q[D][kRows], k[D][kSlots + 4], v[kSlots][D], p[kSlots][kRows + 4];
 };
+template <int D, int R>
+struct AccountSmem {
+  static constexpr int kRows = 16 * R;
+  float k[D][kRows], q[D][kSlots + 4], lse[kSlots], part[kRows][17];
+};
+// the R rows of a thread side by side
+template <int R>
+__device__ __forceinline__ void load_rows(const float *from, float (&x)[R]) {
+  if constexpr (R == 4) {
+    const float4 v = *reinterpret_cast<const float4 *>(from);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+    x[0] = *from;
+  }
+}
 
 // Rows of 64 slots (or queries) on their way from memory: thread (r = tid & 63, c = tid >> 6) has 16-byte chunks c, c + 4, ... of row r
 template <int D>
@@ -37,8 +53,9 @@ struct Staged {
       x[i] = row ? reinterpret_cast<const float4 *>(row)[(threadIdx.x >> 6) + 4 * i] : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   template <int W>
-  __device__ __forceinline__ void store_by_feature(float (&to)[D][W], float scale) {
+  __device__ __forceinline__ void store_by_feature(float (&to)[D][W], float scale) {   // (rows beyond W: none are kept)
     const int r = threadIdx.x & 63;
+    if (W < kSlots && r >= W) return;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int c = ((threadIdx.x >> 6) + 4 * i) * 4;
@@ -51,22 +68,23 @@ struct Staged {
   }
 };
 
-// s[a][c] = row 4 ty + a of q times row 4 tx + c of k
-template <int D>
-__device__ __forceinline__ void scores(const float (&q)[D][kRows], const float (&k)[D][kPad], float (&s)[4][4]) {
+// s[a][c] = row R ty + a of `kept` times row 4 tx + c of `other`
+template <int D, int R>
+__device__ __forceinline__ void scores(const float (&kept)[D][16 * R], const float (&other)[D][kSlots + 4], float (&s)[R][4]) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+  for (int a = 0; a < R; ++a)
 #pragma unroll
     for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
 #pragma unroll 8
   for (int d = 0; d < D; ++d) {
-    const float4 x = *reinterpret_cast<const float4 *>(&q[d][ty * 4]), y = *reinterpret_cast<const float4 *>(&k[d][tx * 4]);
-    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float x[R], y[4];
+    load_rows<R>(&kept[d][ty * R], x);
+    load_rows<4>(&other[d][tx * 4], y);
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < R; ++a)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[a][c] = fmaf(xs[a], ys[c], s[a][c]);
+      for (int c = 0; c < 4; ++c) s[a][c] = fmaf(x[a], y[c], s[a][c]);
   }
 }
 
@@ -117,11 +135,11 @@ __device__ __forceinline__ Place place_of(const PagedParams &p, int want, int to
   return at;
 }
 
-template <int D, int G>
+template <int D, int G, int R>
 __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __grid_constant__ PagedParams p) {
-  constexpr int TOK = kRows / G, N = D / 64;
+  constexpr int TOK = 16 * R / G, N = D / 64;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  auto &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
+  auto &sm = *reinterpret_cast<Smem<D, R> *>(smem_raw);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int g = int(blockIdx.x % unsigned(p.Hkv));
   // (the last tokens, whose windows are the longest, first)
@@ -145,9 +163,9 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
                                  size_t(g * G + r_mine % G) * D
                            : nullptr);
   a.store_by_feature(sm.q, p.scale_log2);
-  float o[4][4 * N], m[4], l[4];
+  float o[R][4 * N], m[R], l[R];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < R; ++i) {
     m[i] = -CUDART_INF_F, l[i] = 0.f;
 #pragma unroll
     for (int c = 0; c < 4 * N; ++c) o[i][c] = 0.f;
@@ -161,13 +179,13 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     b.store(sm.v);
     __syncthreads();
     if (t + 1 < st.n) a.load(row_of(p.k, st.slot(t + 1) + r_mine)), b.load(row_of(p.v, st.slot(t + 1) + r_mine));
-    float s[4][4];
-    scores<D>(sm.q, sm.k, s);
+    float s[R][4];
+    scores<D, R>(sm.q, sm.k, s);
     const bool whole = j0 + kSlots - 1 <= q0 && (p.window < 0 || j0 > q1 - p.window || j0 + kSlots <= p.n_sink);
     bool grows = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int mine = q0 + (ty * 4 + i) / G;
+    for (int i = 0; i < R; ++i) {
+      const int mine = q0 + (ty * R + i) / G;
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         if (!whole && !paged_sees(p, mine, j0 + tx * 4 + c)) s[i][c] = -CUDART_INF_F;
@@ -176,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     }
     if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < R; ++i) {
         float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
         for (int w = 1; w < 16; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -189,25 +207,28 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
       const float ref = m[i] == -CUDART_INF_F ? 0.f : m[i];
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[i][c] = ex2(s[i][c] - ref), l[i] += s[i][c];
     }
     // (the rows of a warp's weights are read by that warp alone)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) *reinterpret_cast<float4 *>(&sm.p[tx * 4 + c][ty * 4]) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+    for (int c = 0; c < 4; ++c) {
+      if constexpr (R == 4) *reinterpret_cast<float4 *>(&sm.p[tx * 4 + c][ty * R]) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+      else sm.p[tx * 4 + c][ty] = s[0][c];
+    }
     __syncwarp();
 #pragma unroll 8
     for (int j = 0; j < kSlots; ++j) {
-      const float4 w = *reinterpret_cast<const float4 *>(&sm.p[j][ty * 4]);
-      const float ws[4] = {w.x, w.y, w.z, w.w};
+      float ws[R];
+      load_rows<R>(&sm.p[j][ty * R], ws);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const float4 v = *reinterpret_cast<const float4 *>(&sm.v[j][n * 64 + tx * 4]);
         const float vs[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < R; ++i)
 #pragma unroll
           for (int c = 0; c < 4; ++c) o[i][n * 4 + c] = fmaf(ws[i], vs[c], o[i][n * 4 + c]);
       }
@@ -215,14 +236,14 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     __syncwarp();
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < R; ++i) {
 #pragma unroll
     for (int w = 1; w < 16; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
   }
   if (gridDim.y > 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = ty * 4 + i;
+    for (int i = 0; i < R; ++i) {
+      const int r = ty * R + i;
       if (r >= ntok * G) continue;
       float *rec = split_record(p, D, blockIdx.y, size_t(at.row0 + at.tok0 + r / G), g * G + r % G);
 #pragma unroll
@@ -234,8 +255,8 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
   }
   unsigned again = 0;   // rows of this thread's four that are not finite
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i;
+  for (int i = 0; i < R; ++i) {
+    const int r = ty * R + i;
     if (r >= ntok * G) continue;
     const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
     float chk = inv;
@@ -253,71 +274,76 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
 #pragma unroll 1
   for (int half = 0; half < 2; ++half)   // the warp's two values of ty
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
       if (!__any_sync(0xffffffffu, ((tid >> 4) & 1) == half && ((again >> i) & 1u))) continue;
-      const int r = ((tid >> 5) * 2 + half) * 4 + i;
+      const int r = ((tid >> 5) * 2 + half) * R + i;
       PagedRow<float, D, 1> one;
       one.attend(p, size_t(at.row0 + at.tok0 + r / G), at.seq, q0 + r / G, g, g * G + r % G, false);   // (the sums of the scores were right)
     }
 }
 
-// A CTA takes tiles of 64 slots of one (sequence, KV head) in turns: the weights of all new tokens' rows, 64 at a time.  A thread adds up
-// its own rows' weights for its four slots; the 16 threads of a slot meet once per tile.
-template <int D, int G>
+// A CTA takes tiles of 16 R slots of one (sequence, KV head) in turns: the weights of all new tokens' rows, 64 at a time.  A thread adds up
+// its own rows' weights for its R slots; the 16 threads of a slot meet once per tile.
+template <int D, int G, int R>
 __global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __grid_constant__ PagedParams p) {
-  constexpr int TOK = kRows / G;
+  constexpr int TOK = kSlots / G, kKept = 16 * R;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  auto &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
+  auto &sm = *reinterpret_cast<AccountSmem<D, R> *>(smem_raw);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r_mine = tid & 63;
   int base = 0;   // tiles of the sequences before
   int64_t item = blockIdx.x;
   for (int b = 0; b < p.batch; ++b) {
     const int len = paged_len(p, b);
     int row0;
-    const int n_new = paged_new(p, b, len, row0), tiles = n_new ? (len + kSlots - 1) / kSlots : 0, q0 = len - n_new;
+    const int n_new = paged_new(p, b, len, row0), tiles = n_new ? (len + kKept - 1) / kKept : 0, q0 = len - n_new;
     for (; item < int64_t(base + tiles) * p.Hkv; item += gridDim.x) {
-      const int f = int(item / p.Hkv), g = int(item - int64_t(f) * p.Hkv), j0 = (f - base) * kSlots;
+      const int f = int(item / p.Hkv), g = int(item - int64_t(f) * p.Hkv), j0 = (f - base) * kKept;
       const int t0 = max(0, j0 - q0);
-      const int t1 = p.window >= 0 && j0 >= p.n_sink ? min(n_new, p.window == 0 ? 0 : j0 + kSlots - 1 + p.window - q0) : n_new;
+      const int t1 = p.window >= 0 && j0 >= p.n_sink ? min(n_new, p.window == 0 ? 0 : j0 + kKept - 1 + p.window - q0) : n_new;
       if (t0 >= t1) continue;
+      float lse = 0.f;   // of the row that this thread brings
       auto load_q = [&](int tok, Staged<D> &x) {
         const int tk = tok + r_mine / G;
         x.load(tk < t1 ? reinterpret_cast<const float *>(p.q) + size_t(row0 + tk) * size_t(p.q_stride) + size_t(g * G + r_mine % G) * D : nullptr);
+        lse = tk < t1 ? p.lse[size_t(row0 + tk) * p.H + g * G + r_mine % G] : 0.f;
       };
-      Staged<D> a;
+      Staged<D> a, k;
+      load_q(t0, a);
       {
-        const int j = j0 + r_mine, page = j < len ? paged_page(p, b, j) : -1;
-        a.load(page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g));
+        const int j = j0 + r_mine, page = r_mine < kKept && j < len ? paged_page(p, b, j) : -1;
+        k.load(page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g));
       }
       __syncthreads();   // the tile before has been read
-      a.store_by_feature(sm.k, 1.f);
-      load_q(t0, a);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      k.store_by_feature(sm.k, 1.f);
+      float sum[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) sum[i] = 0.f;
 #pragma unroll 1
       for (int tok = t0; tok < t1; tok += TOK) {
         __syncthreads();
         a.store_by_feature(sm.q, p.scale_log2);
+        if (tid < kSlots) sm.lse[r_mine] = lse == -CUDART_INF_F ? 0.f : lse * kLog2e;
         __syncthreads();
         if (tok + TOK < t1) load_q(tok + TOK, a);
-        float s[4][4];
-        scores<D>(sm.q, sm.k, s);
+        float s[R][4];
+        scores<D, R>(sm.k, sm.q, s);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = ty * 4 + i, tk = tok + r / G;
+        for (int c = 0; c < 4; ++c) {
+          const int tk = tok + (tx * 4 + c) / G;
           if (tk >= t1) continue;
-          const float lse = p.lse[size_t(row0 + tk) * p.H + g * G + r % G] * kLog2e;
+          const float x = sm.lse[tx * 4 + c];
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (paged_sees(p, q0 + tk, j0 + tx * 4 + c)) sum[c] += ex2(s[i][c] - (lse == -CUDART_INF_F ? 0.f : lse));
+          for (int i = 0; i < R; ++i)
+            if (paged_sees(p, q0 + tk, j0 + ty * R + i)) sum[i] += ex2(s[i][c] - x);
         }
       }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) sm.p[tx * 4 + c][ty] = sum[c];
+      for (int i = 0; i < R; ++i) sm.part[ty * R + i][tx] = sum[i];
       __syncthreads();
-      if (tid < kSlots && j0 + tid < len) {
+      if (tid < kKept && j0 + tid < len) {
         float total = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) total += sm.p[tid][i];
+        for (int i = 0; i < 16; ++i) total += sm.part[tid][i];
         float *w = p.weight + (size_t(b) * p.Hkv + g) * size_t(p.track_stride) + j0 + tid;
         if (total != 0.f) *w += total;   // (a NaN is not 0)
       }
@@ -335,9 +361,13 @@ int dispatch_fma(const glide_paged *h, F &&f) {
 
 int setup_paged_fma(const glide_paged *h) {
   return dispatch_fma(h, [&](auto d, auto g) {
-    constexpr int D = decltype(d)::value, G = decltype(g)::value, kBytes = int(sizeof(Smem<D>));
-    return cudaFuncSetAttribute(paged_prefill_fma_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
-                   cudaFuncSetAttribute(paged_weights_fma_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    auto set = [](auto kernel, size_t bytes) {
+      return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess;
+    };
+    return set(paged_prefill_fma_kernel<D, G, 4>, sizeof(Smem<D, 4>)) && set(paged_prefill_fma_kernel<D, G, 1>, sizeof(Smem<D, 1>)) &&
+                   set(paged_weights_fma_kernel<D, G, 4>, sizeof(AccountSmem<D, 4>)) &&
+                   set(paged_weights_fma_kernel<D, G, 1>, sizeof(AccountSmem<D, 1>))
                ? int(GLIDE_OK)
                : int(GLIDE_ERR_CUDA);
   });
@@ -346,10 +376,16 @@ int setup_paged_fma(const glide_paged *h) {
 int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
   return dispatch_fma(h, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    const int64_t grid = (p.n_tokens / (kRows / G) + p.batch) * p.Hkv;   // at most: each sequence's last tile may be short
-    if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
-    const int splits = paged_splits(p, grid, 2 * kSlots);
-    paged_prefill_fma_kernel<D, G><<<dim3(unsigned(grid), unsigned(splits)), kThreads, sizeof(Smem<D>), st>>>(p);
+    auto ctas = [&](int rows) { return (p.n_tokens / (rows / G) + p.batch) * p.Hkv; };   // at most: each sequence's last tile may be short
+    if (ctas(64) > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
+    // (512 tokens of 4 heads of 64, windows of 64: 36 CTAs of 64 rows or 132 of 16)
+    int splits = 1;
+    if (ctas(64) >= p.sm_count) {
+      paged_prefill_fma_kernel<D, G, 4><<<dim3(unsigned(ctas(64))), kThreads, sizeof(Smem<D, 4>), st>>>(p);
+    } else {
+      splits = paged_splits(p, ctas(16), 2 * kSlots);
+      paged_prefill_fma_kernel<D, G, 1><<<dim3(unsigned(ctas(16)), unsigned(splits)), kThreads, sizeof(Smem<D, 1>), st>>>(p);
+    }
     if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });
@@ -358,9 +394,12 @@ int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStr
 int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
   return dispatch_fma(h, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    const int64_t most = (int64_t(p.most) / kSlots + 1) * p.batch * p.Hkv;
-    const unsigned grid = unsigned(std::min<int64_t>(most, int64_t(p.sm_count) * (D == 64 ? 3 : 1)));
-    paged_weights_fma_kernel<D, G><<<grid, kThreads, sizeof(Smem<D>), st>>>(p);
+    auto tiles = [&](int slots) { return (int64_t(p.most) / slots + 1) * p.batch * p.Hkv; };
+    const int64_t room = int64_t(p.sm_count) * (D == 64 ? 4 : 2);
+    if (tiles(64) >= p.sm_count)
+      paged_weights_fma_kernel<D, G, 4><<<unsigned(std::min(tiles(64), room)), kThreads, sizeof(AccountSmem<D, 4>), st>>>(p);
+    else
+      paged_weights_fma_kernel<D, G, 1><<<unsigned(std::min(tiles(16), room)), kThreads, sizeof(AccountSmem<D, 1>), st>>>(p);
     return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
