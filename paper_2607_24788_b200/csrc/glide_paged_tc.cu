@@ -1,11 +1,13 @@
 // Paged attention of prompts on the 5th-generation tensor cores (tcgen05 + TMEM + TMA), bf16.
 //
-// One CTA (19 warps) owns 256 query rows of one (sequence, KV head): two row tiles X = A, B of 128 rows, a row being (new token, query
-// head of the group), row = token * G + head.
+// A CTA (19 warps, one per SM) draws pieces of work from a counter, the longest first: 256 query rows of one (sequence, KV head), two row
+// tiles X = A, B of 128 rows, a row being (new token, query head of the group), row = token * G + head; or, of few rows behind a long
+// cache, a part of their key tiles, of which it leaves a record per row.  While the softmax threads write one piece's outputs the
+// loader fetches the next one's keys.
 //   warps 0-3, 8-11    softmax of tile A: two threads per row (TMEM lane), 64 columns each
 //   warps 4-7, 12-15   softmax of tile B
 //   warps 16, 17       issue the tcgen05.mma of A and of B (one elected lane), in turns
-//   warp 18            finds the CTA's rows, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
+//   warp 18            draws and finds the work, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
 // Keys come in tiles of 128 slots (multiples of 128): those that hold a visible first token, then those of the window.  Per tile and
 // row tile S = Q K^T into TMEM, the weights P = 2^(s - m) as bf16 over the consumed S columns against a reference m that moves (and O
 // with it) only when the row's maximum grows by more than 2^32, O += P V with V as the MN-major B operand.
@@ -47,6 +49,11 @@ struct PagedMaps {
   CUtensorMap k, v, q;   // q: {d, H, tokens}, boxes of 64 columns x the G heads of a group x 128 / G tokens
 };
 
+// Tokens tok0 .. of sequence seq (< 0: there is no more), KV head g, part `part` of their key tiles
+struct Work {
+  int seq, tok0, g, part, len, n_new, row0;
+};
+
 template <int D>
 struct PrefillSmem {
   static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
@@ -60,9 +67,11 @@ struct PrefillSmem {
   uint64_t bar_p[2];                     // softmax threads of X -> MMA: P is ready (one arrival per warp)
   uint64_t bar_turn[2];                  // the other row tile's batch of products has been issued
   uint64_t bar_tail;                     // V of the last tile has landed (its last rows are zeroed behind that)
+  uint64_t bar_qfree[2];                 // the rows of X in the Q buffer have been read (one arrival per warp)
+  uint64_t bar_work[2], bar_workfree[2]; // the next piece of work stands here; every warp that goes by it has read it
+  Work work[2];
   uint32_t tmem_base;
   int failed;
-  int seq, tok0;                         // the CTA's sequence and first new token; seq < 0: no work
   float exch[kSoftmaxThreads / 2];       // a value of each row on its way between the row's two threads
 };
 
@@ -158,43 +167,71 @@ __device__ __forceinline__ void load_tile(bool leader, const CUtensorMap *map, c
   }
 }
 
+// Tiles of `tokens` new tokens of all sequences; a warp.
+__device__ __forceinline__ int count_tiles(const PagedParams &p, int tokens) {
+  int all = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int b = b0 + int(threadIdx.x & 31);
+    int row0, n = 0;
+    if (b < p.batch) n = paged_new(p, b, paged_len(p, b), row0);
+    all += __reduce_add_sync(0xffffffffu, (n + tokens - 1) / tokens);
+  }
+  return all;
+}
+// The `want`-th of them; a warp.
+__device__ __forceinline__ Work find_tile(const PagedParams &p, int want, int tokens) {
+  const int lane = threadIdx.x & 31;
+  Work w{-1, 0, 0, 0, 0, 0, 0};
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int b = b0 + lane;
+    int row0 = 0, n = 0, len = 0;
+    if (b < p.batch) len = paged_len(p, b), n = paged_new(p, b, len, row0);
+    const int tiles = (n + tokens - 1) / tokens;
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    const unsigned here = __ballot_sync(0xffffffffu, want < inc);
+    if (here) {
+      const int l = __ffs(int(here)) - 1;
+      w.seq = b0 + l;
+      w.tok0 = (want - __shfl_sync(0xffffffffu, inc - tiles, l)) * tokens;
+      w.len = __shfl_sync(0xffffffffu, len, l);
+      w.n_new = __shfl_sync(0xffffffffu, n, l);
+      w.row0 = __shfl_sync(0xffffffffu, row0, l);
+      return w;
+    }
+    want -= __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return w;
+}
+
 template <int D, int G, bool LSE>
 __global__ void __launch_bounds__(kThreads, 1)
-paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none) {
-  // gridDim.y > 1: few rows behind long caches; each part of the key tiles has a CTA, which leaves a record per row
+paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none, int parts) {
   using Sm = PrefillSmem<D>;
   constexpr int TOKT = kRows / G, TOKC = 2 * TOKT, S = Sm::kStages, kHalf = D / 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int *failed = &sm.failed;
-  const int g = int(blockIdx.x % unsigned(p.Hkv));
   const bool aligned = (smem_u32(smem_raw) & 1023u) == 0;   // (the swizzled tiles have to start on a multiple of 1024)
-  if (warp == kLoadWarp) {
-    // the CTA's rows: tiles of TOKC new tokens, counted through the sequences; the last ones, whose windows are the longest, first
-    int want = int(gridDim.x / unsigned(p.Hkv)) - 1 - int(blockIdx.x / unsigned(p.Hkv));
-    int seq = -1, tok0 = 0;
-    for (int b0 = 0; b0 < p.batch && seq < 0; b0 += 32) {
-      const int b = b0 + lane;
-      int row0, n = 0;
-      if (b < p.batch) n = paged_new(p, b, paged_len(p, b), row0);
-      const int tiles = (n + TOKC - 1) / TOKC;
-      int inc = tiles;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-      }
-      const unsigned here = __ballot_sync(0xffffffffu, want < inc);
-      if (here) {
-        const int l = __ffs(int(here)) - 1;
-        seq = b0 + l;
-        tok0 = (want - __shfl_sync(0xffffffffu, inc - tiles, l)) * TOKC;
-      } else {
-        want -= __shfl_sync(0xffffffffu, inc, 31);
-      }
+  if (warp == kLoadWarp && lane == 0) {
+    for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), 1), mbar_init(smem_u32(&sm.bar_free[s]), 2);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(smem_u32(&sm.bar_q[x]), 1);
+      mbar_init(smem_u32(&sm.bar_qfree[x]), kSoftmaxThreads / 32 / 2);
+      mbar_init(smem_u32(&sm.bar_s[x]), 1);
+      mbar_init(smem_u32(&sm.bar_turn[x]), 1);
+      mbar_init(smem_u32(&sm.bar_p[x]), kSoftmaxThreads / 32 / 2);
+      mbar_init(smem_u32(&sm.bar_work[x]), 1);
+      mbar_init(smem_u32(&sm.bar_workfree[x]), kLoadWarp);
     }
-    if (lane == 0) sm.seq = seq, sm.tok0 = tok0;
+    mbar_init(smem_u32(&sm.bar_tail), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sm.failed = aligned ? 0 : 1;
   } else if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -203,44 +240,42 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
-  const int b = sm.seq, tok0 = sm.tok0;
-  if (b < 0) {
-    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-    return;
-  }
-  int row0;
-  const int len = paged_len(p, b), n_new = paged_new(p, b, len, row0);
-  const int ntok = min(TOKC, n_new - tok0), ntokA = min(TOKT, ntok), ntokB = ntok - ntokA;
-  const bool hasB = ntokB > 0;
-  const int tq0 = len - n_new + tok0, tq_last = tq0 + ntok - 1;   // slots of the CTA's queries
-  KeyTiles kt = key_tiles(p, tq0, tq_last);
-  if (gridDim.y > 1) {
-    const int all = kt.n;
-    kt.k0 = int(int64_t(all) * blockIdx.y / gridDim.y);
-    kt.n = int(int64_t(all) * (blockIdx.y + 1) / gridDim.y) - kt.k0;
-  }
-  const int n_tiles = kt.n;
-  if (tid == 0) {
-    const int n_rows = hasB ? 2 : 1;
-    for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), 1), mbar_init(smem_u32(&sm.bar_free[s]), n_rows);
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(smem_u32(&sm.bar_q[x]), 1);
-      mbar_init(smem_u32(&sm.bar_s[x]), 1);
-      mbar_init(smem_u32(&sm.bar_turn[x]), 1);
-      mbar_init(smem_u32(&sm.bar_p[x]), kSoftmaxThreads / 32 / 2);
+  // The piece of work at hand, the same for all warps.  Counts that run on from piece to piece are each warp's own.
+  int b = 0, g = 0, tok0 = 0, row0 = 0, ntokA = 0, ntokB = 0, tq0 = 0, tq_last = 0, n_tiles = 0, part = 0;
+  KeyTiles kt{0, 0, 0, 0};
+  int jobs = 0;                                    // K and V tiles of the pieces before
+  auto set_work = [&](const Work &w) {
+    jobs += 2 * n_tiles;
+    b = w.seq, g = w.g, tok0 = w.tok0, row0 = w.row0, part = w.part;
+    const int ntok = min(TOKC, w.n_new - tok0);
+    ntokA = min(TOKT, ntok), ntokB = ntok - ntokA;
+    tq0 = w.len - w.n_new + tok0, tq_last = tq0 + ntok - 1;   // slots of the piece's queries
+    kt = key_tiles(p, tq0, tq_last);
+    if (parts > 1) {
+      const int all = kt.n;
+      kt.k0 = int(int64_t(all) * part / parts);
+      kt.n = int(int64_t(all) * (part + 1) / parts) - kt.k0;
     }
-    mbar_init(smem_u32(&sm.bar_tail), 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    sm.failed = aligned ? 0 : 1;
-  }
-  __syncthreads();
+    n_tiles = kt.n;
+  };
+  // Piece number i, as the loader has put it down (a whole warp; false: there is no more, or a time-out)
+  auto next_work = [&](int i) {
+    const bool got = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_work[i & 1]), uint32_t(i >> 1) & 1u, failed));
+    Work w{-1, 0, 0, 0, 0, 0, 0};
+    if (got) w = *const_cast<const Work *>(&sm.work[i & 1]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.bar_workfree[i & 1]));
+    if (w.seq < 0) return false;
+    set_work(w);
+    return true;
+  };
   const uint32_t sQ0 = smem_u32(sm.q[0]), sKV0 = smem_u32(sm.kv[0]);
   auto q_addr = [&](int x) { return sQ0 + uint32_t(x) * Sm::kTileBytes; };
   auto kv_addr = [&](int slot) { return sKV0 + uint32_t(slot) * Sm::kTileBytes; };
   // slots of row tile x's queries; whether it has key tile k
   auto x_q0 = [&](int x) { return tq0 + x * TOKT; };
   auto x_q1 = [&](int x) { return tq0 + x * TOKT + (x ? ntokB : ntokA) - 1; };
-  auto has = [&](int x, int k) { return k >= 0 && k < n_tiles && tile_seen(p, x_q0(x), x_q1(x), kt.slot(k)); };
+  auto has = [&](int x, int k) { return k >= 0 && k < n_tiles && (x == 0 || ntokB > 0) && tile_seen(p, x_q0(x), x_q1(x), kt.slot(k)); };
   auto last_of = [&](int x) {   // its last key tile; -1: none
     int k = n_tiles - 1;
     while (k >= 0 && !has(x, k)) --k;
@@ -254,13 +289,11 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     // What the row's two threads have in common goes through sm.exch behind barriers of the two warps, which every thread of a pair
     // passes equally often: after a time-out the waits return at once and the loops run on, storing nothing.
     const int X = (warp >> 2) & 1, H = warp >> 3, row = tid & 127;
-    const int ntokX = X ? ntokB : ntokA;
     const int tok_r = row / G;
-    const int mine = x_q0(X) + tok_r;               // this row's slot
     const uint32_t tS = tmem + (uint32_t((warp & 3) * 32) << 16) + uint32_t(X) * 128u + uint32_t(H) * 64u;
     const uint32_t tO = tmem + (uint32_t((warp & 3) * 32) << 16) + 256u + uint32_t(X) * D + uint32_t(H) * kHalf;
     float m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f;   // of this thread's columns: weights as O has them; exact ones
-    uint32_t n_s = 0;                               // batches of products waited for
+    uint32_t n_s = 0, n_q = 0;                      // batches of products waited for; Q tiles of X so far
     bool ok = true;
     auto wait_s = [&]() {
       if (ok) ok = mbar_wait(smem_u32(&sm.bar_s[X]), n_s & 1u, failed);
@@ -412,15 +445,21 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       l_sum += sum0 + sum1;
       if (LSE) x_sum += ex0 + ex1;
     };
-    if (ntokX > 0) {
+    for (int it = 0;; ++it) {
+      // (both warps of a pair stop together: after a time-out too)
+      if (pair_any(!next_work(it) || !ok)) break;
+      const int ntokX = X ? ntokB : ntokA;
+      if (ntokX == 0) continue;
+      const int mine = x_q0(X) + tok_r;             // this row's slot
+      m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f;
       const int w = p.window < 0 ? kMostSlots : p.window;
       int before = -1;                              // the key tile that this row tile had before
       for (int k = 0; k < n_tiles; ++k) {
         if (!has(X, k)) continue;
         wait_s();
         if (tid == X * kRows) {                     // S of the tile and P V of the tile before have completed
-          mbar_arrive(smem_u32(&sm.bar_free[2 * k % S]));
-          if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(2 * before + 1) % S]));
+          mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * k) % S]));
+          if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * before + 1) % S]));
         }
         const int j0 = kt.slot(k);
         const bool whole = j0 + kKT - 1 <= x_q0(X) && (j0 > x_q1(X) - w || j0 + kKT <= p.n_sink);
@@ -439,10 +478,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const float l_row = row_sum_of(l_sum);
       const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
+      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_q[X]), n_q & 1u, failed));   // (Q, which no product has waited for)
+      n_q += n_tiles != 0;
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
-      if (gridDim.y > 1) {
-        float *rec = split_record(p, D, blockIdx.y, out_row, g * G + row % G);
+      if (parts > 1) {
+        float *rec = split_record(p, D, part, out_row, g * G + row % G);
 #pragma unroll 1
         for (int c0 = 0; c0 < kHalf && before >= 0; c0 += 32) {
           uint32_t r[32];
@@ -500,6 +541,9 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         }
       }
       }
+      fence_async_smem();                           // (the next Q tile comes by TMA)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.bar_qfree[X]));
     }
   } else if (warp < kLoadWarp) {
     // =========================== MMA warps ===========================
@@ -508,106 +552,157 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const int x = __shfl_sync(0xffffffffu, warp, 0) - kMmaWarp;   // the row tile
     const uint32_t tS = tm + uint32_t(x) * 128u, tO = tm + 256u + uint32_t(x) * D;
-    const int last = x == 0 || hasB ? last_of(x) : -1;
-    uint32_t p_phase = 0;                          // parity of the next P
-    bool ok = x == 0 || hasB, first_s = true, first_o = true;
+    uint32_t n_p = 0, n_q = 0, n_turn = 0;          // operands P, Q tiles of x, turns so far
+    bool ok = true;
     auto wait = [&](uint64_t &bar, uint32_t parity) {
-      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, failed));
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity & 1u, failed));
       return ok;
     };
     auto commit = [&](uint64_t &bar) {
       if (leader) mma_commit(smem_u32(&bar));
     };
-    // k = -1: the first S product; then per key tile P V of the tile and S of the next one, the two row tiles in turns
-    for (int k = -1; k < n_tiles && ok; ++k) {
-      const int seqV = 2 * k + 1, seqK = 2 * k + 2;
-      const bool more = k + 1 < n_tiles, pv = has(x, k), qk = has(x, k + 1);
-      if (k >= 0) wait(sm.bar_full[seqV % S], uint32_t(seqV / S) & 1u);
-      if (ok && more) wait(sm.bar_full[seqK % S], uint32_t(seqK / S) & 1u);
-      if (ok && qk && first_s) wait(sm.bar_q[x], 0u);
-      if (ok && hasB && (x == 1 || k >= 0)) wait(sm.bar_turn[x], uint32_t(x == 1 ? k + 1 : k) & 1u);
-      if (ok && pv) {
-        wait(sm.bar_p[x], p_phase);
-        p_phase ^= 1u;
-        tc_fence_after();
+    for (int it = 0; ok && next_work(it); ++it) {
+      const int last = last_of(x);
+      bool first_s = true, first_o = true;
+      // k = -1: the first S product; then per key tile P V of the tile and S of the next one, the two row tiles in turns
+      for (int k = -1; k < n_tiles && ok; ++k, ++n_turn) {
+        const int seqV = jobs + 2 * k + 1, seqK = jobs + 2 * k + 2;
+        const bool more = k + 1 < n_tiles, pv = has(x, k), qk = has(x, k + 1);
+        if (k >= 0) wait(sm.bar_full[seqV % S], uint32_t(seqV / S));
+        if (ok && more) wait(sm.bar_full[seqK % S], uint32_t(seqK / S));
+        if (ok && qk && first_s) wait(sm.bar_q[x], n_q);
+        if (ok && (x == 1 || n_turn > 0)) wait(sm.bar_turn[x], x == 1 ? n_turn : n_turn - 1);
+        if (ok && pv) {
+          wait(sm.bar_p[x], n_p++);
+          tc_fence_after();
+        }
+        if (!ok) break;
+        if (pv) {
+          issue_values<D>(leader, tO, tS, kv_addr(seqV % S), !first_o);
+          first_o = false;
+          if (k == last) commit(sm.bar_s[x]);        // O is complete
+        }
+        if (qk) {
+          issue_scores<D>(leader, tS, q_addr(x), kv_addr(seqK % S));
+          first_s = false;
+          commit(sm.bar_s[x]);
+        }
+        if (leader) {
+          mbar_arrive(smem_u32(&sm.bar_turn[x ^ 1]));
+          if (pv && k == last) mma_commit(smem_u32(&sm.bar_free[seqV % S]));
+          if (!pv && k >= 0) mbar_arrive(smem_u32(&sm.bar_free[seqV % S]));   // (a tile of which this row tile sees nothing)
+          if (!qk && more) mbar_arrive(smem_u32(&sm.bar_free[seqK % S]));
+        }
       }
-      if (!ok) break;
-      if (pv) {
-        issue_values<D>(leader, tO, tS, kv_addr(seqV % S), !first_o);
-        first_o = false;
-        if (k == last) commit(sm.bar_s[x]);        // O is complete
-      }
-      if (qk) {
-        issue_scores<D>(leader, tS, q_addr(x), kv_addr(seqK % S));
-        first_s = false;
-        commit(sm.bar_s[x]);
-      }
-      if (leader) {
-        if (hasB) mbar_arrive(smem_u32(&sm.bar_turn[x ^ 1]));
-        if (pv && k == last) mma_commit(smem_u32(&sm.bar_free[seqV % S]));
-        if (!pv && k >= 0) mbar_arrive(smem_u32(&sm.bar_free[seqV % S]));   // (a tile of which this row tile sees nothing)
-        if (!qk && more) mbar_arrive(smem_u32(&sm.bar_free[seqK % S]));
-      }
+      n_q += n_tiles && (x == 0 || ntokB > 0) ? 1u : 0u;
     }
   } else {
     // =========================== loader warp ===========================
     const int rows = min(1 << p.page_shift, kKT), pieces = kKT / rows;
-    bool ok = true;
-    int asked = 0;                                 // K and V tiles
-    if (lane == 0) {
-      for (int x = 0; x < (hasB && n_tiles ? 2 : n_tiles ? 1 : 0); ++x) {
-        const uint32_t bar = smem_u32(&sm.bar_q[x]);
-        mbar_expect_tx(bar, Sm::kTileBytes);
-        for (int hf = 0; hf < D / 64; ++hf) tma_load_3d(q_addr(x) + hf * kBoxBytes, &maps.q, hf * 64, g * G, row0 + tok0 + x * TOKT, bar);
-      }
-    }
     const bool leader = elect_one();
-    int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
+    const int tiles = count_tiles(p, TOKC), total = tiles * p.Hkv * parts;
+    bool ok = true;
+    uint32_t n_q[2] = {0, 0}, n_use[2] = {0, 0}, n_tail = 0;   // Q tiles, pieces with rows in X, tails so far
+    int asked = 0;                                 // K and V tiles
+    int drawn = 0;
+    if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
+    for (int it = 0; ok; ++it) {
+      // the last tokens, whose windows are the longest, first
+      const int item = __shfl_sync(0xffffffffu, drawn, 0);
+      Work w{-1, 0, 0, 0, 0, 0, 0};
+      if (item < total) {
+        const int t = item / (p.Hkv * parts), rest = item - t * p.Hkv * parts;
+        w = find_tile(p, tiles - 1 - t, TOKC);
+        w.g = rest / parts, w.part = rest - w.g * parts;
+      }
+      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_workfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed));
+      if (!ok) break;
+      if (lane == 0) {
+        sm.work[it & 1] = w;
+        mbar_arrive(smem_u32(&sm.bar_work[it & 1]));
+        if (w.seq >= 0) drawn = atomicAdd(p.status + 1, 1);
+      }
+      if (w.seq < 0) break;
+      set_work(w);
+      int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
+      // The first tiles may come while the piece before is still being written out, Q_X when its rows have been.
+      auto ask_q = [&](int x) {
+        if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed));
+        ++n_use[x];
+        if (!ok || !n_tiles) return;
+        ++n_q[x];
+        if (leader) {
+          const uint32_t bar = smem_u32(&sm.bar_q[x]);
+          mbar_expect_tx(bar, Sm::kTileBytes);
+          for (int hf = 0; hf < D / 64; ++hf) tma_load_3d(q_addr(x) + hf * kBoxBytes, &maps.q, hf * 64, g * G, row0 + tok0 + x * TOKT, bar);
+        }
+      };
+      const int latest = min(2 * n_tiles, S - 1) - 1;   // the tile behind which Q is waited for (no product is needed for those before it)
+      bool q_asked = false;
+      if (n_tiles == 0) {
+        ask_q(0);
+        if (ok && ntokB) ask_q(1);
+      }
 #pragma unroll 1
-    for (int k = 0; k < n_tiles && ok; ++k) {
-      const int j0 = kt.slot(k), page = piece_page(p, next, tq0, tq_last, j0, pieces, rows, none);
-      if (k + 1 < n_tiles) next = piece_entry(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows);
+      for (int k = 0; k < n_tiles && ok; ++k) {
+        const int j0 = kt.slot(k), page = piece_page(p, next, tq0, tq_last, j0, pieces, rows, none);
+        if (k + 1 < n_tiles) next = piece_entry(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows);
 #pragma unroll 1
-      for (int is_v = 0; is_v < 2; ++is_v) {
-        const int job = 2 * k + is_v, slot = job % S;
-        const uint32_t bar = smem_u32(&sm.bar_full[slot]);
-        if (job >= S) ok = mbar_wait(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        // V rows behind the CTA's last token: whatever they hold, their weights are 0 and they have to be finite
-        const bool tail = is_v && j0 + kKT - 1 > tq_last;
-        const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
-        if (leader) mbar_expect_tx(to, Sm::kTileBytes);
-        load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
-        ++asked;
-        if (tail) {
-          ok = __all_sync(0xffffffffu, mbar_wait(to, 0u, failed));
+        for (int is_v = 0; is_v < 2 && ok; ++is_v) {
+          const int job = jobs + 2 * k + is_v, slot = job % S;
+          const uint32_t bar = smem_u32(&sm.bar_full[slot]);
+          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed));
           if (!ok) break;
-          for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
+          // V rows behind the piece's last token: whatever they hold, their weights are 0 and they have to be finite
+          const bool tail = is_v && j0 + kKT - 1 > tq_last;
+          const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
+          if (leader) mbar_expect_tx(to, Sm::kTileBytes);
+          load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
+          ++asked;
+          if (!q_asked) {
+            bool now = 2 * k + is_v == latest;
+            if (!now) {
+              now = n_use[0] == 0 || mbar_test(smem_u32(&sm.bar_qfree[0]), (n_use[0] - 1) & 1u);
+              now = now && (!ntokB || n_use[1] == 0 || mbar_test(smem_u32(&sm.bar_qfree[1]), (n_use[1] - 1) & 1u));
+              now = __all_sync(0xffffffffu, now);
+            }
+            if (now) {
+              q_asked = true;
+              ask_q(0);
+              if (ok && ntokB) ask_q(1);
+            }
+          }
+          if (tail) {
+            ok = __all_sync(0xffffffffu, mbar_wait(to, n_tail++ & 1u, failed)) && ok;
+            if (!ok) break;
+            for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
 #pragma unroll
-            for (int hf = 0; hf < D / 64; ++hf)
-              *reinterpret_cast<uint4 *>(sm.kv[slot] + hf * kBoxBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar);
+              for (int hf = 0; hf < D / 64; ++hf)
+                *reinterpret_cast<uint4 *>(sm.kv[slot] + hf * kBoxBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+          }
         }
       }
     }
-    if (!ok) {   // after a time-out: no copy outlives the CTA
+    if (!ok) {   // after a time-out: no copy outlives the CTA (a barrier whose last phase has ended lets go at once)
       int alone = 0;
-      for (int x = 0; x < (hasB ? 2 : 1); ++x) mbar_wait(smem_u32(&sm.bar_q[x]), 0u, &alone);
-      for (int job = max(0, asked - S); job < asked; ++job) {
-        const bool tail = (job & 1) && kt.slot(job >> 1) + kKT - 1 > tq_last;
-        alone = 0;
-        if (tail) mbar_wait(smem_u32(&sm.bar_tail), 0u, &alone);
-        else mbar_wait(smem_u32(&sm.bar_full[job % S]), uint32_t(job / S) & 1u, &alone);
-      }
+      for (int x = 0; x < 2; ++x)
+        if (n_q[x]) alone = 0, mbar_wait(smem_u32(&sm.bar_q[x]), (n_q[x] - 1) & 1u, &alone);
+      for (int job = max(0, asked - S); job < asked; ++job) alone = 0, mbar_wait(smem_u32(&sm.bar_full[job % S]), uint32_t(job / S) & 1u, &alone);
+      alone = 0;
+      mbar_wait(smem_u32(&sm.bar_tail), n_tail & 1u, &alone);
     }
   }
   // after a time-out the waits return at once and nothing is stored; the CTA meets here either way
   tc_fence_before();
   __syncthreads();
-  if (tid == 0 && sm.failed) atomicExch(p.status, kDevWaitTimeout);
+  if (tid == 0) {
+    if (sm.failed) atomicExch(p.status, kDevWaitTimeout);
+    // the counters as the next call wants them: the last CTA has drawn its last number, and so have all
+    if (atomicAdd(p.status + 2, 1) == int(gridDim.x) - 1) p.status[1] = p.status[2] = 0;
+  }
   if (warp == kMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -961,9 +1056,9 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
     const size_t bytes = sizeof(PrefillSmem<D>);
     const int splits = paged_splits(p, grid, 4 * kKT);
-    dim3 blocks = dim3(unsigned(grid), unsigned(splits));
-    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);
-    else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages);
+    const unsigned blocks = unsigned(std::min<int64_t>(grid * splits, p.sm_count));
+    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
+    else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
     if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });

@@ -65,6 +65,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *failed = 1;
   return false;
 }
+// ... for a wait that may last as long as other warps' work on a whole piece (of millions of keys: tenths of a second)
+__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed) {
+  for (int i = 0; i < 1024; ++i) {
+    int out = 0;
+    if (mbar_wait(bar, parity, &out)) return true;
+    if (*failed) return false;
+  }
+  *failed = 1;
+  return false;
+}
+// whether the phase has completed already
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{.reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
