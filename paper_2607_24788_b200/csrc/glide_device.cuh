@@ -25,12 +25,12 @@ __device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepco
 // before is does not matter.  It hides the launch of calls that follow one another; a call after idle is no faster.  The tcgen05
 // kernels are launched in the ordinary way: chained, they took as long or longer (carry and attention of 8001 tokens layer by layer).
 template <typename... KernelArgs, typename... Args>
-cudaError_t launch_chained(void (*kernel)(KernelArgs...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t stream, Args &&...args) {
+cudaError_t launch_chained(void (*kernel)(KernelArgs...), dim3 blocks, unsigned threads, size_t smem, cudaStream_t stream, Args &&...args) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

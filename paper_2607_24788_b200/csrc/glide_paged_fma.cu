@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
   auto &sm = *reinterpret_cast<Smem<D, R> *>(smem_raw);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int g = int(blockIdx.x % unsigned(p.Hkv));
+  wait_for_predecessor();
   // (the last tokens, whose windows are the longest, first)
   const Place at = place_of(p, int(gridDim.x / unsigned(p.Hkv)) - 1 - int(blockIdx.x / unsigned(p.Hkv)), TOK);
   if (at.seq < 0) return;
@@ -290,6 +291,7 @@ __global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __gri
   extern __shared__ __align__(16) unsigned char smem_raw[];
   auto &sm = *reinterpret_cast<AccountSmem<D, R> *>(smem_raw);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r_mine = tid & 63;
+  wait_for_predecessor();
   int base = 0;   // tiles of the sequences before
   int64_t item = blockIdx.x;
   for (int b = 0; b < p.batch; ++b) {
@@ -378,15 +380,15 @@ int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStr
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     auto ctas = [&](int rows) { return (p.n_tokens / (rows / G) + p.batch) * p.Hkv; };   // at most: each sequence's last tile may be short
     if (ctas(64) > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
-    // (512 tokens of 4 heads of 64, windows of 64: 36 CTAs of 64 rows or 132 of 16)
-    int splits = 1;
-    if (ctas(64) >= p.sm_count) {
-      paged_prefill_fma_kernel<D, G, 4><<<dim3(unsigned(ctas(64))), kThreads, sizeof(Smem<D, 4>), st>>>(p);
-    } else {
-      splits = paged_splits(p, ctas(16), 2 * kSlots);
-      paged_prefill_fma_kernel<D, G, 1><<<dim3(unsigned(ctas(16)), unsigned(splits)), kThreads, sizeof(Smem<D, 1>), st>>>(p);
-    }
-    if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
+    // (512 tokens of 4 heads of 64, windows of 64: 36 CTAs of 64 rows took 26 us, 132 of 16 took 19)
+    if (ctas(64) >= p.sm_count)
+      return launch_chained(paged_prefill_fma_kernel<D, G, 4>, dim3(unsigned(ctas(64))), kThreads, sizeof(Smem<D, 4>), st, p) == cudaSuccess
+                 ? int(GLIDE_OK)
+                 : int(GLIDE_ERR_CUDA);
+    const int splits = paged_splits(p, ctas(16), 2 * kSlots);
+    if (launch_chained(paged_prefill_fma_kernel<D, G, 1>, dim3(unsigned(ctas(16)), unsigned(splits)), kThreads, sizeof(Smem<D, 1>), st, p) !=
+        cudaSuccess)
+      return int(GLIDE_ERR_CUDA);
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });
 }
@@ -396,11 +398,12 @@ int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStr
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     auto tiles = [&](int slots) { return (int64_t(p.most) / slots + 1) * p.batch * p.Hkv; };
     const int64_t room = int64_t(p.sm_count) * (D == 64 ? 4 : 2);
-    if (tiles(64) >= p.sm_count)
-      paged_weights_fma_kernel<D, G, 4><<<unsigned(std::min(tiles(64), room)), kThreads, sizeof(AccountSmem<D, 4>), st>>>(p);
-    else
-      paged_weights_fma_kernel<D, G, 1><<<unsigned(std::min(tiles(16), room)), kThreads, sizeof(AccountSmem<D, 1>), st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    const bool small = tiles(64) < p.sm_count;
+    const cudaError_t rc = small ? launch_chained(paged_weights_fma_kernel<D, G, 1>, dim3(unsigned(std::min(tiles(16), room))), kThreads,
+                                                  sizeof(AccountSmem<D, 1>), st, p)
+                                 : launch_chained(paged_weights_fma_kernel<D, G, 4>, dim3(unsigned(std::min(tiles(64), room))), kThreads,
+                                                  sizeof(AccountSmem<D, 4>), st, p);
+    return rc == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
 
