@@ -330,9 +330,9 @@ int glide_stream_schedule(const glide_config *cfg, int32_t n_sms, int64_t smem_l
  *   - What a slot holds that a query does not see does not reach its output, infinities and NaN included.
  *   - Offsets into the pool are 64 bits wide.  Rows of out, lse, weight and pos that belong to no sequence are left alone.
  *   - The calls allocate nothing and do not synchronise.  The workspace holds what the kernels of one call hand to each
- *     other: calls of one handle, replayed ones included, have to follow one another (stream order); calls that may run at
- *     the same time need handles of their own, which may share the pages.  Nothing in it outlives a call but the status word.
- *   - Results do not depend on timing: sums are joined in a fixed order, without atomics.
+ *     other, and counters that are 0 between calls: calls of one handle, replayed ones included, have to follow one another
+ *     (stream order); calls that may run at the same time need handles of their own, which may share the pages.
+ *   - Results do not depend on timing: no sum is made by atomics, and parts are joined in a fixed order.
  */
 typedef struct glide_paged glide_paged; /* opaque, host side */
 
@@ -378,7 +378,7 @@ typedef struct {
 int glide_paged_workspace_bytes(const glide_paged_config *cfg, size_t *bytes_out);
 
 /* Build a handle over the caller's pages and a workspace (256-byte aligned).  Both must stay alive until
- * glide_paged_destroy.  The status word is cleared on `stream`. */
+ * glide_paged_destroy and the end of the calls' work.  Waits for `stream`. */
 int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *dev_v_pages, void *dev_workspace,
                        size_t workspace_bytes, void *stream, glide_paged **out);
 int glide_paged_destroy(glide_paged *p);
@@ -418,7 +418,8 @@ int glide_paged_evict(glide_paged *p, const glide_paged_call *call, int64_t budg
  * weights read are looked at when dev_starts is given.  Host only, no CUDA calls. */
 int glide_paged_check_call(const glide_paged_config *cfg, const glide_paged_call *call);
 
-/* The handle's status word (0: nothing was recorded since the last call), read and cleared.  Synchronises `stream`. */
+/* The handle's status word, read and cleared (0: nothing was recorded since; 3: a wait inside a kernel ran out; 4: a page id,
+ * 5: a length or starts out of range).  Synchronises `stream`. */
 int glide_paged_device_status(glide_paged *p, void *stream, int32_t *status_out);
 
 /* Static, NUL-terminated description of a status code. */

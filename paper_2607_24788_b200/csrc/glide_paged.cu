@@ -115,10 +115,8 @@ unsigned blocks_of(int64_t items) { return unsigned((items + kWarps - 1) / kWarp
 
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
-    return launch_chained(paged_store_kernel<typename decltype(t)::type, decltype(d)::value>, unsigned((p.n_tokens + kStoreTokens - 1) / kStoreTokens),
-                          kWarps * 32, 0, st, p) == cudaSuccess
-               ? int(GLIDE_OK)
-               : int(GLIDE_ERR_CUDA);
+    return launch_status(launch_chained(paged_store_kernel<typename decltype(t)::type, decltype(d)::value>,
+                                        unsigned((p.n_tokens + kStoreTokens - 1) / kStoreTokens), kWarps * 32, 0, st, p));
   });
 }
 
@@ -131,10 +129,8 @@ int paged_splits(const PagedParams &p, int64_t ctas, int least) {
 
 int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st) {
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
-    return launch_chained(paged_join_kernel<typename decltype(t)::type, decltype(d)::value>, blocks_of(p.n_tokens * p.H), kWarps * 32, 0, st, p,
-                          splits) == cudaSuccess
-               ? int(GLIDE_OK)
-               : int(GLIDE_ERR_CUDA);
+    return launch_status(launch_chained(paged_join_kernel<typename decltype(t)::type, decltype(d)::value>, blocks_of(p.n_tokens * p.H),
+                                        kWarps * 32, 0, st, p, splits));
   });
 }
 

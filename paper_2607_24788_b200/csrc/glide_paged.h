@@ -108,6 +108,14 @@ __device__ __forceinline__ float *split_record(const PagedParams &p, int head_di
 int paged_splits(const PagedParams &p, int64_t ctas, int least);
 int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st);
 
+// (host) status of a launch; an error is taken off the runtime's record
+inline int launch_status(cudaError_t rc) {
+  if (rc == cudaSuccess) rc = cudaPeekAtLastError();
+  if (rc == cudaSuccess) return GLIDE_OK;
+  cudaGetLastError();
+  return GLIDE_ERR_CUDA;
+}
+
 int launch_paged_store(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);    // bf16
 int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStream_t st);

@@ -687,12 +687,10 @@ int launch(const PagedParams &p, cudaStream_t st) {
   const int units = p.batch * p.Hkv;
   int grid = int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kWarps - 1) / kWarps, p.sm_count, kMaxGrid})));
   if (units <= std::min(p.sm_count, kMaxGrid)) grid = std::max(grid, units);
-  if (launch_chained(paged_decode_kernel<T, D, G>, unsigned(grid), kThreads, sizeof(Smem<T, D, G>), st, p) != cudaSuccess) return GLIDE_ERR_CUDA;
-  if (!p.weight) return GLIDE_OK;
+  const int rc = launch_status(launch_chained(paged_decode_kernel<T, D, G>, unsigned(grid), kThreads, sizeof(Smem<T, D, G>), st, p));
+  if (rc || !p.weight) return rc;
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(longest / (2 * kAccountThreads), p.sm_count * 8 / units)));
-  if (launch_chained(paged_account_kernel<G, Sh::kTile>, unsigned(units * parts), kAccountThreads, 0, st, p, parts, D) != cudaSuccess)
-    return GLIDE_ERR_CUDA;
-  return GLIDE_OK;
+  return launch_status(launch_chained(paged_account_kernel<G, Sh::kTile>, unsigned(units * parts), kAccountThreads, 0, st, p, parts, D));
 }
 
 }  // namespace

@@ -266,7 +266,7 @@ int launch(const PagedParams &p, EvictParams e, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, paged_evict_kernel<T, D>, p, e) == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+  return launch_status(cudaLaunchKernelEx(&cfg, paged_evict_kernel<T, D>, p, e));
 }
 
 }  // namespace

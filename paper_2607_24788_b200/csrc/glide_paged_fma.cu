@@ -382,14 +382,10 @@ int launch_paged_prefill_fma(const glide_paged *h, const PagedParams &p, cudaStr
     if (ctas(64) > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
     // (512 tokens of 4 heads of 64, windows of 64: 36 CTAs of 64 rows took 26 us, 132 of 16 took 19)
     if (ctas(64) >= p.sm_count)
-      return launch_chained(paged_prefill_fma_kernel<D, G, 4>, dim3(unsigned(ctas(64))), kThreads, sizeof(Smem<D, 4>), st, p) == cudaSuccess
-                 ? int(GLIDE_OK)
-                 : int(GLIDE_ERR_CUDA);
+      return launch_status(launch_chained(paged_prefill_fma_kernel<D, G, 4>, dim3(unsigned(ctas(64))), kThreads, sizeof(Smem<D, 4>), st, p));
     const int splits = paged_splits(p, ctas(16), 2 * kSlots);
-    if (launch_chained(paged_prefill_fma_kernel<D, G, 1>, dim3(unsigned(ctas(16)), unsigned(splits)), kThreads, sizeof(Smem<D, 1>), st, p) !=
-        cudaSuccess)
-      return int(GLIDE_ERR_CUDA);
-    return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
+    const int rc = launch_status(launch_chained(paged_prefill_fma_kernel<D, G, 1>, dim3(unsigned(ctas(16)), unsigned(splits)), kThreads, sizeof(Smem<D, 1>), st, p));
+    return rc || splits == 1 ? rc : launch_paged_join(h, p, splits, st);
   });
 }
 
@@ -403,7 +399,7 @@ int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStr
                                                   sizeof(AccountSmem<D, 1>), st, p)
                                  : launch_chained(paged_weights_fma_kernel<D, G, 4>, dim3(unsigned(std::min(tiles(64), room))), kThreads,
                                                   sizeof(AccountSmem<D, 4>), st, p);
-    return rc == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    return launch_status(rc);
   });
 }
 

@@ -25,6 +25,7 @@ int plan(const glide_paged_config *in, glide_paged *h) {
     return GLIDE_ERR_INVALID_ARG;
   if (c.io_dtype != GLIDE_F32 && c.io_dtype != GLIDE_BF16) return GLIDE_ERR_UNSUPPORTED;
   if ((c.head_dim != 64 && c.head_dim != 128) || c.n_q_heads % c.n_kv_heads) return GLIDE_ERR_UNSUPPORTED;
+  if (int64_t(c.n_q_heads) * c.head_dim > (1 << 24)) return GLIDE_ERR_UNSUPPORTED;
   const int G = c.n_q_heads / c.n_kv_heads;
   if (G != 1 && G != 2 && G != 4 && G != 8) return GLIDE_ERR_UNSUPPORTED;
   int shift = 4;
@@ -46,7 +47,6 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   const int64_t layer_pages = c.layer_stride / c.page_stride;
   if (layer_pages * (c.n_layers - 1) + c.n_pages > INT32_MAX) return GLIDE_ERR_UNSUPPORTED;
   if ((c.max_tokens / kPagedTile + 2) * c.max_batch * c.n_kv_heads > INT32_MAX / 2) return GLIDE_ERR_UNSUPPORTED;
-  if (int64_t(c.n_q_heads) * c.head_dim > (1 << 24)) return GLIDE_ERR_UNSUPPORTED;
   if (c.softmax_scale == 0.f) c.softmax_scale = 1.0f / std::sqrt(float(d));
   h->cfg = c;
   h->group = G;
@@ -176,7 +176,8 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
     }
   }
   if (ok && h->cfg.io_dtype == GLIDE_F32) ok = setup_paged_fma(h) == GLIDE_OK;
-  ok = ok && setup_paged_decode(h) == GLIDE_OK && setup_paged_evict(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess;
+  ok = ok && setup_paged_decode(h) == GLIDE_OK && setup_paged_evict(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess &&
+       cudaStreamSynchronize(as_stream(stream)) == cudaSuccess;   // (so that the first call may be on any stream)
   if (!ok) {
     cudaGetLastError();
     delete h;

@@ -296,7 +296,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     uint32_t n_s = 0, n_q = 0;                      // batches of products waited for; Q tiles of X so far
     bool ok = true;
     auto wait_s = [&]() {
-      if (ok) ok = mbar_wait(smem_u32(&sm.bar_s[X]), n_s & 1u, failed);
+      if (ok) ok = mbar_wait_long(smem_u32(&sm.bar_s[X]), n_s & 1u, failed);
       ++n_s;
       tc_fence_after();
       ok = __all_sync(0xffffffffu, ok);             // warp-uniform
@@ -478,7 +478,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const float l_row = row_sum_of(l_sum);
       const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
-      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_q[X]), n_q & 1u, failed));   // (Q, which no product has waited for)
+      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed));   // (Q, which no product has waited for)
       n_q += n_tiles != 0;
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
@@ -555,7 +555,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     uint32_t n_p = 0, n_q = 0, n_turn = 0;          // operands P, Q tiles of x, turns so far
     bool ok = true;
     auto wait = [&](uint64_t &bar, uint32_t parity) {
-      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity & 1u, failed));
+      ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&bar), parity & 1u, failed));
       return ok;
     };
     auto commit = [&](uint64_t &bar) {
@@ -615,7 +615,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         w = find_tile(p, tiles - 1 - t, TOKC);
         w.g = rest / parts, w.part = rest - w.g * parts;
       }
-      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_workfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed));
+      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_workfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed));
       if (!ok) break;
       if (lane == 0) {
         sm.work[it & 1] = w;
@@ -627,7 +627,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
       // The first tiles may come while the piece before is still being written out, Q_X when its rows have been.
       auto ask_q = [&](int x) {
-        if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed));
+        if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed));
         ++n_use[x];
         if (!ok || !n_tiles) return;
         ++n_q[x];
@@ -651,7 +651,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int is_v = 0; is_v < 2 && ok; ++is_v) {
           const int job = jobs + 2 * k + is_v, slot = job % S;
           const uint32_t bar = smem_u32(&sm.bar_full[slot]);
-          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed));
+          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed));
           if (!ok) break;
           // V rows behind the piece's last token: whatever they hold, their weights are 0 and they have to be finite
           const bool tail = is_v && j0 + kKT - 1 > tq_last;
@@ -673,7 +673,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             }
           }
           if (tail) {
-            ok = __all_sync(0xffffffffu, mbar_wait(to, n_tail++ & 1u, failed)) && ok;
+            ok = __all_sync(0xffffffffu, mbar_wait_long(to, n_tail++ & 1u, failed)) && ok;
             if (!ok) break;
             for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
 #pragma unroll
@@ -1059,7 +1059,7 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const unsigned blocks = unsigned(std::min<int64_t>(grid * splits, p.sm_count));
     if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
     else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
-    if (cudaGetLastError() != cudaSuccess) return int(GLIDE_ERR_CUDA);
+    if (const int rc = launch_status(cudaSuccess)) return rc;
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });
 }
@@ -1075,7 +1075,7 @@ int launch_paged_weights_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const int64_t most = (int64_t(p.most) / kKT + 1) * p.batch * p.Hkv;
     const unsigned grid = unsigned(std::min<int64_t>(most, p.sm_count));
     paged_weights_tc_kernel<D, G><<<grid, kAccThreads, sizeof(AccountSmem<D>), st>>>(p, maps, h->map_pages);
-    return cudaGetLastError() == cudaSuccess ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
+    return launch_status(cudaSuccess);
   });
 }
 

@@ -65,9 +65,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *failed = 1;
   return false;
 }
-// ... for a wait that may last as long as other warps' work on a whole piece (of millions of keys: tenths of a second)
+// ... for a wait that may last as long as other warps' work on a whole piece, rows that are computed once more among it.  (A try that
+// fails takes 1.4 us: kWaitLimit of them 1.4 s, these 23 s.)
 __device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed) {
-  for (int i = 0; i < 1024; ++i) {
+  for (int i = 0; i < 16; ++i) {
     int out = 0;
     if (mbar_wait(bar, parity, &out)) return true;
     if (*failed) return false;

@@ -46,7 +46,9 @@ def test_configurations(kw, code):
 def test_workspace_holds_a_steps_scores_only_where_weights_are_kept():
     a, b = workspace(weights=1)[1], workspace(weights=0)[1]
     assert abs(a - b - 4 * 8 * 1000 * 4) <= 512
-    assert workspace(weights=1, max_tokens=2000)[1] - a == pytest.approx(4 * 8 * 1000 * 4, abs=512)
+    assert workspace(max_tokens=4000)[1] - workspace(max_tokens=2000)[1] == pytest.approx(4 * 8 * 2000 * 4, abs=512)
+    # beyond 1024 tokens: the records of prompts of few rows behind long caches
+    assert workspace(weights=0, max_tokens=1025)[1] - workspace(weights=0, max_tokens=1024)[1] <= 16384 * (128 + 4) * 4
 
 
 def call(**kw):
