@@ -36,8 +36,8 @@ struct Smem {
   int hist[2][kBins];     // (two: the next digit's counts while other CTAs still read this one's)
   int warp_sums[32];
   uint32_t digit;
-  int before, ties_before;   // slots below the digit; slots of the digit in the CTAs before this one (of the last digit: equal to T)
-  int counts[2];          // this CTA's holes and movers
+  int count, before, ties_before;   // slots of the digit that T has; slots below the digit; slots of the digit in the CTAs before this one (of the last digit: equal to T)
+  int2 counts;            // this CTA's holes and movers
   unsigned long long least[32];
   unsigned long long cta_least;
 };
@@ -132,8 +132,9 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     }
     cluster.sync();
     best = ~0ull;
-    for (int r = 0; r < ranks; ++r) {
-      const unsigned long long x = *cluster.map_shared_rank(&sm.cta_least, r);
+#pragma unroll
+    for (int r = 0; r < kMostCluster; ++r) {
+      const unsigned long long x = r < ranks ? *cluster.map_shared_rank(&sm.cta_least, r) : ~0ull;
       best = x < best ? x : best;
     }
     least = uint32_t(best >> 32);
@@ -167,10 +168,15 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
       }
       int total;
       const int before = block_scan(c, sm.warp_sums, total);
-      if (before < quota && quota <= before + c) sm.digit = uint32_t(tid), sm.before = before, sm.ties_before = mine;
+      if (before < quota && quota <= before + c) sm.digit = uint32_t(tid), sm.before = before, sm.ties_before = mine, sm.count = c;
       __syncthreads();
       least |= sm.digit << shift;
       quota -= sm.before;
+      if (quota == sm.count) {   // all that share the digits so far leave
+        least |= (1u << shift) - 1u;
+        quota = INT32_MAX;
+        break;
+      }
     }
   }
   int moves = 0;
@@ -190,13 +196,15 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     int hole = block_scan(holes, sm.warp_sums, total), mover = 0, all_movers = 0;
     const int all_holes = total;
     if (begin + n > kept) mover = block_scan(movers, sm.warp_sums, all_movers);   // (the same for the CTA)
-    if (tid == 0) sm.counts[0] = all_holes, sm.counts[1] = all_movers;
+    if (tid == 0) sm.counts = make_int2(all_holes, all_movers);
     cluster.sync();
-    for (int r = 0; r < ranks; ++r) {
-      const int *c = cluster.map_shared_rank(&sm.counts[0], r);
-      const int h = c[0];
-      if (r < rank) hole += h, mover += c[1];
-      moves += h;
+    int2 c[kMostCluster];   // (all on their way together)
+#pragma unroll
+    for (int r = 0; r < kMostCluster; ++r) c[r] = r < ranks ? *cluster.map_shared_rank(&sm.counts, r) : make_int2(0, 0);
+#pragma unroll
+    for (int r = 0; r < kMostCluster; ++r) {
+      if (r < rank) hole += c[r].x, mover += c[r].y;
+      moves += c[r].x;
     }
     at = tie;
     for (int i = i0; i < i1; ++i) {
