@@ -301,7 +301,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       tc_fence_after();
       ok = __all_sync(0xffffffffu, ok);             // warp-uniform
     };
-    auto hand_over = [&]() {
+    auto hand_over = [&]() {   // this thread's TMEM accesses precede the MMAs that read P and overwrite S
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.bar_p[X]));
@@ -337,20 +337,30 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         tmem_st32(tO + c0, r);
       }
     };
+    float top_w = 0.f;                              // largest weight of the last tile that soft_tile has taken
+    // Weights beyond 2^32: the reference catches up with them (a power of two, so that nothing is rounded) before it moves on, or what a
+    // row has gathered would be multiplied by a factor below the least number.  Returns the factor.
+    auto catch_up = [&](float w) {
+      if (!(w >= kMostWeight)) return 1.f;
+      const float e = w < CUDART_INF_F ? fminf(floorf(lg2(w)), 126.f) : w;   // (2^-127 is below the least normal number)
+      m_ref += e;
+      return ex2(-e);
+    };
     // the lazy reference for a tile whose largest score over this thread's columns is mx; returns what the weights are taken against
     auto move_ref = [&](float mx, bool first) {
       auto grows = [&]() {
         const float ms = mx * p.scale_log2;
         return ms > m_ref + kLazy || (m_ref == -CUDART_INF_F && ms > -CUDART_INF_F);
       };
-      if (pair_any(grows())) {
+      if (pair_any(grows() || top_w >= kMostWeight)) {
         mx = row_max_of(mx);
-        float f = 1.f;
+        float f = catch_up(row_max_of(top_w));
         if (grows()) {
           mx *= p.scale_log2;
-          f = m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
+          f *= m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
           m_ref = mx;
         }
+        top_w = 0.f;
         if (!first && __any_sync(0xffffffffu, f != 1.f)) scale_o(f);
         l_sum *= f, x_sum *= f;
       }
@@ -360,16 +370,16 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       int lo, hi, sink;   // of this thread's 64 columns, those lo .. hi and 0 .. sink are seen
     };
     auto seen_of = [](const Bounds &v, int c) { return column_mask(c, v.lo, v.hi) | column_mask(c, -1, v.sink); };
-    // A later key tile against the reference as it is, in one pass; the largest weight says afterwards whether that was right.
-    // Otherwise (false, to both threads of all rows of the pair) nothing has happened and the tile goes through soft_tile_masked.
+    // A later key tile against the reference as it is, in one pass.  (The first half of P handed over while the second is made: the MMA
+    // warp holds its turn for longer, 2 to 7 % slower.)  Weights may grow to the end of the numbers' range; beyond 2^32 the next tile moves the reference.  A row whose weights leave the range
+    // all the same, or with an argument that exp2_fma does not take, ends with a sum that is no finite number and is computed by itself.
     auto soft_tile = [&](auto masked, const Bounds &v) {
-      float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
+      float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f, odd0 = 0.f, odd1 = 0.f, most = -CUDART_INF_F;
       const float mr = m_ref;
-      float odd0 = 0.f, odd1 = 0.f;                 // not finite if an argument of exp2_fma is not
-      uint32_t pk[32], mx2 = 0u;
+      uint32_t mx2 = 0u;
 #pragma unroll
       for (int c = 0; c < 64; c += 32) {
-        uint32_t x[32];
+        uint32_t x[32], pk[16];
         tmem_ld32(tS + c, x);
         if (decltype(masked)::value) {
           const uint32_t m = seen_of(v, c);
@@ -382,25 +392,26 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
           if (!LSE && !decltype(masked)::value && e < kByFma) {
             add2(odd0, odd1, a0, a1);
+            most = max3(most, a0, a1);
             exp2_fma<3>(a0, a1);
           } else {
             a0 = ex2(a0), a1 = ex2(a1);
           }
           if (LSE) add2(ex0, ex1, a0, a1);
-          const uint32_t w2 = pack_bf16x2(a0, a1);
-          mx2 = max_bf16x2(mx2, w2);
-          add2(sum0, sum1, bf16_lo(w2), bf16_hi(w2));   // the sum uses the weights as the tensor core sees them
-          pk[(c >> 1) + e] = w2;
+          pk[e] = pack_bf16x2(a0, a1);
+          mx2 = max_bf16x2(mx2, pk[e]);
+          add2(sum0, sum1, bf16_lo(pk[e]), bf16_hi(pk[e]));   // the sum uses the weights as the tensor core sees them
         }
+        tmem_st16(tS + (c >> 1), pk);
       }
-      const float mx = fmaxf(bf16_lo(mx2), bf16_hi(mx2));
-      if (pair_any(!(mx < kMostWeight) || !isfinite(odd0 + odd1))) return false;
-      tmem_st32(tS, pk);
+      tmem_wait_st();
+      hand_over();
+      top_w = fmaxf(bf16_lo(mx2), bf16_hi(mx2));
       l_sum += sum0 + sum1;
+      if (!isfinite(odd0 + odd1) || most > 126.f) l_sum = CUDART_NAN_F;
       if (LSE) x_sum += ex0 + ex1;
-      return true;
     };
-    // ... against a reference that moves first; for rows that have none yet, and tiles that soft_tile leaves alone
+    // ... against a reference that moves first; for rows that have none yet, and behind weights that are big
     auto soft_tile_masked = [&](const Bounds &v, bool first) {
       float mx = -CUDART_INF_F, sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
 #pragma unroll 1
@@ -451,11 +462,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const int ntokX = X ? ntokB : ntokA;
       if (ntokX == 0) continue;
       const int mine = x_q0(X) + tok_r;             // this row's slot
-      m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f;
+      m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f, top_w = 0.f;
       const int w = p.window < 0 ? kMostSlots : p.window;
       int before = -1;                              // the key tile that this row tile had before
       for (int k = 0; k < n_tiles; ++k) {
         if (!has(X, k)) continue;
+        const bool move = pair_any(before < 0 || top_w >= kMostWeight || m_ref == -CUDART_INF_F);   // (before the wait, beside the products)
         wait_s();
         if (tid == X * kRows) {                     // S of the tile and P V of the tile before have completed
           mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * k) % S]));
@@ -465,14 +477,14 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         const bool whole = j0 + kKT - 1 <= x_q0(X) && (j0 > x_q1(X) - w || j0 + kKT <= p.n_sink);
         const int c0 = j0 + H * 64;
         const Bounds v{mine - w + 1 - c0, mine - c0, min(p.n_sink - 1, mine) - c0};
-        bool done = false;
-        // (what is asked here is the same in both warps of a pair: their threads share the rows)
-        if (before >= 0 && !__any_sync(0xffffffffu, m_ref == -CUDART_INF_F)) {
-          if (whole) done = soft_tile(std::false_type{}, v);
-          else done = soft_tile(std::true_type{}, v);
+        if (move) {
+          soft_tile_masked(v, before < 0);
+          hand_over();
+        } else if (whole) {
+          soft_tile(std::false_type{}, v);
+        } else {
+          soft_tile(std::true_type{}, v);
         }
-        if (!done) soft_tile_masked(v, before < 0);
-        hand_over();                                // this thread's TMEM accesses precede the MMAs that read P and overwrite S
         before = k;
       }
       const float l_row = row_sum_of(l_sum);
@@ -483,6 +495,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
       if (parts > 1) {
+        const float f = catch_up(row_max_of(top_w));   // (records are added up against the largest of their references)
         float *rec = split_record(p, D, part, out_row, g * G + row % G);
 #pragma unroll 1
         for (int c0 = 0; c0 < kHalf && before >= 0; c0 += 32) {
@@ -491,10 +504,10 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
             if (live && ok)
-              *reinterpret_cast<float4 *>(rec + H * kHalf + c0 + i) = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]),
-                                                                                  __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+              *reinterpret_cast<float4 *>(rec + H * kHalf + c0 + i) = make_float4(__uint_as_float(r[i]) * f, __uint_as_float(r[i + 1]) * f,
+                                                                                  __uint_as_float(r[i + 2]) * f, __uint_as_float(r[i + 3]) * f);
         }
-        if (H == 0 && live && ok) *reinterpret_cast<float4 *>(rec + D) = make_float4(m_ref, l_row, x_row, 0.f);
+        if (H == 0 && live && ok) *reinterpret_cast<float4 *>(rec + D) = make_float4(m_ref, l_row * f, x_row * f, 0.f);
       } else {
       const float inv = live && before >= 0 && l_row != 0.f ? 1.0f / l_row : 0.f;
       float chk0 = 0.f, chk1 = 0.f;                 // finite if all values of the row are
@@ -531,13 +544,15 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
       if (LSE && H == 0 && live && ok) p.lse[out_row * p.H + g * G + row % G] = PagedRow<bf16, D, 1>::paged_lse(m_ref, x_row);
       // rows of which either half is not finite, by the first warp of the pair when both have stored
-      const bool bad = live && (!isfinite((chk0 + chk1) * inv) || !isfinite(inv));
+      const bool bad = live && (!isfinite((chk0 + chk1) * inv) || !isfinite(l_row));
       unsigned again = __ballot_sync(0xffffffffu, row_sum_of(bad ? 1.f : 0.f) > 0.f);
+      const unsigned sums_off = __ballot_sync(0xffffffffu, LSE && live && !isfinite(x_row));
       if (H == 0 && ok) {
         for (; again; again &= again - 1) {
           const int rr = (row & ~31) + __ffs(int(again)) - 1;
           PagedRow<bf16, D, 1> one;
-          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, false);   // (the sums of the scores were right)
+          // (its lse was right unless its weights had left the range)
+          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u);
         }
       }
       }

@@ -78,7 +78,8 @@ def reference(c, window=-1, n_sink=0, layer=0, scale=None, rounded=None):
       reference subtracted from it by 4u A more, 2^x by 4u relative; so every weight by w = 2 (e + 8u A) + 16u + n 2u (its own and the row
       sum's, whose n terms are summed in fp32), relative
       outputs: sum_j p_j |v_j - o| (w + r) + 2u (n + 4) sum_j p_j |v_j| + the rounding of o, with r = 2^-8 (bf16 weights in the product)
-      lse: e + 8u A + 8u + n 2u + 2u |lse|;  weights: sum of the terms' w, and one rounding per term and of the sum"""
+      lse: e + 8u A + 8u + n 2u + 2u |lse|;  weights: sum of the terms' w, and one rounding per term and of the sum; a term below
+      the least normal number, 2^-126, may be 0"""
     u = 2.0 ** -24
     d, G = c.d, c.G
     scale = d ** -0.5 if scale is None else scale
@@ -114,7 +115,7 @@ def reference(c, window=-1, n_sink=0, layer=0, scale=None, rounded=None):
             lse[row:row + T, h] = total
             lse_tol[row:row + T, h] = e + 8 * u + cnt * 2 * u + 2 * u * total.abs().nan_to_num(posinf=0.0)
             given[b, h // G, :n] += p.sum(0)
-            given_tol[b, h // G, :n] += (p * (w + u * (T * G + 2))[:, None]).sum(0)
+            given_tol[b, h // G, :n] += (p * (w + u * (T * G + 2))[:, None]).sum(0) + T * 2.0 ** -126
     return out, tol, lse, lse_tol, given, given_tol
 
 

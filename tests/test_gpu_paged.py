@@ -419,6 +419,22 @@ def test_evict_long(n, budget):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("amp", [30.0, 300.0])
+def test_scores_that_grow_by_hundreds_from_tile_to_tile(dtype, amp):
+    """Weights against the first tile's maximum would leave the range of the numbers."""
+    check_prefill(Cache([0, 300], [700, 200], 4, 2, 64, dtype, 64, amp=amp))
+    check_prefill(Cache([0, 300], [700, 200], 4, 2, 128, dtype, 16, amp=amp), 300, 3)
+    check_prefill(Cache([6000], [9], 4, 2, 128, dtype, 64, amp=amp))
+    check_decode(Cache([6000, 300], [1, 1], 4, 2, 128, dtype, 64, amp=amp), track=True)
+    # ... and without lse
+    c = Cache([0, 300], [700, 200], 4, 2, 128, dtype, 64, amp=amp)
+    out = torch.empty_like(c.q)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, c.k, c.v, out)
+    want, tol = reference(c)[:2]
+    check(out, want, tol, "out")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_a_run_of_them_together(dtype):
     """A prompt, its weights, an eviction, then steps that each add a token and give one slot up: outputs against the definition
     over the rows that the cache holds, positions against a list that is kept beside it."""
