@@ -106,8 +106,8 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     p.tickets[b] = 0;   // as the next call wants it
     e.new_lens[b] = kept;
   }
+  int moves = 0;
   uint32_t least = 0;   // T
-  int least_before = 0; // (one slot that leaves) whether it lies in a CTA before this one
   int quota = leave;    // slots equal to T that leave: the rank (from 1) of T among the slots that share the digits so far
   if (leave == 1) {
     unsigned long long best = ~0ull;
@@ -137,8 +137,10 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
       const unsigned long long x = r < ranks ? *cluster.map_shared_rank(&sm.cta_least, r) : ~0ull;
       best = x < best ? x : best;
     }
-    least = uint32_t(best >> 32);
-    least_before = int(uint32_t(best)) < begin;   // (then no tie here leaves)
+    // the last slot moves into its place, unless it is the one that leaves
+    const int slot = int(uint32_t(best));
+    moves = slot < kept ? 1 : 0;
+    if (moves && rank == 0 && tid == 0) pairs[0] = slot, pairs[1] = kept;
   } else if (leave > 0) {
 #pragma unroll 1
     for (int step = 0; step < 4; ++step) {
@@ -179,13 +181,12 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
       }
     }
   }
-  int moves = 0;
-  if (leave > 0) {
-    // ties of the threads before (and the CTAs before: of one slot that leaves, the least of all, there is one)
+  if (leave > 1) {
+    // ties of the threads before, and of the CTAs before
     const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
     int ties = 0, total;
     for (int i = i0; i < i1; ++i) ties += key(i) == least;
-    int tie = block_scan(ties, sm.warp_sums, total) + (leave > 1 ? sm.ties_before : least_before);
+    int tie = block_scan(ties, sm.warp_sums, total) + sm.ties_before;
     auto gone = [&](uint32_t k, int &at) { return k < least || (k == least && at++ < quota); };
     int holes = 0, movers = 0, at = tie;
     for (int i = i0; i < i1; ++i) {

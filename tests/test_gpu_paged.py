@@ -535,6 +535,106 @@ def test_calls_back_to_back():
         assert torch.equal(a.view(torch.int16 if a.dtype is BF16 else torch.int32), b.view(torch.int16 if b.dtype is BF16 else torch.int32))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_most_sequences(dtype):
+    """1024 of them: prompts of no, one or a few tokens behind some, then a step, their account, an eviction."""
+    new = [(7 * i) % 5 for i in range(1024)]
+    check_prefill(Cache([(13 * i) % 40 for i in range(1024)], new, 2, 1, 64, dtype, 16, weights=True), 20, 1)
+    c = Cache([(29 * i) % 70 for i in range(1024)], [1] * 1024, 2, 1, 64, dtype, 16)
+    check_decode(c, track=True)
+    want = evicted(c, c.weight.cpu(), c.pos.cpu(), c.lens, c.lens, 30, 10, 2)
+    lens = c.lens_dev.clone()
+    c.handle.glide_paged_evict(c.table, lens, c.lens_dev, c.weight, c.pos, 30, lens, recent=10, n_sink=2)
+    assert same(c.weight.cpu(), want[0]) and torch.equal(c.pos.cpu(), want[1]) and same(c.k_pages, want[2]) and same(c.v_pages, want[3])
+    assert lens.tolist() == [min(n, 30) for n in c.lens] and c.handle.glide_paged_device_status() == 0
+
+
+def test_evict_more_slots_than_a_block_can_hold():
+    """So many units that each has one block, and more slots than its shared memory has room for."""
+    n = 60000
+    c = Cache([n] + [i % 50 for i in range(99)], [0] * 100, 1, 1, 64, BF16, 256)
+    g = torch.Generator().manual_seed(3)
+    for budget in (20000, n - 1):
+        weight = torch.randint(0, 5000, c.weight.shape, generator=g).float().cuda()
+        pos = torch.randint(0, 2 * n, c.weight.shape, generator=g).int().cuda()
+        seen = torch.full((100,), 2 * n, dtype=torch.int32, device="cuda")
+        want = evicted(c, weight.cpu(), pos.cpu(), c.lens, seen.tolist(), budget, 50, 4)
+        new_lens = torch.empty_like(c.lens_dev)
+        c.handle.glide_paged_evict(c.table, c.lens_dev, seen, weight, pos, budget, new_lens, recent=50, n_sink=4)
+        assert torch.equal(weight.cpu(), want[0]) and torch.equal(pos.cpu(), want[1]) and same(c.k_pages, want[2]) and same(c.v_pages, want[3])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_new_tokens_and_tables_of_few_columns(dtype):
+    c = Cache([30, 20], [0, 0], 4, 2, 64, dtype, 16)
+    q, k = torch.zeros(5, 4, 64, dtype=dtype, device="cuda"), torch.zeros(5, 2, 64, dtype=dtype, device="cuda")
+    out, lse, weight = torch.full_like(q, 7.0), torch.full((5, 4), 7.0, device="cuda"), c.weight.clone()
+    for _ in range(2):
+        c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q, k, k, out, lse=lse)
+        c.handle.glide_paged_weights(c.table, c.lens_dev, c.starts, q, lse, c.weight)
+    assert (out == 7.0).all() and (lse == 7.0).all() and torch.equal(c.weight, weight)
+    c.check_pages()
+    # the handle may hold more slots than the call's table has columns for; the table's rows lie further apart
+    c = Cache([40, 3], [5, 1], 4, 2, 64, dtype, 16, slots=400)
+    assert c.table.shape[1] == 25
+    c.table = c.table[:, :3]
+    check_prefill(c, weights=False)
+    assert c.handle.glide_paged_device_status() == 0
+    lens = torch.tensor([49, 4], dtype=torch.int32, device="cuda")     # (a slot more than three pages hold)
+    out = torch.empty(2, 4, 64, dtype=dtype, device="cuda")
+    c.handle.glide_paged_decode(c.table, lens, c.q[:2].contiguous(), None, None, out)
+    assert c.handle.glide_paged_device_status() == 5
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_captured_turn(dtype):
+    """Prompt, account, eviction and step captured as one graph: replays with other inputs and lengths against eager calls."""
+    def turn(c, t):
+        c.handle.glide_paged_prefill(c.table, t["lens"], c.starts, t["q"], t["k"], t["v"], t["out"], lse=t["lse"], weight=t["weight"], pos=t["pos"], seen=t["seen"])
+        c.handle.glide_paged_weights(c.table, t["lens"], c.starts, t["q"], t["lse"], t["weight"])
+        c.handle.glide_paged_evict(c.table, t["lens"], t["seen"], t["weight"], t["pos"], 100, t["lens"], recent=20, n_sink=2)
+        t["lens"].add_(1)
+        t["seen"].add_(1)
+        c.handle.glide_paged_decode(c.table, t["lens"], t["q"][:2], t["k"][:2], t["v"][:2], t["out2"], weight=t["weight"], pos=t["pos"], seen=t["seen"])
+
+    def fresh(seed):
+        c = Cache([1500, 20], [60, 90], 8, 2, 64, dtype, 32, seed=1, slots=1600)
+        g = torch.Generator().manual_seed(seed)
+        for name in ("q", "k", "v"):
+            setattr(c, name, torch.randn(getattr(c, name).shape, generator=g).to(dtype).cuda())
+        t = dict(q=c.q, k=c.k, v=c.v, out=torch.zeros_like(c.q), lse=torch.zeros(150, 8, device="cuda"), out2=torch.zeros_like(c.q[:2]),
+                 weight=torch.rand(c.weight.shape, generator=g).cuda(), pos=torch.arange(c.slots, dtype=torch.int32).expand(c.pos.shape).contiguous().cuda(),
+                 lens=torch.tensor([1560 - 7 * seed, 110], dtype=torch.int32, device="cuda"))
+        t["seen"] = t["lens"].clone()
+        return c, t
+
+    c, t = fresh(0)
+    start = {n: x.clone() for n, x in t.items()}
+    pages = c.k_pages.clone(), c.v_pages.clone()
+
+    def reset(values):
+        for n, x in values.items():
+            t[n].copy_(x)
+        c.k_pages.copy_(pages[0])
+        c.v_pages.copy_(pages[1])
+
+    turn(c, t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    reset(start)
+    with torch.cuda.graph(graph):
+        turn(c, t)
+    for seed in range(3):
+        other, u = fresh(seed)
+        reset({n: x.clone() for n, x in u.items()})
+        graph.replay()
+        turn(other, u)
+        for n in ("out", "lse", "out2", "weight", "pos", "lens"):
+            assert torch.equal(t[n], u[n]), n
+        assert same(c.k_pages, other.k_pages) and same(c.v_pages, other.v_pages)
+        assert c.handle.glide_paged_device_status() == 0
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 2^32 elements: pages at its end."""
     page, Hkv, d = 256, 8, 128
