@@ -413,6 +413,9 @@ def glide_paged_workspace_bytes(cfg: glide_paged_config) -> int:
     return int(out.value)
 
 
+_I32, _F32 = torch.int32, torch.float32
+
+
 class GlidePaged:
     """Softmax attention over a paged cache (include/glide.h): k_pages, v_pages [L][n_pages][H_kv][page_size][d] are the
     caller's (views of equal strides will do), a torch workspace and the handle are owned here.  Tables are int32 [B][cols], lens,
@@ -445,104 +448,115 @@ class GlidePaged:
         self._pack = struct.Struct("@iiPiiqPPqqqqqPPPq").pack_into
         assert struct.calcsize("@iiPiiqPPqqqqqPPPq") == ctypes.sizeof(glide_paged_call)
 
+    # (A tensor's shape is asked for once, as a whole: .size(i) and .stride(i) take three times as long, and a short step is bound by
+    # the host's time for its call.)
     def _ints(self, t: torch.Tensor, n: int, what: str) -> int:
-        assert t.dtype is torch.int32 and t.dim() == 1 and t.size(0) == n and t.is_contiguous() and t.get_device() == self._index, \
-            f"{what}: int32 [{n}] on {self.device}"
+        assert t.dtype is _I32 and t.shape == (n,) and t.is_contiguous() and t.get_device() == self._index, f"{what}: int32 [{n}] on {self.device}"
         return t.data_ptr()
 
     def _rows(self, t: torch.Tensor, rows: int, heads: int, what: str):
         """Address and token stride (0: side by side) of [rows][heads][d] whose heads lie side by side."""
-        assert (t.dtype is self.dtype and t.dim() == 3 and t.size(0) == rows and t.size(1) == heads and t.size(2) == self.d
-                and t.get_device() == self._index), f"{what}: {self.dtype} [{rows}][{heads}][{self.d}] on {self.device}"
+        assert t.dtype is self.dtype and t.shape == (rows, heads, self.d) and t.get_device() == self._index, \
+            f"{what}: {self.dtype} [{rows}][{heads}][{self.d}] on {self.device}"
         if t.is_contiguous():
             return t.data_ptr(), 0
-        assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.d), f"{what}: a token's heads have to lie side by side"
-        return t.data_ptr(), t.stride(0) if rows > 1 else 0
+        stride = t.stride()
+        assert stride[2] == 1 and (heads == 1 or stride[1] == self.d), f"{what}: a token's heads have to lie side by side"
+        return t.data_ptr(), stride[0] if rows > 1 else 0
 
     def _track(self, t: torch.Tensor, B: int, dtype, what: str):
-        assert (t.dtype is dtype and t.dim() == 3 and t.size(0) == B and t.size(1) == self.Hkv and t.is_contiguous()
-                and t.get_device() == self._index), f"{what}: {dtype} [{B}][{self.Hkv}][slots] on {self.device}"
-        return t.data_ptr(), t.size(2)
+        shape = t.shape
+        assert t.dtype is dtype and len(shape) == 3 and shape[:2] == (B, self.Hkv) and t.is_contiguous() and t.get_device() == self._index, \
+            f"{what}: {dtype} [{B}][{self.Hkv}][slots] on {self.device}"
+        return t.data_ptr(), shape[2]
 
     def _lse(self, lse, rows: int):
         if lse is None:
             return None
-        assert (lse.dtype is torch.float32 and lse.dim() == 2 and lse.size(0) == rows and lse.size(1) == self.H and lse.is_contiguous()
-                and lse.get_device() == self._index), f"lse: fp32 [{rows}][{self.H}] on {self.device}"
+        assert lse.dtype is _F32 and lse.shape == (rows, self.H) and lse.is_contiguous() and lse.get_device() == self._index, \
+            f"lse: fp32 [{rows}][{self.H}] on {self.device}"
         return lse.data_ptr()
 
-    def _run(self, where: str, stream, fn, layer: int, table, lens, starts, rows, q, k, v, out, window: int, n_sink: int, weight, pos, seen, *args):
-        """Checks the tensors, writes the call and makes it: fn(handle, call, addresses of q, k, v, out as far as there are, *args)."""
-        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.get_device() == self._index, \
-            f"table: int32 [B][cols] on {self.device}"
-        B, cols = table.size(0), table.size(1)
-        if rows is None:
-            rows = B
-        p_starts = 0 if starts is None else self._ints(starts, B + 1, "starts")
-        q_stride = kv_stride = out_stride = p_weight = p_pos = track = 0
-        addresses = []
-        if q is not False:   # (False: this call has no such argument)
-            p_q = None
-            if q is not None:
-                p_q, q_stride = self._rows(q, rows, self.H, "q")
-            addresses.append(p_q)
-        if k is not False:
-            assert (k is None) == (v is None), "k and v: both or neither"
-            p_k = p_v = None
-            if k is not None:
-                p_k, kv_stride = self._rows(k, rows, self.Hkv, "k")
-                p_v, stride = self._rows(v, rows, self.Hkv, "v")
-                assert stride == kv_stride, "k and v: equal strides"
-            addresses += (p_k, p_v)
-        if out is not False:
-            p_out = None
-            if out is not None:
-                p_out, out_stride = self._rows(out, rows, self.H, "out")
-            addresses.append(p_out)
+    def _write_call(self, layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen) -> None:
+        """Checks what the calls share and writes it down; rows None: one per sequence."""
+        shape = table.shape
+        assert table.dtype is _I32 and len(shape) == 2 and table.get_device() == self._index, f"table: int32 [B][cols] on {self.device}"
+        B, cols = shape
+        stride = cols
+        if not table.is_contiguous():
+            stride, inner = table.stride()
+            assert inner == 1, "table: entries of a sequence side by side"
+            stride = stride if B > 1 else cols
+        p_weight = p_pos = p_seen = p_starts = track = 0
         if weight is not None:
-            p_weight, track = self._track(weight, B, torch.float32, "weight")
+            p_weight, track = self._track(weight, B, _F32, "weight")
         if pos is not None:
-            p_pos, slots = self._track(pos, B, torch.int32, "pos")
+            p_pos, slots = self._track(pos, B, _I32, "pos")
             assert track in (0, slots), "weight and pos: as many slots"
             track = slots
-        self._pack(self._call, 0, layer, B, table.data_ptr(), cols, n_sink, table.stride(0) if B > 1 else cols, self._ints(lens, B, "lens"), p_starts,
-                   rows, q_stride, kv_stride, out_stride, window, p_weight, p_pos, 0 if seen is None else self._ints(seen, B, "seen"), track)
+        if seen is not None:
+            p_seen = self._ints(seen, B, "seen")
+        if starts is not None:
+            p_starts = self._ints(starts, B + 1, "starts")
+        self._pack(self._call, 0, layer, B, table.data_ptr(), cols, n_sink, stride, self._ints(lens, B, "lens"), p_starts, B if rows is None else rows,
+                   *strides, window, p_weight, p_pos, p_seen, track)
+
+    def _run(self, where: str, stream, fn, *args) -> None:
         if self._index == _current_device():
-            rc = fn(self._h, self._callp, *addresses, *args, _stream(stream))
+            rc = fn(self._h, self._callp, *args, _stream(stream))
         else:
             with torch.cuda.device(self.device):
-                rc = fn(self._h, self._callp, *addresses, *args, _stream(stream))
+                rc = fn(self._h, self._callp, *args, _stream(stream))
         if rc:
             _check(rc, where)
+
+    def _qkv(self, q, k, v, out, rows: int):
+        """Addresses of q, k, v, out as far as there are, and their strides."""
+        p_q = p_k = p_v = p_out = None
+        q_stride = kv_stride = out_stride = 0
+        if q is not None:
+            p_q, q_stride = self._rows(q, rows, self.H, "q")
+        assert (k is None) == (v is None), "k and v: both or neither"
+        if k is not None:
+            p_k, kv_stride = self._rows(k, rows, self.Hkv, "k")
+            p_v, stride = self._rows(v, rows, self.Hkv, "v")
+            assert stride == kv_stride, "k and v: equal strides"
+        if out is not None:
+            p_out, out_stride = self._rows(out, rows, self.H, "out")
+        return (p_q, p_k, p_v, p_out), (q_stride, kv_stride, out_stride)
 
     def glide_paged_prefill(self, table, lens, starts, q, k, v, out=None, lse=None, window: int = -1, n_sink: int = 0, weight=None,
                             pos=None, seen=None, layer: int = 0, stream=None) -> None:
         """Stores the new tokens (rows starts[b] .. starts[b + 1] - 1 of k, v; None: they are in the cache) and, with out, attends."""
-        rows = (k if k is not None else q).size(0)
-        self._run("glide_paged_prefill", stream, self.lib.glide_paged_prefill, layer, table, lens, starts, rows, q, k, v, out, window, n_sink,
-                  weight, pos, seen, self._lse(lse, rows))
+        rows = (k if k is not None else q).shape[0]
+        tensors, strides = self._qkv(q, k, v, out, rows)
+        self._write_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen)
+        self._run("glide_paged_prefill", stream, self.lib.glide_paged_prefill, *tensors, self._lse(lse, rows))
 
     def glide_paged_decode(self, table, lens, q, k, v, out, lse=None, window: int = -1, n_sink: int = 0, weight=None, pos=None,
                            seen=None, layer: int = 0, stream=None) -> None:
         """One new token per sequence: stored at slot lens[b] - 1 (k, v None: it is in the cache), attends; weight: the account."""
-        self._run("glide_paged_decode", stream, self.lib.glide_paged_decode, layer, table, lens, None, None, q, k, v, out, window, n_sink,
-                  weight, pos, seen, self._lse(lse, table.size(0)))
+        rows = table.shape[0]
+        tensors, strides = self._qkv(q, k, v, out, rows)
+        self._write_call(layer, table, lens, None, rows, strides, window, n_sink, weight, pos, seen)
+        self._run("glide_paged_decode", stream, self.lib.glide_paged_decode, *tensors, self._lse(lse, rows))
 
     def glide_paged_weights(self, table, lens, starts, q, lse, weight, window: int = -1, n_sink: int = 0, layer: int = 0, stream=None) -> None:
         """Adds the weights that the tokens q with the row sums lse (of glide_paged_prefill) give every slot to the account."""
-        rows = q.size(0)
-        self._run("glide_paged_weights", stream, self.lib.glide_paged_weights, layer, table, lens, starts, rows, q, False, False, False, window,
-                  n_sink, weight, None, None, self._lse(lse, rows))
+        rows = q.shape[0]
+        tensors, strides = self._qkv(q, None, None, None, rows)
+        self._write_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, None, None)
+        self._run("glide_paged_weights", stream, self.lib.glide_paged_weights, tensors[0], self._lse(lse, rows))
 
     def glide_paged_evict(self, table, lens, seen, weight, pos, budget: int, new_lens, recent: int = 0, n_sink: int = 0, weight_out=None,
                           pos_out=None, layer: int = 0, stream=None) -> None:
         """Every (sequence, KV head) keeps min(lens[b], budget) slots; weight_out, pos_out None: the account changes in place."""
-        B = table.size(0)
-        p_weight, slots = self._track(weight if weight_out is None else weight_out, B, torch.float32, "weight_out")
-        p_pos, pos_slots = self._track(pos if pos_out is None else pos_out, B, torch.int32, "pos_out")
-        assert slots == pos_slots == weight.size(2), "the accounts: as many slots"
-        self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, layer, table, lens, None, None, False, False, False, False, -1,
-                  n_sink, weight, pos, seen, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
+        B = table.shape[0]
+        p_weight, slots = self._track(weight if weight_out is None else weight_out, B, _F32, "weight_out")
+        p_pos, pos_slots = self._track(pos if pos_out is None else pos_out, B, _I32, "pos_out")
+        assert slots == pos_slots == weight.shape[2], "the accounts: as many slots"
+        self._write_call(layer, table, lens, None, None, (0, 0, 0), -1, n_sink, weight, pos, seen)
+        self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
 
     def glide_paged_device_status(self) -> int:
         """The status word of the device-side checks, read and cleared (0: nothing was recorded)."""
