@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     }
     if (lane == 0) {
       const size_t at = size_t(u) * size_t(p.track_stride) + i;
-      if (keep && !paged_sees(p, i, i)) p.weight[at] = 0.f;   // (otherwise the join kernel writes it)
+      if (keep && !paged_sees(p, i, i)) p.weight[at] = 0.f;   // (otherwise the account's kernel writes it)
       if (p.pos) p.pos[at] = p.seen[b] - 1;
     }
   }

@@ -2,10 +2,10 @@
 //
 // A cluster of up to 8 CTAs owns one (sequence, KV head), each CTA a run of its slots.  The weights become unsigned numbers in the floats'
 // order (protected slots above all others) and stay in shared memory; e = len - kept slots leave: those below the e-th least number T,
-// and of those equal to T the lowest slots.  T is found by four digits of 8 bits: a histogram per CTA, added up over the cluster
-// through distributed shared memory by every CTA for itself (three digits of 11, 11 and 10 bits took 22800 cycles for 32768 slots: 2048
-// counts of eight CTAs are read by each of them) (one slot that leaves, as in the steady state of a decode loop, is found as
-// a minimum instead).  The freed slots below the new length and the kept ones behind it are listed in slot order; the i-th of one moves
+// and of those equal to T the lowest slots.  T is found by up to four digits of 8 bits: a histogram per CTA, added up over
+// the cluster through distributed shared memory by every CTA for itself.  (Three digits of 11, 11 and 10 bits: 22800 cycles for 32768 slots of 8
+// clusters against 20000, as each CTA reads 2048 counts of eight.)  One slot that leaves, as in the steady state of a decode loop, is found
+// as a minimum instead, and the last slot takes its place.  The freed slots below the new length and the kept ones behind it are listed in slot order; the i-th of one moves
 // into the i-th of the other: sources lie behind the new length and targets before it, so no move waits for another.
 // Bound: the chain of small steps (a meeting of the cluster per digit); the rows of many moves by memory.
 #include <cooperative_groups.h>

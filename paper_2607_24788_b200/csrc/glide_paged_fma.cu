@@ -1,10 +1,14 @@
 // Paged attention of prompts on the CUDA cores, fp32.
 //
 // A CTA of 256 threads owns 64 query rows (token * G + head) of one (sequence, KV head) and goes through tiles of 64 slots; a thread
-// (ty, tx) of 16 x 16 has rows 4 ty .. 4 ty + 3 and slots 4 tx .. 4 tx + 3 of the scores and columns 4 tx .. (and 64 + 4 tx ..) of the
-// output.  Where that makes fewer CTAs than the GPU has SMs, a CTA owns 16 rows (the account: 16 slots), one per thread.  Q and K lie in shared memory by feature, so that a step of the product takes two 16-byte reads for 16 multiply-adds; the
-// next tile's rows are on their way in registers meanwhile.  Weights are taken against a reference that moves when a score exceeds
-// it by more than 8 in the exponent.  Bound: the multiply-adds.
+// (ty, tx) of 16 x 16 has rows 4 ty .. 4 ty + 3 and slots tx, tx + 16, .. of the scores and columns 4 tx .. (and 64 + 4 tx ..) of the
+// output.  Where that makes fewer CTAs than the GPU has SMs, a CTA owns 16 rows (the account: 16 slots), one per thread.  Rows come by
+// cp.async, a tile ahead, and lie in shared memory as in memory, their 16-byte chunks exchanged by the row's low bits so that 16 rows are read in
+// the two turns that 256 bytes take; four features of a row, or a row's weights of four slots, are one read.  (By feature, through
+// registers, a lane per row: 32 lines a load and a turn per line.  512 tokens of 4 heads of 64, windows of 64, prompt and account: 43 us, this 33;
+// 1000 tokens of 32 / 8 heads of 128: 962 us, this 725.)
+// Weights are taken against a reference that moves when a score exceeds it by more than 8 in the exponent.  Bound: shared-memory reads for
+// 16 rows, the multiply-adds for 64.
 // What a row does not see does not reach it: scores are selected; rows of V that no row of the CTA sees are zeros; a row whose output
 // is not finite all the same is computed once more by itself.
 #include <algorithm>
@@ -23,68 +27,49 @@ constexpr float kLazy = 8.0f;
 // R rows per thread of the operand that the CTA keeps, 4 of the one that it goes through
 template <int D, int R>
 struct Smem {
-  static constexpr int kRows = 16 * R;
-  float q[D][kRows], k[D][kSlots + 4], v[kSlots][D], p[kSlots][kRows + 4];
+  float q[16 * R][D], k[2][kSlots][D], v[2][kSlots][D], p[16 * R][kSlots + 4];
 };
 template <int D, int R>
 struct AccountSmem {
-  static constexpr int kRows = 16 * R;
-  float k[D][kRows], q[D][kSlots + 4], lse[kSlots], part[kRows][17];
+  float k[16 * R][D], q[2][kSlots][D], lse[2][kSlots], part[16 * R][17];
 };
-// the R rows of a thread side by side
-template <int R>
-__device__ __forceinline__ void load_rows(const float *from, float (&x)[R]) {
-  if constexpr (R == 4) {
-    const float4 v = *reinterpret_cast<const float4 *>(from);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-  } else {
-    x[0] = *from;
-  }
-}
-
-// Rows of 64 slots (or queries) on their way from memory: thread (r = tid & 63, c = tid >> 6) has 16-byte chunks c, c + 4, ... of row r
+// index of 16-byte chunk c of row r
 template <int D>
-struct Staged {
-  static constexpr int kEach = D / 16;
-  float4 x[kEach];
-  __device__ __forceinline__ void load(const float *row) {   // nullptr: zeros
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      x[i] = row ? reinterpret_cast<const float4 *>(row)[(threadIdx.x >> 6) + 4 * i] : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  template <int W>
-  __device__ __forceinline__ void store_by_feature(float (&to)[D][W], float scale) {   // (rows beyond W: none are kept)
-    const int r = threadIdx.x & 63;
-    if (W < kSlots && r >= W) return;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int c = ((threadIdx.x >> 6) + 4 * i) * 4;
-      to[c][r] = x[i].x * scale, to[c + 1][r] = x[i].y * scale, to[c + 2][r] = x[i].z * scale, to[c + 3][r] = x[i].w * scale;
-    }
-  }
-  __device__ __forceinline__ void store(float (&to)[kSlots][D]) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) *reinterpret_cast<float4 *>(&to[threadIdx.x & 63][((threadIdx.x >> 6) + 4 * i) * 4]) = x[i];
+__device__ __forceinline__ int chunk_at(int r, int c) { return r * D + ((c ^ (r & 7)) << 2); }
+template <int N>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Rows of a tile that a thread copies: chunk `chunk` of rows row(0), row(1), ...
+template <int D>
+struct Copy {
+  static constexpr int kChunks = D / 4, kAtOnce = kThreads / kChunks, kEach = kSlots / kAtOnce;
+  static __device__ __forceinline__ int chunk() { return threadIdx.x % kChunks; }
+  static __device__ __forceinline__ int row(int i) { return threadIdx.x / kChunks + i * kAtOnce; }
+  // row r from `src` (its first element; nullptr: zeros)
+  static __device__ __forceinline__ void ask(float *tile, int r, const float *src, const void *anywhere) {
+    cp_async16(smem_u32(tile + chunk_at<D>(r, chunk())), src ? static_cast<const void *>(src + chunk() * 4) : anywhere, src != nullptr);
   }
 };
 
-// s[a][c] = row R ty + a of `kept` times row 4 tx + c of `other`
+// s[a][c] = row R ty + a of `kept` times row tx + 16 c of `other`
 template <int D, int R>
-__device__ __forceinline__ void scores(const float (&kept)[D][16 * R], const float (&other)[D][kSlots + 4], float (&s)[R][4]) {
+__device__ __forceinline__ void scores(const float *kept, const float *other, float (&s)[R][4]) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
   for (int a = 0; a < R; ++a)
 #pragma unroll
     for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
-#pragma unroll 8
-  for (int d = 0; d < D; ++d) {
-    float x[R], y[4];
-    load_rows<R>(&kept[d][ty * R], x);
-    load_rows<4>(&other[d][tx * 4], y);
+#pragma unroll 4
+  for (int ch = 0; ch < D / 4; ++ch) {
+    float4 x[R], y[4];
+#pragma unroll
+    for (int a = 0; a < R; ++a) x[a] = *reinterpret_cast<const float4 *>(kept + chunk_at<D>(ty * R + a, ch));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4 *>(other + chunk_at<D>(tx + 16 * c, ch));
 #pragma unroll
     for (int a = 0; a < R; ++a)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[a][c] = fmaf(x[a], y[c], s[a][c]);
+      for (int c = 0; c < 4; ++c) s[a][c] = fmaf(x[a].x, y[c].x, fmaf(x[a].y, y[c].y, fmaf(x[a].z, y[c].z, fmaf(x[a].w, y[c].w, s[a][c]))));
   }
 }
 
@@ -153,17 +138,40 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     st.t0 = int(int64_t(all) * blockIdx.y / gridDim.y);
     st.n = int(int64_t(all) * (blockIdx.y + 1) / gridDim.y) - st.t0;
   }
-  const int r_mine = tid & 63;   // the row of Q, K, V that this thread brings
-  auto row_of = [&](const void *pages, int j) -> const float * {
-    if (j > q1 || (p.window >= 0 && j <= q0 - p.window && j >= p.n_sink)) return nullptr;
-    const int page = paged_page(p, at.seq, j);
-    return page < 0 ? nullptr : reinterpret_cast<const float *>(pages) + paged_row(p, page, j, g);
+  using Cp = Copy<D>;
+  // the table's entries for this thread's rows of tile t (looked at a tile later); -1 where no row of the CTA sees the slot
+  auto entries = [&](int t, int (&e)[Cp::kEach]) {
+#pragma unroll
+    for (int i = 0; i < Cp::kEach; ++i) {
+      const int j = t < st.n ? st.slot(t) + Cp::row(i) : INT32_MAX;
+      const bool seen = j <= q1 && !(p.window >= 0 && j <= q0 - p.window && j >= p.n_sink);
+      e[i] = seen ? p.table[size_t(at.seq) * size_t(p.table_stride) + size_t(j >> p.page_shift)] : -1;
+    }
   };
-  Staged<D> a, b;
-  a.load(r_mine < ntok * G ? reinterpret_cast<const float *>(p.q) + size_t(at.row0 + at.tok0 + r_mine / G) * size_t(p.q_stride) +
-                                 size_t(g * G + r_mine % G) * D
-                           : nullptr);
-  a.store_by_feature(sm.q, p.scale_log2);
+  auto ask = [&](int t, const int (&e)[Cp::kEach]) {
+#pragma unroll
+    for (int i = 0; i < Cp::kEach; ++i) {
+      const int j = st.slot(t) + Cp::row(i);
+      const bool good = unsigned(e[i]) < unsigned(p.n_pages);
+      if (!good && j <= q1 && !(p.window >= 0 && j <= q0 - p.window && j >= p.n_sink)) atomicExch(p.status, kDevBadPage);
+      const size_t from = good ? paged_row(p, e[i], j, g) : 0;
+      Cp::ask(&sm.k[t & 1][0][0], Cp::row(i), good ? reinterpret_cast<const float *>(p.k) + from : nullptr, p.k);
+      Cp::ask(&sm.v[t & 1][0][0], Cp::row(i), good ? reinterpret_cast<const float *>(p.v) + from : nullptr, p.k);
+    }
+  };
+  int entry[Cp::kEach];
+  entries(0, entry);
+#pragma unroll
+  for (int i = 0; i < Cp::kEach; ++i) {
+    const int r = Cp::row(i);
+    if (r < 16 * R)
+      Cp::ask(&sm.q[0][0], r, r < ntok * G ? reinterpret_cast<const float *>(p.q) + size_t(at.row0 + at.tok0 + r / G) * size_t(p.q_stride) +
+                                                 size_t(g * G + r % G) * D
+                                           : nullptr, p.q);
+  }
+  if (st.n) ask(0, entry);
+  cp_async_commit();
+  entries(1, entry);
   float o[R][4 * N], m[R], l[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -171,25 +179,23 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
 #pragma unroll
     for (int c = 0; c < 4 * N; ++c) o[i][c] = 0.f;
   }
-  if (st.n) a.load(row_of(p.k, st.slot(0) + r_mine)), b.load(row_of(p.v, st.slot(0) + r_mine));
 #pragma unroll 1
   for (int t = 0; t < st.n; ++t) {
     const int j0 = st.slot(t);
-    __syncthreads();   // the tile before has been read
-    a.store_by_feature(sm.k, 1.f);
-    b.store(sm.v);
+    if (t + 1 < st.n) ask(t + 1, entry);
+    cp_async_commit();
+    entries(t + 2, entry);
+    wait_copies<1>();
     __syncthreads();
-    if (t + 1 < st.n) a.load(row_of(p.k, st.slot(t + 1) + r_mine)), b.load(row_of(p.v, st.slot(t + 1) + r_mine));
     float s[R][4];
-    scores<D, R>(sm.q, sm.k, s);
+    scores<D, R>(&sm.q[0][0], &sm.k[t & 1][0][0], s);
     const bool whole = j0 + kSlots - 1 <= q0 && (p.window < 0 || j0 > q1 - p.window || j0 + kSlots <= p.n_sink);
     bool grows = false;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int mine = q0 + (ty * R + i) / G;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (!whole && !paged_sees(p, mine, j0 + tx * 4 + c)) s[i][c] = -CUDART_INF_F;
+      for (int c = 0; c < 4; ++c) s[i][c] = whole || paged_sees(p, mine, j0 + tx + 16 * c) ? s[i][c] * p.scale_log2 : -CUDART_INF_F;
       const float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
       grows |= top > m[i] + kLazy || (m[i] == -CUDART_INF_F && top > -CUDART_INF_F);
     }
@@ -207,34 +213,39 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
         for (int c = 0; c < 4 * N; ++c) o[i][c] *= f;
       }
     }
+    // (the rows of a warp's weights are read by that warp alone)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const float ref = m[i] == -CUDART_INF_F ? 0.f : m[i];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[i][c] = ex2(s[i][c] - ref), l[i] += s[i][c];
-    }
-    // (the rows of a warp's weights are read by that warp alone)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if constexpr (R == 4) *reinterpret_cast<float4 *>(&sm.p[tx * 4 + c][ty * R]) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
-      else sm.p[tx * 4 + c][ty] = s[0][c];
-    }
-    __syncwarp();
-#pragma unroll 8
-    for (int j = 0; j < kSlots; ++j) {
-      float ws[R];
-      load_rows<R>(&sm.p[j][ty * R], ws);
-#pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const float4 v = *reinterpret_cast<const float4 *>(&sm.v[j][n * 64 + tx * 4]);
-        const float vs[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) o[i][n * 4 + c] = fmaf(ws[i], vs[c], o[i][n * 4 + c]);
+      for (int c = 0; c < 4; ++c) {
+        s[i][c] = ex2(s[i][c] - ref), l[i] += s[i][c];
+        sm.p[ty * R + i][tx + 16 * c] = s[i][c];
       }
     }
     __syncwarp();
+    const float *v = &sm.v[t & 1][0][0];
+#pragma unroll 4
+    for (int j = 0; j < kSlots; j += 4) {
+      float w[R][4];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float4 x = *reinterpret_cast<const float4 *>(&sm.p[ty * R + i][j]);
+        w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
+      }
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float4 y = *reinterpret_cast<const float4 *>(v + chunk_at<D>(j + jj, n * 16 + tx));
+          const float ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[i][n * 4 + c] = fmaf(w[i][jj], ys[c], o[i][n * 4 + c]);
+        }
+    }
+    __syncthreads();   // the tile has been read
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -290,7 +301,8 @@ __global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __gri
   constexpr int TOK = kSlots / G, kKept = 16 * R;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   auto &sm = *reinterpret_cast<AccountSmem<D, R> *>(smem_raw);
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r_mine = tid & 63;
+  using Cp = Copy<D>;
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   wait_for_predecessor();
   int base = 0;   // tiles of the sequences before
   int64_t item = blockIdx.x;
@@ -303,41 +315,49 @@ __global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __gri
       const int t0 = max(0, j0 - q0);
       const int t1 = p.window >= 0 && j0 >= p.n_sink ? min(n_new, p.window == 0 ? 0 : j0 + kKept - 1 + p.window - q0) : n_new;
       if (t0 >= t1) continue;
-      float lse = 0.f;   // of the row that this thread brings
-      auto load_q = [&](int tok, Staged<D> &x) {
-        const int tk = tok + r_mine / G;
-        x.load(tk < t1 ? reinterpret_cast<const float *>(p.q) + size_t(row0 + tk) * size_t(p.q_stride) + size_t(g * G + r_mine % G) * D : nullptr);
-        lse = tk < t1 ? p.lse[size_t(row0 + tk) * p.H + g * G + r_mine % G] : 0.f;
+      auto ask = [&](int tok, int buf) {   // rows of the tokens from tok on, and their row sums
+#pragma unroll
+        for (int i = 0; i < Cp::kEach; ++i) {
+          const int r = Cp::row(i), tk = tok + r / G;
+          Cp::ask(&sm.q[buf][0][0], r, tk < t1 ? reinterpret_cast<const float *>(p.q) + size_t(row0 + tk) * size_t(p.q_stride) + size_t(g * G + r % G) * D : nullptr, p.q);
+        }
+        const int tk = tok + tid / G;
+        if (tid < kSlots && tk < t1)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&sm.lse[buf][tid])), "l"(p.lse + size_t(row0 + tk) * p.H + g * G + tid % G)
+                       : "memory");
       };
-      Staged<D> a, k;
-      load_q(t0, a);
-      {
-        const int j = j0 + r_mine, page = r_mine < kKept && j < len ? paged_page(p, b, j) : -1;
-        k.load(page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g));
-      }
       __syncthreads();   // the tile before has been read
-      k.store_by_feature(sm.k, 1.f);
+#pragma unroll
+      for (int i = 0; i < Cp::kEach; ++i) {
+        const int r = Cp::row(i), j = j0 + r;
+        if (r >= kKept) continue;
+        const int page = j < len ? paged_page(p, b, j) : -1;
+        Cp::ask(&sm.k[0][0], r, page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g), p.k);
+      }
+      ask(t0, 0);
+      cp_async_commit();
       float sum[R];
 #pragma unroll
       for (int i = 0; i < R; ++i) sum[i] = 0.f;
+      int buf = 0;
 #pragma unroll 1
-      for (int tok = t0; tok < t1; tok += TOK) {
+      for (int tok = t0; tok < t1; tok += TOK, buf ^= 1) {
+        if (tok + TOK < t1) ask(tok + TOK, buf ^ 1);
+        cp_async_commit();
+        wait_copies<1>();
         __syncthreads();
-        a.store_by_feature(sm.q, p.scale_log2);
-        if (tid < kSlots) sm.lse[r_mine] = lse == -CUDART_INF_F ? 0.f : lse * kLog2e;
-        __syncthreads();
-        if (tok + TOK < t1) load_q(tok + TOK, a);
         float s[R][4];
-        scores<D, R>(sm.k, sm.q, s);
+        scores<D, R>(&sm.k[0][0], &sm.q[buf][0][0], s);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const int tk = tok + (tx * 4 + c) / G;
+          const int r = tx + 16 * c, tk = tok + r / G;
           if (tk >= t1) continue;
-          const float x = sm.lse[tx * 4 + c];
+          const float lse = sm.lse[buf][r], x = lse == -CUDART_INF_F ? 0.f : lse * kLog2e;
 #pragma unroll
           for (int i = 0; i < R; ++i)
-            if (paged_sees(p, q0 + tk, j0 + ty * R + i)) sum[i] += ex2(s[i][c] - x);
+            if (paged_sees(p, q0 + tk, j0 + ty * R + i)) sum[i] += ex2(fmaf(s[i][c], p.scale_log2, -x));
         }
+        __syncthreads();   // the rows have been read
       }
 #pragma unroll
       for (int i = 0; i < R; ++i) sm.part[ty * R + i][tx] = sum[i];
