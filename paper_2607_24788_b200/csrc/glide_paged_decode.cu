@@ -399,8 +399,7 @@ template <typename T, int D, int G>
 __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, int c0, int c1, int t0, int share, bool keep) {
   const int tid = threadIdx.x, lane = tid & 31;
   constexpr int kEach = (G * D + kThreads - 1) / kThreads;   // outputs of a thread; those of a warp are of one head each
-  constexpr int kRecord = G * (D + 3);
-  // (the code is kept short: few CTAs come here, and each fetches it anew)
+  constexpr int kRecord = G * (D + 3), kAhead = 32 / kEach < 16 ? 32 / kEach : 16;
   float M[kEach], L[kEach], X[kEach], sum[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) M[e] = -CUDART_INF_F, L[e] = X[e] = sum[e] = 0.f;
@@ -409,28 +408,35 @@ __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, 
   for (int c = c0; c <= c1; c += 32) {
     const int some = min(32, c1 + 1 - c);
     const float *rec = record<D, G>(p, c, 0), *rec0 = rec + (c == c0 ? first * kRecord : 0);
-    float f[kEach], part[kEach], top[kEach];
+    float f[kEach], part[kEach], top[kEach], v[kEach][kAhead], m[kEach], l[kEach], x[kEach];
+    // (the sums of record c + lane and the first records' values on their way together: a trip to L2 and back is some 900 cycles)
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int h = min((tid + e * kThreads) / D, G - 1);
-      float m = -CUDART_INF_F, l = 0.f, x = 0.f;             // of record c + lane
-      if (lane < some) {
-        const float *r = (lane ? rec + lane * 2 * kRecord : rec0) + G * D + h;
-        m = __ldcg(r), l = __ldcg(r + G), x = __ldcg(r + 2 * G);
-      }
-      top[e] = warp_max(m);
-      f[e] = part_factor(m, top[e]);
-      const float ls = warp_sum(l * f[e]), xs = warp_sum(x * f[e]), now = fmaxf(M[e], top[e]), fa = part_factor(M[e], now);
+      const float *r = (lane ? rec + lane * 2 * kRecord : rec0) + G * D + h;
+      const bool there = lane < some;
+      m[e] = there ? __ldcg(r) : -CUDART_INF_F, l[e] = there ? __ldcg(r + G) : 0.f, x[e] = there ? __ldcg(r + 2 * G) : 0.f;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        v[e][k] = k < some && tid + e * kThreads < G * D ? __ldcg((k ? rec + k * 2 * kRecord : rec0) + tid + e * kThreads) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      top[e] = warp_max(m[e]);
+      f[e] = part_factor(m[e], top[e]);
+      const float ls = warp_sum(l[e] * f[e]), xs = warp_sum(x[e] * f[e]), now = fmaxf(M[e], top[e]), fa = part_factor(M[e], now);
       L[e] = fmaf(L[e], fa, ls * part_factor(top[e], now)), X[e] = fmaf(X[e], fa, xs * part_factor(top[e], now));
       sum[e] *= fa, part[e] = 0.f, M[e] = now;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) part[e] = fmaf(v[e][k], __shfl_sync(0xffffffffu, f[e], k), part[e]);
     }
 #pragma unroll 8
-    for (int k = 0; k < some; ++k) {
-      const float *r = (k ? rec + k * 2 * kRecord : rec0) + tid;
+    for (int k = kAhead; k < some; ++k) {
+      const float *r = rec + k * 2 * kRecord + tid;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const float v = tid + e * kThreads < G * D ? __ldcg(r + e * kThreads) : 0.f;
-        part[e] = fmaf(v, __shfl_sync(0xffffffffu, f[e], k), part[e]);
+        const float w = tid + e * kThreads < G * D ? __ldcg(r + e * kThreads) : 0.f;
+        part[e] = fmaf(w, __shfl_sync(0xffffffffu, f[e], k), part[e]);
       }
     }
 #pragma unroll
