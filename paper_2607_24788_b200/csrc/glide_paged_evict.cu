@@ -150,13 +150,11 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
         if (tid < kBins) hist[tid] = 0;
         __syncthreads();
       }
-      for (int i0 = warp * 32; i0 < n; i0 += kThreads) {
-        const int i = i0 + lane;
-        const uint32_t k = i < n ? key(i) : 0u;
-        const bool in = i < n && (step == 0 || (k >> (shift + 8)) == (least >> (shift + 8)));
-        const uint32_t digit = in ? (k >> shift) & 255u : 256u;
-        const unsigned same = __match_any_sync(0xffffffffu, digit);   // (weights lie within a few octaves: lanes often share a bin)
-        if (in && lane == __ffs(int(same)) - 1) atomicAdd(&hist[digit], __popc(same));
+      // (lanes that share a bin, as weights of a few octaves often do, added up by __match_any_sync first: 28.0 us instead of 26.3 for
+      // 8 x 32768 slots)
+      for (int i = tid; i < n; i += kThreads) {
+        const uint32_t k = key(i);
+        if (step == 0 || (k >> (shift + 8)) == (least >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
       }
       cluster.sync();
       int c = 0, mine = 0;   // of bin tid: all CTAs', the ones before this CTA's
