@@ -23,7 +23,7 @@ namespace glide {
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 8;             // (12: a unit's tiles end sooner, its meeting later: 0 to 3 us longer between 600 and 4500 slots)
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxGrid = 256;          // CTAs that the records are laid out for
 constexpr float kLazy = 8.0f;
@@ -50,7 +50,7 @@ struct Smem {
   static constexpr int kSlots = G == 8 ? kWarps / 2 : kWarps;         // warps whose O is here at a time when a CTA's warps meet
   float o[kSlots][G][D + 4];
   float m[kWarps][G], l[kWarps][G], e[kWarps][G];                     // maximum; sum of the weights as O has them; exact sum
-  float q[sizeof(T) == 4 ? G : 1][D];                                 // fp32: the unit's queries, scaled
+  alignas(16) float q[sizeof(T) == 4 ? G : 1][D];                     // fp32: the unit's queries, scaled (read 16 bytes at a time)
   float p[sizeof(T) == 4 ? kWarps : 1][Shape<T, D>::kTile][G];        // fp32: a tile's weights
   int len[kMaxPagedBatch], prefix[kMaxPagedBatch + 1];                // slots; tiles of the sequences before
   int warp_sums[kWarps], warp_most[kWarps];
