@@ -398,6 +398,7 @@ def make_paged_config(k_pages: torch.Tensor, n_q_heads: int, max_batch: int, max
     """The configuration of pages k_pages [L][n_pages][H_kv][page_size][d], which may be a view with other strides."""
     assert k_pages.dim() == 5 and k_pages.stride(4) == 1, "pages are [L][n_pages][H_kv][page_size][d], features side by side"
     L, n, hkv, page, d = k_pages.shape
+    assert k_pages.stride(3) >= d, "pages: slots that share memory"   # (strides of 0 would say "side by side" to the library)
     cfg = glide_paged_config(n_layers=L, n_q_heads=n_q_heads, n_kv_heads=hkv, head_dim=d,
                              io_dtype={torch.float32: GLIDE_F32, torch.bfloat16: GLIDE_BF16}[k_pages.dtype], page_size=page, n_pages=n,
                              max_batch=int(max_batch), max_tokens=int(max_tokens), softmax_scale=float(softmax_scale), weights=int(bool(weights)))
@@ -462,7 +463,10 @@ class GlidePaged:
             return t.data_ptr(), 0
         stride = t.stride()
         assert stride[2] == 1 and (heads == 1 or stride[1] == self.d), f"{what}: a token's heads have to lie side by side"
-        return t.data_ptr(), stride[0] if rows > 1 else 0
+        if rows == 1:
+            return t.data_ptr(), 0
+        assert stride[0] >= heads * self.d, f"{what}: tokens that share memory"   # (0 would say "side by side" to the library)
+        return t.data_ptr(), stride[0]
 
     def _track(self, t: torch.Tensor, B: int, dtype, what: str):
         shape = t.shape

@@ -92,3 +92,35 @@ def test_the_pages_strides_are_those_of_the_tensor():
     cfg = glide.make_paged_config(k, 4, 2, 100)
     assert (cfg.layer_stride, cfg.page_stride, cfg.head_stride, cfg.row_stride) == (40960, 4096, 64, 128)
     assert (cfg.n_layers, cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim) == (3, 10, 2, 32, 64)
+
+
+def binding(H=4, Hkv=2, d=64):
+    """A GlidePaged without a handle, whose tensors live on the host: what it checks and packs before the library is called."""
+    h = object.__new__(glide.GlidePaged)
+    h.device, h._index, h.dtype, h.H, h.Hkv, h.d, h._h = torch.device("cpu"), -1, torch.float32, H, Hkv, d, None
+    return h
+
+
+def test_rows_that_share_memory_are_refused():
+    """A token stride of 0 (an expanded view) says "side by side" to the library, which would read and write behind the tensor."""
+    h = binding()
+    row = torch.zeros(1, 4, 64)
+    assert h._rows(row, 1, 4, "q")[1] == 0
+    assert h._rows(row.expand(1, 4, 64), 1, 4, "q")[1] == 0
+    assert h._rows(torch.zeros(5, 6, 64)[:, :4], 5, 4, "q")[1] == 6 * 64
+    assert h._rows(torch.zeros(5, 4, 64)[:, ::4], 5, 1, "k")[1] == 4 * 64
+    for shared in (row.expand(5, 4, 64), torch.zeros(9 * 64).as_strided((5, 4, 64), (64, 64, 1))):
+        with pytest.raises(AssertionError):
+            h._rows(shared, 5, 4, "q")
+    with pytest.raises(AssertionError):
+        h._rows(torch.zeros(1, 1, 64).expand(5, 1, 64), 5, 1, "k")
+    with pytest.raises(AssertionError):
+        h._qkv(torch.zeros(5, 4, 64), None, None, row.expand(5, 4, 64), 5)
+
+
+def test_pages_that_share_memory_are_refused():
+    """Strides that are all 0 say "side by side" too."""
+    row = torch.zeros(64)
+    for shape in ((1, 8, 2, 16, 64), (3, 8, 2, 16, 64)):
+        with pytest.raises(AssertionError):
+            glide.make_paged_config(row.expand(shape), 4, 2, 100)
