@@ -386,15 +386,17 @@ int glide_paged_destroy(glide_paged *p);
 /* Store the new tokens of every sequence (dev_k, dev_v [n_tokens][H_kv][d]) in the last slots of its length and, unless
  * dev_out is NULL, attend: dev_q, dev_out [n_tokens][H][d], dev_lse fp32 [n_tokens][H] or NULL.  With dev_k and dev_v NULL
  * the tokens are in the cache already.  Where dev_weight / dev_pos are given, the new slots' account starts at 0 and
- * their positions are seen - T_b ... seen - 1; the weights of this call are not added (glide_paged_weights does that).
+ * their positions are seen - T_b ... seen - 1, with dev_k and dev_v or without; the weights of this call are not added
+ * (glide_paged_weights does that).
  * With bf16 I/O the outputs with dev_lse and without it may differ in their last bits. */
 int glide_paged_prefill(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
                         void *dev_out, float *dev_lse, void *stream);
 
 /* One new token for every sequence: row b of dev_q, dev_out [B][H][d], dev_k, dev_v [B][H_kv][d], dev_lse [B][H] or NULL.
  * The token is stored at slot lens[b] - 1 and attends; with dev_k and dev_v NULL it is in the cache already.  Where
- * dev_weight is given, the weights of the step are added to the account (the new slot's starts at 0), and dev_pos, if
- * given, receives the new slot's position.  A sequence of length 0 stores nothing.  The cache is read once, split over
+ * dev_weight is given, the weights of the step are added to the account: the new slot's starts at 0, but with dev_k and
+ * dev_v NULL it goes on from what it is.  dev_pos, if given, receives the new slot's position, with dev_k and dev_v or
+ * without.  A sequence of length 0 stores nothing.  The cache is read once, split over
  * its length across the GPU and joined. */
 int glide_paged_decode(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
                        void *dev_out, float *dev_lse, void *stream);

@@ -24,7 +24,8 @@ __device__ bool row_of(const PagedParams &p, int64_t r, int &b, int &slot) {
   return r >= row0 && r < row0 + n;
 }
 
-// A block per 16 new tokens: their places are looked up by a lane each, then all threads copy, 16 bytes of K and of V at a time.  Bound: the
+// A block per 16 new tokens: their places are looked up by a lane each, which also starts their account and writes their positions; then,
+// where the call brings K and V, all threads copy, 16 bytes of each at a time.  Bound: the
 // rows' bytes.  (A warp per token and head, which looked its place up by itself: 30 us for 12401 tokens of 8 heads of 256 bytes, this 16.)
 constexpr int kStoreTokens = 16;
 template <typename T, int D>
@@ -38,8 +39,8 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
     int b, slot;
     int64_t at = -1;
     if (r < p.n_tokens && row_of(p, r, b, slot)) {
-      const int page = paged_page(p, b, slot);
-      if (page >= 0) at = int64_t(paged_row(p, page, slot, 0));
+      const int page = p.new_k ? paged_page(p, b, slot) : 0;   // (rows that are in the cache already: the table may hold anything)
+      if (p.new_k && page >= 0) at = int64_t(paged_row(p, page, slot, 0));
       if (p.weight || p.pos) {
         const int pos = p.seen[b] - paged_len(p, b) + slot;
         for (int g = 0; g < p.Hkv && page >= 0; ++g) {
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
     place[threadIdx.x] = at;
   }
   __syncthreads();
-  const int row = p.Hkv * kChunks, all = kStoreTokens * row;   // 16-byte pieces
+  const int row = p.Hkv * kChunks, all = p.new_k ? kStoreTokens * row : 0;   // 16-byte pieces
 #pragma unroll 4
   for (int i = threadIdx.x; i < all; i += kWarps * 32) {
     const int t = i / row, rest = i - t * row, g = rest / kChunks, c = (rest - g * kChunks) * (16 / int(sizeof(T)));

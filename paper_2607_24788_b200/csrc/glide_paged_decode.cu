@@ -552,8 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
   // the new tokens' rows and places in the account (nothing below reads them: the tile takes the row from the call)
   for (int u = int(blockIdx.x) * kWarps + warp; u < p.batch * p.Hkv; u += int(gridDim.x) * kWarps) {
     const int b = u / p.Hkv, g = u - b * p.Hkv, i = sm.len[b] - 1;
-    if (i < 0 || !p.new_k) continue;
-    const int page = paged_page(p, b, i);
+    if (i < 0) continue;
+    const int page = p.new_k ? paged_page(p, b, i) : -1;
     if (page >= 0 && lane < Sh::kChunks) {
       const size_t to = paged_row(p, page, i, g), from = size_t(b) * size_t(p.kv_stride) + size_t(g) * D;
       reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.k) + to)[lane] = reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.new_k) + from)[lane];
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     }
     if (lane == 0) {
       const size_t at = size_t(u) * size_t(p.track_stride) + i;
-      if (keep && !paged_sees(p, i, i)) p.weight[at] = 0.f;   // (otherwise the account's kernel writes it)
+      if (keep && p.new_k && !paged_sees(p, i, i)) p.weight[at] = 0.f;   // (otherwise the account's kernel writes it)
       if (p.pos) p.pos[at] = p.seen[b] - 1;
     }
   }

@@ -203,7 +203,7 @@ int glide_paged_prefill(glide_paged *h, const glide_paged_call *call, const void
     return GLIDE_ERR_INVALID_ARG;
   if (p.n_tokens == 0) return GLIDE_OK;
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
-  if (dev_k) {
+  if (dev_k || p.weight || p.pos) {
     const int r = launch_paged_store(h, p, as_stream(stream));
     if (r) return r;
   }

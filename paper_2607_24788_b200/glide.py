@@ -531,7 +531,8 @@ class GlidePaged:
 
     def glide_paged_prefill(self, table, lens, starts, q, k, v, out=None, lse=None, window: int = -1, n_sink: int = 0, weight=None,
                             pos=None, seen=None, layer: int = 0, stream=None) -> None:
-        """Stores the new tokens (rows starts[b] .. starts[b + 1] - 1 of k, v; None: they are in the cache) and, with out, attends."""
+        """Stores the new tokens (rows starts[b] .. starts[b + 1] - 1 of k, v; None: they are in the cache) and, with out, attends.
+        weight, pos: the new slots' account starts at 0 and their positions are written (k, v or not)."""
         rows = (k if k is not None else q).shape[0]
         tensors, strides = self._qkv(q, k, v, out, rows)
         self._write_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen)
@@ -539,7 +540,8 @@ class GlidePaged:
 
     def glide_paged_decode(self, table, lens, q, k, v, out, lse=None, window: int = -1, n_sink: int = 0, weight=None, pos=None,
                            seen=None, layer: int = 0, stream=None) -> None:
-        """One new token per sequence: stored at slot lens[b] - 1 (k, v None: it is in the cache), attends; weight: the account."""
+        """One new token per sequence: stored at slot lens[b] - 1 (k, v None: it is in the cache), attends; weight: the account, to which
+        the step's weights are added (the new slot's starts at 0, with k, v None from what it is); pos: the slot's position is written."""
         rows = table.shape[0]
         tensors, strides = self._qkv(q, k, v, out, rows)
         self._write_call(layer, table, lens, None, rows, strides, window, n_sink, weight, pos, seen)

@@ -1,0 +1,56 @@
+"""Calls of the paged attention that its documentation allows, beside the ordinary ones: tokens that are in the cache already, tables
+whose unseen entries hold anything, no tokens at all."""
+import pytest
+import torch
+
+from tests.paged_util import BF16, F32, Cache, check, reference
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_account_and_positions_of_a_prompt_that_is_in_the_cache(dtype):
+    """k, v None: the new slots' account starts at 0 and their positions are written all the same, also where nothing is seen and the
+    table holds nothing."""
+    c = Cache([0, 40, 5], [30, 17, 0], 4, 2, 64, dtype, 16)
+    out = torch.empty_like(c.q)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, c.k, c.v, out)
+    start, want_weight, want_pos = (c.weight.clone(), c.pos.clone()), c.weight.clone(), c.pos.clone()
+    seen = torch.tensor([30, 1057, 9], dtype=torch.int32, device="cuda")
+    for b, first in ((0, 0), (1, 1040)):
+        new = slice(c.before[b], c.lens[b])
+        want_weight[b, :, new] = 0.0
+        want_pos[b, :, new] = torch.arange(first, first + c.new[b], dtype=torch.int32, device="cuda")
+    for window, table in ((-1, c.table), (0, torch.full_like(c.table, -1))):
+        c.weight.copy_(start[0])
+        c.pos.copy_(start[1])
+        c.handle.glide_paged_prefill(table, c.lens_dev, c.starts, c.q, None, None, out, window=window, weight=c.weight, pos=c.pos, seen=seen)
+        assert torch.equal(c.weight, want_weight) and torch.equal(c.pos, want_pos)
+        check(out, *reference(c, window)[:2], "out")
+    c.check_pages()
+    assert c.handle.glide_paged_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_position_of_a_step_that_is_in_the_cache(dtype):
+    """k, v None: the slot's position is written, its account goes on from what it is."""
+    c = Cache([99, 10, 0], [1, 1, 1], 4, 2, 64, dtype, 16)
+    out, again = torch.empty_like(c.q), torch.empty_like(c.q)
+    c.handle.glide_paged_decode(c.table, c.lens_dev, c.q, c.k, c.v, out)
+    weight, pos = c.weight.clone(), c.pos.clone()
+    seen = torch.tensor([500, 11, 7], dtype=torch.int32, device="cuda")
+    for window, table in ((-1, c.table), (0, torch.full_like(c.table, -1))):
+        for track in (dict(weight=c.weight, pos=c.pos), dict(pos=c.pos)):
+            c.weight.copy_(weight)
+            c.pos.copy_(pos)
+            c.handle.glide_paged_decode(table, c.lens_dev, c.q, None, None, again, window=window, seen=seen, **track)
+            want, tol, _, _, given, given_tol = reference(c, window)
+            check(again, want, tol, "out")
+            if "weight" not in track:
+                given.zero_()
+            check(c.weight, weight.double() + given, given_tol + weight * 2.0 ** -23, "weight")
+            want_pos = pos.clone()
+            for b, n in enumerate(c.lens):
+                want_pos[b, :, n - 1] = seen[b] - 1
+            assert torch.equal(c.pos, want_pos)
+    assert c.handle.glide_paged_device_status() == 0
