@@ -97,6 +97,8 @@ __device__ __forceinline__ size_t paged_row(const PagedParams &p, int page, int 
 __device__ __forceinline__ bool paged_sees(const PagedParams &p, int i, int j) {
   return j <= i && (p.window < 0 || j > i - p.window || j < p.n_sink);
 }
+// Whether some query of slots [q0, q1] sees slot j: the first one at or behind it does, if any.  (Table entries of other slots may hold anything.)
+__device__ __forceinline__ bool paged_seen_by(const PagedParams &p, int q0, int q1, int j) { return j <= q1 && paged_sees(p, max(q0, j), j); }
 
 // Prompts of few rows: the key tiles are cut into parts, each of which leaves a record per (token, query head): O [d] against 2^m, then m,
 // the sum that O goes with, the exact sum, 0.

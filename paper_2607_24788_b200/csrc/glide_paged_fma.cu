@@ -144,8 +144,7 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
 #pragma unroll
     for (int i = 0; i < Cp::kEach; ++i) {
       const int j = t < st.n ? st.slot(t) + Cp::row(i) : INT32_MAX;
-      const bool seen = j <= q1 && !(p.window >= 0 && j <= q0 - p.window && j >= p.n_sink);
-      e[i] = seen ? p.table[size_t(at.seq) * size_t(p.table_stride) + size_t(j >> p.page_shift)] : -1;
+      e[i] = paged_seen_by(p, q0, q1, j) ? p.table[size_t(at.seq) * size_t(p.table_stride) + size_t(j >> p.page_shift)] : -1;
     }
   };
   auto ask = [&](int t, const int (&e)[Cp::kEach]) {
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     for (int i = 0; i < Cp::kEach; ++i) {
       const int j = st.slot(t) + Cp::row(i);
       const bool good = unsigned(e[i]) < unsigned(p.n_pages);
-      if (!good && j <= q1 && !(p.window >= 0 && j <= q0 - p.window && j >= p.n_sink)) atomicExch(p.status, kDevBadPage);
+      if (!good && paged_seen_by(p, q0, q1, j)) atomicExch(p.status, kDevBadPage);
       const size_t from = good ? paged_row(p, e[i], j, g) : 0;
       Cp::ask(&sm.k[t & 1][0][0], Cp::row(i), good ? reinterpret_cast<const float *>(p.k) + from : nullptr, p.k);
       Cp::ask(&sm.v[t & 1][0][0], Cp::row(i), good ? reinterpret_cast<const float *>(p.v) + from : nullptr, p.k);
@@ -331,7 +330,7 @@ __global__ void __launch_bounds__(kThreads) paged_weights_fma_kernel(const __gri
       for (int i = 0; i < Cp::kEach; ++i) {
         const int r = Cp::row(i), j = j0 + r;
         if (r >= kKept) continue;
-        const int page = j < len ? paged_page(p, b, j) : -1;
+        const int page = paged_seen_by(p, q0, len - 1, j) ? paged_page(p, b, j) : -1;
         Cp::ask(&sm.k[0][0], r, page < 0 ? nullptr : reinterpret_cast<const float *>(p.k) + paged_row(p, page, j, g), p.k);
       }
       ask(t0, 0);

@@ -54,3 +54,35 @@ def test_position_of_a_step_that_is_in_the_cache(dtype):
                 want_pos[b, :, n - 1] = seen[b] - 1
             assert torch.equal(c.pos, want_pos)
     assert c.handle.glide_paged_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window,n_sink", [(20, 2), (0, 3), (40, 0)])
+def test_table_entries_that_nobody_sees_may_hold_anything(dtype, window, n_sink):
+    """So many units that the fp32 account takes 64 slots at a time, which span four pages."""
+    before = [200 + 17 * b for b in range(8)]
+    for new in ([5] * 8, [1] * 8):
+        c = Cache(before, new, 8, 4, 64, dtype, 16)
+        lse = torch.empty(c.q.shape[:2], device="cuda")
+        out = torch.empty_like(c.q)
+        c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, c.k, c.v, None)
+        want, tol, want_lse, lse_tol, given, given_tol = reference(c, window, n_sink)
+        table, weight = c.table.clone(), c.weight.clone()
+        for b, n in enumerate(c.lens):
+            i, j = torch.arange(c.before[b], n)[:, None], torch.arange(n)[None]
+            seen = ((j <= i) & ((j > i - window) | (j < n_sink))).any(0)
+            for col in range(table.shape[1]):
+                if not seen[col * 16:col * 16 + 16].any():
+                    table[b, col] = (-1, 1 << 30, c.k_pages.shape[1])[col % 3]
+        assert c.handle.glide_paged_device_status() == 0
+        c.handle.glide_paged_prefill(table, c.lens_dev, c.starts, c.q, None, None, out, lse=lse, window=window, n_sink=n_sink)
+        check(out, want, tol, "out")
+        check(lse, want_lse, lse_tol, "lse")
+        assert c.handle.glide_paged_device_status() == 0
+        c.handle.glide_paged_weights(table, c.lens_dev, c.starts, c.q, lse, c.weight, window=window, n_sink=n_sink)
+        check(c.weight, weight.double() + given, given_tol + weight * 2.0 ** -23, "weight")
+        assert c.handle.glide_paged_device_status() == 0
+        if max(new) == 1:
+            c.handle.glide_paged_decode(table, c.lens_dev, c.q, None, None, out, window=window, n_sink=n_sink)
+            check(out, want, tol, "out")
+            assert c.handle.glide_paged_device_status() == 0
