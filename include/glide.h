@@ -364,7 +364,7 @@ typedef struct {
   int64_t table_stride;
   const int32_t *dev_lens;   /* device [B]: slots each sequence holds, this call's new tokens among them */
   const int32_t *dev_starts; /* device [B + 1]: the new tokens of sequence b are rows starts[b] .. starts[b + 1] - 1 */
-  int64_t n_tokens;          /* rows of q, k, v, out (prefill, weights): at least starts[B] */
+  int64_t n_tokens;          /* rows of q, k, v, out (prefill, weights): at least starts[B]; 0: nothing is done, and they may be NULL */
   int64_t q_stride, kv_stride, out_stride; /* elements between tokens of q, of k and v, of out; 0: H d, H_kv d, H d.  The
                               heads of a token lie side by side; strides are multiples of 16 bytes */
   int64_t window;            /* newest slots that a query sees, its own among them; < 0: all */

@@ -198,10 +198,10 @@ int glide_paged_prefill(glide_paged *h, const glide_paged_call *call, const void
   PagedParams p;
   const int rc = params_of(h, call, kNeedStarts, &p);
   if (rc) return rc;
+  if (p.n_tokens == 0) return GLIDE_OK;   // (tensors without a row may have no address)
   if ((!dev_k) != (!dev_v) || (!dev_k && !dev_out) || (dev_out && !dev_q) || (!dev_out && dev_lse) || misaligned(dev_q) ||
       misaligned(dev_k) || misaligned(dev_v) || misaligned(dev_out) || (reinterpret_cast<uintptr_t>(dev_lse) & 3u))
     return GLIDE_ERR_INVALID_ARG;
-  if (p.n_tokens == 0) return GLIDE_OK;
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
   if (dev_k || p.weight || p.pos) {
     const int r = launch_paged_store(h, p, as_stream(stream));
@@ -228,8 +228,9 @@ int glide_paged_weights(glide_paged *h, const glide_paged_call *call, const void
   PagedParams p;
   const int rc = params_of(h, call, kNeedStarts, &p);
   if (rc) return rc;
-  if (!dev_q || misaligned(dev_q) || !dev_lse || (reinterpret_cast<uintptr_t>(dev_lse) & 3u) || !p.weight) return GLIDE_ERR_INVALID_ARG;
-  if (p.n_tokens == 0) return GLIDE_OK;
+  if (!p.weight) return GLIDE_ERR_INVALID_ARG;
+  if (p.n_tokens == 0) return GLIDE_OK;   // (tensors without a row may have no address)
+  if (!dev_q || misaligned(dev_q) || !dev_lse || (reinterpret_cast<uintptr_t>(dev_lse) & 3u)) return GLIDE_ERR_INVALID_ARG;
   p.q = dev_q, p.lse = const_cast<float *>(dev_lse);
   return h->cfg.io_dtype == GLIDE_BF16 ? launch_paged_weights_tc(h, p, as_stream(stream)) : launch_paged_weights_fma(h, p, as_stream(stream));
 }

@@ -86,3 +86,16 @@ def test_table_entries_that_nobody_sees_may_hold_anything(dtype, window, n_sink)
             c.handle.glide_paged_decode(table, c.lens_dev, c.q, None, None, out, window=window, n_sink=n_sink)
             check(out, want, tol, "out")
             assert c.handle.glide_paged_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_calls_without_a_token(dtype):
+    """Tensors of no rows, as a batch of sequences that wait has them."""
+    c = Cache([30, 20], [0, 0], 4, 2, 64, dtype, 16)
+    q, k, lse, weight = c.q[:0], c.k[:0], torch.empty(0, 4, device="cuda"), c.weight.clone()
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q, k, k, torch.empty_like(q), lse=lse, weight=c.weight, pos=c.pos)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, None, k, k)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q, None, None, torch.empty_like(q))
+    c.handle.glide_paged_weights(c.table, c.lens_dev, c.starts, q, lse, c.weight)
+    assert torch.equal(c.weight, weight) and c.handle.glide_paged_device_status() == 0
+    c.check_pages()
