@@ -58,13 +58,19 @@ struct PagedRow {
       if (with_lse && lane == 0) p.lse[row * size_t(p.H) + head0 + h] = paged_lse(m[h], l[h]);
     }
   }
-  // all of it: the call's row `row`, slot i of sequence b
-  __device__ __forceinline__ void attend(const PagedParams &p, size_t row, int b, int i, int g, int head0, bool with_lse) {
+  // all of it: the call's row `row`, slot i of sequence b.  moves (or NULL) counts runs of slots, for those who wait.
+  __device__ __forceinline__ void attend(const PagedParams &p, size_t row, int b, int i, int g, int head0, bool with_lse, uint32_t *moves = nullptr) {
     load_q(p, row, head0);
     int first, second;
     paged_ranges(p, i, first, second);
-    for (int j = 0; j < first; ++j) slot(p, b, g, j);
-    for (int j = second; j <= i; ++j) slot(p, b, g, j);
+    auto run = [&](int j, int end) {
+      for (; j < end; ++j) {
+        slot(p, b, g, j);
+        if (moves && (j & 1023) == 0 && (threadIdx.x & 31) == 0) atomicAdd(moves, 1u);
+      }
+    };
+    run(0, first);
+    run(second, i + 1);
     store(p, row, head0, with_lse);
   }
   // natural logarithm of a row sum l taken against 2^m

@@ -72,6 +72,7 @@ struct PrefillSmem {
   Work work[2];
   uint32_t tmem_base;
   int failed;
+  uint32_t moves;                        // steps of the rows that are computed once more
   float exch[kSoftmaxThreads / 2];       // a value of each row on its way between the row's two threads
 };
 
@@ -217,6 +218,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int *failed = &sm.failed;
+  const volatile uint32_t *moves = &sm.moves;
   const bool aligned = (smem_u32(smem_raw) & 1023u) == 0;   // (the swizzled tiles have to start on a multiple of 1024)
   if (warp == kLoadWarp && lane == 0) {
     for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), 1), mbar_init(smem_u32(&sm.bar_free[s]), 2);
@@ -232,6 +234,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     mbar_init(smem_u32(&sm.bar_tail), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sm.failed = aligned ? 0 : 1;
+    sm.moves = 0;
   } else if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -260,7 +263,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   };
   // Piece number i, as the loader has put it down (a whole warp; false: there is no more, or a time-out)
   auto next_work = [&](int i) {
-    const bool got = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_work[i & 1]), uint32_t(i >> 1) & 1u, failed));
+    const bool got = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_work[i & 1]), uint32_t(i >> 1) & 1u, failed, moves));
     Work w{-1, 0, 0, 0, 0, 0, 0};
     if (got) w = *const_cast<const Work *>(&sm.work[i & 1]);
     __syncwarp();
@@ -296,7 +299,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     uint32_t n_s = 0, n_q = 0;                      // batches of products waited for; Q tiles of X so far
     bool ok = true;
     auto wait_s = [&]() {
-      if (ok) ok = mbar_wait_long(smem_u32(&sm.bar_s[X]), n_s & 1u, failed);
+      if (ok) ok = mbar_wait_long(smem_u32(&sm.bar_s[X]), n_s & 1u, failed, moves);
       ++n_s;
       tc_fence_after();
       ok = __all_sync(0xffffffffu, ok);             // warp-uniform
@@ -490,7 +493,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const float l_row = row_sum_of(l_sum);
       const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
-      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed));   // (Q, which no product has waited for)
+      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));   // (Q, which no product has waited for)
       n_q += n_tiles != 0;
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
@@ -552,7 +555,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           const int rr = (row & ~31) + __ffs(int(again)) - 1;
           PagedRow<bf16, D, 1> one;
           // (its lse was right unless its weights had left the range)
-          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u);
+          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u, &sm.moves);
         }
       }
       }
@@ -570,7 +573,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     uint32_t n_p = 0, n_q = 0, n_turn = 0;          // operands P, Q tiles of x, turns so far
     bool ok = true;
     auto wait = [&](uint64_t &bar, uint32_t parity) {
-      ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&bar), parity & 1u, failed));
+      ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&bar), parity & 1u, failed, moves));
       return ok;
     };
     auto commit = [&](uint64_t &bar) {
@@ -630,7 +633,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         w = find_tile(p, tiles - 1 - t, TOKC);
         w.g = rest / parts, w.part = rest - w.g * parts;
       }
-      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_workfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed));
+      if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_workfree[it & 1]), uint32_t((it >> 1) - 1) & 1u, failed, moves));
       if (!ok) break;
       if (lane == 0) {
         sm.work[it & 1] = w;
@@ -642,7 +645,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
       // The first tiles may come while the piece before is still being written out, Q_X when its rows have been.
       auto ask_q = [&](int x) {
-        if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed));
+        if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed, moves));
         ++n_use[x];
         if (!ok || !n_tiles) return;
         ++n_q[x];
@@ -666,7 +669,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int is_v = 0; is_v < 2 && ok; ++is_v) {
           const int job = jobs + 2 * k + is_v, slot = job % S;
           const uint32_t bar = smem_u32(&sm.bar_full[slot]);
-          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed));
+          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed, moves));
           if (!ok) break;
           // V rows behind the piece's last token: whatever they hold, their weights are 0 and they have to be finite
           const bool tail = is_v && j0 + kKT - 1 > tq_last;
@@ -688,7 +691,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             }
           }
           if (tail) {
-            ok = __all_sync(0xffffffffu, mbar_wait_long(to, n_tail++ & 1u, failed)) && ok;
+            ok = __all_sync(0xffffffffu, mbar_wait_long(to, n_tail++ & 1u, failed, moves)) && ok;
             if (!ok) break;
             for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
 #pragma unroll

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "glide_device.cuh"
+#include "glide_waits.h"
 
 namespace glide {
 
@@ -65,16 +66,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *failed = 1;
   return false;
 }
-// ... for a wait that may last as long as other warps' work on a whole piece, rows that are computed once more among it.  (A try that
-// fails takes 1.4 us: kWaitLimit of them 1.4 s, these 23 s.)
-__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed) {
-  for (int i = 0; i < 16; ++i) {
-    int out = 0;
-    if (mbar_wait(bar, parity, &out)) return true;
-    if (*failed) return false;
-  }
-  *failed = 1;
-  return false;
+// ... for a wait that may last as long as other warps' work on a whole piece, rows that are computed once more among it, of which *moves counts
+// the steps.  (A try that fails takes 1.4 us: kWaitLimit of them 1.4 s; it gives up after 23 s without a step.)
+__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed, const volatile uint32_t *moves) {
+  const bool landed = wait_while_moving(
+      [&] {
+        int out = 0;
+        return mbar_wait(bar, parity, &out);
+      },
+      [&] { return *failed != 0; }, [&] { return *moves; }, 16);
+  if (!landed) *failed = 1;
+  return landed;
 }
 // whether the phase has completed already
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {

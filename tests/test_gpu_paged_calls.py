@@ -1,5 +1,7 @@
 """Calls of the paged attention that its documentation allows, beside the ordinary ones: tokens that are in the cache already, tables
 whose unseen entries hold anything, no tokens at all."""
+import math
+
 import pytest
 import torch
 
@@ -99,3 +101,23 @@ def test_calls_without_a_token(dtype):
     c.handle.glide_paged_weights(c.table, c.lens_dev, c.starts, q, lse, c.weight)
     assert torch.equal(c.weight, weight) and c.handle.glide_paged_device_status() == 0
     c.check_pages()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,page,before", [(128, 64, [3000, 50]), (64, 16, [100, 3000])])
+def test_rows_that_all_see_a_value_that_is_not_finite(dtype, d, page, before):
+    """Every row is computed once more by itself, whole and in parts: its other columns are what they should be."""
+    for new in ([150, 40], [6, 5]):
+        c = Cache(before, new, 8, 2, d, dtype, page)
+        want, tol, want_lse, lse_tol, _, _ = reference(c)
+        out, lse = torch.empty_like(c.q), torch.empty(c.q.shape[:2], device="cuda")
+        for b in range(2):
+            page_of, off = c.place(b, torch.tensor(5, device="cuda"))
+            c.v_pages[0][page_of, :, off, 3] = (math.nan, math.inf)[b]
+        for i in range(2):
+            c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, c.k, c.v, out, lse=lse if i else None)
+            assert not out[..., 3].isfinite().any()
+            some = [x for x in range(d) if x != 3]
+            check(out[..., some], want[..., some], tol[..., some], "out")
+        check(lse, want_lse, lse_tol, "lse")
+        assert c.handle.glide_paged_device_status() == 0
