@@ -105,8 +105,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_co
   }
   if (p.lse && lane == 0) p.lse[r * p.H + head] = PagedRow<T, D, 1>::paged_lse(M, X);
   if (!__all_sync(0xffffffffu, fine)) {   // (0 times what a slot holds that the row does not see, for one)
-    PagedRow<T, D, 1> one;
-    one.attend(p, size_t(r), b, i, head / (p.H / p.Hkv), head, p.lse && !isfinite(X));
+    paged_row_alone<T, D>(p, size_t(r), b, i, head / (p.H / p.Hkv), head, p.lse && !isfinite(X), nullptr);
   }
 }
 

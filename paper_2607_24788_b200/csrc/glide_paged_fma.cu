@@ -288,8 +288,7 @@ __global__ void __launch_bounds__(kThreads) paged_prefill_fma_kernel(const __gri
     for (int i = 0; i < R; ++i) {
       if (!__any_sync(0xffffffffu, ((tid >> 4) & 1) == half && ((again >> i) & 1u))) continue;
       const int r = ((tid >> 5) * 2 + half) * R + i;
-      PagedRow<float, D, 1> one;
-      one.attend(p, size_t(at.row0 + at.tok0 + r / G), at.seq, q0 + r / G, g, g * G + r % G, false);   // (the sums of the scores were right)
+      paged_row_alone<float, D>(p, size_t(at.row0 + at.tok0 + r / G), at.seq, q0 + r / G, g, g * G + r % G, false, nullptr);   // (the sums of the scores were right)
     }
 }
 

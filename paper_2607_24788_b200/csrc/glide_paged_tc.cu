@@ -546,16 +546,17 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (ok && tk < ntokX) *reinterpret_cast<uint4 *>(obase + size_t(tk) * size_t(p.out_stride) + (rr - tk * G) * D) = val;
       }
       if (LSE && H == 0 && live && ok) p.lse[out_row * p.H + g * G + row % G] = PagedRow<bf16, D, 1>::paged_lse(m_ref, x_row);
-      // rows of which either half is not finite, by the first warp of the pair when both have stored
+      // rows of which either half is not finite, by the two warps of the pair in turns when both have stored
       const bool bad = live && (!isfinite((chk0 + chk1) * inv) || !isfinite(l_row));
       unsigned again = __ballot_sync(0xffffffffu, row_sum_of(bad ? 1.f : 0.f) > 0.f);
       const unsigned sums_off = __ballot_sync(0xffffffffu, LSE && live && !isfinite(x_row));
-      if (H == 0 && ok) {
-        for (; again; again &= again - 1) {
+      if (ok) {
+#pragma unroll 1
+        for (int turn = 0; again; again &= again - 1, turn ^= 1) {
+          if (turn != H) continue;
           const int rr = (row & ~31) + __ffs(int(again)) - 1;
-          PagedRow<bf16, D, 1> one;
           // (its lse was right unless its weights had left the range)
-          one.attend(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u, &sm.moves);
+          paged_row_alone<bf16, D>(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u, &sm.moves);
         }
       }
       }
