@@ -331,7 +331,8 @@ int glide_stream_schedule(const glide_config *cfg, int32_t n_sms, int64_t smem_l
  *   - Offsets into the pool are 64 bits wide.  Rows of out, lse, weight and pos that belong to no sequence are left alone.
  *   - The calls allocate nothing and do not synchronise.  The workspace holds what the kernels of one call hand to each
  *     other, and counters that are 0 between calls: calls of one handle, replayed ones included, have to follow one another
- *     (stream order); calls that may run at the same time need handles of their own, which may share the pages.
+ *     (stream order); calls that may run at the same time need handles of their own, which may share the pages.  Several host
+ *     threads may call with one handle: the launches of a call stay together.
  *   - Results do not depend on timing: no sum is made by atomics, and parts are joined in a fixed order.
  */
 typedef struct glide_paged glide_paged; /* opaque, host side */

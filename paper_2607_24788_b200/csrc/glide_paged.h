@@ -3,6 +3,8 @@
 
 #include <cuda.h>
 
+#include <mutex>
+
 #include "glide_internal.h"
 
 typedef CUresult (*TensorMapEncoder)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -23,6 +25,7 @@ struct glide_paged {
                                     // slots x 64 columns
   int32_t map_pages = 0;            // pages in the maps: of all layers
   void *encode = nullptr;           // cuTensorMapEncodeTiled
+  std::mutex launching;             // held over a call's launches, which share the workspace: no other thread's come between them
 };
 
 namespace glide {

@@ -1,6 +1,7 @@
 // Paged softmax attention: checks, the handle, the calls (include/glide.h, "softmax attention over a paged cache").
 #include <algorithm>
 #include <cmath>
+#include <memory>
 #include <new>
 
 #include "glide_paged.h"
@@ -150,15 +151,15 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
                        size_t workspace_bytes, void *stream, glide_paged **out) {
   if (!out) return GLIDE_ERR_INVALID_ARG;
   *out = nullptr;
-  glide_paged plan_h;
-  int rc = plan(cfg, &plan_h);
+  std::unique_ptr<glide_paged> owned(new (std::nothrow) glide_paged);
+  glide_paged *h = owned.get();
+  if (!h) return GLIDE_ERR_INVALID_ARG;
+  const int rc = plan(cfg, h);
   if (rc) return rc;
   if (!dev_k_pages || !dev_v_pages || misaligned(dev_k_pages) || misaligned(dev_v_pages) || !dev_workspace ||
       (reinterpret_cast<uintptr_t>(dev_workspace) & 255u))
     return GLIDE_ERR_INVALID_ARG;
-  if (workspace_bytes < plan_h.total) return GLIDE_ERR_WORKSPACE_TOO_SMALL;
-  glide_paged *h = new (std::nothrow) glide_paged(plan_h);
-  if (!h) return GLIDE_ERR_INVALID_ARG;
+  if (workspace_bytes < h->total) return GLIDE_ERR_WORKSPACE_TOO_SMALL;
   h->ws = static_cast<unsigned char *>(dev_workspace);
   h->k = static_cast<unsigned char *>(dev_k_pages);
   h->v = static_cast<unsigned char *>(dev_v_pages);
@@ -180,10 +181,9 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
        cudaStreamSynchronize(as_stream(stream)) == cudaSuccess;   // (so that the first call may be on any stream)
   if (!ok) {
     cudaGetLastError();
-    delete h;
     return GLIDE_ERR_CUDA;
   }
-  *out = h;
+  *out = owned.release();
   return GLIDE_OK;
 }
 
@@ -203,6 +203,7 @@ int glide_paged_prefill(glide_paged *h, const glide_paged_call *call, const void
       misaligned(dev_k) || misaligned(dev_v) || misaligned(dev_out) || (reinterpret_cast<uintptr_t>(dev_lse) & 3u))
     return GLIDE_ERR_INVALID_ARG;
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
+  const std::lock_guard<std::mutex> together(h->launching);
   if (dev_k || p.weight || p.pos) {
     const int r = launch_paged_store(h, p, as_stream(stream));
     if (r) return r;
@@ -221,6 +222,7 @@ int glide_paged_decode(glide_paged *h, const glide_paged_call *call, const void 
     return GLIDE_ERR_INVALID_ARG;
   if (p.weight && !h->cfg.weights) return GLIDE_ERR_UNSUPPORTED;
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
+  const std::lock_guard<std::mutex> together(h->launching);
   return launch_paged_decode(h, p, as_stream(stream));
 }
 
@@ -232,6 +234,7 @@ int glide_paged_weights(glide_paged *h, const glide_paged_call *call, const void
   if (p.n_tokens == 0) return GLIDE_OK;   // (tensors without a row may have no address)
   if (!dev_q || misaligned(dev_q) || !dev_lse || (reinterpret_cast<uintptr_t>(dev_lse) & 3u)) return GLIDE_ERR_INVALID_ARG;
   p.q = dev_q, p.lse = const_cast<float *>(dev_lse);
+  const std::lock_guard<std::mutex> together(h->launching);
   return h->cfg.io_dtype == GLIDE_BF16 ? launch_paged_weights_tc(h, p, as_stream(stream)) : launch_paged_weights_fma(h, p, as_stream(stream));
 }
 
@@ -244,6 +247,7 @@ int glide_paged_evict(glide_paged *h, const glide_paged_call *call, int64_t budg
   if (!p.weight || !p.pos || !dev_weight_out || !dev_pos_out || !dev_new_lens || (dev_weight_out == p.weight) != (dev_pos_out == p.pos) ||
       budget < 1 || recent < 0 || recent > kMostTokens || int64_t(p.n_sink) + recent > budget)
     return GLIDE_ERR_INVALID_ARG;
+  const std::lock_guard<std::mutex> together(h->launching);
   return launch_paged_evict(h, p, int(std::min(budget, kMostTokens)), int(recent), dev_weight_out, dev_pos_out, dev_new_lens,
                             as_stream(stream));
 }

@@ -415,13 +415,17 @@ def glide_paged_workspace_bytes(cfg: glide_paged_config) -> int:
 
 
 _I32, _F32 = torch.int32, torch.float32
+# a call's fields as bytes of its own (one pack instead of a store per field: a step's host time is what counts where the cache is short)
+_pack_call = struct.Struct("@iiPiiqPPqqqqqPPPq").pack
+assert struct.calcsize("@iiPiiqPPqqqqqPPPq") == ctypes.sizeof(glide_paged_call)
 
 
 class GlidePaged:
     """Softmax attention over a paged cache (include/glide.h): k_pages, v_pages [L][n_pages][H_kv][page_size][d] are the
     caller's (views of equal strides will do), a torch workspace and the handle are owned here.  Tables are int32 [B][cols], lens,
     seen and new_lens int32 [B], starts int32 [B + 1], weight fp32 and pos int32 [B][H_kv][slots], all on the pages' device.
-    Calls of one object must follow one another on the GPU; objects of their own may share pages."""
+    Calls of one object must follow one another on the GPU, from whichever host threads they come; objects of their own may share
+    pages."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int,
                  softmax_scale: float = 0.0, weights: bool = True):
@@ -442,12 +446,6 @@ class GlidePaged:
                                                _stream(None), ctypes.byref(handle)), "glide_paged_create")
         self._h = handle
         self._index = self.device.index
-        # the call's fields, written anew by every call (one pack instead of a store per field: a step's host time is what counts
-        # where the cache is short)
-        self._call = ctypes.create_string_buffer(ctypes.sizeof(glide_paged_call))
-        self._callp = ctypes.addressof(self._call)
-        self._pack = struct.Struct("@iiPiiqPPqqqqqPPPq").pack_into
-        assert struct.calcsize("@iiPiiqPPqqqqqPPPq") == ctypes.sizeof(glide_paged_call)
 
     # (A tensor's shape is asked for once, as a whole: .size(i) and .stride(i) take three times as long, and a short step is bound by
     # the host's time for its call.)
@@ -481,8 +479,8 @@ class GlidePaged:
             f"lse: fp32 [{rows}][{self.H}] on {self.device}"
         return lse.data_ptr()
 
-    def _write_call(self, layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen) -> None:
-        """Checks what the calls share and writes it down; rows None: one per sequence."""
+    def _packed_call(self, layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen) -> bytes:
+        """Checks what the calls share and packs it; rows None: one per sequence."""
         shape = table.shape
         assert table.dtype is _I32 and len(shape) == 2 and table.get_device() == self._index, f"table: int32 [B][cols] on {self.device}"
         B, cols = shape
@@ -502,15 +500,15 @@ class GlidePaged:
             p_seen = self._ints(seen, B, "seen")
         if starts is not None:
             p_starts = self._ints(starts, B + 1, "starts")
-        self._pack(self._call, 0, layer, B, table.data_ptr(), cols, n_sink, stride, self._ints(lens, B, "lens"), p_starts, B if rows is None else rows,
-                   *strides, window, p_weight, p_pos, p_seen, track)
+        return _pack_call(layer, B, table.data_ptr(), cols, n_sink, stride, self._ints(lens, B, "lens"), p_starts, B if rows is None else rows,
+                          *strides, window, p_weight, p_pos, p_seen, track)
 
-    def _run(self, where: str, stream, fn, *args) -> None:
+    def _run(self, where: str, stream, fn, call: bytes, *args) -> None:
         if self._index == _current_device():
-            rc = fn(self._h, self._callp, *args, _stream(stream))
+            rc = fn(self._h, call, *args, _stream(stream))
         else:
             with torch.cuda.device(self.device):
-                rc = fn(self._h, self._callp, *args, _stream(stream))
+                rc = fn(self._h, call, *args, _stream(stream))
         if rc:
             _check(rc, where)
 
@@ -535,8 +533,8 @@ class GlidePaged:
         weight, pos: the new slots' account starts at 0 and their positions are written (k, v or not)."""
         rows = (k if k is not None else q).shape[0]
         tensors, strides = self._qkv(q, k, v, out, rows)
-        self._write_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen)
-        self._run("glide_paged_prefill", stream, self.lib.glide_paged_prefill, *tensors, self._lse(lse, rows))
+        call = self._packed_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, pos, seen)
+        self._run("glide_paged_prefill", stream, self.lib.glide_paged_prefill, call, *tensors, self._lse(lse, rows))
 
     def glide_paged_decode(self, table, lens, q, k, v, out, lse=None, window: int = -1, n_sink: int = 0, weight=None, pos=None,
                            seen=None, layer: int = 0, stream=None) -> None:
@@ -544,15 +542,15 @@ class GlidePaged:
         the step's weights are added (the new slot's starts at 0, with k, v None from what it is); pos: the slot's position is written."""
         rows = table.shape[0]
         tensors, strides = self._qkv(q, k, v, out, rows)
-        self._write_call(layer, table, lens, None, rows, strides, window, n_sink, weight, pos, seen)
-        self._run("glide_paged_decode", stream, self.lib.glide_paged_decode, *tensors, self._lse(lse, rows))
+        call = self._packed_call(layer, table, lens, None, rows, strides, window, n_sink, weight, pos, seen)
+        self._run("glide_paged_decode", stream, self.lib.glide_paged_decode, call, *tensors, self._lse(lse, rows))
 
     def glide_paged_weights(self, table, lens, starts, q, lse, weight, window: int = -1, n_sink: int = 0, layer: int = 0, stream=None) -> None:
         """Adds the weights that the tokens q with the row sums lse (of glide_paged_prefill) give every slot to the account."""
         rows = q.shape[0]
         tensors, strides = self._qkv(q, None, None, None, rows)
-        self._write_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, None, None)
-        self._run("glide_paged_weights", stream, self.lib.glide_paged_weights, tensors[0], self._lse(lse, rows))
+        call = self._packed_call(layer, table, lens, starts, rows, strides, window, n_sink, weight, None, None)
+        self._run("glide_paged_weights", stream, self.lib.glide_paged_weights, call, tensors[0], self._lse(lse, rows))
 
     def glide_paged_evict(self, table, lens, seen, weight, pos, budget: int, new_lens, recent: int = 0, n_sink: int = 0, weight_out=None,
                           pos_out=None, layer: int = 0, stream=None) -> None:
@@ -561,8 +559,8 @@ class GlidePaged:
         p_weight, slots = self._track(weight if weight_out is None else weight_out, B, _F32, "weight_out")
         p_pos, pos_slots = self._track(pos if pos_out is None else pos_out, B, _I32, "pos_out")
         assert slots == pos_slots == weight.shape[2], "the accounts: as many slots"
-        self._write_call(layer, table, lens, None, None, (0, 0, 0), -1, n_sink, weight, pos, seen)
-        self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
+        call = self._packed_call(layer, table, lens, None, None, (0, 0, 0), -1, n_sink, weight, pos, seen)
+        self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, call, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
 
     def glide_paged_device_status(self) -> int:
         """The status word of the device-side checks, read and cleared (0: nothing was recorded)."""

@@ -121,3 +121,36 @@ def test_rows_that_all_see_a_value_that_is_not_finite(dtype, d, page, before):
             check(out[..., some], want[..., some], tol[..., some], "out")
         check(lse, want_lse, lse_tol, "lse")
         assert c.handle.glide_paged_device_status() == 0
+
+
+def test_one_handle_from_two_threads():
+    """Calls of several launches, issued by two threads on one stream: bit for bit what they give one after the other."""
+    import threading
+    c = Cache([3000, 700], [6, 6], 8, 2, 64, BF16, 64)
+    c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, None, c.k, c.v)
+    stream = torch.cuda.current_stream()
+    q = [[torch.randn_like(c.q) for _ in range(2)] for _ in range(2)]
+    want, got = [[], []], [[], []]
+
+    def calls(i, results, n):
+        for k in range(n):
+            out, lse, weight = torch.empty_like(c.q), torch.empty(12, 8, device="cuda"), torch.zeros_like(c.weight)
+            kw = dict(window=(-1, 900)[i], stream=stream)
+            c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, q[i][k % 2], None, None, out, lse=lse, **kw)   # (parts and join)
+            c.handle.glide_paged_decode(c.table, c.lens_dev, q[i][k % 2][:2], None, None, out[:2], weight=weight, **kw)   # (step and account)
+            results[i].append((out, lse, weight))
+
+    for i in range(2):
+        calls(i, want, 2)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=calls, args=(i, got, 100)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 100
+        for k, x in enumerate(got[i]):
+            assert all(torch.equal(a, b) for a, b in zip(x, want[i][k % 2]))
+    assert c.handle.glide_paged_device_status() == 0

@@ -124,3 +124,37 @@ def test_pages_that_share_memory_are_refused():
     for shape in ((1, 8, 2, 16, 64), (3, 8, 2, 16, 64)):
         with pytest.raises(AssertionError):
             glide.make_paged_config(row.expand(shape), 4, 2, 100)
+
+
+def test_calls_of_one_object_from_two_threads():
+    """A second thread's call that comes while the library reads the first one's fields does not change them."""
+    import threading
+    h = binding()
+    lens, seen = torch.zeros(2, dtype=torch.int32), []
+    tables = [torch.zeros(2, 3 + i, dtype=torch.int32) for i in range(2)]
+    q, k = torch.zeros(2, 4, 64), torch.zeros(2, 2, 64)
+
+    def step(i):
+        h.glide_paged_decode(tables[i], lens, q, k, k, q, layer=i, stream=type("Stream", (), dict(cuda_stream=0))())
+
+    class Library:
+        @staticmethod
+        def glide_paged_decode(handle, call, *rest):
+            if not seen:
+                seen.append(None)
+                other = threading.Thread(target=step, args=(1,))
+                other.start()
+                other.join()
+            address = call if isinstance(call, int) else ctypes.cast(ctypes.c_char_p(call), ctypes.c_void_p).value
+            fields = glide.glide_paged_call.from_buffer_copy(ctypes.string_at(address, ctypes.sizeof(glide.glide_paged_call)))
+            seen.append((fields.layer, fields.table_cols, fields.dev_table))
+            return 0
+
+    h.lib, h._index = Library, -1
+    current = glide._current_device
+    glide._current_device = lambda: -1
+    try:
+        step(0)
+    finally:
+        glide._current_device = current
+    assert seen[1:] == [(1, 4, tables[1].data_ptr()), (0, 3, tables[0].data_ptr())]
