@@ -412,8 +412,10 @@ int glide_paged_weights(glide_paged *p, const glide_paged_call *call, const void
  * when there are not enough others).  Of the kept slots those at or behind the new length move, in ascending order, into the
  * freed slots below it, in ascending order: keys, values, weight and position; the rest stay where they are.
  * dev_weight_out and dev_pos_out (same layout and stride) receive the account of the kept slots; they may be dev_weight and
- * dev_pos themselves (both or neither).  dev_new_lens [B] receives the new lengths and may be dev_lens.  Pages
- * behind them are the caller's again. */
+ * dev_pos themselves (both or neither).  dev_new_lens [B] receives the new lengths.  It may be dev_lens where no other
+ * layer's call reads those: of layers that share lengths each has to be given the old ones.  Pages behind the new lengths are
+ * the caller's again.  Rows are moved in place, so a page that two sequences' tables name must not be among those below dev_lens
+ * of a sequence that gives slots up. */
 int glide_paged_evict(glide_paged *p, const glide_paged_call *call, int64_t budget, int64_t recent, float *dev_weight_out,
                       int32_t *dev_pos_out, int32_t *dev_new_lens, void *stream);
 

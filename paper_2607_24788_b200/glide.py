@@ -554,7 +554,8 @@ class GlidePaged:
 
     def glide_paged_evict(self, table, lens, seen, weight, pos, budget: int, new_lens, recent: int = 0, n_sink: int = 0, weight_out=None,
                           pos_out=None, layer: int = 0, stream=None) -> None:
-        """Every (sequence, KV head) keeps min(lens[b], budget) slots; weight_out, pos_out None: the account changes in place."""
+        """Every (sequence, KV head) keeps min(lens[b], budget) slots; weight_out, pos_out None: the account changes in place.  new_lens may
+        be lens unless other layers' calls still have to read those."""
         B = table.shape[0]
         p_weight, slots = self._track(weight if weight_out is None else weight_out, B, _F32, "weight_out")
         p_pos, pos_slots = self._track(pos if pos_out is None else pos_out, B, _I32, "pos_out")

@@ -1,10 +1,12 @@
 """Calls of the paged attention that its documentation allows, beside the ordinary ones: tokens that are in the cache already, tables
 whose unseen entries hold anything, no tokens at all."""
 import math
+import os
 
 import pytest
 import torch
 
+from paper_2607_24788_b200 import glide
 from tests.paged_util import BF16, F32, Cache, check, reference
 
 pytestmark = pytest.mark.gpu
@@ -154,3 +156,43 @@ def test_one_handle_from_two_threads():
         for k, x in enumerate(got[i]):
             assert all(torch.equal(a, b) for a, b in zip(x, want[i][k % 2]))
     assert c.handle.glide_paged_device_status() == 0
+
+
+def readme_example():
+    """The README's lines that use GlidePaged."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        lines = f.read().split("\n")
+    first = next(i for i, x in enumerate(lines) if "GlidePaged(" in x)
+    while lines[first - 1].startswith("    "):
+        first -= 1
+    last = first
+    while last < len(lines) and lines[last].startswith("    "):
+        last += 1
+    return "\n".join(x[4:] for x in lines[first:last])
+
+
+def test_the_readme_example():
+    """Layers that share a table and lengths: each comes out as it does by itself."""
+    L, B, H, Hkv, d, page, T = 2, 2, 32, 4, 64, 64, [4200, 4300]
+    g = torch.Generator(device="cuda").manual_seed(0)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    slots = 4352
+    ids = torch.randperm(B * slots // page, generator=torch.Generator().manual_seed(0)).int().cuda()
+    start = dict(k_pages=torch.zeros(L, len(ids), Hkv, page, d, dtype=BF16, device="cuda"), w=torch.rand(L, B, Hkv, slots, device="cuda"),
+                 v_pages=torch.zeros(L, len(ids), Hkv, page, d, dtype=BF16, device="cuda"), pos=torch.zeros(L, B, Hkv, slots, dtype=torch.int32, device="cuda"),
+                 q=rnd(L, sum(T), H, d) * 3, k=rnd(L, sum(T), Hkv, d), v=rnd(L, sum(T), Hkv, d), q1=rnd(L, B, H, d), k1=rnd(L, B, Hkv, d), v1=rnd(L, B, Hkv, d),
+                 out=torch.zeros(L, sum(T), H, d, dtype=BF16, device="cuda"), o1=torch.zeros(L, B, H, d, dtype=BF16, device="cuda"),
+                 lse=torch.zeros(sum(T), H, device="cuda"), table=ids.view(B, -1), lens=torch.tensor(T, dtype=torch.int32, device="cuda"),
+                 new_lens=torch.zeros(B, dtype=torch.int32, device="cuda"), starts=torch.tensor([0, T[0], sum(T)], dtype=torch.int32, device="cuda"))
+    start["seen"] = start["lens"].clone()
+    shared = {n: x.clone() for n, x in start.items()}
+    exec(readme_example(), dict(glide=glide, L=L, **shared))
+    assert shared["lens"].tolist() == [4097, 4097] and shared["seen"].tolist() == [4201, 4301]
+    assert (shared["w"][:, :, :, 4096] > 0).all() and (shared["pos"][..., 4096] == shared["seen"][:, None] - 1).all()
+    per_layer = {"k_pages", "v_pages", "w", "pos", "q", "k", "v", "q1", "k1", "v1", "out", "o1"}
+    for l in range(L):
+        alone = {n: (x[l:l + 1] if n in per_layer else x).clone() for n, x in start.items()}
+        exec(readme_example(), dict(glide=glide, L=1, **alone))
+        for n in sorted(per_layer):
+            assert torch.equal(alone[n][0], shared[n][l]), (l, n)
