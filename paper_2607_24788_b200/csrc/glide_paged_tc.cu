@@ -621,8 +621,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const bool leader = elect_one();
     const int tiles = count_tiles(p, TOKC), total = tiles * p.Hkv * parts;
     bool ok = true;
-    uint32_t n_q[2] = {0, 0}, n_use[2] = {0, 0}, n_tail = 0;   // Q tiles, pieces with rows in X, tails so far
-    int asked = 0;                                 // K and V tiles
+    AskedCopies asked;                             // Q, K and V tiles, tails so far
+    uint32_t n_use[2] = {0, 0};                    // pieces with rows in X
     int drawn = 0;
     if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
     for (int it = 0; ok; ++it) {
@@ -649,7 +649,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed, moves));
         ++n_use[x];
         if (!ok || !n_tiles) return;
-        ++n_q[x];
+        ++asked.q[x];
         if (leader) {
           const uint32_t bar = smem_u32(&sm.bar_q[x]);
           mbar_expect_tx(bar, Sm::kTileBytes);
@@ -677,7 +677,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
           if (leader) mbar_expect_tx(to, Sm::kTileBytes);
           load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
-          ++asked;
+          ++asked.tiles;
+          if (tail) ++asked.tails, asked.untrimmed = job;
           if (!q_asked) {
             bool now = 2 * k + is_v == latest;
             if (!now) {
@@ -692,7 +693,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             }
           }
           if (tail) {
-            ok = __all_sync(0xffffffffu, mbar_wait_long(to, n_tail++ & 1u, failed, moves)) && ok;
+            ok = __all_sync(0xffffffffu, mbar_wait_long(to, (asked.tails - 1) & 1u, failed, moves)) && ok;
             if (!ok) break;
             for (int i = (tq_last + 1 - j0) * 8 + lane; i < kKT * 8; i += 32)
 #pragma unroll
@@ -701,17 +702,16 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
+            asked.untrimmed = -1;
           }
         }
       }
     }
-    if (!ok) {   // after a time-out: no copy outlives the CTA (a barrier whose last phase has ended lets go at once)
-      int alone = 0;
-      for (int x = 0; x < 2; ++x)
-        if (n_q[x]) alone = 0, mbar_wait(smem_u32(&sm.bar_q[x]), (n_q[x] - 1) & 1u, &alone);
-      for (int job = max(0, asked - S); job < asked; ++job) alone = 0, mbar_wait(smem_u32(&sm.bar_full[job % S]), uint32_t(job / S) & 1u, &alone);
-      alone = 0;
-      mbar_wait(smem_u32(&sm.bar_tail), n_tail & 1u, &alone);
+    if (!ok) {   // after a time-out: no copy outlives the CTA
+      wait_for_copies(asked, S, [&](int what, int which, uint32_t parity) {
+        int alone = 0;   // (whoever has given up)
+        mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_q[which] : what == kCopyTile ? &sm.bar_full[which] : &sm.bar_tail), parity, &alone);
+      });
     }
   }
   // after a time-out the waits return at once and nothing is stored; the CTA meets here either way
@@ -970,6 +970,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const bool leader = elect_one();
     bool ok = true;
     int done = 0, kn = 0;
+    AskedCopies asked;   // K tiles as its copies of two barriers, Q tiles as its ring
     int drawn = 0;
     if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
     for (int it = 0; ok; ++it) {
@@ -991,6 +992,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const uint32_t bar_k = smem_u32(&sm.bar_k[kn & 1]);
       if (leader) mbar_expect_tx(bar_k, Sm::kTileBytes);
       load_tile<D>(leader, &maps.k, p, smem_u32(sm.k[kn & 1]), page, kt.j0, kt.g, pieces, rows, bar_k);
+      ++asked.q[kn & 1];
       ++kn;
       for (int i = 0; i < n; ++i) {
         const int t = done + i, st = t % kAccStages, tok = kt.t0 + i * TOKT;
@@ -1012,13 +1014,15 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           for (int hf = 0; hf < D / 64; ++hf)
             tma_load_3d(smem_u32(sm.q[st]) + hf * kBoxBytes, &maps.q, hf * 64, kt.g * G, kt.row0 + tok, bar);
         }
+        ++asked.tiles;
       }
       done += n;
     }
-    if (!ok) {   // after a time-out: no copy outlives the CTA (each barrier's last phase ends, or has ended)
-      int alone = 0;
-      for (int i = 0; i < 2 && i < kn; ++i) mbar_wait(smem_u32(&sm.bar_k[(kn - 1 - i) & 1]), uint32_t((kn - 1 - i) >> 1) & 1u, &alone);
-      for (int i = 0; i < kAccStages; ++i) alone = 0, mbar_wait(smem_u32(&sm.bar_full[i]), 0u, &alone), alone = 0, mbar_wait(smem_u32(&sm.bar_full[i]), 1u, &alone);
+    if (!ok) {   // after a time-out: no copy outlives the CTA
+      wait_for_copies(asked, kAccStages, [&](int what, int which, uint32_t parity) {
+        int alone = 0;
+        mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_k[which] : &sm.bar_full[which]), parity, &alone);
+      });
     }
   }
   tc_fence_before();
