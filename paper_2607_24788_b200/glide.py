@@ -425,7 +425,7 @@ class GlidePaged:
     caller's (views of equal strides will do), a torch workspace and the handle are owned here.  Tables are int32 [B][cols], lens,
     seen and new_lens int32 [B], starts int32 [B + 1], weight fp32 and pos int32 [B][H_kv][slots], all on the pages' device.
     Calls of one object must follow one another on the GPU, from whichever host threads they come; objects of their own may share
-    pages."""
+    pages.  The object has to live until its calls on streams other than the one that it was made on have ended."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int,
                  softmax_scale: float = 0.0, weights: bool = True):
@@ -563,11 +563,11 @@ class GlidePaged:
         call = self._packed_call(layer, table, lens, None, None, (0, 0, 0), -1, n_sink, weight, pos, seen)
         self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, call, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
 
-    def glide_paged_device_status(self) -> int:
-        """The status word of the device-side checks, read and cleared (0: nothing was recorded)."""
+    def glide_paged_device_status(self, stream=None) -> int:
+        """The status word of the device-side checks, read and cleared behind what `stream` has been given (0: nothing was recorded)."""
         out = ctypes.c_int32(0)
         with torch.cuda.device(self.device):
-            _check(self.lib.glide_paged_device_status(self._h, _stream(None), ctypes.byref(out)), "glide_paged_device_status")
+            _check(self.lib.glide_paged_device_status(self._h, _stream(stream), ctypes.byref(out)), "glide_paged_device_status")
         return int(out.value)
 
     def glide_paged_destroy(self) -> None:

@@ -158,3 +158,18 @@ def test_calls_of_one_object_from_two_threads():
     finally:
         glide._current_device = current
     assert seen[1:] == [(1, 4, tables[1].data_ptr()), (0, 3, tables[0].data_ptr())]
+
+
+def test_the_status_is_that_of_the_stream_it_is_asked_for():
+    """Read on another stream, it could come before the calls have recorded anything, and clear what they record."""
+    h, asked = binding(), []
+
+    class Library:
+        @staticmethod
+        def glide_paged_device_status(handle, stream, out):
+            asked.append(stream)
+            return 0
+
+    h.lib, h.device = Library, None   # (no device to change to)
+    assert h.glide_paged_device_status(stream=type("Stream", (), dict(cuda_stream=77))()) == 0
+    assert asked == [77]
