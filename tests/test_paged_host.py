@@ -1,4 +1,5 @@
 """What the paged attention refuses, and the workspace it asks for (host only)."""
+import contextlib
 import ctypes
 
 import pytest
@@ -160,7 +161,7 @@ def test_calls_of_one_object_from_two_threads():
     assert seen[1:] == [(1, 4, tables[1].data_ptr()), (0, 3, tables[0].data_ptr())]
 
 
-def test_the_status_is_that_of_the_stream_it_is_asked_for():
+def test_the_status_is_that_of_the_stream_it_is_asked_for(monkeypatch):
     """Read on another stream, it could come before the calls have recorded anything, and clear what they record."""
     h, asked = binding(), []
 
@@ -170,6 +171,7 @@ def test_the_status_is_that_of_the_stream_it_is_asked_for():
             asked.append(stream)
             return 0
 
-    h.lib, h.device = Library, None   # (no device to change to)
+    h.lib = Library
+    monkeypatch.setattr(glide.torch.cuda, "device", lambda _: contextlib.nullcontext())
     assert h.glide_paged_device_status(stream=type("Stream", (), dict(cuda_stream=77))()) == 0
     assert asked == [77]
