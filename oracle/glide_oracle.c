@@ -441,10 +441,6 @@ void glide_oracle_cell_prefill_ex(glide_oracle_cell *c, int64_t T, const double 
   int d = c->d, dp = c->dp, H = c->H, Hkv = c->Hkv;
   int64_t w = c->w, n0 = c->n, delay = c->delay;
   int64_t count = (sel == NULL && n_sel < 0) ? T : n_sel;
-  double *phiq = (double *)malloc(sizeof(double) * dp);
-  double *phik = (double *)malloc(sizeof(double) * dp);
-  double *num = (double *)malloc(sizeof(double) * d);
-  double *numl = (double *)malloc(sizeof(double) * d);
 
 /* token j (absolute index) of KV head g: from the call if j >= n0, else from the ring */
 #define TOK_K(j, g) ((j) >= n0 ? k + ((size_t)((j)-n0) * Hkv + (g)) * d \
@@ -454,6 +450,14 @@ void glide_oracle_cell_prefill_ex(glide_oracle_cell *c, int64_t T, const double 
 #define TOK_G(j, g) ((j) >= n0 ? (gate ? gate[(size_t)((j)-n0) * Hkv + (g)] : 1.0) \
                                : c->Gr[(size_t)(g) * w + (size_t)((j) % w)])
 
+  /* positions by threads: each is summed by one thread, in the order below, from tokens and a state that nothing here changes */
+#pragma omp parallel if (count * T > 4096)
+  {
+  double *phiq = (double *)malloc(sizeof(double) * dp);
+  double *phik = (double *)malloc(sizeof(double) * dp);
+  double *num = (double *)malloc(sizeof(double) * d);
+  double *numl = (double *)malloc(sizeof(double) * d);
+#pragma omp for schedule(dynamic, 4)
   for (int64_t si = 0; si < count; ++si) {
     int64_t rel = sel ? sel[si] : si;
     int64_t t = n0 + rel;
@@ -501,9 +505,15 @@ void glide_oracle_cell_prefill_ex(glide_oracle_cell *c, int64_t T, const double 
       combine(c->merge, d, M, num, den, numl, denl, out + ((size_t)si * H + h) * d);
     }
   }
+  free(phiq);
+  free(phik);
+  free(num);
+  free(numl);
+  }
 
   /* state by definition: fold tokens [max(0,n0-delay), n0+T-delay) in order ... */
   int64_t n1 = n0 + T;
+  double *phik = (double *)malloc(sizeof(double) * dp);
   for (int g = 0; g < Hkv; ++g) {
     int64_t e_lo = n0 - delay;
     if (e_lo < 0) e_lo = 0;
@@ -527,10 +537,7 @@ void glide_oracle_cell_prefill_ex(glide_oracle_cell *c, int64_t T, const double 
 #undef TOK_V
 #undef TOK_G
   c->n = n1;
-  free(phiq);
   free(phik);
-  free(num);
-  free(numl);
 }
 
 void glide_oracle_cell_prefill(glide_oracle_cell *c, int64_t T, const double *q,
