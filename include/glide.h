@@ -388,8 +388,7 @@ int glide_paged_destroy(glide_paged *p);
  * dev_out is NULL, attend: dev_q, dev_out [n_tokens][H][d], dev_lse fp32 [n_tokens][H] or NULL.  With dev_k and dev_v NULL
  * the tokens are in the cache already.  Where dev_weight / dev_pos are given, the new slots' account starts at 0 and
  * their positions are seen - T_b ... seen - 1, with dev_k and dev_v or without; the weights of this call are not added
- * (glide_paged_weights does that).
- * With bf16 I/O the outputs with dev_lse and without it may differ in their last bits. */
+ * (glide_paged_weights does that).  The outputs with dev_lse and without it are the same. */
 int glide_paged_prefill(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
                         void *dev_out, float *dev_lse, void *stream);
 

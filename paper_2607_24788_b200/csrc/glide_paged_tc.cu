@@ -39,10 +39,6 @@ constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
 // pass over the tile: 8 sequences of up to 2048 tokens, windows of 256 with 4 first tokens 228 us with 8, 169 with 32, 171 with 64.
 constexpr float kLazy = 32.0f, kMostWeight = 0x1p32f;
-// Of 16 pairs of weights, those that soft_tile makes by multiply-adds where their exact sum is not asked for (which would take the longer
-// polynomial).  8001 tokens, 32 / 8 heads: 487 us with 0, 474 with 4, 486 with 6, 506 with 8; 4 x 1000 tokens behind 131072 8.69, 8.52, 8.77,
-// 9.15 ms.  With exact sums 4 took 2 % longer than 0.
-constexpr int kByFma = 4;
 constexpr int kMostSlots = 1 << 30;
 
 struct PagedMaps {
@@ -374,10 +370,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     };
     auto seen_of = [](const Bounds &v, int c) { return column_mask(c, v.lo, v.hi) | column_mask(c, -1, v.sink); };
     // A later key tile against the reference as it is, in one pass.  (The first half of P handed over while the second is made: the MMA
-    // warp holds its turn for longer, 2 to 7 % slower.)  Weights may grow to the end of the numbers' range; beyond 2^32 the next tile moves the reference.  A row whose weights leave the range
-    // all the same, or with an argument that exp2_fma does not take, ends with a sum that is no finite number and is computed by itself.
+    // warp holds its turn for longer, 2 to 7 % slower.  4, 6 or 8 of 16 pairs of exponentials by multiply-adds, with a cubic: 8001 tokens, 32 / 8
+    // heads, 524 us with none, 536, 549, 568; 4 x 1000 tokens behind 131072 8.5 ms, 8.7, 8.9, 9.3, all under the power limit.)  Weights may grow
+    // to the end of the numbers' range; beyond 2^32 the next tile moves the reference.  A row whose weights leave the range all the same ends
+    // with a sum that is no finite number and is computed by itself.
     auto soft_tile = [&](auto masked, const Bounds &v) {
-      float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f, odd0 = 0.f, odd1 = 0.f, most = -CUDART_INF_F;
+      float sum0 = 0.f, sum1 = 0.f, ex0 = 0.f, ex1 = 0.f;
       const float mr = m_ref;
       uint32_t mx2 = 0u;
 #pragma unroll
@@ -393,13 +391,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int e = 0; e < 16; ++e) {
           float a0, a1;
           fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
-          if (!LSE && !decltype(masked)::value && e < kByFma) {
-            add2(odd0, odd1, a0, a1);
-            most = max3(most, a0, a1);
-            exp2_fma<3>(a0, a1);
-          } else {
-            a0 = ex2(a0), a1 = ex2(a1);
-          }
+          a0 = ex2(a0), a1 = ex2(a1);
           if (LSE) add2(ex0, ex1, a0, a1);
           pk[e] = pack_bf16x2(a0, a1);
           mx2 = max_bf16x2(mx2, pk[e]);
@@ -411,7 +403,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       hand_over();
       top_w = fmaxf(bf16_lo(mx2), bf16_hi(mx2));
       l_sum += sum0 + sum1;
-      if (!isfinite(odd0 + odd1) || most > 126.f) l_sum = CUDART_NAN_F;
       if (LSE) x_sum += ex0 + ex1;
     };
     // ... against a reference that moves first; for rows that have none yet, and behind weights that are big
@@ -741,8 +732,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 constexpr int kAccThreads = 576;
 constexpr int kAccMmaWarp = 16, kAccLoadWarp = 17;
 constexpr int kAccStages = 4;
-// Of 8 pairs of a thread's weights, those made by multiply-adds (2 x 4096 tokens, prefill and account, 32 / 8 heads: 425 us with 0, 414 with 4
-// of the first pair of each four, 421 with 5, 442 with 8).
+// Of a thread's 8 times 4 weights of 32 columns, those of which the first two are made by multiply-adds (2 x 4096 tokens, prompt and account,
+// 32 / 8 heads: 445.7 us with 0, 443.9 with 2, 444.6 with 4, 456 with 6).
 constexpr int kAccByFma = 4;
 
 template <int D>
@@ -902,7 +893,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
               fma2v(a2, a3, __uint_as_float(x[e * 4 + 2]), __uint_as_float(x[e * 4 + 3]), p.scale_log2, l4.z, l4.w);
               if (decltype(fast)::value && e < kAccByFma) {
                 add2(odd0, odd1, a0, a1);
-                exp2_fma<5>(a0, a1);
+                exp2_fma(a0, a1);
                 a2 = ex2(a2), a3 = ex2(a3);
               } else {
                 if (!decltype(fast)::value) {
@@ -992,7 +983,7 @@ paged_weights_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const uint32_t bar_k = smem_u32(&sm.bar_k[kn & 1]);
       if (leader) mbar_expect_tx(bar_k, Sm::kTileBytes);
       load_tile<D>(leader, &maps.k, p, smem_u32(sm.k[kn & 1]), page, kt.j0, kt.g, pieces, rows, bar_k);
-      ++asked.q[kn & 1];
+      ++(kn & 1 ? asked.q[1] : asked.q[0]);
       ++kn;
       for (int i = 0; i < n; ++i) {
         const int t = done + i, st = t % kAccStages, tok = kt.t0 + i * TOKT;

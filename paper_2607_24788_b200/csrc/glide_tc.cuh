@@ -219,9 +219,8 @@ __device__ __forceinline__ void fma2p(float &a0, float &a1, float x0, float x1, 
 }
 // 2^a0, 2^a1 by multiply-adds, for a share of the exponentials where the special function unit (16 a cycle and SM) is what
 // the others wait for: a = n + f with n the nearest whole number (by adding 3 2^22, which leaves n in the low bits), 2^f by a polynomial
-// on [-1/2, 1/2], n added to the exponent.  The polynomials are minimax for the relative error (Remez exchange): degree 3 7.5e-5,
-// degree 5 7.5e-8.  Below -126 the result is 2^-126.  No argument above 127, no infinity and no NaN.
-template <int DEGREE>
+// on [-1/2, 1/2], n added to the exponent.  The polynomial, of degree 5, is minimax for the relative error (Remez exchange), 7.5e-8.  Below
+// -126 the result is 2^-126.  No argument above 127, no infinity and no NaN.
 __device__ __forceinline__ void exp2_fma(float &a0, float &a1) {
   constexpr float kBig = 12582912.0f;
   a0 = fmaxf(a0, -126.f), a1 = fmaxf(a1, -126.f);
@@ -230,20 +229,12 @@ __device__ __forceinline__ void exp2_fma(float &a0, float &a1) {
   float n0 = t0, n1 = t1;
   add2(n0, n1, -kBig, -kBig);
   add2(a0, a1, -n0, -n1);
-  float p0, p1;
-  if (DEGREE == 3) {
-    p0 = p1 = 0.05517167f;
-    fma2p(p0, p1, a0, a1, 0.24261112f);
-    fma2p(p0, p1, a0, a1, 0.69326099f);
-    fma2p(p0, p1, a0, a1, 0.99992807f);
-  } else {
-    p0 = p1 = 0.00132765f;
-    fma2p(p0, p1, a0, a1, 0.00967554f);
-    fma2p(p0, p1, a0, a1, 0.05550713f);
-    fma2p(p0, p1, a0, a1, 0.2402212f);
-    fma2p(p0, p1, a0, a1, 0.69314697f);
-    fma2p(p0, p1, a0, a1, 1.00000007f);
-  }
+  float p0 = 0.00132765f, p1 = 0.00132765f;
+  fma2p(p0, p1, a0, a1, 0.00967554f);
+  fma2p(p0, p1, a0, a1, 0.05550713f);
+  fma2p(p0, p1, a0, a1, 0.2402212f);
+  fma2p(p0, p1, a0, a1, 0.69314697f);
+  fma2p(p0, p1, a0, a1, 1.00000007f);
   a0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
   a1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
 }

@@ -196,3 +196,16 @@ def test_the_readme_example():
         exec(readme_example(), dict(glide=glide, L=1, **alone))
         for n in sorted(per_layer):
             assert torch.equal(alone[n][0], shared[n][l]), (l, n)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window,n_sink", [(-1, 0), (300, 4)])
+def test_outputs_with_row_sums_and_without(dtype, window, n_sink):
+    for before, new in (([100, 0, 1500], [300, 200, 5]), ([2500], [6])):
+        c = Cache(before, new, 8, 2, 128, dtype, 64)
+        c.q[:, ::2] *= 50.0   # (references that move)
+        out = [torch.empty_like(c.q) for _ in range(2)]
+        for i in range(2):
+            c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, c.k, c.v, out[i], window=window, n_sink=n_sink,
+                                         lse=torch.empty(c.q.shape[:2], device="cuda") if i else None)
+        assert torch.equal(*out) and out[0].isfinite().all()
