@@ -405,7 +405,7 @@ int glide_paged_decode(glide_paged *p, const glide_paged_call *call, const void 
  * over the same tokens, mask and scale) give every slot to the account dev_weight. */
 int glide_paged_weights(glide_paged *p, const glide_paged_call *call, const void *dev_q, const float *dev_lse, void *stream);
 
-/* Every sequence keeps min(lens[b], budget) slots; each KV head chooses its own.  Slots with a position below n_sink or at
+/* Every sequence keeps min(lens[b], budget) slots; each KV head chooses its own (handles with weights 1).  Slots with a position below n_sink or at
  * or above seen[b] - recent are protected (n_sink + recent <= budget); of the others those of least dev_weight leave, of
  * equal ones the lowest slots first (a NaN counts as larger than any number; protected slots leave, lowest first, only
  * when there are not enough others).  Of the kept slots those at or behind the new length move, in ascending order, into the

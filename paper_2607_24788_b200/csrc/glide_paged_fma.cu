@@ -7,8 +7,10 @@
 // the two turns that 256 bytes take; four features of a row, or a row's weights of four slots, are one read.  (By feature, through
 // registers, a lane per row: 32 lines a load and a turn per line.  512 tokens of 4 heads of 64, windows of 64, prompt and account: 43 us, this 33;
 // 1000 tokens of 32 / 8 heads of 128: 962 us, this 725.)
-// Weights are taken against a reference that moves when a score exceeds it by more than 8 in the exponent.  Bound: shared-memory reads for
-// 16 rows, the multiply-adds for 64.
+// Weights are taken against a reference that moves when a score exceeds it by more than 8 in the exponent.  Bound (1000 tokens of 32 / 8 heads of
+// 128): with 16 rows (the account there, 445 us) shared-memory reads, 0.84 of a turn per cycle; with 64 (the prompt, 320 us, 26 TFLOP/s) no
+// unit, 42 % of the multiply-adds' cycles and 0.59 of shared memory's turns: 177 KiB leave one CTA of 8 warps per SM for d = 128, two warps per
+// scheduler, which wait for their reads and for one another.
 // What a row does not see does not reach it: scores are selected; rows of V that no row of the CTA sees are zeros; a row whose output
 // is not finite all the same is computed once more by itself.
 #include <algorithm>
