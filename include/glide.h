@@ -63,7 +63,8 @@ typedef enum {
   GLIDE_ERR_SCRATCH_LIMIT = 7        /* glide_decode_step_noalloc: the split-K scratch would not fit the static buffer */
 } glide_status;
 
-typedef enum { GLIDE_F32 = 0, GLIDE_BF16 = 1 } glide_dtype;
+/* GLIDE_BF16_CACHE4 (paged handles only): bf16 tensors, pages whose values are held in 4 bits. */
+typedef enum { GLIDE_F32 = 0, GLIDE_BF16 = 1, GLIDE_BF16_CACHE4 = 4 } glide_dtype;
 
 /* Feature map of the linear part.  GLIDE_PHI_SOFTMAX is the paper's default
  * (Sec. III-B): phi(x) = softmax over the head_dim entries of x, no parameters,
@@ -334,6 +335,14 @@ int glide_stream_schedule(const glide_config *cfg, int32_t n_sms, int64_t smem_l
  *     (stream order); calls that may run at the same time need handles of their own, which may share the pages.  Several host
  *     threads may call with one handle: the launches of a call stay together.
  *   - Results do not depend on timing: no sum is made by atomics, and parts are joined in a fixed order.
+ *
+ * Pages in 4 bits (GLIDE_BF16_CACHE4).  A row (the d values of a slot's key or value, of one KV head) stands on 16 levels:
+ *     low = min_i x_i,   step = bf16((max_i x_i - low) * (1.0f / 15)),   code_i = rint((x_i - low) / step) in 0 .. 15 (step 0: 0),
+ * with x the bf16 row that a bf16 cache would hold and the arithmetic in fp32, and it stands for low + step * code_i: off by at most
+ * half a step, and 15 / 256 of a step for the step's own rounding.  A row that holds an infinity or a NaN, or whose range is no bf16
+ * number, stands for NaN.  A page holds for every KV head a block of page_size * (d / 2 + 4) bytes: the slots' codes, d / 2 bytes each (byte
+ * i: feature 2i in the low bits, 2i + 1 in the high ones), then for each slot two bf16 numbers, step and low.  Prefill, decode, append,
+ * read and the status take such handles; the account of weights (weights has to be 0), eviction, bounds and sparse steps do not.
  */
 typedef struct glide_paged glide_paged; /* opaque, host side */
 
@@ -342,14 +351,15 @@ typedef struct {
   int32_t n_q_heads;       /* H; H / H_kv in {1, 2, 4, 8} */
   int32_t n_kv_heads;      /* H_kv */
   int32_t head_dim;        /* d in {64, 128} */
-  int32_t io_dtype;        /* glide_dtype of q, k, v, out and the pages */
+  int32_t io_dtype;        /* glide_dtype of q, k, v, out and the pages; GLIDE_BF16_CACHE4: bf16, and pages in 4 bits */
   int32_t page_size;       /* tokens of a page: 16, 32, 64, 128 or 256 */
   int32_t n_pages;         /* pages of the pool, per layer */
   int32_t max_batch;       /* most sequences of a call, <= 1024 */
   int64_t max_tokens;      /* most slots of a sequence, <= 2^30 */
   int64_t layer_stride, page_stride, head_stride, row_stride; /* elements between layers, pages, KV heads and slots of the
                               pool, multiples of 16 bytes, layer_stride a multiple of page_stride; all 0:
-                              [n_layers][n_pages][H_kv][page_size][d] */
+                              [n_layers][n_pages][H_kv][page_size][d].  GLIDE_BF16_CACHE4: bytes, row_stride d / 2 + 4 (what a slot
+                              takes of its head's block, below); all 0: [n_layers][n_pages][H_kv][page_size * (d / 2 + 4)] */
   float softmax_scale;     /* 0 selects 1/sqrt(head_dim) */
   int32_t weights;         /* 1: the account of weights can be kept (a decode step then needs max_batch * H * max_tokens
                               floats of workspace) */
@@ -418,12 +428,57 @@ int glide_paged_weights(glide_paged *p, const glide_paged_call *call, const void
 int glide_paged_evict(glide_paged *p, const glide_paged_call *call, int64_t budget, int64_t recent, float *dev_weight_out,
                       int32_t *dev_pos_out, int32_t *dev_new_lens, void *stream);
 
+/* Rotation of queries and keys by their tokens' positions, in pairs of features (a, b) of the first rot_dim ones:
+ *     a' = a cos - b sin,   b' = b cos + a sin
+ * with pair i's angle at position t in row t, entry i of the tables; each product and sum is rounded to fp32, the result once to the I/O
+ * dtype.  The features behind rot_dim stay as they are. */
+typedef struct {
+  const float *dev_cos, *dev_sin; /* device fp32 [n_positions][rot_dim / 2], rows `stride` apart, 16-byte aligned */
+  int64_t n_positions;            /* >= 1.  A token at another position is recorded in the status word and takes the nearest row */
+  int64_t stride;                 /* floats, a multiple of 4; 0: rot_dim / 2 */
+  int32_t rot_dim;                /* a multiple of 16, at most head_dim */
+  int32_t neighbours;             /* 0: pair i is features i and i + rot_dim / 2; 1: 2i and 2i + 1 */
+} glide_rotation;
+
+/* Bring in the new tokens of every sequence (dev_starts, as for prefill; dev_starts NULL: one for each sequence, row b, as for a decode
+ * step): queries and keys are rotated by the tokens' positions, seen - T_b ... seen - 1 (rotation NULL: not), keys and values stored in the last
+ * slots of the sequence's length, queries written to dev_q_out.  dev_q [n_tokens][H][d] (rows q_stride apart) and dev_q_out (rows
+ * out_stride apart) both or neither; dev_q_out may be dev_q itself with equal strides, otherwise the two must not overlap.  Where
+ * dev_weight / dev_pos are given, the new slots' account starts at 0 and their positions are written.  A prefill or decode call with dev_k and
+ * dev_v NULL then attends.  Without dev_starts, n_tokens and the window are ignored. */
+int glide_paged_append(glide_paged *p, const glide_paged_call *call, const glide_rotation *rotation, const void *dev_q, const void *dev_k,
+                       const void *dev_v, void *dev_q_out, void *stream);
+
+/* The rows that the slots of the call's new tokens hold (dev_starts as for append), into dev_k, dev_v [n_tokens][H_kv][d], rows kv_stride
+ * apart: what the cache's values are, rounded to the I/O dtype (only values in 4 bits need that).  With starts over whole sequences, a way of
+ * handing them to another cache. */
+int glide_paged_read(glide_paged *p, const glide_paged_call *call, void *dev_k, void *dev_v, void *stream);
+
+/* Bounds of the keys, page by page, for sparse steps: dev_bounds [n_pages][H_kv][2][d] in the I/O dtype, of the call's layer (16-byte
+ * aligned), holds the least and the largest value of every feature over the page's slots.  Written are those of the pages that hold new
+ * tokens (dev_starts as for append; starts over whole sequences: all of their pages), over the slots below the sequence's length.
+ * A NaN makes both bounds of its feature NaN.  Prompts are stored, then this is called; steps keep the bounds themselves. */
+int glide_paged_bounds(glide_paged *p, const glide_paged_call *call, void *dev_bounds, void *stream);
+
+/* One new token for every sequence, as glide_paged_decode, over n_picks of its pages, which every KV head chooses for itself: the page of the
+ * token's own slot, the pages of the first n_sink slots, and of the others those of the largest score
+ *     max over the query heads of the KV head, of  sum_f max(q_f low_f, q_f high_f)
+ * (what no key of the page exceeds; summed in 64 bits; equal ones: the first; a score that is NaN counts as the largest).  A sequence of
+ * n_picks pages or fewer is attended to whole.  The bounds of the token's own page take its key in first, where the token is the page's first
+ * they become it; with dev_k and dev_v NULL the key is the cache's.  The slots of the chosen pages are seen all; the call's window has to
+ * be negative, the pages of the first n_sink slots and one more at most n_picks, the account is not kept (dev_weight NULL).
+ * dev_picks int32 [B][H_kv][n_picks] receives the chosen columns of the table, ascending, -1 behind the last; dev_scores,
+ * [B][H_kv][table_cols] of 8 bytes, is work space. */
+int glide_paged_decode_sparse(glide_paged *p, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
+                              void *dev_out, float *dev_lse, void *dev_bounds, int32_t n_picks, int32_t *dev_picks, double *dev_scores,
+                              void *stream);
+
 /* What a call with these fields would be refused with (GLIDE_OK: it would not).  The fields that only prefill and
  * weights read are looked at when dev_starts is given.  Host only, no CUDA calls. */
 int glide_paged_check_call(const glide_paged_config *cfg, const glide_paged_call *call);
 
 /* The handle's status word, read and cleared (0: nothing was recorded since; 3: a wait inside a kernel ran out; 4: a page id,
- * 5: a length or starts out of range).  Synchronises `stream`. */
+ * 5: a length or starts, 6: a position out of range).  Synchronises `stream`. */
 int glide_paged_device_status(glide_paged *p, void *stream, int32_t *status_out);
 
 /* Static, NUL-terminated description of a status code. */

@@ -9,21 +9,6 @@ namespace {
 
 constexpr int kWarps = 8;
 
-// Sequence of row r of the call, its slot; false for rows of no sequence.
-__device__ bool row_of(const PagedParams &p, int64_t r, int &b, int &slot) {
-  int lo = 0, hi = p.batch;
-  while (hi - lo > 1) {   // the last sequence that starts at or before r
-    const int mid = (lo + hi) >> 1;
-    if (p.starts[mid] <= r) lo = mid; else hi = mid;
-  }
-  b = lo;
-  const int len = paged_len(p, b);
-  int row0;
-  const int n = paged_new(p, b, len, row0);
-  slot = len - n + int(r - row0);
-  return r >= row0 && r < row0 + n;
-}
-
 // A block per 16 new tokens: their places are looked up by a lane each, which also starts their account and writes their positions; then,
 // where the call brings K and V, all threads copy, 16 bytes of each at a time.  Bound: the
 // rows' bytes.  (A warp per token and head, which looked its place up by itself: 30 us for 12401 tokens of 8 heads of 256 bytes, this 16.)
@@ -38,7 +23,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
     const int64_t r = r0 + threadIdx.x;
     int b, slot;
     int64_t at = -1;
-    if (r < p.n_tokens && row_of(p, r, b, slot)) {
+    if (r < p.n_tokens && paged_row_of(p, r, b, slot)) {
       const int page = p.new_k ? paged_page(p, b, slot) : 0;   // (rows that are in the cache already: the table may hold anything)
       if (p.new_k && page >= 0) at = int64_t(paged_row(p, page, slot, 0));
       if (p.weight || p.pos) {
@@ -69,8 +54,9 @@ __global__ void __launch_bounds__(kWarps * 32) paged_store_kernel(const __grid_c
 }
 
 // One warp per (new token, query head): the records of the row's parts, added up in their order.
-template <typename T, int D>
+template <typename C, int D>
 __global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_constant__ PagedParams p, int splits) {
+  using T = Io<C>;
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31;
   const int64_t item = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
@@ -78,7 +64,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_co
   const int head = int(item - r * p.H);
   wait_for_predecessor();
   int b, i;
-  if (r >= p.n_tokens || !row_of(p, r, b, i)) return;
+  if (r >= p.n_tokens || !paged_row_of(p, r, b, i)) return;
   float M = -CUDART_INF_F, L = 0.f, X = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -105,7 +91,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_co
   }
   if (p.lse && lane == 0) p.lse[r * p.H + head] = PagedRow<T, D, 1>::paged_lse(M, X);
   if (!__all_sync(0xffffffffu, fine)) {   // (0 times what a slot holds that the row does not see, for one)
-    paged_row_alone<T, D>(p, size_t(r), b, i, head / (p.H / p.Hkv), head, p.lse && !isfinite(X), nullptr);
+    paged_row_alone<C, D>(p, size_t(r), b, i, head / (p.H / p.Hkv), head, p.lse && !isfinite(X), nullptr);
   }
 }
 
@@ -128,6 +114,10 @@ int paged_splits(const PagedParams &p, int64_t ctas, int least) {
 }
 
 int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st) {
+  if (h->codes) {
+    const auto kernel = h->cfg.head_dim == 64 ? paged_join_kernel<Code4, 64> : paged_join_kernel<Code4, 128>;
+    return launch_status(launch_chained(kernel, blocks_of(p.n_tokens * p.H), kWarps * 32, 0, st, p, splits));
+  }
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
     return launch_status(launch_chained(paged_join_kernel<typename decltype(t)::type, decltype(d)::value>, blocks_of(p.n_tokens * p.H),
                                         kWarps * 32, 0, st, p, splits));

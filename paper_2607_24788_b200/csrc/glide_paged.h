@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 
 #include <mutex>
 
@@ -17,6 +18,7 @@ struct glide_paged {
   int sm_count = 0;
   int group = 1;
   int page_shift = 4;
+  bool codes = false;               // GLIDE_BF16_CACHE4: the pages' strides are bytes
   int64_t layer_pages = 0;          // page numbers from one layer to the next: layer_stride / page_stride
   unsigned char *ws = nullptr;
   unsigned char *k = nullptr, *v = nullptr;
@@ -30,7 +32,7 @@ struct glide_paged {
 
 namespace glide {
 
-enum : int { kDevBadPage = 4, kDevBadLength = 5 };   // status codes beside glide_internal.h's
+enum : int { kDevBadPage = 4, kDevBadLength = 5, kDevBadPosition = 6 };   // status codes beside glide_internal.h's
 
 constexpr int kMaxPagedBatch = 1024;
 constexpr int kPagedTile = 16;        // slots of a decode tile: no tile crosses a page
@@ -61,7 +63,24 @@ struct PagedParams {
   float *logits;                      // [batch][Hkv][most][G]: scores of a decode step whose weights are kept
   int32_t *moves;                     // (the same memory) evict: [batch][Hkv][most / 2] pairs of slots
   int32_t sm_count;
+  const int32_t *picks;               // sparse steps: [batch][Hkv][n_picks] columns of the table, ascending, -1 behind the last
+  int32_t n_picks, n_cols;            // n_cols: of the table
 };
+
+// What a page holds, as kernels are told it: rows of T, or rows in 4 bits.  Io: the type of q, k, v and out beside it.
+struct Code4 {};
+template <typename C>
+struct IoOf {
+  using type = C;
+};
+template <>
+struct IoOf<Code4> {
+  using type = __nv_bfloat16;
+};
+template <typename C>
+using Io = typename IoOf<C>::type;
+// Levels of a row in 4 bits (bf16 step in the low half, lowest one above it): bytes behind the codes of its head's block
+constexpr int kLevelBytes = 4;
 
 // Lengths as the kernels use them: what is out of range is recorded and clamped.
 __device__ __forceinline__ int paged_len(const PagedParams &p, int b) {
@@ -81,6 +100,20 @@ __device__ __forceinline__ int paged_new(const PagedParams &p, int b, int len, i
     n = 0;
   }
   return n;
+}
+// Sequence of row r of the call, its slot; false for rows of no sequence.
+__device__ __forceinline__ bool paged_row_of(const PagedParams &p, int64_t r, int &b, int &slot) {
+  int lo = 0, hi = p.batch;
+  while (hi - lo > 1) {   // the last sequence that starts at or before r
+    const int mid = (lo + hi) >> 1;
+    if (p.starts[mid] <= r) lo = mid; else hi = mid;
+  }
+  b = lo;
+  const int len = paged_len(p, b);
+  int row0;
+  const int n = paged_new(p, b, len, row0);
+  slot = len - n + int(r - row0);
+  return r >= row0 && r < row0 + n;
 }
 // Page of a slot; a bad id is recorded and gives -1.
 __device__ __forceinline__ int paged_page(const PagedParams &p, int b, int slot) {
@@ -113,6 +146,14 @@ __device__ __forceinline__ float *split_record(const PagedParams &p, int head_di
 int paged_splits(const PagedParams &p, int64_t ctas, int least);
 int launch_paged_join(const glide_paged *h, const PagedParams &p, int splits, cudaStream_t st);
 
+// The new tokens of a call on their way in (glide_paged_append).
+struct PagedAppend {
+  const float *cos, *sin;             // NULL: no rotation
+  int64_t n_positions, stride;
+  int32_t rot_dim, neighbours;
+  void *q_out;                        // rows PagedParams::out_stride apart
+};
+
 // (host) status of a launch; an error is taken off the runtime's record
 inline int launch_status(cudaError_t rc) {
   if (rc == cudaSuccess) rc = cudaPeekAtLastError();
@@ -129,6 +170,10 @@ int launch_paged_weights_fma(const glide_paged *h, const PagedParams &p, cudaStr
 int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st);
 int launch_paged_evict(const glide_paged *h, const PagedParams &p, int budget, int recent, float *weight_out, int32_t *pos_out,
                        int32_t *new_lens, cudaStream_t st);
+int launch_paged_append(const glide_paged *h, const PagedParams &p, const PagedAppend &a, cudaStream_t st);
+int launch_paged_read(const glide_paged *h, const PagedParams &p, void *k, void *v, cudaStream_t st);
+int launch_paged_bounds(const glide_paged *h, const PagedParams &p, void *bounds, cudaStream_t st);
+int launch_paged_select(const glide_paged *h, const PagedParams &p, void *bounds, int32_t *picks, double *scores, cudaStream_t st);
 size_t paged_record_bytes(const glide_paged_config &cfg);
 int setup_paged_decode(const glide_paged *h);   // what the device's context has to know of the kernels, once per handle
 int setup_paged_tc(const glide_paged *h);

@@ -9,12 +9,17 @@
 //          (the sum that O is divided by takes the rounded ones: every weight is off by at most 2^-8 of itself; lse and the account
 //          take the exact ones), turned by movmatrix,
 //          O^T += V_tile^T P.
+//   4 bits codes become bf16 numbers by their bits (0x4300 | code is 128 + code).  K: a lane has a quarter of two slots' features, in the order in
+//          which the codes lie, the queries' fragments in the same order; 128 sum q is taken off before the product, a row's levels are
+//          put on its scores.  V: a lane has an eighth of four slots' features, two slots' codes are brought together by byte permutation,
+//          136 is taken off (exact); the step goes to the weight, the lowest level + 8 steps are added up apart, in fp32.
 //   fp32   2 or 4 lanes per slot, all query heads; weights through shared memory; a lane has D / 32 columns of O.
 // At a unit's end the eight warps meet; a unit that lies in one CTA is written out, one that was cut leaves a record (maximum, sums, O
 // per head) per CTA, and the CTA that leaves the last one adds them up in slot order.  A step whose weights are kept also leaves
 // its scores (4 bytes per slot and query head, 3 % of the rows' bytes), which a second kernel turns into weights.
 // Bound: the rows' bytes from memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "glide_paged_rows.cuh"
 #include "glide_tc.cuh"
@@ -42,6 +47,18 @@ struct Shape {
   static __device__ __forceinline__ int at(int r, int c) {
     return r * kRowBytes + ((c ^ ((sizeof(T) == 4 ? r * kParts : r) & 7)) << 4);
   }
+};
+
+// Rows in 4 bits: a tile is [16 slots' codes of K][their levels][of V ...].
+template <int D>
+struct Shape<Code4, D> {
+  static constexpr int kTile = 16;
+  static constexpr int kCodes = kTile * D / 2, kHalf = kCodes + kTile * kLevelBytes;   // bytes of codes; of K or V
+  static constexpr int kTileBytes = 2 * kHalf;
+  static constexpr int kStages = 16384 / kTileBytes;
+  static constexpr int kRowBytes = 2 * D;   // (of q)
+  // where 16-byte piece i of V's codes lies: the eight slots 2c, 2c + 1, .. of a quarter warp in different banks
+  static __device__ __forceinline__ int at_v(int i) { return ((i & ~7) | ((i & 7) ^ (D == 128 ? ((i >> 3) & 3) << 1 : ((i >> 3) & 1) << 1))) << 4; }
 };
 
 template <typename T, int D, int G>
@@ -76,7 +93,14 @@ __device__ __forceinline__ SeqTiles tiles_of(const PagedParams &p, int len) {
 }
 
 // Tiles of the sequences before each one, times the KV heads; every thread of the block.  Returns the most tiles of a unit.
-template <int TILE, int THREADS>
+// ... of a sparse step: those of the chosen pages, of which all but the last, the newest, are whole
+template <int TILE>
+__device__ __forceinline__ int picked_tiles(const PagedParams &p, int len) {
+  if (len == 0) return 0;
+  const int newest = (len - 1) >> p.page_shift;
+  return (min(newest + 1, p.n_picks) - 1) * ((1 << p.page_shift) / TILE) + (len - (newest << p.page_shift) + TILE - 1) / TILE;
+}
+template <int TILE, int THREADS, bool PICKED = false>
 __device__ __forceinline__ int prefix_of(const PagedParams &p, int *len, int *prefix, int *warp_sums, int *warp_most) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int base = 0, most = 0;
@@ -86,7 +110,7 @@ __device__ __forceinline__ int prefix_of(const PagedParams &p, int *len, int *pr
     if (b < p.batch) {
       const int l = paged_len(p, b);
       len[b] = l;
-      n = tiles_of<TILE>(p, l).n;
+      n = PICKED ? picked_tiles<TILE>(p, l) : tiles_of<TILE>(p, l).n;
     }
     most = max(most, n);
     n *= p.Hkv;
@@ -156,6 +180,14 @@ __device__ __forceinline__ uint32_t turn(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
+}
+
+// Code p and code p + 4 of eight as two bf16 numbers, 128 more than they are
+__device__ __forceinline__ uint32_t pair_of(uint32_t codes, int p) { return ((codes >> (4 * p)) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 // The state of one warp in one unit, bf16.  Thread (r = lane / 4, c = lane % 4) has the scores of slots r and r + 8 of a tile for the
@@ -271,6 +303,162 @@ struct WarpUnit {
       for (int e = 0; e < 4; ++e) {
         const int h = (lane & 3) * 2 + (e & 1);
         if (h < G) f(h, k * 16 + (lane >> 2) + (e >> 1) * 8, o[k][e]);
+      }
+  }
+};
+
+// Rows in 4 bits.  Thread (r = lane / 4, c = lane % 4) has scores as above; of O^T, features r D / 8 + 2k and + 2k + 1 of every k.
+template <int D, int G>
+struct WarpUnit<Code4, D, G> {
+  uint32_t q[D / 16][2];
+  float o[D / 16][4];
+  float m[2], x[2], z[2];   // maxima; sums of the weights; of the weights times the middle level of their rows, low + 8 step
+  float off[2], qs[2];      // -128 sum q; sum q in the scores' unit
+
+  template <typename S>
+  __device__ __forceinline__ void begin(const PagedParams &p, S &, int b, int g) {
+    const int lane = threadIdx.x & 31, h = lane >> 2;
+    constexpr int F = D / 4;   // features of a lane
+    const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + size_t(b) * size_t(p.q_stride) +
+                                                       size_t(g * G + h) * D + (lane & 3) * F);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < F / 8; ++j) {
+      const uint4 w = h < G ? src[j] : make_uint4(0u, 0u, 0u, 0u);
+      q[2 * j][0] = __byte_perm(w.x, w.z, 0x5410), q[2 * j][1] = __byte_perm(w.x, w.z, 0x7632);
+      q[2 * j + 1][0] = __byte_perm(w.y, w.w, 0x5410), q[2 * j + 1][1] = __byte_perm(w.y, w.w, 0x7632);
+      sum += ((bf16_lo(w.x) + bf16_hi(w.x)) + (bf16_lo(w.y) + bf16_hi(w.y))) + ((bf16_lo(w.z) + bf16_hi(w.z)) + (bf16_lo(w.w) + bf16_hi(w.w)));
+    }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float all = __shfl_sync(0xffffffffu, sum, ((lane & 3) * 2 + i) * 4);
+      off[i] = -128.f * all, qs[i] = all * p.scale_log2;
+      m[i] = -CUDART_INF_F, x[i] = z[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+  }
+  template <typename S>
+  __device__ __forceinline__ void tile(const PagedParams &p, S &, const unsigned char *buf, uint32_t mask, float *) {
+    using Sh = Shape<Code4, D>;
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    const unsigned char *V = buf + Sh::kHalf;
+    // scores
+    constexpr int W = D / 32;   // words of eight codes that a lane has of a K row
+    uint32_t k0[W], k1[W];
+    if constexpr (W == 4) {
+      const uint4 a = *reinterpret_cast<const uint4 *>(buf + r * 64 + c * 16), b = *reinterpret_cast<const uint4 *>(buf + (r + 8) * 64 + c * 16);
+      k0[0] = a.x, k0[1] = a.y, k0[2] = a.z, k0[3] = a.w, k1[0] = b.x, k1[1] = b.y, k1[2] = b.z, k1[3] = b.w;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2 *>(buf + r * 32 + c * 8), b = *reinterpret_cast<const uint2 *>(buf + (r + 8) * 32 + c * 8);
+      k0[0] = a.x, k0[1] = a.y, k1[0] = b.x, k1[1] = b.y;
+    }
+    uint32_t kl[2], vl[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      kl[e] = *reinterpret_cast<const uint32_t *>(buf + Sh::kCodes + (r + 8 * e) * 4);
+      vl[e] = *reinterpret_cast<const uint32_t *>(V + Sh::kCodes + (r + 8 * e) * 4);
+      vl[e] = (mask >> (r + 8 * e)) & 1u ? vl[e] : 0u;   // (what is not seen is no NaN either)
+    }
+    float s0[4] = {off[0], off[1], off[0], off[1]}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const int pr = (ks & 1) * 2;
+      const uint32_t a[4] = {pair_of(k0[ks >> 1], pr), pair_of(k1[ks >> 1], pr), pair_of(k0[ks >> 1], pr + 1), pair_of(k1[ks >> 1], pr + 1)};
+      mma16816(ks & 1 ? s1 : s0, a, q[ks][0], q[ks][1]);
+    }
+    float s[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool seen = (mask >> (r + (e >> 1) * 8)) & 1u;
+      const float step = bf16_lo(kl[e >> 1]) * p.scale_log2, low = bf16_hi(kl[e >> 1]);
+      s[e] = seen ? fmaf(s0[e] + s1[e], step, low * qs[e & 1]) : -CUDART_INF_F;
+    }
+    bool grows = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float top = fmaxf(s[i], s[i + 2]);
+      grows |= top > m[i] + kLazy || (m[i] == -CUDART_INF_F && top > -CUDART_INF_F);
+    }
+    if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float top = fmaxf(s[i], s[i + 2]);
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        top = fmaxf(top, m[i]);
+        const float f = m[i] == -CUDART_INF_F ? 0.f : ex2(m[i] - top);
+        m[i] = top;
+        x[i] *= f, z[i] *= f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) o[k][i] *= f, o[k][i + 2] *= f;
+      }
+    }
+    uint32_t pk[2];
+    const float r0 = m[0] == -CUDART_INF_F ? 0.f : m[0], r1 = m[1] == -CUDART_INF_F ? 0.f : m[1];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float step = bf16_lo(vl[e]), mid = fmaf(8.f, step, bf16_hi(vl[e]));
+      const float w0 = ex2(s[e * 2] - r0), w1 = ex2(s[e * 2 + 1] - r1);
+      x[0] += w0, x[1] += w1;
+      z[0] = fmaf(w0, mid, z[0]), z[1] = fmaf(w1, mid, z[1]);
+      pk[e] = turn(pack_bf16x2(w0 * step, w1 * step));   // (rounded as the product needs it: a weight's share of v - mid is off by at most 2^-8 of itself)
+    }
+    // O
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {   // eight features of the lane at a time
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int slot = 2 * c + (i & 1) + (i >> 1) * 8, at = slot * (D / 2) + r * (D / 16) + j * 4;
+        w[i] = *reinterpret_cast<const uint32_t *>(V + Sh::at_v(at >> 4) + (at & 15));
+      }
+      const uint32_t v01[2] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632)};
+      const uint32_t v23[2] = {__byte_perm(w[2], w[3], 0x5410), __byte_perm(w[2], w[3], 0x7632)};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = (2 * k) & 3, h = k >> 1;
+        constexpr uint32_t kMid = 0xc308c308u;   // -136, twice
+        const uint32_t a[4] = {add_bf16x2(pair_of(v01[h], n), kMid), add_bf16x2(pair_of(v01[h], n + 1), kMid),
+                               add_bf16x2(pair_of(v23[h], n), kMid), add_bf16x2(pair_of(v23[h], n + 1), kMid)};
+        mma16816(o[j * 4 + k], a, pk[0], pk[1]);
+      }
+    }
+  }
+  template <typename S>
+  __device__ __forceinline__ void put_sums(S &sm, int warp) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) x[i] += __shfl_xor_sync(0xffffffffu, x[i], w), z[i] += __shfl_xor_sync(0xffffffffu, z[i], w);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) o[k][i] += z[i], o[k][i + 2] += z[i];
+      const int h = (lane & 3) * 2 + i;
+      if (lane < 4 && h < G) sm.m[warp][h] = m[i], sm.l[warp][h] = sm.e[warp][h] = x[i];
+    }
+  }
+  __device__ __forceinline__ void scale(float factor) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = __shfl_sync(0xffffffffu, factor, (threadIdx.x & 3) * 2 + i);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) o[k][i] *= f, o[k][i + 2] *= f;
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F &&f) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int h = (lane & 3) * 2 + (e & 1);
+        if (h < G) f(h, (lane >> 2) * (D / 8) + 2 * k + (e >> 1), o[k][e]);
       }
   }
 };
@@ -459,15 +647,17 @@ __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, 
   }
 }
 
-template <typename T, int D, int G>
+template <typename C, int D, int G, bool PICKED>
 __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_constant__ PagedParams p) {
-  using Sh = Shape<T, D>;
+  using Sh = Shape<C, D>;
+  using T = Io<C>;
+  constexpr bool kCodes = std::is_same<C, Code4>::value;
   constexpr int S = Sh::kStages;
   extern __shared__ __align__(128) unsigned char smem_raw[];
-  auto &sm = *reinterpret_cast<Smem<T, D, G> *>(smem_raw);
+  auto &sm = *reinterpret_cast<Smem<C, D, G> *>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_for_predecessor();
-  const int most = prefix_of<Sh::kTile, kThreads>(p, sm.len, sm.prefix, sm.warp_sums, sm.warp_most);
+  const int most = prefix_of<Sh::kTile, kThreads, PICKED>(p, sm.len, sm.prefix, sm.warp_sums, sm.warp_most);
   const int total = sm.prefix[p.batch], share = share_of(total, int(gridDim.x)), units = p.batch * p.Hkv;
   int lo = int(min(int64_t(total), int64_t(blockIdx.x) * share)), hi = min(total, lo + share);
   if (units <= int(gridDim.x) && most <= share + kCutCost) {   // a unit for each CTA
@@ -482,13 +672,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     TileInfo t;
     if (i >= mine) return t;
     const int f = lo + warp + i * kWarps, b = seq_of(sm.prefix, p.batch, f), len = sm.len[b];
-    const SeqTiles st = tiles_of<Sh::kTile>(p, len);
+    SeqTiles st{0, 0, 0, 0, 0};
+    if (PICKED) st.n = (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv;
+    else st = tiles_of<Sh::kTile>(p, len);
     const int rest = f - sm.prefix[b], g = rest / st.n, k = rest - g * st.n;
-    t.slot = (k < st.sinks ? k : st.first + k - st.sinks) * Sh::kTile;
     t.unit = b * p.Hkv + g;
+    if (PICKED) {
+      const int per = (1 << p.page_shift) / Sh::kTile, j = k / per;
+      t.slot = (p.picks[size_t(t.unit) * size_t(p.n_picks) + j] << p.page_shift) + (k - j * per) * Sh::kTile;
+    } else {
+      t.slot = (k < st.sinks ? k : st.first + k - st.sinks) * Sh::kTile;
+    }
     const int page = paged_page(p, b, t.slot);
     if (page < 0) return t;
-    t.at = int64_t(paged_row(p, page, t.slot, g));
+    if (kCodes) t.at = int64_t(size_t(page) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride));   // (the head's block)
+    else t.at = int64_t(paged_row(p, page, t.slot, g));
     auto below = [](int n) { return n <= 0 ? 0u : n >= Sh::kTile ? (1u << Sh::kTile) - 1u : (1u << n) - 1u; };
     t.rows = (below(len - t.slot) & ~below(st.vis_begin - t.slot)) | below(st.vis_end - t.slot);
     if (p.new_k && len - 1 - t.slot < Sh::kTile) t.rows |= kFresh | uint32_t(len - 1 - t.slot) << 16;
@@ -506,6 +704,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       const uint32_t mask = __shfl_sync(0xffffffffu, now.rows, i & 31);
       rows[S - 1] = mask;
       slots[S - 1] = __shfl_sync(0xffffffffu, now.slot, i & 31);
+      if constexpr (kCodes) {   // all of the tile: what is not seen has no weight, and codes are finite
+        const int row = slots[S - 1] & ((1 << p.page_shift) - 1);
+        const unsigned char *k = reinterpret_cast<const unsigned char *>(p.k) + at, *v = reinterpret_cast<const unsigned char *>(p.v) + at;
+        const uint32_t dst = smem_u32(sm.ring[warp][i % S]);
+#pragma unroll
+        for (int c0 = 0; c0 < Sh::kCodes / 16; c0 += 32) {
+          const int c = c0 + lane;
+          cp_async16(dst + c * 16, k + row * (D / 2) + c * 16);
+          cp_async16(dst + Sh::kHalf + Sh::at_v(c), v + row * (D / 2) + c * 16);
+        }
+        const int levels = ((D / 2) << p.page_shift) + row * kLevelBytes + (lane & 3) * 16;
+        if (lane < 8) cp_async16(dst + (lane < 4 ? 0 : Sh::kHalf) + Sh::kCodes + (lane & 3) * 16, (lane < 4 ? k : v) + levels);
+        cp_async_commit();
+        return;
+      } else {
       const int unit = __shfl_sync(0xffffffffu, now.unit, i & 31);
       constexpr int kAtOnce = 32 / Sh::kChunks;   // rows that a warp fetches at once
       const int c = lane % Sh::kChunks, r0 = lane / Sh::kChunks;
@@ -536,6 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
           cp_async16(dst + Sh::kTile * Sh::kRowBytes + Sh::at(row, c), vs, seen);
         }
       }
+      }
     }
     cp_async_commit();
   };
@@ -550,6 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
   for (int s = 0; s < S; ++s) ask(s);
 
   // the new tokens' rows and places in the account (nothing below reads them: the tile takes the row from the call)
+  if constexpr (!kCodes)
   for (int u = int(blockIdx.x) * kWarps + warp; u < p.batch * p.Hkv; u += int(gridDim.x) * kWarps) {
     const int b = u / p.Hkv, g = u - b * p.Hkv, i = sm.len[b] - 1;
     if (i < 0) continue;
@@ -577,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
   for (int at = lo; at < hi;) {
     const int b = seq_of(sm.prefix, p.batch, at), n = (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv, g = (at - sm.prefix[b]) / n;
     const int t0 = sm.prefix[b] + g * n, end = min(hi, t0 + n);
-    WarpUnit<T, D, G> unit;
+    WarpUnit<C, D, G> unit;
     unit.begin(p, sm, b, g);
     float *scores = keep ? p.logits + size_t(b * p.Hkv + g) * size_t(p.most) * G : nullptr;
 #pragma unroll 1
@@ -604,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       factor = part_factor(sm.m[warp][lane], M);
     }
     unit.scale(factor);
-    constexpr int kSlots = Smem<T, D, G>::kSlots;
+    constexpr int kSlots = Smem<C, D, G>::kSlots;
     if (warp >= kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - (kWarps - kSlots)][h][c] = x; });
     __syncthreads();
     if (kSlots < kWarps) {
@@ -688,16 +903,16 @@ __global__ void __launch_bounds__(kAccountThreads) paged_account_kernel(const __
   }
 }
 
-template <typename T, int D, int G>
+template <typename C, int D, int G, bool PICKED>
 int launch(const PagedParams &p, cudaStream_t st) {
-  using Sh = Shape<T, D>;
+  using Sh = Shape<C, D>;
   // tiles that the sequences can have at most: no more CTAs than their warps can have
-  const int64_t longest = p.window < 0 ? p.most : std::min<int64_t>(p.most, int64_t(p.window) + p.n_sink + 2 * Sh::kTile);
+  const int64_t longest = PICKED ? std::min<int64_t>(p.most, int64_t(p.n_picks) << p.page_shift) : p.window < 0 ? p.most : std::min<int64_t>(p.most, int64_t(p.window) + p.n_sink + 2 * Sh::kTile);
   const int64_t tiles = (longest / Sh::kTile + 2) * p.Hkv * p.batch;
   const int units = p.batch * p.Hkv;
   int grid = int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kWarps - 1) / kWarps, p.sm_count, kMaxGrid})));
   if (units <= std::min(p.sm_count, kMaxGrid)) grid = std::max(grid, units);
-  const int rc = launch_status(launch_chained(paged_decode_kernel<T, D, G>, unsigned(grid), kThreads, sizeof(Smem<T, D, G>), st, p));
+  const int rc = launch_status(launch_chained(paged_decode_kernel<C, D, G, PICKED>, unsigned(grid), kThreads, sizeof(Smem<C, D, G>), st, p));
   if (rc || !p.weight) return rc;
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(longest / (2 * kAccountThreads), p.sm_count * 8 / units)));
   return launch_status(launch_chained(paged_account_kernel<G, Sh::kTile>, unsigned(units * parts), kAccountThreads, 0, st, p, parts, D));
@@ -710,20 +925,40 @@ size_t paged_record_bytes(const glide_paged_config &c) {
   return size_t(kMaxGrid * 2 * G * (c.head_dim + 3) + int64_t(c.max_batch) * c.n_q_heads) * sizeof(float);
 }
 
+namespace {
+
+// f(what a page holds, D, G)
+template <typename F>
+int dispatch_pages(const glide_paged *h, F &&f) {
+  if (h->codes) return dispatch_config(GLIDE_BF16, h->cfg.head_dim, h->group, [&](auto, auto d, auto g) { return f(TypeTag<Code4>{}, d, g); });
+  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, f);
+}
+template <typename C, int D, int G, bool PICKED>
+bool setup() {
+  static_assert(sizeof(Smem<C, D, G>) <= 232448, "shared memory of one CTA");
+  return cudaFuncSetAttribute(paged_decode_kernel<C, D, G, PICKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Smem<C, D, G>))) == cudaSuccess;
+}
+
+}  // namespace
+
 int setup_paged_decode(const glide_paged *h) {
-  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
-    using T = typename decltype(t)::type;
+  return dispatch_pages(h, [&](auto c, auto d, auto g) {
+    using C = typename decltype(c)::type;
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    static_assert(sizeof(Smem<T, D, G>) <= 232448, "shared memory of one CTA");
-    return cudaFuncSetAttribute(paged_decode_kernel<T, D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Smem<T, D, G>))) == cudaSuccess
-               ? int(GLIDE_OK)
-               : int(GLIDE_ERR_CUDA);
+    bool ok = setup<C, D, G, false>();
+    if constexpr (!std::is_same<C, Code4>::value) ok = ok && setup<C, D, G, true>();
+    return ok ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
 
 int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t st) {
-  return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, [&](auto t, auto d, auto g) {
-    return launch<typename decltype(t)::type, decltype(d)::value, decltype(g)::value>(p, st);
+  return dispatch_pages(h, [&](auto c, auto d, auto g) {
+    using C = typename decltype(c)::type;
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    if constexpr (!std::is_same<C, Code4>::value) {
+      if (p.picks) return launch<C, D, G, true>(p, st);
+    }
+    return launch<C, D, G, false>(p, st);
   });
 }
 

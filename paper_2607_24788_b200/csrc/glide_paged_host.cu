@@ -14,6 +14,8 @@ constexpr int64_t kMostTokens = int64_t(1) << 30;
 constexpr size_t kControlBytes = 256;
 
 size_t elem_bytes(const glide_paged_config &c) { return c.io_dtype == GLIDE_F32 ? 4 : 2; }
+bool in_codes(const glide_paged_config &c) { return c.io_dtype == GLIDE_BF16_CACHE4; }
+size_t page_elem_bytes(const glide_paged_config &c) { return in_codes(c) ? 1 : elem_bytes(c); }   // what the pages' strides count
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Checks a configuration and fills in the strides; lays out the workspace.
@@ -24,7 +26,8 @@ int plan(const glide_paged_config *in, glide_paged *h) {
       c.max_tokens > kMostTokens || c.layer_stride < 0 || c.page_stride < 0 || c.head_stride < 0 || c.row_stride < 0 ||
       (c.weights != 0 && c.weights != 1) || !(c.softmax_scale >= 0.f) || !std::isfinite(c.softmax_scale))
     return GLIDE_ERR_INVALID_ARG;
-  if (c.io_dtype != GLIDE_F32 && c.io_dtype != GLIDE_BF16) return GLIDE_ERR_UNSUPPORTED;
+  if (c.io_dtype != GLIDE_F32 && c.io_dtype != GLIDE_BF16 && !in_codes(c)) return GLIDE_ERR_UNSUPPORTED;
+  if (in_codes(c) && c.weights) return GLIDE_ERR_UNSUPPORTED;
   if ((c.head_dim != 64 && c.head_dim != 128) || c.n_q_heads % c.n_kv_heads) return GLIDE_ERR_UNSUPPORTED;
   if (int64_t(c.n_q_heads) * c.head_dim > (1 << 24)) return GLIDE_ERR_UNSUPPORTED;
   const int G = c.n_q_heads / c.n_kv_heads;
@@ -34,15 +37,21 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   if (shift > 8 || c.max_batch > kMaxPagedBatch) return GLIDE_ERR_UNSUPPORTED;
   const int64_t d = c.head_dim;
   if (!c.layer_stride && !c.page_stride && !c.head_stride && !c.row_stride) {
-    c.row_stride = d;
-    c.head_stride = d * c.page_size;
+    c.row_stride = in_codes(c) ? d / 2 + kLevelBytes : d;
+    c.head_stride = c.row_stride * c.page_size;
     c.page_stride = c.head_stride * c.n_kv_heads;
     c.layer_stride = c.page_stride * c.n_pages;
   }
-  const int64_t step = int64_t(16 / elem_bytes(c));
+  const int64_t step = int64_t(16 / page_elem_bytes(c));
   const int64_t strides[4] = {c.layer_stride, c.page_stride, c.head_stride, c.row_stride};
-  for (int64_t s : strides)
-    if (s < d || s % step || s >= (int64_t(1) << 38)) return GLIDE_ERR_INVALID_ARG;
+  if (in_codes(c)) {   // a head's block: codes, then levels
+    if (c.row_stride != d / 2 + kLevelBytes) return GLIDE_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+      if (strides[i] < c.row_stride * c.page_size || strides[i] % step || strides[i] >= (int64_t(1) << 38)) return GLIDE_ERR_INVALID_ARG;
+  } else {
+    for (int64_t s : strides)
+      if (s < d || s % step || s >= (int64_t(1) << 38)) return GLIDE_ERR_INVALID_ARG;
+  }
   if (c.layer_stride % c.page_stride) return GLIDE_ERR_INVALID_ARG;
   // page numbers and the tiles of a decode step are 32-bit numbers in the kernels
   const int64_t layer_pages = c.layer_stride / c.page_stride;
@@ -50,6 +59,7 @@ int plan(const glide_paged_config *in, glide_paged *h) {
   if ((c.max_tokens / kPagedTile + 2) * c.max_batch * c.n_kv_heads > INT32_MAX / 2) return GLIDE_ERR_UNSUPPORTED;
   if (c.softmax_scale == 0.f) c.softmax_scale = 1.0f / std::sqrt(float(d));
   h->cfg = c;
+  h->codes = in_codes(c);
   h->group = G;
   h->page_shift = shift;
   h->layer_pages = layer_pages;
@@ -113,8 +123,9 @@ int params_of(const glide_paged *h, const glide_paged_call *a, int need, PagedPa
   p.n_sink = int32_t(std::min<int64_t>(a->n_sink, kMostTokens));
   p.scale_log2 = c.softmax_scale * 1.4426950408889634f;
   p.page0 = int32_t(h->layer_pages * a->layer);
-  p.k = h->k + size_t(a->layer) * size_t(c.layer_stride) * size_t(e);
-  p.v = h->v + size_t(a->layer) * size_t(c.layer_stride) * size_t(e);
+  p.k = h->k + size_t(a->layer) * size_t(c.layer_stride) * page_elem_bytes(c);
+  p.v = h->v + size_t(a->layer) * size_t(c.layer_stride) * page_elem_bytes(c);
+  p.n_cols = a->table_cols;
   p.page_stride = c.page_stride;
   p.head_stride = c.head_stride;
   p.row_stride = c.row_stride;
@@ -133,6 +144,13 @@ int params_of(const glide_paged *h, const glide_paged_call *a, int need, PagedPa
 }
 
 cudaStream_t as_stream(void *s) { return static_cast<cudaStream_t>(s); }
+
+// ... of calls over rows of new tokens, of starts or (without them) one for each sequence
+int rows_of_call(const glide_paged *h, const glide_paged_call *a, PagedParams *out) {
+  const int rc = params_of(h, a, a && a->dev_starts ? kNeedStarts : 0, out);
+  if (!rc && !out->starts) out->n_tokens = out->batch;
+  return rc;
+}
 
 }  // namespace
 
@@ -165,7 +183,7 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
   h->v = static_cast<unsigned char *>(dev_v_pages);
   bool ok = cudaGetDevice(&h->device) == cudaSuccess &&
             cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device) == cudaSuccess;
-  if (ok && h->cfg.io_dtype == GLIDE_BF16) {
+  if (ok && h->cfg.io_dtype != GLIDE_F32) {
     void *f = nullptr;
     cudaDriverEntryPointQueryResult found;
     ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) == cudaSuccess && f &&
@@ -173,11 +191,11 @@ int glide_paged_create(const glide_paged_config *cfg, void *dev_k_pages, void *d
     if (ok) {
       h->encode = f;
       const auto fn = reinterpret_cast<TensorMapEncoder>(f);
-      ok = encode_pages(fn, &h->kpage, h, h->k) && encode_pages(fn, &h->vpage, h, h->v) && setup_paged_tc(h) == GLIDE_OK;
+      ok = (h->codes || (encode_pages(fn, &h->kpage, h, h->k) && encode_pages(fn, &h->vpage, h, h->v))) && setup_paged_tc(h) == GLIDE_OK;
     }
   }
   if (ok && h->cfg.io_dtype == GLIDE_F32) ok = setup_paged_fma(h) == GLIDE_OK;
-  ok = ok && setup_paged_decode(h) == GLIDE_OK && setup_paged_evict(h) == GLIDE_OK && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess &&
+  ok = ok && setup_paged_decode(h) == GLIDE_OK && (h->codes || setup_paged_evict(h) == GLIDE_OK) && cudaMemsetAsync(h->ws, 0, h->off_records, as_stream(stream)) == cudaSuccess &&
        cudaStreamSynchronize(as_stream(stream)) == cudaSuccess;   // (so that the first call may be on any stream)
   if (!ok) {
     cudaGetLastError();
@@ -205,11 +223,11 @@ int glide_paged_prefill(glide_paged *h, const glide_paged_call *call, const void
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
   const std::lock_guard<std::mutex> together(h->launching);
   if (dev_k || p.weight || p.pos) {
-    const int r = launch_paged_store(h, p, as_stream(stream));
+    const int r = h->codes ? launch_paged_append(h, p, PagedAppend{}, as_stream(stream)) : launch_paged_store(h, p, as_stream(stream));
     if (r) return r;
   }
   if (!dev_out) return GLIDE_OK;
-  return h->cfg.io_dtype == GLIDE_BF16 ? launch_paged_prefill_tc(h, p, as_stream(stream)) : launch_paged_prefill_fma(h, p, as_stream(stream));
+  return h->cfg.io_dtype != GLIDE_F32 ? launch_paged_prefill_tc(h, p, as_stream(stream)) : launch_paged_prefill_fma(h, p, as_stream(stream));
 }
 
 int glide_paged_decode(glide_paged *h, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
@@ -220,16 +238,88 @@ int glide_paged_decode(glide_paged *h, const glide_paged_call *call, const void 
   if ((!dev_k) != (!dev_v) || !dev_q || !dev_out || misaligned(dev_q) || misaligned(dev_k) || misaligned(dev_v) ||
       misaligned(dev_out) || (reinterpret_cast<uintptr_t>(dev_lse) & 3u))
     return GLIDE_ERR_INVALID_ARG;
-  if (p.weight && !h->cfg.weights) return GLIDE_ERR_UNSUPPORTED;
+  if (p.weight && !h->cfg.weights) return GLIDE_ERR_UNSUPPORTED;   // (as of all handles in 4 bits)
   p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
   const std::lock_guard<std::mutex> together(h->launching);
+  if (h->codes && (dev_k || p.pos)) {   // (the steps' kernel takes rows in 4 bits from the pages)
+    PagedParams a = p;
+    a.starts = nullptr, a.n_tokens = p.batch, a.q = nullptr;
+    const int r = launch_paged_append(h, a, PagedAppend{}, as_stream(stream));
+    if (r) return r;
+    p.new_k = p.new_v = nullptr, p.pos = nullptr;
+  }
   return launch_paged_decode(h, p, as_stream(stream));
+}
+
+int glide_paged_append(glide_paged *h, const glide_paged_call *call, const glide_rotation *rotation, const void *dev_q, const void *dev_k,
+                       const void *dev_v, void *dev_q_out, void *stream) {
+  PagedParams p;
+  const int rc = rows_of_call(h, call, &p);
+  if (rc) return rc;
+  PagedAppend a{};
+  if (rotation) {
+    const glide_rotation &r = *rotation;
+    a.cos = r.dev_cos, a.sin = r.dev_sin, a.n_positions = r.n_positions, a.stride = r.stride ? r.stride : r.rot_dim / 2;
+    a.rot_dim = r.rot_dim, a.neighbours = r.neighbours;
+    if (!a.cos || !a.sin || misaligned(a.cos) || misaligned(a.sin) || a.n_positions < 1 || a.rot_dim < 16 || a.rot_dim % 16 ||
+        a.rot_dim > h->cfg.head_dim || a.stride < a.rot_dim / 2 || a.stride % 4 || (a.neighbours != 0 && a.neighbours != 1))
+      return GLIDE_ERR_INVALID_ARG;
+  }
+  if (p.n_tokens == 0) return GLIDE_OK;
+  if (!dev_k || !dev_v || (!dev_q) != (!dev_q_out) || (dev_q && dev_q == dev_q_out && p.q_stride != p.out_stride) || misaligned(dev_q) ||
+      misaligned(dev_k) || misaligned(dev_v) || misaligned(dev_q_out))
+    return GLIDE_ERR_INVALID_ARG;
+  p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v;
+  a.q_out = dev_q_out;
+  const std::lock_guard<std::mutex> together(h->launching);
+  return launch_paged_append(h, p, a, as_stream(stream));
+}
+
+int glide_paged_read(glide_paged *h, const glide_paged_call *call, void *dev_k, void *dev_v, void *stream) {
+  PagedParams p;
+  const int rc = rows_of_call(h, call, &p);
+  if (rc) return rc;
+  if (p.n_tokens == 0) return GLIDE_OK;
+  if (!dev_k || !dev_v || misaligned(dev_k) || misaligned(dev_v)) return GLIDE_ERR_INVALID_ARG;
+  const std::lock_guard<std::mutex> together(h->launching);
+  return launch_paged_read(h, p, dev_k, dev_v, as_stream(stream));
+}
+
+int glide_paged_bounds(glide_paged *h, const glide_paged_call *call, void *dev_bounds, void *stream) {
+  PagedParams p;
+  const int rc = rows_of_call(h, call, &p);
+  if (rc) return rc;
+  if (h->codes) return GLIDE_ERR_UNSUPPORTED;
+  if (!dev_bounds || misaligned(dev_bounds)) return GLIDE_ERR_INVALID_ARG;
+  if (p.n_tokens == 0) return GLIDE_OK;
+  const std::lock_guard<std::mutex> together(h->launching);
+  return launch_paged_bounds(h, p, dev_bounds, as_stream(stream));
+}
+
+int glide_paged_decode_sparse(glide_paged *h, const glide_paged_call *call, const void *dev_q, const void *dev_k, const void *dev_v,
+                              void *dev_out, float *dev_lse, void *dev_bounds, int32_t n_picks, int32_t *dev_picks, double *dev_scores,
+                              void *stream) {
+  PagedParams p;
+  const int rc = params_of(h, call, 0, &p);
+  if (rc) return rc;
+  if (h->codes || p.weight) return GLIDE_ERR_UNSUPPORTED;
+  if ((!dev_k) != (!dev_v) || !dev_q || !dev_out || misaligned(dev_q) || misaligned(dev_k) || misaligned(dev_v) || misaligned(dev_out) ||
+      (reinterpret_cast<uintptr_t>(dev_lse) & 3u) || !dev_bounds || misaligned(dev_bounds) || !dev_picks ||
+      (reinterpret_cast<uintptr_t>(dev_picks) & 3u) || !dev_scores || (reinterpret_cast<uintptr_t>(dev_scores) & 7u) || p.window >= 0 ||
+      n_picks < 1 || ((int64_t(p.n_sink) + h->cfg.page_size - 1) >> h->page_shift) + 1 > n_picks)
+    return GLIDE_ERR_INVALID_ARG;
+  p.q = dev_q, p.new_k = dev_k, p.new_v = dev_v, p.out = dev_out, p.lse = dev_lse;
+  p.n_picks = n_picks, p.picks = dev_picks;
+  const std::lock_guard<std::mutex> together(h->launching);
+  const int r = launch_paged_select(h, p, dev_bounds, dev_picks, dev_scores, as_stream(stream));
+  return r ? r : launch_paged_decode(h, p, as_stream(stream));
 }
 
 int glide_paged_weights(glide_paged *h, const glide_paged_call *call, const void *dev_q, const float *dev_lse, void *stream) {
   PagedParams p;
   const int rc = params_of(h, call, kNeedStarts, &p);
   if (rc) return rc;
+  if (h->codes) return GLIDE_ERR_UNSUPPORTED;
   if (!p.weight) return GLIDE_ERR_INVALID_ARG;
   if (p.n_tokens == 0) return GLIDE_OK;   // (tensors without a row may have no address)
   if (!dev_q || misaligned(dev_q) || !dev_lse || (reinterpret_cast<uintptr_t>(dev_lse) & 3u)) return GLIDE_ERR_INVALID_ARG;

@@ -2,6 +2,8 @@
 // for which it is the slow way round: a row of 20000 slots takes 2.5 ms in bf16 (D = 128), 3.2 in fp32.  (Slot by slot 7.6.)
 #pragma once
 
+#include <type_traits>
+
 #include "glide_device.cuh"
 #include "glide_paged.h"
 
@@ -13,9 +15,10 @@ __device__ __forceinline__ void paged_ranges(const PagedParams &p, int i, int &f
   first = min(min(p.n_sink, second), i + 1);
 }
 
-// G query heads from head0 on, which read KV head g
-template <typename T, int D, int G>
+// G query heads from head0 on, which read KV head g; C: what the pages hold
+template <typename C, int D, int G>
 struct PagedRow {
+  using T = Io<C>;
   static constexpr int E = D / 32;
   float q[G][E], m[G], l[G], acc[G][E];
   __device__ __forceinline__ void load_q(const PagedParams &p, size_t row, int head0) {
@@ -28,19 +31,41 @@ struct PagedRow {
       m[h] = -CUDART_INF_F, l[h] = 0.f;
     }
   }
+  // Where a slot's row is.  Rows in 4 bits: the head's block (bytes) and the slot's number in its page, 8 bits.
+  static __device__ __forceinline__ size_t place_of(const PagedParams &p, int page, int slot, int g) {
+    if constexpr (std::is_same<C, Code4>::value) {
+      const size_t block = page < 0 ? 0 : size_t(page) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride);
+      return block << 8 | size_t(slot & ((1 << p.page_shift) - 1));
+    } else {
+      return paged_row(p, page, slot, g);
+    }
+  }
+  static __device__ __forceinline__ void load_row(const PagedParams &p, const void *pages, size_t place, float (&x)[E]) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (std::is_same<C, Code4>::value) {
+      const int off = int(place & 255u);
+      const unsigned char *block = reinterpret_cast<const unsigned char *>(pages) + (place >> 8);
+      const uint32_t levels = *reinterpret_cast<const uint32_t *>(block + ((D / 2) << p.page_shift) + off * kLevelBytes);
+      const unsigned char *codes = block + off * (D / 2) + lane * (E / 2);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        x[e] = fmaf(float((codes[e / 2] >> (4 * (e & 1))) & 15), __uint_as_float(levels << 16), __uint_as_float(levels & 0xffff0000u));
+    } else {
+      load_elems<T, E>(reinterpret_cast<const T *>(pages) + place + lane * E, x);
+    }
+  }
   // n <= 32 slots, of which lane i has the i-th one's place: kAtOnce at a time.  (8: no faster in bf16, and the kernels that call this
   // keep more registers free for it: 8 prompts of up to 2048 tokens 170 us instead of 155.)
   static constexpr int kAtOnce = 4;
   __device__ __forceinline__ void slots(const PagedParams &p, size_t place, int n) {
-    const int lane = threadIdx.x & 31;
 #pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += kAtOnce) {
       float k[kAtOnce][E], v[kAtOnce][E];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const size_t at = __shfl_sync(0xffffffffu, place, min(i0 + i, n - 1)) + lane * E;   // (no branch, so that the loads go out together)
-        load_elems<T, E>(reinterpret_cast<const T *>(p.k) + at, k[i]);
-        load_elems<T, E>(reinterpret_cast<const T *>(p.v) + at, v[i]);
+        const size_t at = __shfl_sync(0xffffffffu, place, min(i0 + i, n - 1));   // (no branch, so that the loads go out together)
+        load_row(p, p.k, at, k[i]);
+        load_row(p, p.v, at, v[i]);
       }
 #pragma unroll
       for (int h = 0; h < G; ++h) {
@@ -93,13 +118,13 @@ struct PagedRow {
     paged_ranges(p, i, first, second);
     const int lane = threadIdx.x & 31;
     auto run = [&](int j, int end) {
-      auto place_of = [&](int at) { return at < end ? paged_row(p, paged_page(p, b, at), at, g) : size_t(0); };
-      size_t next = place_of(j + lane);
+      auto place = [&](int at) { return at < end ? place_of(p, paged_page(p, b, at), at, g) : size_t(0); };
+      size_t next = place(j + lane);
 #pragma unroll 1
       for (; j < end; j += 32) {
-        const size_t place = next;
-        next = place_of(j + 32 + lane);   // (on its way while these are gone through)
-        slots(p, place, min(32, end - j));
+        const size_t here = next;
+        next = place(j + 32 + lane);   // (on its way while these are gone through)
+        slots(p, here, min(32, end - j));
         if (moves && lane == 0) atomicAdd(moves, 1u);
       }
     };
@@ -114,9 +139,9 @@ struct PagedRow {
 };
 
 // (a call, so that the kernels' own loops are laid out without it)
-template <typename T, int D>
+template <typename C, int D>
 __device__ __noinline__ void paged_row_alone(const PagedParams &p, size_t row, int b, int i, int g, int head, bool with_lse, uint32_t *moves) {
-  PagedRow<T, D, 1> one;
+  PagedRow<C, D, 1> one;
   one.attend(p, row, b, i, g, head, with_lse, moves);
 }
 

@@ -8,13 +8,17 @@
 //   warps 4-7, 12-15   softmax of tile B
 //   warps 16, 17       issue the tcgen05.mma of A and of B (one elected lane), in turns
 //   warp 18            draws and finds the work, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
-// Keys come in tiles of 128 slots (multiples of 128): those that hold a visible first token, then those of the window.  Per tile and
-// row tile S = Q K^T into TMEM, the weights P = 2^(s - m) as bf16 over the consumed S columns against a reference m that moves (and O
-// with it) only when the row's maximum grows by more than 2^32, O += P V with V as the MN-major B operand.
-// TMEM columns: S_A [0,128) S_B [128,256) O_A [256,256+d) O_B behind it.
-// Nothing that a row does not see reaches it: scores are selected, not added to; slots behind the CTA's last token are zeros in V's
-// buffer; and a row whose output is not finite all the same (0 times an infinity or a NaN of a masked slot before them) is computed
-// once more by itself, from the slots that it sees.
+//   warps 19-22        (pages in 4 bits) make tiles of the codes and levels that warp 18 has loaded into a small ring of their own, a piece
+//                      per page; slots that nobody sees are 0
+// Pages in 4 bits.  A key is mid + step n with mid = low + 8 step and n = code - 8, -8 .. 7, three bits and a sign: step n is a number of 11
+// bits, which fp16 has.  So S = sum q (step n) + mid sum q is computed as it stands: both as fp16 operands, the second term as four more
+// columns of the product, (hi, lo) of mid against (hi, lo) of sum q.  fp16 is short of exponents, so a key tile is scaled by a power of two
+// to below 2^-6, a query row by the threads that it belongs to, to below 2^7, and the scores are scaled back where they are multiplied by the
+// softmax scale anyway.  (Exact for rows whose step is 2^-8 of the tile's largest or more, others are off by 2^-19 of the tile's largest key at
+// most.  Keys rounded to bf16 put scores off by 0.005, outputs by 0.006 of their norm.)  A value is rounded to bf16 once, like the weights: off by
+// at most 2^-8 of itself.  Both come out of one fused multiply-add for two codes where they lie in the word: four bits at the bottom of
+// an fp16 or bf16 number are code times its least subnormal number, the next four 16 times that.  Which leaves the features of eight in the
+// order 0 4 1 5 2 6 3 7, in keys, values, and so in Q and O.
 // Every mbarrier wait is bounded; on a time-out the CTA records kDevWaitTimeout, leaves its loops, frees its TMEM columns and returns.
 #include <algorithm>
 #include <cstring>
@@ -35,6 +39,8 @@ constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
 constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
+constexpr int kUnpackWarps = 4, kRawStages = 2;   // pages in 4 bits
+constexpr int kCodeThreads = 768;                 // (whole warpgroups, which give each other registers)
 // How far (in the exponent) scores may exceed a row's reference before it moves.  Weights, sums and O are floating numbers: the reference only
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
 // pass over the tile: 8 sequences of up to 2048 tokens, windows of 256 with 4 first tokens 228 us with 8, 169 with 32, 171 with 64.
@@ -50,13 +56,21 @@ struct Work {
   int seq, tok0, g, part, len, n_new, row0;
 };
 
-template <int D>
+template <int D, bool CODES>
 struct PrefillSmem {
   static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
-  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kStages = CODES ? (D == 128 ? 4 : 6) : D == 128 ? 5 : 8;
+  static constexpr int kRaw = CODES ? kRawStages : 1, kRawBytes = CODES ? kKT * (D / 2 + kLevelBytes) : 16;
   unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
   unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
-  uint64_t bar_full[kStages];            // the buffer's K or V tile has landed
+  alignas(16) unsigned char raw[kRaw][kRawBytes];   // pages in 4 bits: the tiles' codes, then levels
+  uint64_t bar_raw[kRaw], bar_rawfree[kRaw];        // they have landed; the unpacking warps have read them
+  uint32_t raw_pieces[kRaw];             // bit i: piece i of the tile has been loaded
+  // the four further columns of Q_A, Q_B and of the key tiles, 16 bytes a row (a key tile's as long as its buffer), and the zeros that make them 16
+  alignas(128) unsigned char more_q[CODES ? 2 : 1][CODES ? kRows * 16 : 16], more_k[CODES ? kStages / 2 : 1][CODES ? kKT * 16 : 16], zeros[CODES ? kRows * 16 : 16];
+  float k_scale[4];                      // what the last key tiles have been divided by (read until the row tiles have the next one's scores)
+  uint64_t bar_qmade[2];                 // Q_X is in fp16 (one arrival per warp)
+  uint64_t bar_full[kStages];            // the buffer's K or V tile has landed (pages in 4 bits: has been made, one arrival per warp)
   uint64_t bar_free[kStages];            // the MMAs that read the buffer have completed (one arrival per row tile)
   uint64_t bar_q[2];                     // Q_X staged
   uint64_t bar_s[2];                     // MMA -> softmax threads of X: the products issued for X so far have completed
@@ -77,13 +91,13 @@ __device__ __forceinline__ uint32_t sw128(int row, int c16) {
   return uint32_t((c16 >> 3) * kBoxBytes + row * 128 + (((c16 & 7) ^ (row & 7)) << 4));
 }
 // instruction descriptor: fp32 accumulate, bf16 A and B, M = 128; b_mn: B is MN-major
-__device__ __forceinline__ uint32_t make_idesc(int n, bool b_mn) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? (1u << 16) : 0u) | (uint32_t(n >> 3) << 17) | ((128u >> 4) << 24);
+__device__ __forceinline__ uint32_t make_idesc(int n, bool b_mn, bool f16 = false) {   // (f16: A and B)
+  return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn ? (1u << 16) : 0u) | (uint32_t(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 // S = A B^T, 128 x 128 x D, both K-major tiles; called by the whole warp with uniform operands, one lane issues
-template <int D>
+template <int D, bool F16 = false>
 __device__ __forceinline__ void issue_scores(bool leader, uint32_t tmem_d, uint32_t a_tile, uint32_t b_tile) {
-  const uint32_t idesc = make_idesc(128, false), a0 = desc_lo(a_tile, 16), b0 = desc_lo(b_tile, 16);
+  const uint32_t idesc = make_idesc(128, false, F16), a0 = desc_lo(a_tile, 16), b0 = desc_lo(b_tile, 16);
   if (leader) {
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
@@ -95,6 +109,17 @@ __device__ __forceinline__ void issue_scores(bool leader, uint32_t tmem_d, uint3
           : "memory");
     }
   }
+}
+// S += the four further columns: 16-byte rows, eight to a core matrix, without swizzle; the other half of the 16 columns is the zeros
+__device__ __forceinline__ void issue_more(bool leader, uint32_t tmem_d, uint32_t a_rows, uint32_t b_rows, uint32_t zeros) {
+  constexpr uint32_t kHi = (128u >> 4) | (1u << 14);
+  const uint32_t idesc = make_idesc(128, false, true), a = desc_lo(a_rows, zeros - a_rows), b = desc_lo(b_rows, zeros - b_rows);
+  if (leader)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(tmem_d),
+        "r"(a), "r"(b), "r"(idesc), "r"(1u), "r"(kHi)
+        : "memory");
 }
 // O (+)= P V, 128 x D x 128: P in TMEM (32-bit column c = elements 2c, 2c + 1; elements 64 .. from column 64 on), V MN-major
 template <int D>
@@ -205,10 +230,90 @@ __device__ __forceinline__ Work find_tile(const PagedParams &p, int want, int to
   return w;
 }
 
-template <int D, int G, bool LSE>
-__global__ void __launch_bounds__(kThreads, 1)
+constexpr float kValueScale = 0x1p-40f;   // of pages in 4 bits: values in the tiles are 2^-40 of what they are, so that 2^133 steps are bf16 numbers
+constexpr float kMoreScale = 0x1p10f;     // mid is 2^10 times as large as its tile would have it, sum q as much smaller: neither's low part falls below fp16
+
+// A power of two that brings x (not negative) into [2^e, 2^(e + 1)), as far as there is one, and what undoes it
+__device__ __forceinline__ float scale_to(float x, int e, float &undo) {
+  const int field = x > 0.f && isfinite(x) ? min(max(254 + e - int(__float_as_uint(x) >> 23), 1), 253) : 127;
+  undo = __uint_as_float(uint32_t(254 - field) << 23);
+  return __uint_as_float(uint32_t(field) << 23);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// x as fp16 pairs (hi, lo) and what the columns of a product that makes (a hi + a lo) (b hi + b lo) need: {hi, lo, hi, lo} or {hi, hi, lo, lo}
+__device__ __forceinline__ uint4 more_columns(float x, bool keys) {
+  const uint32_t hi = pack_f16x2(x, 0.f) & 0xffffu;
+  float back;
+  asm("{\n\t.reg .b16 h, z;\n\tmov.b32 {h, z}, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(back) : "r"(hi));
+  const uint32_t lo = pack_f16x2(x - back, 0.f) & 0xffffu;
+  return keys ? make_uint4(hi | lo << 16, hi | lo << 16, 0u, 0u) : make_uint4(hi | hi << 16, lo | lo << 16, 0u, 0u);
+}
+
+// A tile of codes and levels becomes a tile of rows, 128-byte swizzle: keys as fp16, step n, with mid in more columns, both times a power
+// of two of the tile; values as bf16.  Rows at or behind `rows` and those of pieces (of 2^piece_shift rows) that have not been loaded are 0.
+// A thread has 32 features of a row at a time; the threads of a quarter warp read and write different banks.
+template <int D, bool KEYS>
+__device__ __forceinline__ void unpack_tile(unsigned char *tile, unsigned char *more, float *k_scale, const unsigned char *raw, uint32_t pieces, int piece_shift,
+                                            int rows) {
+  constexpr int kLanes = D / 32, kAtOnce = 32 / kLanes * kUnpackWarps;   // threads of a row; rows at once
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kLoadWarp - 1;
+  const int c = lane % kLanes, r0 = warp * (32 / kLanes) + lane / kLanes;
+  auto there = [&](int row) { return row < rows && (pieces >> (row >> piece_shift)) & 1u; };
+  auto levels_of = [&](int row) { return there(row) ? *reinterpret_cast<const uint32_t *>(raw + kKT * (D / 2) + row * kLevelBytes) : 0u; };
+  float scale = 1.f;
+  if (KEYS) {   // (every warp looks at all levels)
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < kKT / 32; ++i) {
+      const uint32_t levels = levels_of(i * 32 + lane);
+      const float low = bf16_hi(levels), x = fmaxf(fabsf(low), fabsf(fmaf(15.f, bf16_lo(levels), low)));   // (a step is 2 / 15 of it at most)
+      if (isfinite(x)) top = max(top, __float_as_uint(x));
+    }
+    float undo;
+    scale = scale_to(__uint_as_float(__reduce_max_sync(0xffffffffu, top)), -7, undo);
+    if (warp == 0 && lane == 0) *k_scale = undo;
+  }
+#pragma unroll
+  for (int i = 0; i < kKT / kAtOnce; ++i) {
+    const int row = r0 + i * kAtOnce;
+    uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t levels = levels_of(row);
+    if (there(row)) codes = *reinterpret_cast<const uint4 *>(raw + row * (D / 2) + c * 16);
+    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint32_t step0, step1, add;   // for codes in the lowest four bits; in the next four; what is added
+    if (KEYS) {
+      const float s = bf16_lo(levels) * scale;
+      step0 = pack_f16x2(s * 0x1p24f, s * 0x1p24f), step1 = pack_f16x2(s * 0x1p20f, s * 0x1p20f), add = pack_f16x2(s * -8.f, s * -8.f);
+      if (c == 0) *reinterpret_cast<uint4 *>(more + row * 16) = more_columns(fmaf(8.f, bf16_lo(levels), bf16_hi(levels)) * (scale * kMoreScale), true);
+    } else {
+      const float s = bf16_lo(levels) * kValueScale, low = bf16_hi(levels) * kValueScale;
+      step0 = pack_bf16x2(s * 0x1p66f * 0x1p67f, s * 0x1p66f * 0x1p67f), step1 = pack_bf16x2(s * 0x1p64f * 0x1p65f, s * 0x1p64f * 0x1p65f), add = pack_bf16x2(low, low);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {   // (piece j, or j ^ 2 in every other half row: a quarter warp's pieces in different banks)
+      const uint32_t word = D == 128 ? (c & 2 ? w[j ^ 2] : w[j]) : w[j];
+      uint32_t v[4];   // features 0, 4, 1, 5, 2, 6, 3, 7 of eight
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const uint32_t x = (n & 2 ? word >> 8 : word) & (n & 1 ? 0x00f000f0u : 0x000f000fu);
+        if (KEYS) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[n]) : "r"(x), "r"(n & 1 ? step1 : step0), "r"(add));
+        else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[n]) : "r"(x), "r"(n & 1 ? step1 : step0), "r"(add));
+      }
+      *reinterpret_cast<uint4 *>(tile + sw128(row, c * 4 + (j ^ (c & 2)))) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+  }
+}
+
+template <int D, int G, bool LSE, bool CODES>
+__global__ void __launch_bounds__(CODES ? kCodeThreads : kThreads, 1)
 paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps maps, int none, int parts) {
-  using Sm = PrefillSmem<D>;
+  using Sm = PrefillSmem<D, CODES>;
+  using C = std::conditional_t<CODES, Code4, bf16>;
+  constexpr int R = Sm::kRaw;
   constexpr int TOKT = kRows / G, TOKC = 2 * TOKT, S = Sm::kStages, kHalf = D / 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
@@ -217,7 +322,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   const volatile uint32_t *moves = &sm.moves;
   const bool aligned = (smem_u32(smem_raw) & 1023u) == 0;   // (the swizzled tiles have to start on a multiple of 1024)
   if (warp == kLoadWarp && lane == 0) {
-    for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), 1), mbar_init(smem_u32(&sm.bar_free[s]), 2);
+    for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), CODES ? kUnpackWarps : 1), mbar_init(smem_u32(&sm.bar_free[s]), 2);
+    if (CODES)
+      for (int s = 0; s < R; ++s) {
+        mbar_init(smem_u32(&sm.bar_raw[s]), 1), mbar_init(smem_u32(&sm.bar_rawfree[s]), kUnpackWarps);
+        mbar_init(smem_u32(&sm.bar_qmade[s]), kSoftmaxThreads / 32 / 2);
+      }
     for (int x = 0; x < 2; ++x) {
       mbar_init(smem_u32(&sm.bar_q[x]), 1);
       mbar_init(smem_u32(&sm.bar_qfree[x]), kSoftmaxThreads / 32 / 2);
@@ -225,7 +335,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       mbar_init(smem_u32(&sm.bar_turn[x]), 1);
       mbar_init(smem_u32(&sm.bar_p[x]), kSoftmaxThreads / 32 / 2);
       mbar_init(smem_u32(&sm.bar_work[x]), 1);
-      mbar_init(smem_u32(&sm.bar_workfree[x]), kLoadWarp);
+      mbar_init(smem_u32(&sm.bar_workfree[x]), kLoadWarp + (CODES ? kUnpackWarps : 0));
     }
     mbar_init(smem_u32(&sm.bar_tail), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -235,6 +345,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (CODES && tid < kRows) *reinterpret_cast<uint4 *>(sm.zeros + tid * 16) = make_uint4(0u, 0u, 0u, 0u);
+  if (CODES) fence_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -281,6 +393,11 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     return k;
   };
 
+  // 768 threads are launched with 80 registers each: the softmax threads (512) get 96, the others (256) keep 48, as many in all
+  if (CODES) {
+    if (tid < kSoftmaxThreads) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+  }
   if (!aligned) {
     // (nothing is in flight; the status word tells)
   } else if (tid < kSoftmaxThreads) {
@@ -336,6 +453,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         tmem_st32(tO + c0, r);
       }
     };
+    float scale = p.scale_log2;                     // from S to exponents
     float top_w = 0.f;                              // largest weight of the last tile that soft_tile has taken
     // Weights beyond 2^32: the reference catches up with them (a power of two, so that nothing is rounded) before it moves on, or what a
     // row has gathered would be multiplied by a factor below the least number.  Returns the factor.
@@ -348,14 +466,14 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     // the lazy reference for a tile whose largest score over this thread's columns is mx; returns what the weights are taken against
     auto move_ref = [&](float mx, bool first) {
       auto grows = [&]() {
-        const float ms = mx * p.scale_log2;
+        const float ms = mx * scale;
         return ms > m_ref + kLazy || (m_ref == -CUDART_INF_F && ms > -CUDART_INF_F);
       };
       if (pair_any(grows() || top_w >= kMostWeight)) {
         mx = row_max_of(mx);
         float f = catch_up(row_max_of(top_w));
         if (grows()) {
-          mx *= p.scale_log2;
+          mx *= scale;
           f *= m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
           m_ref = mx;
         }
@@ -365,6 +483,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
       return m_ref == -CUDART_INF_F ? 0.f : m_ref;
     };
+    // where feature i of eight stands in O
+    auto in_order = [](int i) { return CODES ? (i & 3) * 2 + (i >> 2) : i; };
     struct Bounds {
       int lo, hi, sink;   // of this thread's 64 columns, those lo .. hi and 0 .. sink are seen
     };
@@ -390,7 +510,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float a0, a1;
-          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
+          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), scale, -mr);
           a0 = ex2(a0), a1 = ex2(a1);
           if (LSE) add2(ex0, ex1, a0, a1);
           pk[e] = pack_bf16x2(a0, a1);
@@ -438,7 +558,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float a0, a1;
-          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), p.scale_log2, -mr);
+          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), scale, -mr);
           a0 = ex2(a0), a1 = ex2(a1);
           if (LSE) add2(ex0, ex1, a0, a1);
           pk[e] = pack_bf16x2(a0, a1);
@@ -457,6 +577,36 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       if (ntokX == 0) continue;
       const int mine = x_q0(X) + tok_r;             // this row's slot
       m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f, top_w = 0.f;
+      float q_undo = 1.f;
+      if (CODES && n_tiles) {                       // Q to fp16, where it lies; of a row its sum too
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));
+        constexpr int kChunks = kHalf / 8;
+        float top = 0.f, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4 *>(sm.q[X] + sw128(row, H * kChunks + i));
+          const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            top = fmaxf(top, fmaxf(fabsf(bf16_lo(w4[e])), fabsf(bf16_hi(w4[e]))));
+            sum += bf16_lo(w4[e]) + bf16_hi(w4[e]);
+          }
+        }
+        const float f = scale_to(row_max_of(top), 6, q_undo);
+        sum = row_sum_of(sum);
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          uint4 *at = reinterpret_cast<uint4 *>(sm.q[X] + sw128(row, H * kChunks + i));
+          const uint4 v = *at;
+          *at = make_uint4(pack_f16x2(bf16_lo(v.x) * f, bf16_lo(v.z) * f), pack_f16x2(bf16_hi(v.x) * f, bf16_hi(v.z) * f),   // (in the keys' order)
+                           pack_f16x2(bf16_lo(v.y) * f, bf16_lo(v.w) * f), pack_f16x2(bf16_hi(v.y) * f, bf16_hi(v.w) * f));
+        }
+        if (H == 0) *reinterpret_cast<uint4 *>(sm.more_q[X] + row * 16) = more_columns(sum * (f / kMoreScale), false);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.bar_qmade[X]));
+        q_undo *= p.scale_log2;
+      }
       const int w = p.window < 0 ? kMostSlots : p.window;
       int before = -1;                              // the key tile that this row tile had before
       for (int k = 0; k < n_tiles; ++k) {
@@ -467,6 +617,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * k) % S]));
           if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * before + 1) % S]));
         }
+        if (CODES) scale = q_undo * *const_cast<volatile float *>(&sm.k_scale[((jobs >> 1) + k) & 3]);
         const int j0 = kt.slot(k);
         const bool whole = j0 + kKT - 1 <= x_q0(X) && (j0 > x_q1(X) - w || j0 + kKT <= p.n_sink);
         const int c0 = j0 + H * 64;
@@ -484,26 +635,27 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       const float l_row = row_sum_of(l_sum);
       const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
-      else if (n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));   // (Q, which no product has waited for)
+      else if (!CODES && n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));   // (Q, which no product has waited for)
       n_q += n_tiles != 0;
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
       if (parts > 1) {
         const float f = catch_up(row_max_of(top_w));   // (records are added up against the largest of their references)
+        const float fo = CODES ? f / kValueScale : f;
         float *rec = split_record(p, D, part, out_row, g * G + row % G);
 #pragma unroll 1
         for (int c0 = 0; c0 < kHalf && before >= 0; c0 += 32) {
           uint32_t r[32];
           tmem_ld32(tO + c0, r);
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            if (live && ok)
-              *reinterpret_cast<float4 *>(rec + H * kHalf + c0 + i) = make_float4(__uint_as_float(r[i]) * f, __uint_as_float(r[i + 1]) * f,
-                                                                                  __uint_as_float(r[i + 2]) * f, __uint_as_float(r[i + 3]) * f);
+          for (int i = 0; i < 32; i += 4) {
+            auto o = [&](int n) { return __uint_as_float(r[(i & ~7) + in_order((i & 7) + n)]) * fo; };
+            if (live && ok) *reinterpret_cast<float4 *>(rec + H * kHalf + c0 + i) = make_float4(o(0), o(1), o(2), o(3));
+          }
         }
         if (H == 0 && live && ok) *reinterpret_cast<float4 *>(rec + D) = make_float4(m_ref, l_row * f, x_row * f, 0.f);
       } else {
-      const float inv = live && before >= 0 && l_row != 0.f ? 1.0f / l_row : 0.f;
+      const float inv = live && before >= 0 && l_row != 0.f ? (CODES ? 1.0f / kValueScale : 1.0f) / l_row : 0.f;
       float chk0 = 0.f, chk1 = 0.f;                 // finite if all values of the row are
 #pragma unroll 1
       for (int c0 = 0; c0 < kHalf; c0 += 32) {
@@ -521,7 +673,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           uint32_t pk[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            pk[e] = pack_bf16x2(__uint_as_float(r[q4 * 8 + e * 2]) * inv, __uint_as_float(r[q4 * 8 + e * 2 + 1]) * inv);
+            pk[e] = pack_bf16x2(__uint_as_float(r[q4 * 8 + in_order(e * 2)]) * inv, __uint_as_float(r[q4 * 8 + in_order(e * 2 + 1)]) * inv);
           *reinterpret_cast<uint4 *>(sm.q[X] + sw128(row, H * (kHalf / 8) + (c0 >> 3) + q4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
         }
       }
@@ -547,7 +699,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           if (turn != H) continue;
           const int rr = (row & ~31) + __ffs(int(again)) - 1;
           // (its lse was right unless its weights had left the range)
-          paged_row_alone<bf16, D>(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u, &sm.moves);
+          paged_row_alone<C, D>(p, size_t(row0 + tok0 + X * TOKT + rr / G), b, x_q0(X) + rr / G, g, g * G + rr % G, (sums_off >> (rr & 31)) & 1u, &sm.moves);
         }
       }
       }
@@ -580,7 +732,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         const bool more = k + 1 < n_tiles, pv = has(x, k), qk = has(x, k + 1);
         if (k >= 0) wait(sm.bar_full[seqV % S], uint32_t(seqV / S));
         if (ok && more) wait(sm.bar_full[seqK % S], uint32_t(seqK / S));
-        if (ok && qk && first_s) wait(sm.bar_q[x], n_q);
+        if (ok && qk && first_s) wait(CODES ? sm.bar_qmade[x] : sm.bar_q[x], n_q);
         if (ok && (x == 1 || n_turn > 0)) wait(sm.bar_turn[x], x == 1 ? n_turn : n_turn - 1);
         if (ok && pv) {
           wait(sm.bar_p[x], n_p++);
@@ -593,7 +745,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           if (k == last) commit(sm.bar_s[x]);        // O is complete
         }
         if (qk) {
-          issue_scores<D>(leader, tS, q_addr(x), kv_addr(seqK % S));
+          issue_scores<D, CODES>(leader, tS, q_addr(x), kv_addr(seqK % S));
+          if (CODES) issue_more(leader, tS, smem_u32(sm.more_q[x]), smem_u32(sm.more_k[(seqK >> 1) % (S / 2)]), smem_u32(sm.zeros));
           first_s = false;
           commit(sm.bar_s[x]);
         }
@@ -605,6 +758,34 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         }
       }
       n_q += n_tiles && (x == 0 || ntokB > 0) ? 1u : 0u;
+    }
+  } else if (CODES && warp > kLoadWarp + kUnpackWarps) {
+    // (a warpgroup has four warps)
+  } else if (CODES && warp > kLoadWarp) {
+    // =========================== unpacking warps ===========================
+    const int piece_shift = min(p.page_shift, 7);
+    bool ok = true;
+    auto wait = [&](uint64_t &bar, int phase) {
+      ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&bar), uint32_t(phase) & 1u, failed, moves)) && ok;
+    };
+    for (int it = 0; ok && next_work(it); ++it) {
+#pragma unroll 1
+      for (int k = 0; k < 2 * n_tiles && ok; ++k) {
+        const int job = jobs + k, slot = job % S, from = job % R;
+        wait(sm.bar_raw[from], job / R);
+        if (ok && job >= S) wait(sm.bar_free[slot], job / S - 1);
+        if (!ok) break;
+        const uint32_t there = *const_cast<volatile uint32_t *>(&sm.raw_pieces[from]);
+        const int seen = tq_last + 1 - kt.slot(k >> 1);
+        if (k & 1) unpack_tile<D, false>(sm.kv[slot], nullptr, nullptr, sm.raw[from], there, piece_shift, seen);
+        else unpack_tile<D, true>(sm.kv[slot], sm.more_k[(job >> 1) % (S / 2)], &sm.k_scale[(job >> 1) & 3], sm.raw[from], there, piece_shift, seen);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&sm.bar_full[slot]));
+          mbar_arrive(smem_u32(&sm.bar_rawfree[from]));
+        }
+      }
     }
   } else {
     // =========================== loader warp ===========================
@@ -661,14 +842,38 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         for (int is_v = 0; is_v < 2 && ok; ++is_v) {
           const int job = jobs + 2 * k + is_v, slot = job % S;
           const uint32_t bar = smem_u32(&sm.bar_full[slot]);
-          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed, moves));
+          if constexpr (CODES) {
+            const int to = job % R;
+            if (job >= R) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_rawfree[to]), uint32_t(job / R - 1) & 1u, failed, moves));
+            if (!ok) break;
+            const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && page != none);
+            const uint32_t raw = smem_u32(sm.raw[to]), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2), levels = uint32_t(rows) * kLevelBytes;
+            if (leader) {
+              sm.raw_pieces[to] = there;
+              mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * (codes + levels));
+            }
+#pragma unroll 1
+            for (int i = 0; i < pieces; ++i) {
+              const int pg = __shfl_sync(0xffffffffu, page, i);
+              if (leader && (there >> i) & 1u) {
+                const int off = (j0 + i * rows) & ((1 << p.page_shift) - 1);
+                const unsigned char *block = reinterpret_cast<const unsigned char *>(is_v ? p.v : p.k) + size_t(pg - p.page0) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride);
+                bulk_load(raw + i * codes, block + off * (D / 2), codes, raw_bar);
+                bulk_load(raw + kKT * (D / 2) + i * levels, block + ((D / 2) << p.page_shift) + off * kLevelBytes, levels, raw_bar);
+              }
+            }
+            ++asked.tiles;
+          }
+          if (!CODES && job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[slot]), uint32_t(job / S - 1) & 1u, failed, moves));
           if (!ok) break;
           // V rows behind the piece's last token: whatever they hold, their weights are 0 and they have to be finite
-          const bool tail = is_v && j0 + kKT - 1 > tq_last;
+          const bool tail = !CODES && is_v && j0 + kKT - 1 > tq_last;
           const uint32_t to = tail ? smem_u32(&sm.bar_tail) : bar;
-          if (leader) mbar_expect_tx(to, Sm::kTileBytes);
-          load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
-          ++asked.tiles;
+          if constexpr (!CODES) {
+            if (leader) mbar_expect_tx(to, Sm::kTileBytes);
+            load_tile<D>(leader, is_v ? &maps.v : &maps.k, p, kv_addr(slot), page, j0, g, pieces, rows, to);
+            ++asked.tiles;
+          }
           if (tail) ++asked.tails, asked.untrimmed = job;
           if (!q_asked) {
             bool now = 2 * k + is_v == latest;
@@ -699,9 +904,9 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
     }
     if (!ok) {   // after a time-out: no copy outlives the CTA
-      wait_for_copies(asked, S, [&](int what, int which, uint32_t parity) {
+      wait_for_copies(asked, CODES ? R : S, [&](int what, int which, uint32_t parity) {
         int alone = 0;   // (whoever has given up)
-        mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_q[which] : what == kCopyTile ? &sm.bar_full[which] : &sm.bar_tail), parity, &alone);
+        mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_q[which] : what == kCopyTile ? (CODES ? &sm.bar_raw[which] : &sm.bar_full[which]) : &sm.bar_tail), parity, &alone);
       });
     }
   }
@@ -1047,14 +1252,15 @@ int dispatch_tc(const glide_paged *h, F &&f) {
 
 int setup_paged_tc(const glide_paged *h) {
   return dispatch_tc(h, [&](auto d, auto g) {
-    constexpr int D = decltype(d)::value, G = decltype(g)::value, kBytes = int(sizeof(PrefillSmem<D>));
-    static_assert(kBytes <= 232448, "shared memory of one CTA");
-    return cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
-                   cudaFuncSetAttribute(paged_prefill_tc_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) == cudaSuccess &&
-                   cudaFuncSetAttribute(paged_weights_tc_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(AccountSmem<D>))) ==
-                       cudaSuccess
-               ? int(GLIDE_OK)
-               : int(GLIDE_ERR_CUDA);
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    auto allow = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess; };
+    static_assert(sizeof(PrefillSmem<D, false>) <= 232448 && sizeof(PrefillSmem<D, true>) <= 232448, "shared memory of one CTA");
+    const bool ok = h->codes ? allow(paged_prefill_tc_kernel<D, G, false, true>, sizeof(PrefillSmem<D, true>)) &&
+                                   allow(paged_prefill_tc_kernel<D, G, true, true>, sizeof(PrefillSmem<D, true>))
+                             : allow(paged_prefill_tc_kernel<D, G, false, false>, sizeof(PrefillSmem<D, false>)) &&
+                                   allow(paged_prefill_tc_kernel<D, G, true, false>, sizeof(PrefillSmem<D, false>)) &&
+                                   allow(paged_weights_tc_kernel<D, G>, sizeof(AccountSmem<D>));
+    return ok ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
 
@@ -1068,11 +1274,16 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const int64_t tiles = p.n_tokens / (2 * kRows / G) + p.batch;   // at most: each sequence's last one may be short
     const int64_t grid = tiles * p.Hkv;
     if (grid > INT32_MAX) return int(GLIDE_ERR_UNSUPPORTED);
-    const size_t bytes = sizeof(PrefillSmem<D>);
     const int splits = paged_splits(p, grid, 4 * kKT);
     const unsigned blocks = unsigned(std::min<int64_t>(grid * splits, p.sm_count));
-    if (p.lse) paged_prefill_tc_kernel<D, G, true><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
-    else paged_prefill_tc_kernel<D, G, false><<<blocks, kThreads, bytes, st>>>(p, maps, h->map_pages, splits);
+    auto start = [&](auto codes) {
+      constexpr bool CODES = decltype(codes)::value;
+      const int threads = CODES ? kCodeThreads : kThreads;
+      if (p.lse) paged_prefill_tc_kernel<D, G, true, CODES><<<blocks, threads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
+      else paged_prefill_tc_kernel<D, G, false, CODES><<<blocks, threads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
+    };
+    if (h->codes) start(std::true_type{});
+    else start(std::false_type{});
     if (const int rc = launch_status(cudaSuccess)) return rc;
     return splits > 1 ? launch_paged_join(h, p, splits, st) : int(GLIDE_OK);
   });

@@ -16,7 +16,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libglide.so")
 
-GLIDE_F32, GLIDE_BF16 = 0, 1
+GLIDE_F32, GLIDE_BF16, GLIDE_BF16_CACHE4 = 0, 1, 4
 GLIDE_PHI_SOFTMAX, GLIDE_PHI_PROJ_SOFTMAX2 = 0, 1
 GLIDE_MERGE_SHARED, GLIDE_MERGE_SUM_EVICTED, GLIDE_MERGE_SUM_ALL = 0, 1, 2
 GLIDE_DECODE_AUTO, GLIDE_DECODE_MMA, GLIDE_DECODE_FMA, GLIDE_DECODE_STREAM = 0, 1, 2, 3
@@ -62,6 +62,11 @@ class glide_paged_call(ctypes.Structure):
                 ("n_sink", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("dev_lens", ctypes.c_void_p), ("dev_starts", ctypes.c_void_p)] + \
                [(n, ctypes.c_int64) for n in ("n_tokens", "q_stride", "kv_stride", "out_stride", "window")] + \
                [(n, ctypes.c_void_p) for n in ("dev_weight", "dev_pos", "dev_seen")] + [("track_stride", ctypes.c_int64)]
+
+
+class glide_rotation(ctypes.Structure):
+    _fields_ = [("dev_cos", ctypes.c_void_p), ("dev_sin", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("rot_dim", ctypes.c_int32), ("neighbours", ctypes.c_int32)]
 
 
 class glide_layer_info_t(ctypes.Structure):
@@ -114,6 +119,10 @@ def load_library() -> ctypes.CDLL:
     lib.glide_paged_decode.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
     lib.glide_paged_weights.argtypes = [vp, vp, vp, vp, vp]
     lib.glide_paged_evict.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp]
+    lib.glide_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.glide_paged_read.argtypes = [vp, vp, vp, vp, vp]
+    lib.glide_paged_bounds.argtypes = [vp, vp, vp, vp]
+    lib.glide_paged_decode_sparse.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.glide_paged_check_call.argtypes = [pagedp, callp]
     lib.glide_paged_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.glide_strerror.argtypes = [ctypes.c_int]
@@ -124,6 +133,7 @@ def load_library() -> ctypes.CDLL:
                  "glide_layer_info", "glide_export_state", "glide_import_state", "glide_reset",
                  "glide_device_status", "glide_decode_launch_info", "glide_paged_workspace_bytes", "glide_paged_create",
                  "glide_paged_destroy", "glide_paged_prefill", "glide_paged_decode", "glide_paged_weights", "glide_paged_evict",
+                 "glide_paged_append", "glide_paged_read", "glide_paged_bounds", "glide_paged_decode_sparse",
                  "glide_paged_check_call", "glide_paged_device_status"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -393,9 +403,29 @@ class Glide:
         return dict(launches=a.value, work_items=b.value, grid=c.value)
 
 
+def paged4_row_bytes(head_dim: int) -> int:
+    """Bytes that a slot of a page in 4 bits takes of its KV head's block: the codes, then (behind all slots' codes) the levels."""
+    return head_dim // 2 + 4
+
+
 def make_paged_config(k_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int, softmax_scale: float = 0.0,
-                      weights: bool = True) -> glide_paged_config:
-    """The configuration of pages k_pages [L][n_pages][H_kv][page_size][d], which may be a view with other strides."""
+                      weights: bool = True, head_dim: Optional[int] = None) -> glide_paged_config:
+    """The configuration of pages k_pages [L][n_pages][H_kv][page_size][d], which may be a view with other strides; with head_dim, of pages
+    in 4 bits: uint8 [L][n_pages][H_kv][page_size * (head_dim / 2 + 4)], a head's block side by side."""
+    if head_dim is not None:
+        assert k_pages.dim() == 4 and k_pages.dtype is torch.uint8 and k_pages.stride(3) == 1, \
+            "pages in 4 bits are uint8 [L][n_pages][H_kv][page_size * (head_dim / 2 + 4)]"
+        L, n, hkv, block = k_pages.shape
+        row = paged4_row_bytes(head_dim)
+        assert block % row == 0, f"pages in 4 bits: {row} bytes for each slot of a block"
+        assert hkv == 1 or k_pages.stride(2) >= block, "pages: heads that share memory"
+        cfg = glide_paged_config(n_layers=L, n_q_heads=n_q_heads, n_kv_heads=hkv, head_dim=head_dim, io_dtype=GLIDE_BF16_CACHE4, page_size=block // row,
+                                 n_pages=n, max_batch=int(max_batch), max_tokens=int(max_tokens), softmax_scale=float(softmax_scale),
+                                 weights=int(bool(weights)), row_stride=row)
+        cfg.head_stride = int(k_pages.stride(2)) if hkv > 1 else block
+        cfg.page_stride = int(k_pages.stride(1)) if n > 1 else hkv * cfg.head_stride
+        cfg.layer_stride = int(k_pages.stride(0)) if L > 1 else max(1, n) * cfg.page_stride
+        return cfg
     assert k_pages.dim() == 5 and k_pages.stride(4) == 1, "pages are [L][n_pages][H_kv][page_size][d], features side by side"
     L, n, hkv, page, d = k_pages.shape
     assert k_pages.stride(3) >= d, "pages: slots that share memory"   # (strides of 0 would say "side by side" to the library)
@@ -414,6 +444,21 @@ def glide_paged_workspace_bytes(cfg: glide_paged_config) -> int:
     return int(out.value)
 
 
+class GlideRotation:
+    """The rotation of queries and keys by their positions: cos, sin fp32 [n_positions][rot_dim / 2] on the GPU, a row for each position (views of
+    equal strides will do).  neighbours: pair i is features 2i and 2i + 1, otherwise i and i + rot_dim / 2."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, neighbours: bool = False):
+        assert cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.dim() == 2 and cos.shape == sin.shape and cos.device == sin.device, \
+            "cos and sin: fp32 [n_positions][rot_dim / 2]"
+        assert cos.stride() == sin.stride() and cos.stride(1) == 1, "cos and sin: equal strides, a position's entries side by side"
+        n, half = cos.shape
+        assert n == 1 or cos.stride(0) >= half, "cos and sin: positions that share memory"
+        self.device, self._keep = cos.device, (cos, sin)
+        self.packed = bytes(glide_rotation(dev_cos=cos.data_ptr(), dev_sin=sin.data_ptr(), n_positions=n, stride=cos.stride(0) if n > 1 else half,
+                                           rot_dim=2 * half, neighbours=int(bool(neighbours))))
+
+
 _I32, _F32 = torch.int32, torch.float32
 # a call's fields as bytes of its own (one pack instead of a store per field: a step's host time is what counts where the cache is short)
 _pack_call = struct.Struct("@iiPiiqPPqqqqqPPPq").pack
@@ -424,18 +469,19 @@ class GlidePaged:
     """Softmax attention over a paged cache (include/glide.h): k_pages, v_pages [L][n_pages][H_kv][page_size][d] are the
     caller's (views of equal strides will do), a torch workspace and the handle are owned here.  Tables are int32 [B][cols], lens,
     seen and new_lens int32 [B], starts int32 [B + 1], weight fp32 and pos int32 [B][H_kv][slots], all on the pages' device.
+    With head_dim the pages are held in 4 bits: uint8 [L][n_pages][H_kv][page_size * (head_dim / 2 + 4)], all else bf16 (weights has to be False).
     Calls of one object must follow one another on the GPU, from whichever host threads they come; objects of their own may share
     pages.  The object has to live until its calls on streams other than the one that it was made on have ended."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_batch: int, max_tokens: int,
-                 softmax_scale: float = 0.0, weights: bool = True):
+                 softmax_scale: float = 0.0, weights: bool = True, head_dim: Optional[int] = None):
         self.lib = load_library()
         assert k_pages.is_cuda and v_pages.device == k_pages.device and v_pages.dtype == k_pages.dtype
         assert v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
-        self.device, self.dtype = k_pages.device, k_pages.dtype
-        self.L, _, self.Hkv, self.page_size, self.d = k_pages.shape
+        self.device, self.dtype = k_pages.device, torch.bfloat16 if head_dim is not None else k_pages.dtype
+        self.cfg = make_paged_config(k_pages, n_q_heads, max_batch, max_tokens, softmax_scale, weights, head_dim)
+        self.L, self.n_pages, self.Hkv, self.page_size, self.d = (getattr(self.cfg, n) for n in ("n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim"))
         self.H, self.max_batch, self.max_tokens = int(n_q_heads), int(max_batch), int(max_tokens)
-        self.cfg = make_paged_config(k_pages, n_q_heads, max_batch, max_tokens, softmax_scale, weights)
         self.workspace_bytes = glide_paged_workspace_bytes(self.cfg)
         self._keep = (k_pages, v_pages)
         with torch.cuda.device(self.device):
@@ -562,6 +608,58 @@ class GlidePaged:
         assert slots == pos_slots == weight.shape[2], "the accounts: as many slots"
         call = self._packed_call(layer, table, lens, None, None, (0, 0, 0), -1, n_sink, weight, pos, seen)
         self._run("glide_paged_evict", stream, self.lib.glide_paged_evict, call, budget, recent, p_weight, p_pos, self._ints(new_lens, B, "new_lens"))
+
+    def glide_paged_append(self, table, lens, starts, q, k, v, q_out=None, rotation: Optional["GlideRotation"] = None, weight=None, pos=None,
+                           seen=None, layer: int = 0, stream=None) -> None:
+        """Brings in the new tokens (rows starts[b] .. starts[b + 1] - 1; starts None: row b of sequence b): k rotated by the tokens' positions,
+        seen - T_b ... seen - 1, and v are stored, q rotated goes to q_out (q itself, or a tensor that does not overlap it; both None: no
+        queries).  Prefill or decode with k, v None then attends."""
+        assert (q is None) == (q_out is None), "q and q_out: both or neither"
+        rows = k.shape[0]
+        assert starts is not None or rows == table.shape[0], "without starts: one new token for each sequence"
+        (p_q, p_k, p_v, p_out), strides = self._qkv(q, k, v, q_out, rows)
+        call = self._packed_call(layer, table, lens, starts, rows, strides, -1, 0, weight, pos, seen)
+        turn = None
+        if rotation is not None:
+            assert rotation.device == self.device, f"rotation: on {self.device}"
+            turn = rotation.packed
+        self._run("glide_paged_append", stream, self.lib.glide_paged_append, call, turn, p_q, p_k, p_v, p_out)
+
+    def glide_paged_read(self, table, lens, starts, k, v, layer: int = 0, stream=None) -> None:
+        """What the slots of the tokens that starts names (None: the newest of each sequence) hold, into the rows of k and v."""
+        rows = k.shape[0]
+        assert starts is not None or rows == table.shape[0], "without starts: one row for each sequence"
+        (_, p_k, p_v, _), strides = self._qkv(None, k, v, None, rows)
+        call = self._packed_call(layer, table, lens, starts, rows, strides, -1, 0, None, None, None)
+        self._run("glide_paged_read", stream, self.lib.glide_paged_read, call, p_k, p_v)
+
+    def _bounds(self, bounds):
+        assert bounds.dtype is self.dtype and bounds.shape == (self.n_pages, self.Hkv, 2, self.d) and bounds.is_contiguous() and \
+            bounds.get_device() == self._index, f"bounds: {self.dtype} [{self.n_pages}][{self.Hkv}][2][{self.d}] on {self.device}"
+        return bounds.data_ptr()
+
+    def glide_paged_bounds(self, table, lens, starts, bounds, n_tokens: Optional[int] = None, layer: int = 0, stream=None) -> None:
+        """bounds [n_pages][H_kv][2][d], of the layer: least and largest key values of the pages that hold the tokens that starts names (None: the
+        newest of each sequence).  n_tokens: starts[B] or more (None: as many as the sequences can hold, which only costs time)."""
+        most = min(self.max_tokens, table.shape[1] * self.page_size) * table.shape[0]
+        rows = None if starts is None else most if n_tokens is None else int(n_tokens)
+        call = self._packed_call(layer, table, lens, starts, rows, (0, 0, 0), -1, 0, None, None, None)
+        self._run("glide_paged_bounds", stream, self.lib.glide_paged_bounds, call, self._bounds(bounds))
+
+    def glide_paged_decode_sparse(self, table, lens, q, k, v, out, bounds, picks, scores, lse=None, n_sink: int = 0, pos=None, seen=None,
+                                  layer: int = 0, stream=None) -> None:
+        """One new token per sequence, over picks.shape[2] of its pages (its own, those of the first n_sink slots, and those of the largest
+        score), which go to picks int32 [B][H_kv][n].  bounds [n_pages][H_kv][2][d] takes the new keys in; scores float64 [B][H_kv][cols]
+        is work space.  k, v None: the token is in the cache already."""
+        B, cols = table.shape
+        tensors, strides = self._qkv(q, k, v, out, B)
+        assert picks.dtype is _I32 and picks.dim() == 3 and picks.shape[:2] == (B, self.Hkv) and picks.is_contiguous() and picks.get_device() == self._index, \
+            f"picks: int32 [{B}][{self.Hkv}][n] on {self.device}"
+        assert scores.dtype is torch.float64 and scores.shape == (B, self.Hkv, cols) and scores.is_contiguous() and scores.get_device() == self._index, \
+            f"scores: float64 [{B}][{self.Hkv}][{cols}] on {self.device}"
+        call = self._packed_call(layer, table, lens, None, B, strides, -1, n_sink, None, pos, seen)
+        self._run("glide_paged_decode_sparse", stream, self.lib.glide_paged_decode_sparse, call, *tensors, self._lse(lse, B), self._bounds(bounds),
+                  picks.shape[2], picks.data_ptr(), scores.data_ptr())
 
     def glide_paged_device_status(self, stream=None) -> int:
         """The status word of the device-side checks, read and cleared behind what `stream` has been given (0: nothing was recorded)."""
