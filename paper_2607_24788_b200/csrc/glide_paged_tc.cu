@@ -8,17 +8,20 @@
 //   warps 4-7, 12-15   softmax of tile B
 //   warps 16, 17       issue the tcgen05.mma of A and of B (one elected lane), in turns
 //   warp 18            draws and finds the work, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
-//   warps 19-22        (pages in 4 bits) make tiles of the codes and levels that warp 18 has loaded into a small ring of their own, a piece
-//                      per page; slots that nobody sees are 0
-// Pages in 4 bits.  A key is mid + step n with mid = low + 8 step and n = code - 8, -8 .. 7, three bits and a sign: step n is a number of 11
+// Pages in 4 bits.  The loader fetches a tile's codes and levels, a piece per page, into a buffer for keys or one for values; the softmax
+// threads of A make the key tiles of them, two tiles ahead, those of B the value tiles, one ahead, when they have handed a tile's weights over and
+// would wait for its products.  (Four warps of their own: 862 us for 8001 tokens, 32 / 8 heads, of which 270 were waits for them.)
+//   A key is mid + step n with mid = low + 8 step and n = code - 8, -8 .. 7, three bits and a sign: step n is a number of 11
 // bits, which fp16 has.  So S = sum q (step n) + mid sum q is computed as it stands: both as fp16 operands, the second term as four more
 // columns of the product, (hi, lo) of mid against (hi, lo) of sum q.  fp16 is short of exponents, so a key tile is scaled by a power of two
 // to below 2^-6, a query row by the threads that it belongs to, to below 2^7, and the scores are scaled back where they are multiplied by the
-// softmax scale anyway.  (Exact for rows whose step is 2^-8 of the tile's largest or more, others are off by 2^-19 of the tile's largest key at
-// most.  Keys rounded to bf16 put scores off by 0.005, outputs by 0.006 of their norm.)  A value is rounded to bf16 once, like the weights: off by
-// at most 2^-8 of itself.  Both come out of one fused multiply-add for two codes where they lie in the word: four bits at the bottom of
-// an fp16 or bf16 number are code times its least subnormal number, the next four 16 times that.  Which leaves the features of eight in the
-// order 0 4 1 5 2 6 3 7, in keys, values, and so in Q and O.
+// softmax scale anyway.  (Exact for rows whose step is 2^-8 of the tile's largest key or more, others are off by 2^-19 of that at most.  Keys
+// rounded to bf16 put scores off by 0.005, outputs by 0.006 of their norm.)  A value is rounded to fp16 once, and so are the weights: off by at most
+// 2^-11 of themselves, or a value by 2^-16 of the largest that its scale went by.  The values' scale is a power of two as well, from the piece's
+// first tile on, until a tile has values four to eight times as large; then O is scaled as where a reference moves.  A key or value comes out of
+// one fused multiply-add for two codes where they lie in the word: four bits at the bottom of an fp16 number are code times its least
+// subnormal number, the next four 16 times that.  Which leaves the features of eight in the order 0 4 1 5 2 6 3 7, in keys, values, and so in
+// Q and O.  What a slot's codes are multiplied by, the scales and the further columns come from warp 19.
 // Every mbarrier wait is bounded; on a time-out the CTA records kDevWaitTimeout, leaves its loops, frees its TMEM columns and returns.
 #include <algorithm>
 #include <cstring>
@@ -39,12 +42,12 @@ constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
 constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
-constexpr int kUnpackWarps = 4, kRawStages = 2;   // pages in 4 bits
-constexpr int kCodeThreads = 768;                 // (whole warpgroups, which give each other registers)
+constexpr int kLevelWarp = 19, kCodeThreads = 640, kUnpackWarps = 8, kRawStages = 2;   // pages in 4 bits
 // How far (in the exponent) scores may exceed a row's reference before it moves.  Weights, sums and O are floating numbers: the reference only
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
 // pass over the tile: 8 sequences of up to 2048 tokens, windows of 256 with 4 first tokens 228 us with 8, 169 with 32, 171 with 64.
 constexpr float kLazy = 32.0f, kMostWeight = 0x1p32f;
+constexpr float kLazyHalf = 14.0f;    // ... of weights that are fp16 numbers
 constexpr int kMostSlots = 1 << 30;
 
 struct PagedMaps {
@@ -60,15 +63,17 @@ template <int D, bool CODES>
 struct PrefillSmem {
   static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
   static constexpr int kStages = CODES ? (D == 128 ? 4 : 6) : D == 128 ? 5 : 8;
-  static constexpr int kRaw = CODES ? kRawStages : 1, kRawBytes = CODES ? kKT * (D / 2 + kLevelBytes) : 16;
+  static constexpr int kRaw = CODES ? kRawStages : 1, kRawKeys = kKT * (D / 2 + 2 * kLevelBytes);   // (with the keys come their and the values' levels)
   unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
   unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
-  alignas(16) unsigned char raw[kRaw][kRawBytes];   // pages in 4 bits: the tiles' codes, then levels
+  alignas(16) unsigned char raw[CODES ? kRawKeys + kKT * D / 2 : 16];   // pages in 4 bits: a key tile's codes and levels; a value tile's codes
   uint64_t bar_raw[kRaw], bar_rawfree[kRaw];        // they have landed; the unpacking warps have read them
   uint32_t raw_pieces[kRaw];             // bit i: piece i of the tile has been loaded
   // the four further columns of Q_A, Q_B and of the key tiles, 16 bytes a row (a key tile's as long as its buffer), and the zeros that make them 16
   alignas(128) unsigned char more_q[CODES ? 2 : 1][CODES ? kRows * 16 : 16], more_k[CODES ? kStages / 2 : 1][CODES ? kKT * 16 : 16], zeros[CODES ? kRows * 16 : 16];
-  float k_scale[4];                      // what the last key tiles have been divided by (read until the row tiles have the next one's scores)
+  float k_undo[4], v_undo[4];            // what undoes the last tiles' scales (read until the row tiles have the next one's scores)
+  uint2 steps[6][CODES ? kKT : 1];       // per slot, as fp16 pairs: 2^24 steps as the tile is scaled, what is added; of two key tiles, of four value tiles
+  uint64_t bar_levels[4];                // all this of a key tile and the value tile behind it stands here (B may be two tiles behind warp 19)
   uint64_t bar_qmade[2];                 // Q_X is in fp16 (one arrival per warp)
   uint64_t bar_full[kStages];            // the buffer's K or V tile has landed (pages in 4 bits: has been made, one arrival per warp)
   uint64_t bar_free[kStages];            // the MMAs that read the buffer have completed (one arrival per row tile)
@@ -122,9 +127,9 @@ __device__ __forceinline__ void issue_more(bool leader, uint32_t tmem_d, uint32_
         : "memory");
 }
 // O (+)= P V, 128 x D x 128: P in TMEM (32-bit column c = elements 2c, 2c + 1; elements 64 .. from column 64 on), V MN-major
-template <int D>
+template <int D, bool F16 = false>
 __device__ __forceinline__ void issue_values(bool leader, uint32_t tmem_d, uint32_t tmem_a, uint32_t b_tile, bool accumulate) {
-  const uint32_t idesc = make_idesc(D, true), b0 = desc_lo(b_tile, kBoxBytes);
+  const uint32_t idesc = make_idesc(D, true, F16), b0 = desc_lo(b_tile, kBoxBytes);
   if (leader) {
 #pragma unroll
     for (int ks = 0; ks < kKT / 16; ++ks)
@@ -230,7 +235,7 @@ __device__ __forceinline__ Work find_tile(const PagedParams &p, int want, int to
   return w;
 }
 
-constexpr float kValueScale = 0x1p-40f;   // of pages in 4 bits: values in the tiles are 2^-40 of what they are, so that 2^133 steps are bf16 numbers
+
 constexpr float kMoreScale = 0x1p10f;     // mid is 2^10 times as large as its tile would have it, sum q as much smaller: neither's low part falls below fp16
 
 // A power of two that brings x (not negative) into [2^e, 2^(e + 1)), as far as there is one, and what undoes it
@@ -253,46 +258,54 @@ __device__ __forceinline__ uint4 more_columns(float x, bool keys) {
   return keys ? make_uint4(hi | lo << 16, hi | lo << 16, 0u, 0u) : make_uint4(hi | hi << 16, lo | lo << 16, 0u, 0u);
 }
 
-// A tile of codes and levels becomes a tile of rows, 128-byte swizzle: keys as fp16, step n, with mid in more columns, both times a power
-// of two of the tile; values as bf16.  Rows at or behind `rows` and those of pieces (of 2^piece_shift rows) that have not been loaded are 0.
-// A thread has 32 features of a row at a time; the threads of a quarter warp read and write different banks.
-template <int D, bool KEYS>
-__device__ __forceinline__ void unpack_tile(unsigned char *tile, unsigned char *more, float *k_scale, const unsigned char *raw, uint32_t pieces, int piece_shift,
-                                            int rows) {
-  constexpr int kLanes = D / 32, kAtOnce = 32 / kLanes * kUnpackWarps;   // threads of a row; rows at once
-  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kLoadWarp - 1;
-  const int c = lane % kLanes, r0 = warp * (32 / kLanes) + lane / kLanes;
-  auto there = [&](int row) { return row < rows && (pieces >> (row >> piece_shift)) & 1u; };
-  auto levels_of = [&](int row) { return there(row) ? *reinterpret_cast<const uint32_t *>(raw + kKT * (D / 2) + row * kLevelBytes) : 0u; };
-  float scale = 1.f;
-  if (KEYS) {   // (every warp looks at all levels)
-    uint32_t top = 0u;
+// A tile of codes and levels becomes a tile of rows, 128-byte swizzle: keys as step n, with mid in more columns, both times a power of two of
+// the tile; values times one of the piece.  Slots that no query of the piece sees (by the window: of [lo, rows) and [0, sinks) some query sees
+// each) and those of pieces (of 2^piece_shift slots) that have not been loaded have levels 0, and so are 0.
+struct TileRows {
+  uint32_t pieces;
+  int piece_shift, lo, rows, sinks;
+  __device__ __forceinline__ bool has(int row) const { return row < rows && (row >= lo || row < sinks) && (pieces >> (row >> piece_shift)) & 1u; }
+};
+// The levels of a key tile and of the value tile behind it (levels [2][kKT]); one warp.
+__device__ __forceinline__ void make_levels(const uint32_t *levels, const TileRows &there, float &v_scale, float *k_undo, float *v_undo, uint2 *k_step, uint2 *v_step, unsigned char *more) {
+  const int lane = threadIdx.x & 31;
+  uint32_t l[2][kKT / 32], top[2] = {0u, 0u};
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
 #pragma unroll
     for (int i = 0; i < kKT / 32; ++i) {
-      const uint32_t levels = levels_of(i * 32 + lane);
-      const float low = bf16_hi(levels), x = fmaxf(fabsf(low), fabsf(fmaf(15.f, bf16_lo(levels), low)));   // (a step is 2 / 15 of it at most)
-      if (isfinite(x)) top = max(top, __float_as_uint(x));
+      const int row = i * 32 + lane;
+      l[which][i] = there.has(row) ? levels[which * kKT + row] : 0u;
+      const float low = bf16_hi(l[which][i]), x = fmaxf(fabsf(low), fabsf(fmaf(15.f, bf16_lo(l[which][i]), low)));   // (a step is 2 / 15 of it at most)
+      if (x < CUDART_INF_F) top[which] = max(top[which], __float_as_uint(x));   // (no NaN either)
     }
-    float undo;
-    scale = scale_to(__uint_as_float(__reduce_max_sync(0xffffffffu, top)), -7, undo);
-    if (warp == 0 && lane == 0) *k_scale = undo;
+  float undo, v_back;
+  const float scale = scale_to(__uint_as_float(__reduce_max_sync(0xffffffffu, top[0])), -7, undo);
+  const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, top[1]));
+  if (v_scale == 0.f || most * v_scale >= 0x1p-6f) v_scale = scale_to(most, -9, v_back);
+  if (lane == 0) *k_undo = undo, *v_undo = 1.f / v_scale;
+#pragma unroll
+  for (int i = 0; i < kKT / 32; ++i) {
+    const int row = i * 32 + lane;
+    const float ks = bf16_lo(l[0][i]) * scale * 0x1p24f, vs = bf16_lo(l[1][i]) * v_scale * 0x1p24f, low = bf16_hi(l[1][i]) * v_scale;
+    k_step[row] = make_uint2(pack_f16x2(ks, ks), pack_f16x2(ks * -0x1p-21f, ks * -0x1p-21f));
+    v_step[row] = make_uint2(pack_f16x2(vs, vs), pack_f16x2(low, low));
+    *reinterpret_cast<uint4 *>(more + row * 16) = more_columns(fmaf(8.f, bf16_lo(l[0][i]), bf16_hi(l[0][i])) * (scale * kMoreScale), true);
   }
+}
+// Codes to rows; the eight warps of a row tile.
+template <int D>
+__device__ __forceinline__ void unpack_tile(unsigned char *tile, const unsigned char *raw, const uint2 *steps) {
+  constexpr int kLanes = D / 32, kAtOnce = 32 / kLanes * kUnpackWarps;   // threads of a row; rows at once
+  const int lane = threadIdx.x & 31, warp = ((threadIdx.x >> 5) & 3) | ((threadIdx.x >> 8) << 2);   // (of the row tile's eight)
+  const int c = lane % kLanes, r0 = warp * (32 / kLanes) + lane / kLanes;
 #pragma unroll
   for (int i = 0; i < kKT / kAtOnce; ++i) {
-    const int row = r0 + i * kAtOnce;
-    uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t levels = levels_of(row);
-    if (there(row)) codes = *reinterpret_cast<const uint4 *>(raw + row * (D / 2) + c * 16);
+    const uint4 codes = *reinterpret_cast<const uint4 *>(raw + r0 * (D / 2) + c * 16 + i * kAtOnce * (D / 2));
+    const uint2 step = steps[r0 + i * kAtOnce];
+    uint32_t step1;   // for codes in a number's bits 4 to 7
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(step1) : "r"(step.x), "r"(0x2c002c00u));
     const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-    uint32_t step0, step1, add;   // for codes in the lowest four bits; in the next four; what is added
-    if (KEYS) {
-      const float s = bf16_lo(levels) * scale;
-      step0 = pack_f16x2(s * 0x1p24f, s * 0x1p24f), step1 = pack_f16x2(s * 0x1p20f, s * 0x1p20f), add = pack_f16x2(s * -8.f, s * -8.f);
-      if (c == 0) *reinterpret_cast<uint4 *>(more + row * 16) = more_columns(fmaf(8.f, bf16_lo(levels), bf16_hi(levels)) * (scale * kMoreScale), true);
-    } else {
-      const float s = bf16_lo(levels) * kValueScale, low = bf16_hi(levels) * kValueScale;
-      step0 = pack_bf16x2(s * 0x1p66f * 0x1p67f, s * 0x1p66f * 0x1p67f), step1 = pack_bf16x2(s * 0x1p64f * 0x1p65f, s * 0x1p64f * 0x1p65f), add = pack_bf16x2(low, low);
-    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {   // (piece j, or j ^ 2 in every other half row: a quarter warp's pieces in different banks)
       const uint32_t word = D == 128 ? (c & 2 ? w[j ^ 2] : w[j]) : w[j];
@@ -300,10 +313,9 @@ __device__ __forceinline__ void unpack_tile(unsigned char *tile, unsigned char *
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const uint32_t x = (n & 2 ? word >> 8 : word) & (n & 1 ? 0x00f000f0u : 0x000f000fu);
-        if (KEYS) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[n]) : "r"(x), "r"(n & 1 ? step1 : step0), "r"(add));
-        else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[n]) : "r"(x), "r"(n & 1 ? step1 : step0), "r"(add));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[n]) : "r"(x), "r"(n & 1 ? step1 : step.x), "r"(step.y));
       }
-      *reinterpret_cast<uint4 *>(tile + sw128(row, c * 4 + (j ^ (c & 2)))) = make_uint4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<uint4 *>(tile + sw128(r0, c * 4 + (D == 128 ? j ^ (c & 2) : j)) + i * kAtOnce * 128) = make_uint4(v[0], v[1], v[2], v[3]);
     }
   }
 }
@@ -324,6 +336,8 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   if (warp == kLoadWarp && lane == 0) {
     for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sm.bar_full[s]), CODES ? kUnpackWarps : 1), mbar_init(smem_u32(&sm.bar_free[s]), 2);
     if (CODES)
+      for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&sm.bar_levels[s]), 1);
+    if (CODES)
       for (int s = 0; s < R; ++s) {
         mbar_init(smem_u32(&sm.bar_raw[s]), 1), mbar_init(smem_u32(&sm.bar_rawfree[s]), kUnpackWarps);
         mbar_init(smem_u32(&sm.bar_qmade[s]), kSoftmaxThreads / 32 / 2);
@@ -335,7 +349,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       mbar_init(smem_u32(&sm.bar_turn[x]), 1);
       mbar_init(smem_u32(&sm.bar_p[x]), kSoftmaxThreads / 32 / 2);
       mbar_init(smem_u32(&sm.bar_work[x]), 1);
-      mbar_init(smem_u32(&sm.bar_workfree[x]), kLoadWarp + (CODES ? kUnpackWarps : 0));
+      mbar_init(smem_u32(&sm.bar_workfree[x]), kLoadWarp + (CODES ? 1 : 0));
     }
     mbar_init(smem_u32(&sm.bar_tail), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -393,11 +407,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     return k;
   };
 
-  // 768 threads are launched with 80 registers each: the softmax threads (512) get 96, the others (256) keep 48, as many in all
-  if (CODES) {
-    if (tid < kSoftmaxThreads) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-  }
   if (!aligned) {
     // (nothing is in flight; the status word tells)
   } else if (tid < kSoftmaxThreads) {
@@ -570,15 +579,95 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       l_sum += sum0 + sum1;
       if (LSE) x_sum += ex0 + ex1;
     };
+    // Pages in 4 bits: weights as fp16 numbers, so the reference moves first where it has to, and O with it; O too where the values' scale has
+    // moved.  Sums of the weights as they are: rounding puts them off by 2^-11 each.
+    auto soft_half = [&](auto masked, const Bounds &v, bool first, float v_ratio) {
+      float mx = -CUDART_INF_F;
+#pragma unroll
+      for (int c = 0; c < 64; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(tS + c, x);
+        if (decltype(masked)::value) {
+          const uint32_t m = seen_of(v, c);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = (m >> i) & 1u ? x[i] : 0xff800000u;
+        }
+        float m4[4] = {mx, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+        mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
+      }
+      auto grows = [&]() {
+        const float ms = mx * scale;
+        return ms > m_ref + kLazyHalf || (m_ref == -CUDART_INF_F && ms > -CUDART_INF_F);
+      };
+      if (pair_any(grows() || v_ratio != 1.f)) {
+        mx = row_max_of(mx);
+        float f = 1.f;
+        if (grows()) {
+          mx *= scale;
+          f = m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
+          m_ref = mx;
+          x_sum *= f;
+        }
+        f *= v_ratio;
+        if (!first && __any_sync(0xffffffffu, f != 1.f)) scale_o(f);
+      }
+      const float mr = m_ref == -CUDART_INF_F ? 0.f : m_ref;
+      float ex0 = 0.f, ex1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < 64; c += 32) {
+        uint32_t x[32], pk[16];
+        tmem_ld32(tS + c, x);
+        if (decltype(masked)::value) {
+          const uint32_t m = seen_of(v, c);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = (m >> i) & 1u ? x[i] : 0xff800000u;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a0, a1;
+          fma2(a0, a1, __uint_as_float(x[e * 2]), __uint_as_float(x[e * 2 + 1]), scale, -mr);
+          a0 = ex2(a0), a1 = ex2(a1);
+          add2(ex0, ex1, a0, a1);
+          pk[e] = pack_f16x2(a0, a1);
+        }
+        tmem_st16(tS + (c >> 1), pk);
+      }
+      tmem_wait_st();
+      hand_over();
+      x_sum += ex0 + ex1;
+    };
+    // Key tile k of the piece (the threads of A) or value tile k (of B).  After a time-out nothing is waited for, nor made.
+    auto unpack = [&](int k) {
+      if (k >= n_tiles) return;
+      const uint32_t job = uint32_t(jobs + 2 * k + X), slot = job % S, from = job % R, tile = job >> 1;
+      auto wait = [&](uint64_t &bar, uint32_t phase) {
+        if (ok) ok = mbar_wait_long(smem_u32(&bar), phase & 1u, failed, moves);
+        ok = __all_sync(0xffffffffu, ok);
+      };
+      wait(sm.bar_levels[tile & 3], tile >> 2);     // (of keys their codes are there too then, and the buffer is free)
+      if (X) {
+        wait(sm.bar_raw[from], job / R);
+        if (job >= S) wait(sm.bar_free[slot], job / S - 1u);
+      }
+      if (ok) unpack_tile<D>(sm.kv[slot], sm.raw + from * Sm::kRawKeys, sm.steps[X ? 2 + (tile & 3) : tile & 1]);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&sm.bar_full[slot]));
+        mbar_arrive(smem_u32(&sm.bar_rawfree[from]));
+      }
+    };
     for (int it = 0;; ++it) {
       // (both warps of a pair stop together: after a time-out too)
       if (pair_any(!next_work(it) || !ok)) break;
       const int ntokX = X ? ntokB : ntokA;
-      if (ntokX == 0) continue;
+      if (!CODES && ntokX == 0) continue;
       const int mine = x_q0(X) + tok_r;             // this row's slot
       m_ref = -CUDART_INF_F, l_sum = 0.f, x_sum = 0.f, top_w = 0.f;
-      float q_undo = 1.f;
-      if (CODES && n_tiles) {                       // Q to fp16, where it lies; of a row its sum too
+      float q_undo = 1.f, v_undo = 0.f;             // of Q; of what O holds
+      if (CODES && n_tiles && ntokX) {              // Q to fp16, where it lies; of a row its sum too
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));
         constexpr int kChunks = kHalf / 8;
         float top = 0.f, sum = 0.f;
@@ -609,20 +698,26 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
       const int w = p.window < 0 ? kMostSlots : p.window;
       int before = -1;                              // the key tile that this row tile had before
-      for (int k = 0; k < n_tiles; ++k) {
-        if (!has(X, k)) continue;
-        const bool move = pair_any(before < 0 || top_w >= kMostWeight || m_ref == -CUDART_INF_F);   // (before the wait, beside the products)
+      for (int k = CODES ? X - 2 : 0; k < n_tiles; ++k) {
+        if (has(X, k)) {
+        const bool move = !CODES && pair_any(before < 0 || top_w >= kMostWeight || m_ref == -CUDART_INF_F);   // (before the wait, beside the products)
         wait_s();
         if (tid == X * kRows) {                     // S of the tile and P V of the tile before have completed
           mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * k) % S]));
           if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * before + 1) % S]));
         }
-        if (CODES) scale = q_undo * *const_cast<volatile float *>(&sm.k_scale[((jobs >> 1) + k) & 3]);
         const int j0 = kt.slot(k);
         const bool whole = j0 + kKT - 1 <= x_q0(X) && (j0 > x_q1(X) - w || j0 + kKT <= p.n_sink);
         const int c0 = j0 + H * 64;
         const Bounds v{mine - w + 1 - c0, mine - c0, min(p.n_sink - 1, mine) - c0};
-        if (move) {
+        if constexpr (CODES) {
+          const int tile = ((jobs >> 1) + k) & 3;
+          const float undo = *const_cast<volatile float *>(&sm.v_undo[tile]), ratio = before < 0 ? 1.f : v_undo / undo;
+          scale = q_undo * *const_cast<volatile float *>(&sm.k_undo[tile]);
+          v_undo = undo;
+          if (whole) soft_half(std::false_type{}, v, before < 0, ratio);
+          else soft_half(std::true_type{}, v, before < 0, ratio);
+        } else if (move) {
           soft_tile_masked(v, before < 0);
           hand_over();
         } else if (whole) {
@@ -631,17 +726,20 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           soft_tile(std::true_type{}, v);
         }
         before = k;
+        }
+        if constexpr (CODES) unpack(k + 2 - X);
       }
-      const float l_row = row_sum_of(l_sum);
-      const float x_row = LSE ? row_sum_of(x_sum) : 0.f;
+      if (CODES && ntokX == 0) continue;
+      const float l_row = row_sum_of(CODES ? x_sum : l_sum);
+      const float x_row = CODES ? l_row : LSE ? row_sum_of(x_sum) : 0.f;
       if (before >= 0) wait_s();                    // every product of X has completed
       else if (!CODES && n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));   // (Q, which no product has waited for)
       n_q += n_tiles != 0;
       const bool live = tok_r < ntokX;
       const size_t out_row = size_t(row0 + tok0 + X * TOKT + tok_r);
       if (parts > 1) {
-        const float f = catch_up(row_max_of(top_w));   // (records are added up against the largest of their references)
-        const float fo = CODES ? f / kValueScale : f;
+        const float f = CODES ? 1.f : catch_up(row_max_of(top_w));   // (records are added up against the largest of their references)
+        const float fo = CODES ? v_undo : f;
         float *rec = split_record(p, D, part, out_row, g * G + row % G);
 #pragma unroll 1
         for (int c0 = 0; c0 < kHalf && before >= 0; c0 += 32) {
@@ -655,7 +753,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         }
         if (H == 0 && live && ok) *reinterpret_cast<float4 *>(rec + D) = make_float4(m_ref, l_row * f, x_row * f, 0.f);
       } else {
-      const float inv = live && before >= 0 && l_row != 0.f ? (CODES ? 1.0f / kValueScale : 1.0f) / l_row : 0.f;
+      const float inv = live && before >= 0 && l_row != 0.f ? (CODES ? v_undo : 1.0f) / l_row : 0.f;
       float chk0 = 0.f, chk1 = 0.f;                 // finite if all values of the row are
 #pragma unroll 1
       for (int c0 = 0; c0 < kHalf; c0 += 32) {
@@ -740,7 +838,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         }
         if (!ok) break;
         if (pv) {
-          issue_values<D>(leader, tO, tS, kv_addr(seqV % S), !first_o);
+          issue_values<D, CODES>(leader, tO, tS, kv_addr(seqV % S), !first_o);
           first_o = false;
           if (k == last) commit(sm.bar_s[x]);        // O is complete
         }
@@ -759,31 +857,25 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
       n_q += n_tiles && (x == 0 || ntokB > 0) ? 1u : 0u;
     }
-  } else if (CODES && warp > kLoadWarp + kUnpackWarps) {
-    // (a warpgroup has four warps)
-  } else if (CODES && warp > kLoadWarp) {
-    // =========================== unpacking warps ===========================
-    const int piece_shift = min(p.page_shift, 7);
-    bool ok = true;
-    auto wait = [&](uint64_t &bar, int phase) {
-      ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&bar), uint32_t(phase) & 1u, failed, moves)) && ok;
-    };
-    for (int it = 0; ok && next_work(it); ++it) {
-#pragma unroll 1
-      for (int k = 0; k < 2 * n_tiles && ok; ++k) {
-        const int job = jobs + k, slot = job % S, from = job % R;
-        wait(sm.bar_raw[from], job / R);
-        if (ok && job >= S) wait(sm.bar_free[slot], job / S - 1);
-        if (!ok) break;
-        const uint32_t there = *const_cast<volatile uint32_t *>(&sm.raw_pieces[from]);
-        const int seen = tq_last + 1 - kt.slot(k >> 1);
-        if (k & 1) unpack_tile<D, false>(sm.kv[slot], nullptr, nullptr, sm.raw[from], there, piece_shift, seen);
-        else unpack_tile<D, true>(sm.kv[slot], sm.more_k[(job >> 1) % (S / 2)], &sm.k_scale[(job >> 1) & 3], sm.raw[from], there, piece_shift, seen);
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(smem_u32(&sm.bar_full[slot]));
-          mbar_arrive(smem_u32(&sm.bar_rawfree[from]));
+  } else if (CODES && warp == kLevelWarp) {
+    // =========================== levels' warp ===========================
+    if constexpr (CODES) {
+      bool ok = true;
+      for (int it = 0; ok && next_work(it); ++it) {
+        float v_scale = 0.f;                          // of the values since the piece's first tile, or one that was much larger
+  #pragma unroll 1
+        for (int k = 0; k < n_tiles; ++k) {
+          const int job = jobs + 2 * k, tile = job >> 1, j0 = kt.slot(k);
+          ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_raw[0]), uint32_t(tile) & 1u, failed, moves));
+          // (the further columns of the tile that had the buffer are free when that is)
+          if (ok && job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[job % S]), uint32_t(job / S - 1) & 1u, failed, moves));
+          if (!ok) break;
+          const TileRows rows{*const_cast<volatile uint32_t *>(&sm.raw_pieces[0]), min(p.page_shift, 7), p.window < 0 ? 0 : tq0 - p.window + 1 - j0, tq_last + 1 - j0, p.n_sink - j0};
+          make_levels(reinterpret_cast<const uint32_t *>(sm.raw + kKT * (D / 2)), rows, v_scale, &sm.k_undo[tile & 3], &sm.v_undo[tile & 3], sm.steps[tile & 1], sm.steps[2 + (tile & 3)],
+                      sm.more_k[tile % (S / 2)]);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sm.bar_levels[tile & 3]));
         }
       }
     }
@@ -828,7 +920,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           for (int hf = 0; hf < D / 64; ++hf) tma_load_3d(q_addr(x) + hf * kBoxBytes, &maps.q, hf * 64, g * G, row0 + tok0 + x * TOKT, bar);
         }
       };
-      const int latest = min(2 * n_tiles, S - 1) - 1;   // the tile behind which Q is waited for (no product is needed for those before it)
+      const int latest = min(2 * n_tiles, CODES ? R : S - 1) - 1;   // the tile behind which Q is waited for (no product is needed for those before it)
       bool q_asked = false;
       if (n_tiles == 0) {
         ask_q(0);
@@ -847,10 +939,10 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             if (job >= R) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_rawfree[to]), uint32_t(job / R - 1) & 1u, failed, moves));
             if (!ok) break;
             const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && page != none);
-            const uint32_t raw = smem_u32(sm.raw[to]), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2), levels = uint32_t(rows) * kLevelBytes;
+            const uint32_t raw = smem_u32(sm.raw + to * Sm::kRawKeys), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2), levels = uint32_t(rows) * kLevelBytes;
             if (leader) {
               sm.raw_pieces[to] = there;
-              mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * (codes + levels));
+              mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * (is_v ? codes : codes + 2 * levels));
             }
 #pragma unroll 1
             for (int i = 0; i < pieces; ++i) {
@@ -859,7 +951,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
                 const int off = (j0 + i * rows) & ((1 << p.page_shift) - 1);
                 const unsigned char *block = reinterpret_cast<const unsigned char *>(is_v ? p.v : p.k) + size_t(pg - p.page0) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride);
                 bulk_load(raw + i * codes, block + off * (D / 2), codes, raw_bar);
-                bulk_load(raw + kKT * (D / 2) + i * levels, block + ((D / 2) << p.page_shift) + off * kLevelBytes, levels, raw_bar);
+                const int at = ((D / 2) << p.page_shift) + off * kLevelBytes;
+                if (!is_v) {   // (with the keys' levels come the values')
+                  bulk_load(raw + kKT * (D / 2) + i * levels, block + at, levels, raw_bar);
+                  bulk_load(raw + kKT * (D / 2 + kLevelBytes) + i * levels, block + (reinterpret_cast<const unsigned char *>(p.v) - reinterpret_cast<const unsigned char *>(p.k)) + at, levels,
+                            raw_bar);
+                }
               }
             }
             ++asked.tiles;
@@ -1278,9 +1375,8 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const unsigned blocks = unsigned(std::min<int64_t>(grid * splits, p.sm_count));
     auto start = [&](auto codes) {
       constexpr bool CODES = decltype(codes)::value;
-      const int threads = CODES ? kCodeThreads : kThreads;
-      if (p.lse) paged_prefill_tc_kernel<D, G, true, CODES><<<blocks, threads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
-      else paged_prefill_tc_kernel<D, G, false, CODES><<<blocks, threads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
+      if (p.lse) paged_prefill_tc_kernel<D, G, true, CODES><<<blocks, CODES ? kCodeThreads : kThreads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
+      else paged_prefill_tc_kernel<D, G, false, CODES><<<blocks, CODES ? kCodeThreads : kThreads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
     };
     if (h->codes) start(std::true_type{});
     else start(std::false_type{});
