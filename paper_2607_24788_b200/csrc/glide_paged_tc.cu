@@ -702,7 +702,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (has(X, k)) {
         const bool move = !CODES && pair_any(before < 0 || top_w >= kMostWeight || m_ref == -CUDART_INF_F);   // (before the wait, beside the products)
         wait_s();
-        if (tid == X * kRows) {                     // S of the tile and P V of the tile before have completed
+        if (!CODES && tid == X * kRows) {           // S of the tile and P V of the tile before have completed
           mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * k) % S]));
           if (before >= 0) mbar_arrive(smem_u32(&sm.bar_free[(jobs + 2 * before + 1) % S]));
         }
@@ -839,18 +839,20 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (!ok) break;
         if (pv) {
           issue_values<D, CODES>(leader, tO, tS, kv_addr(seqV % S), !first_o);
+          if (CODES) commit(sm.bar_free[seqV % S]);  // (not by the softmax threads, which make the tile that comes into the buffer)
           first_o = false;
           if (k == last) commit(sm.bar_s[x]);        // O is complete
         }
         if (qk) {
           issue_scores<D, CODES>(leader, tS, q_addr(x), kv_addr(seqK % S));
           if (CODES) issue_more(leader, tS, smem_u32(sm.more_q[x]), smem_u32(sm.more_k[(seqK >> 1) % (S / 2)]), smem_u32(sm.zeros));
+          if (CODES) commit(sm.bar_free[seqK % S]);
           first_s = false;
           commit(sm.bar_s[x]);
         }
         if (leader) {
           mbar_arrive(smem_u32(&sm.bar_turn[x ^ 1]));
-          if (pv && k == last) mma_commit(smem_u32(&sm.bar_free[seqV % S]));
+          if (!CODES && pv && k == last) mma_commit(smem_u32(&sm.bar_free[seqV % S]));
           if (!pv && k >= 0) mbar_arrive(smem_u32(&sm.bar_free[seqV % S]));   // (a tile of which this row tile sees nothing)
           if (!qk && more) mbar_arrive(smem_u32(&sm.bar_free[seqK % S]));
         }
