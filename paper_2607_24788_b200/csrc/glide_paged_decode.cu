@@ -9,10 +9,10 @@
 //          (the sum that O is divided by takes the rounded ones: every weight is off by at most 2^-8 of itself; lse and the account
 //          take the exact ones), turned by movmatrix,
 //          O^T += V_tile^T P.
-//   4 bits codes become bf16 numbers by their bits (0x4300 | code is 128 + code).  K: a lane has a quarter of two slots' features, in the order in
-//          which the codes lie, the queries' fragments in the same order; 128 sum q is taken off before the product, a row's levels are
-//          put on its scores.  V: a lane has an eighth of four slots' features, two slots' codes are brought together by byte permutation,
-//          136 is taken off (exact); the step goes to the weight, the lowest level + 8 steps are added up apart, in fp32.
+//   4 bits (twelve warps, tiles of 32 slots, or 16 where pages are that short) codes are bf16 operands as they lie, below the least normal number, which
+//          the tensor cores take for what it is: an and for two of them.  K: a lane has a quarter of two slots' features, in the order in which the codes
+//          lie, the queries' fragments in the same order; a row's levels are put on its scores.  V: a lane has an eighth of four slots' features, two
+//          slots' codes are brought together by byte permutation; the step goes to the weight, the middle levels are added up apart, in fp32.
 //   fp32   2 or 4 lanes per slot, all query heads; weights through shared memory; a lane has D / 32 columns of O.
 // At a unit's end the eight warps meet; a unit that lies in one CTA is written out, one that was cut leaves a record (maximum, sums, O
 // per head) per CTA, and the CTA that leaves the last one adds them up in slot order.  A step whose weights are kept also leaves
@@ -28,13 +28,23 @@ namespace glide {
 
 namespace {
 
-constexpr int kWarps = 8;             // (12: a unit's tiles end sooner, its meeting later: 0 to 3 us longer between 600 and 4500 slots)
-constexpr int kThreads = kWarps * 32;
 constexpr int kMaxGrid = 256;          // CTAs that the records are laid out for
 constexpr float kLazy = 8.0f;
 
+// Rows in 4 bits, in tiles of TILE slots
+template <int TILE>
+struct Codes {};
+
+}  // namespace
+template <int TILE>
+struct IoOf<Codes<TILE>> {
+  using type = __nv_bfloat16;
+};
+namespace {
+
 template <typename T, int D>
 struct Shape {
+  static constexpr int kWarps = 8;   // (12: a unit's tiles end sooner, its meeting later: 0 to 3 us longer between 600 and 4500 slots)
   static constexpr int kTile = sizeof(T) == 4 && D == 128 ? 8 : 16;
   static constexpr int kRowBytes = D * int(sizeof(T));
   static constexpr int kChunks = kRowBytes / 16;
@@ -49,13 +59,14 @@ struct Shape {
   }
 };
 
-// Rows in 4 bits: a tile is [16 slots' codes of K][their levels][of V ...].
-template <int D>
-struct Shape<Code4, D> {
-  static constexpr int kTile = 16;
+// A tile is [the slots' codes of K][their levels][of V ...].
+template <int TILE, int D>
+struct Shape<Codes<TILE>, D> {
+  static constexpr int kWarps = 12;
+  static constexpr int kTile = TILE;
   static constexpr int kCodes = kTile * D / 2, kHalf = kCodes + kTile * kLevelBytes;   // bytes of codes; of K or V
   static constexpr int kTileBytes = 2 * kHalf;
-  static constexpr int kStages = 16384 / kTileBytes;
+  static constexpr int kStages = 13312 / kTileBytes;
   static constexpr int kRowBytes = 2 * D;   // (of q)
   // where 16-byte piece i of V's codes lies: the eight slots 2c, 2c + 1, .. of a quarter warp in different banks
   static __device__ __forceinline__ int at_v(int i) { return ((i & ~7) | ((i & 7) ^ (D == 128 ? ((i >> 3) & 3) << 1 : ((i >> 3) & 1) << 1))) << 4; }
@@ -63,6 +74,7 @@ struct Shape<Code4, D> {
 
 template <typename T, int D, int G>
 struct Smem {
+  static constexpr int kWarps = Shape<T, D>::kWarps;
   unsigned char ring[kWarps][Shape<T, D>::kStages][Shape<T, D>::kTileBytes];
   static constexpr int kSlots = G == 8 ? kWarps / 2 : kWarps;         // warps whose O is here at a time when a CTA's warps meet
   float o[kSlots][G][D + 4];
@@ -151,7 +163,7 @@ __device__ __forceinline__ int seq_of(const int *prefix, int batch, int f) {   /
 // 8.3 / 9.8 / 11.8 / 14.4 / 17.2.)
 constexpr int kCutCost = 40;
 // Tiles of a CTA: at least one for each warp.
-__device__ __forceinline__ int share_of(int total, int grid) { return max((total + grid - 1) / grid, kWarps); }
+__device__ __forceinline__ int share_of(int total, int grid, int warps) { return max((total + grid - 1) / grid, warps); }
 template <int D, int G>
 __device__ __forceinline__ float *record(const PagedParams &p, int cta, int which) {
   return p.records + size_t(cta * 2 + which) * (G * (D + 3));   // O [G][D]; maxima, sums, exact sums [G]
@@ -182,13 +194,17 @@ __device__ __forceinline__ uint32_t turn(uint32_t x) {
   return y;
 }
 
-// Code p and code p + 4 of eight as two bf16 numbers, 128 more than they are
-__device__ __forceinline__ uint32_t pair_of(uint32_t codes, int p) { return ((codes >> (4 * p)) & 0x000f000fu) | 0x43004300u; }
-__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+// Codes p and p + 4 of eight, as they lie: bf16 numbers that are 2^-133 times them, or 16 times that for odd p
+__device__ __forceinline__ uint32_t pair_of(uint32_t codes, int p) { return (p & 2 ? codes >> 8 : codes) & (p & 1 ? 0x00f000f0u : 0x000f000fu); }
+// two products at once
+__device__ __forceinline__ void mul2(float &a0, float &a1, float x, float y0, float y1) {
+  asm("{\n\t.reg .b64 x, y, d;\n\tmov.b64 x, {%2, %2};\n\tmov.b64 y, {%3, %4};\n\tmul.rn.f32x2 d, x, y;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(a0), "=f"(a1)
+      : "f"(x), "f"(y0), "f"(y1));
 }
+// 2^e, as far as there is such a normal number
+__device__ __forceinline__ float power_of_2(int e) { return __uint_as_float(uint32_t(min(max(e + 127, 1), 254)) << 23); }
+__device__ __forceinline__ int exponent_of(float x) { return int(__float_as_uint(x) >> 23) - 127; }   // (x not negative)
 
 // The state of one warp in one unit, bf16.  Thread (r = lane / 4, c = lane % 4) has the scores of slots r and r + 8 of a tile for the
 // heads 2c and 2c + 1, and of O^T rows r and r + 8 of every 16 for the same heads.
@@ -307,13 +323,18 @@ struct WarpUnit {
   }
 };
 
-// Rows in 4 bits.  Thread (r = lane / 4, c = lane % 4) has scores as above; of O^T, features r D / 8 + 2k and + 2k + 1 of every k.
-template <int D, int G>
-struct WarpUnit<Code4, D, G> {
+// Rows in 4 bits.  Thread (r = lane / 4, c = lane % 4) has scores as above, of every 16 slots; of O^T, features r D / 8 + 2k and + 2k + 1 of every k.
+// Codes are operands as they lie in their words, bf16 numbers below the least normal one, against queries times 2^s (so that a head's
+// largest is near 2^100) and weights times step 2^w (so that a step is).  A tile's products are added up from 0 and then to O, in which nothing is cut off.
+template <int TILE, int D, int G>
+struct WarpUnit<Codes<TILE>, D, G> {
+  static constexpr int N = TILE / 16;
   uint32_t q[D / 16][2];
-  float o[D / 16][4];
-  float m[2], x[2], z[2];   // maxima; sums of the weights; of the weights times the middle level of their rows, low + 8 step
-  float off[2], qs[2];      // -128 sum q; sum q in the scores' unit
+  float o[D / 16][4];       // times 2^(w - 133), odd features 16 times that
+  float m[2], x[2], z[2];   // maxima; sums of the weights; of the weights times the middle levels of their rows, low + 8 step
+  float y[2];               // sums of the weights times step 2^w as the product has them: 8 of each is to come off O
+  float fq[2], qs[2];       // 2^(133 - s) and sum q, in the scores' unit
+  float fw;                 // 2^w; 0: no tile with a step yet
 
   template <typename S>
   __device__ __forceinline__ void begin(const PagedParams &p, S &, int b, int g) {
@@ -321,22 +342,39 @@ struct WarpUnit<Code4, D, G> {
     constexpr int F = D / 4;   // features of a lane
     const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + size_t(b) * size_t(p.q_stride) +
                                                        size_t(g * G + h) * D + (lane & 3) * F);
-    float sum = 0.f;
+    float sum = 0.f, top = 0.f;
+    uint4 w[F / 8];
 #pragma unroll
     for (int j = 0; j < F / 8; ++j) {
-      const uint4 w = h < G ? src[j] : make_uint4(0u, 0u, 0u, 0u);
-      q[2 * j][0] = __byte_perm(w.x, w.z, 0x5410), q[2 * j][1] = __byte_perm(w.x, w.z, 0x7632);
-      q[2 * j + 1][0] = __byte_perm(w.y, w.w, 0x5410), q[2 * j + 1][1] = __byte_perm(w.y, w.w, 0x7632);
-      sum += ((bf16_lo(w.x) + bf16_hi(w.x)) + (bf16_lo(w.y) + bf16_hi(w.y))) + ((bf16_lo(w.z) + bf16_hi(w.z)) + (bf16_lo(w.w) + bf16_hi(w.w)));
+      w[j] = h < G ? src[j] : make_uint4(0u, 0u, 0u, 0u);
+      const uint32_t x4[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum += bf16_lo(x4[e]) + bf16_hi(x4[e]);
+        top = fmaxf(top, fmaxf(fabsf(bf16_lo(x4[e])), fabsf(bf16_hi(x4[e]))));
+      }
     }
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+    for (int o2 = 1; o2 < 4; o2 <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o2), top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o2));
+    const int e_top = max(exponent_of(top), -126);                            // (an infinity: 128)
+    const int up = max(100 - e_top, 6);                                       // (2^(133 - up) is a number)
+    const float f0 = power_of_2(up / 2), f1 = power_of_2(up - up / 2);        // (2^up may be none)
+    auto scaled = [&](uint32_t a, uint32_t b2, bool high, float f) {           // features of two words, one each, as a pair
+      return high ? pack_bf16x2(bf16_hi(a) * f0 * f1 * f, bf16_hi(b2) * f0 * f1 * f) : pack_bf16x2(bf16_lo(a) * f0 * f1 * f, bf16_lo(b2) * f0 * f1 * f);
+    };
+#pragma unroll
+    for (int j = 0; j < F / 8; ++j) {
+      q[2 * j][0] = scaled(w[j].x, w[j].z, false, 1.f), q[2 * j][1] = scaled(w[j].x, w[j].z, true, 0.0625f);
+      q[2 * j + 1][0] = scaled(w[j].y, w[j].w, false, 1.f), q[2 * j + 1][1] = scaled(w[j].y, w[j].w, true, 0.0625f);
+    }
+    const float undo = power_of_2(133 - up) * p.scale_log2;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float all = __shfl_sync(0xffffffffu, sum, ((lane & 3) * 2 + i) * 4);
-      off[i] = -128.f * all, qs[i] = all * p.scale_log2;
-      m[i] = -CUDART_INF_F, x[i] = z[i] = 0.f;
+      const int from = ((lane & 3) * 2 + i) * 4;
+      fq[i] = __shfl_sync(0xffffffffu, undo, from), qs[i] = __shfl_sync(0xffffffffu, sum, from) * p.scale_log2;
+      m[i] = -CUDART_INF_F, x[i] = z[i] = y[i] = 0.f;
     }
+    fw = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -344,100 +382,144 @@ struct WarpUnit<Code4, D, G> {
   }
   template <typename S>
   __device__ __forceinline__ void tile(const PagedParams &p, S &, const unsigned char *buf, uint32_t mask, float *) {
-    using Sh = Shape<Code4, D>;
+    using Sh = Shape<Codes<TILE>, D>;
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     const unsigned char *V = buf + Sh::kHalf;
-    // scores
     constexpr int W = D / 32;   // words of eight codes that a lane has of a K row
-    uint32_t k0[W], k1[W];
-    if constexpr (W == 4) {
-      const uint4 a = *reinterpret_cast<const uint4 *>(buf + r * 64 + c * 16), b = *reinterpret_cast<const uint4 *>(buf + (r + 8) * 64 + c * 16);
-      k0[0] = a.x, k0[1] = a.y, k0[2] = a.z, k0[3] = a.w, k1[0] = b.x, k1[1] = b.y, k1[2] = b.z, k1[3] = b.w;
-    } else {
-      const uint2 a = *reinterpret_cast<const uint2 *>(buf + r * 32 + c * 8), b = *reinterpret_cast<const uint2 *>(buf + (r + 8) * 32 + c * 8);
-      k0[0] = a.x, k0[1] = a.y, k1[0] = b.x, k1[1] = b.y;
-    }
-    uint32_t kl[2], vl[2];
+    float s[N][4];
+    uint32_t vl[N][2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      kl[e] = *reinterpret_cast<const uint32_t *>(buf + Sh::kCodes + (r + 8 * e) * 4);
-      vl[e] = *reinterpret_cast<const uint32_t *>(V + Sh::kCodes + (r + 8 * e) * 4);
-      vl[e] = (mask >> (r + 8 * e)) & 1u ? vl[e] : 0u;   // (what is not seen is no NaN either)
-    }
-    float s0[4] = {off[0], off[1], off[0], off[1]}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < N; ++t) {
+      const unsigned char *K = buf + (t * 16 + r) * (D / 2) + c * (D / 8);
+      uint32_t k0[W], k1[W];
+      if constexpr (W == 4) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(K), b = *reinterpret_cast<const uint4 *>(K + 8 * 64);
+        k0[0] = a.x, k0[1] = a.y, k0[2] = a.z, k0[3] = a.w, k1[0] = b.x, k1[1] = b.y, k1[2] = b.z, k1[3] = b.w;
+      } else {
+        const uint2 a = *reinterpret_cast<const uint2 *>(K), b = *reinterpret_cast<const uint2 *>(K + 8 * 32);
+        k0[0] = a.x, k0[1] = a.y, k1[0] = b.x, k1[1] = b.y;
+      }
+      float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const int pr = (ks & 1) * 2;
-      const uint32_t a[4] = {pair_of(k0[ks >> 1], pr), pair_of(k1[ks >> 1], pr), pair_of(k0[ks >> 1], pr + 1), pair_of(k1[ks >> 1], pr + 1)};
-      mma16816(ks & 1 ? s1 : s0, a, q[ks][0], q[ks][1]);
-    }
-    float s[4];
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const int pr = (ks & 1) * 2;
+        const uint32_t a[4] = {pair_of(k0[ks >> 1], pr), pair_of(k1[ks >> 1], pr), pair_of(k0[ks >> 1], pr + 1), pair_of(k1[ks >> 1], pr + 1)};
+        mma16816(ks & 1 ? s1 : s0, a, q[ks][0], q[ks][1]);
+      }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool seen = (mask >> (r + (e >> 1) * 8)) & 1u;
-      const float step = bf16_lo(kl[e >> 1]) * p.scale_log2, low = bf16_hi(kl[e >> 1]);
-      s[e] = seen ? fmaf(s0[e] + s1[e], step, low * qs[e & 1]) : -CUDART_INF_F;
+      for (int e = 0; e < 2; ++e) {
+        const int row = t * 16 + r + 8 * e;
+        const bool seen = (mask >> row) & 1u;
+        const uint32_t kl = *reinterpret_cast<const uint32_t *>(buf + Sh::kCodes + row * 4), l = *reinterpret_cast<const uint32_t *>(V + Sh::kCodes + row * 4);
+        vl[t][e] = seen ? l : 0u;   // (what is not seen is no NaN either)
+        float f0, f1, a0 = s0[2 * e], a1 = s0[2 * e + 1], u0, u1;
+        add2(a0, a1, s1[2 * e], s1[2 * e + 1]);
+        mul2(f0, f1, bf16_lo(kl), fq[0], fq[1]);
+        mul2(u0, u1, bf16_hi(kl), qs[0], qs[1]);
+        dot2(u0, u1, a0, a1, f0, f1);
+        s[t][2 * e] = seen ? u0 : -CUDART_INF_F, s[t][2 * e + 1] = seen ? u1 : -CUDART_INF_F;
+      }
     }
-    bool grows = false;
+    float top[2] = {s[0][0], s[0][1]};
+    float step = 0.f;   // the largest of this thread's rows
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float top = fmaxf(s[i], s[i + 2]);
-      grows |= top > m[i] + kLazy || (m[i] == -CUDART_INF_F && top > -CUDART_INF_F);
+    for (int t = 0; t < N; ++t) {
+      if (t) top[0] = fmaxf(top[0], s[t][0]), top[1] = fmaxf(top[1], s[t][1]);
+      top[0] = fmaxf(top[0], s[t][2]), top[1] = fmaxf(top[1], s[t][3]);
+      step = fmaxf(step, fmaxf(bf16_lo(vl[t][0]), bf16_lo(vl[t][1])));   // (a NaN is left out)
     }
-    if (__any_sync(0xffffffffu, grows)) {
+    // (-infinity + 8 is -infinity: a head without a maximum moves with its first score; an infinite step is none)
+    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy || (fw == 0.f ? step > 0.f : step * fw >= 0x1p116f))) {
+      float go = 1.f;   // what the weights' scale makes of O
+      const float most = warp_max(step);
+      if (fw == 0.f ? most > 0.f : most * fw >= 0x1p116f) {
+        const float now = power_of_2(100 - exponent_of(most));
+        go = fw == 0.f ? 1.f : now / fw;
+        fw = now;
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float top = fmaxf(s[i], s[i + 2]);
 #pragma unroll
-        for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-        top = fmaxf(top, m[i]);
-        const float f = m[i] == -CUDART_INF_F ? 0.f : ex2(m[i] - top);
-        m[i] = top;
-        x[i] *= f, z[i] *= f;
+        for (int w = 4; w < 32; w <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], w));
+        top[i] = fmaxf(top[i], m[i]);
+        const float f = m[i] == -CUDART_INF_F ? 0.f : ex2(m[i] - top[i]);
+        m[i] = top[i];
+        x[i] *= f, z[i] *= f, y[i] *= f * go;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) o[k][i] *= f, o[k][i + 2] *= f;
+        for (int k = 0; k < D / 16; ++k) o[k][i] *= f * go, o[k][i + 2] *= f * go;
       }
     }
-    uint32_t pk[2];
-    const float r0 = m[0] == -CUDART_INF_F ? 0.f : m[0], r1 = m[1] == -CUDART_INF_F ? 0.f : m[1];
+    uint32_t pk[N][2];
+    const float r0 = m[0] == -CUDART_INF_F ? 0.f : -m[0], r1 = m[1] == -CUDART_INF_F ? 0.f : -m[1];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float step = bf16_lo(vl[e]), mid = fmaf(8.f, step, bf16_hi(vl[e]));
-      const float w0 = ex2(s[e * 2] - r0), w1 = ex2(s[e * 2 + 1] - r1);
-      x[0] += w0, x[1] += w1;
-      z[0] = fmaf(w0, mid, z[0]), z[1] = fmaf(w1, mid, z[1]);
-      pk[e] = turn(pack_bf16x2(w0 * step, w1 * step));   // (rounded as the product needs it: a weight's share of v - mid is off by at most 2^-8 of itself)
-    }
-    // O
+    for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {   // eight features of the lane at a time
-      uint32_t w[4];
+      for (int e = 0; e < 2; ++e) {
+        float w0 = s[t][2 * e], w1 = s[t][2 * e + 1], p0, p1;
+        add2(w0, w1, r0, r1);
+        w0 = ex2(w0), w1 = ex2(w1);
+        add2(x[0], x[1], w0, w1);
+        const float step = bf16_lo(vl[t][e]), mid = fmaf(8.f, step, bf16_hi(vl[t][e]));
+        dot2(z[0], z[1], w0, w1, mid, mid);
+        mul2(p0, p1, step * fw, w0, w1);
+        pk[t][e] = pack_bf16x2(p0, p1);         // (rounded as the product needs it: a weight's share of v - mid is off by at most 2^-8 of itself)
+        add2(y[0], y[1], bf16_lo(pk[t][e]), bf16_hi(pk[t][e]));
+        pk[t][e] = turn(pk[t][e]);
+      }
+    // O: two slots' codes of a feature side by side
+    constexpr int kPer = D / 8 / 8;   // words of eight codes that a lane has of a V row
+    const int line = (2 * c * (D / 2) + r * (D / 16)) >> 4, in = (r * (D / 16)) & 15;
+    const unsigned char *va = V + Sh::at_v(line) + in, *vb = V + Sh::at_v(line + D / 32) + in;   // slots 2c and 2c + 1; 8 slots on, 4 D bytes
+    uint32_t w[N][4][kPer];
+#pragma unroll
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int slot = 2 * c + (i & 1) + (i >> 1) * 8, at = slot * (D / 2) + r * (D / 16) + j * 4;
-        w[i] = *reinterpret_cast<const uint32_t *>(V + Sh::at_v(at >> 4) + (at & 15));
+        const unsigned char *at = (i & 1 ? vb : va) + (t * 2 + (i >> 1)) * 4 * D;
+        if constexpr (kPer == 2) {
+          const uint2 a = *reinterpret_cast<const uint2 *>(at);
+          w[t][i][0] = a.x, w[t][i][1] = a.y;
+        } else {
+          w[t][i][0] = *reinterpret_cast<const uint32_t *>(at);
+        }
       }
-      const uint32_t v01[2] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632)};
-      const uint32_t v23[2] = {__byte_perm(w[2], w[3], 0x5410), __byte_perm(w[2], w[3], 0x7632)};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int n = (2 * k) & 3, h = k >> 1;
-        constexpr uint32_t kMid = 0xc308c308u;   // -136, twice
-        const uint32_t a[4] = {add_bf16x2(pair_of(v01[h], n), kMid), add_bf16x2(pair_of(v01[h], n + 1), kMid),
-                               add_bf16x2(pair_of(v23[h], n), kMid), add_bf16x2(pair_of(v23[h], n + 1), kMid)};
-        mma16816(o[j * 4 + k], a, pk[0], pk[1]);
+    for (int j = 0; j < kPer; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {   // four of its features
+        float acc[2][4] = {};
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+          const uint32_t v01 = __byte_perm(w[t][0][j], w[t][1][j], h ? 0x7632 : 0x5410), v23 = __byte_perm(w[t][2][j], w[t][3][j], h ? 0x7632 : 0x5410);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t a[4] = {pair_of(v01, 2 * k), pair_of(v01, 2 * k + 1), pair_of(v23, 2 * k), pair_of(v23, 2 * k + 1)};
+            mma16816(acc[k], a, pk[t][0], pk[t][1]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float(&to)[4] = o[j * 4 + h * 2 + k];
+          add2(to[0], to[1], acc[k][0], acc[k][1]);
+          add2(to[2], to[3], acc[k][2], acc[k][3]);
+        }
       }
-    }
   }
   template <typename S>
   __device__ __forceinline__ void put_sums(S &sm, int warp) {
     const int lane = threadIdx.x & 31;
+    const int up = 133 - exponent_of(fw);       // (2^up may be no number)
+    const float u0 = fw == 0.f ? 0.f : power_of_2(up / 2), u1 = power_of_2(up - up / 2), u = fw == 0.f ? 0.f : 1.f / fw;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int w = 4; w < 32; w <<= 1) x[i] += __shfl_xor_sync(0xffffffffu, x[i], w), z[i] += __shfl_xor_sync(0xffffffffu, z[i], w);
+      for (int w = 4; w < 32; w <<= 1) {
+        x[i] += __shfl_xor_sync(0xffffffffu, x[i], w), z[i] += __shfl_xor_sync(0xffffffffu, z[i], w);
+        y[i] += __shfl_xor_sync(0xffffffffu, y[i], w);
+      }
+      z[i] = fmaf(y[i] * u, -8.f, z[i]);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) o[k][i] += z[i], o[k][i + 2] += z[i];
+      for (int k = 0; k < D / 16; ++k) o[k][i] = fmaf(o[k][i] * u0, u1, z[i]), o[k][i + 2] = fmaf(o[k][i + 2] * u0, u1 * 0.0625f, z[i]);
       const int h = (lane & 3) * 2 + i;
       if (lane < 4 && h < G) sm.m[warp][h] = m[i], sm.l[warp][h] = sm.e[warp][h] = x[i];
     }
@@ -472,7 +554,7 @@ struct WarpUnit<float, D, G> {
   template <typename S>
   __device__ __forceinline__ void begin(const PagedParams &p, S &sm, int b, int g) {
     // (every warp of the CTA comes here at the same unit, behind the meeting of the one before)
-    for (int i = threadIdx.x; i < G * D; i += kThreads)
+    for (int i = threadIdx.x; i < G * D; i += Shape<float, D>::kWarps * 32)
       sm.q[i / D][i % D] = reinterpret_cast<const float *>(p.q)[size_t(b) * size_t(p.q_stride) + size_t(g * G + i / D) * D + i % D] * p.scale_log2;
 #pragma unroll
     for (int h = 0; h < G; ++h) {
@@ -587,7 +669,7 @@ constexpr uint32_t kFresh = 0x80000000u;
 __device__ __forceinline__ float part_factor(float m, float M) { return m == -CUDART_INF_F ? 0.f : ex2(m - M); }
 
 // The records of a unit that CTAs c0 .. c1 share, added up in their order, and the outputs; all threads of a CTA.
-template <typename T, int D, int G>
+template <typename T, int D, int G, int kThreads>
 __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, int c0, int c1, int t0, int share, bool keep) {
   const int tid = threadIdx.x, lane = tid & 31;
   constexpr int kEach = (G * D + kThreads - 1) / kThreads;   // outputs of a thread; those of a warp are of one head each
@@ -648,17 +730,18 @@ __device__ __forceinline__ void add_records(const PagedParams &p, int b, int g, 
 }
 
 template <typename C, int D, int G, bool PICKED>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_constant__ PagedParams p) {
+__global__ void __launch_bounds__(Shape<C, D>::kWarps * 32, 1) paged_decode_kernel(const __grid_constant__ PagedParams p) {
   using Sh = Shape<C, D>;
   using T = Io<C>;
-  constexpr bool kCodes = std::is_same<C, Code4>::value;
+  constexpr bool kCodes = !std::is_same<C, T>::value;
+  constexpr int kWarps = Sh::kWarps, kThreads = kWarps * 32;
   constexpr int S = Sh::kStages;
   extern __shared__ __align__(128) unsigned char smem_raw[];
   auto &sm = *reinterpret_cast<Smem<C, D, G> *>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_for_predecessor();
   const int most = prefix_of<Sh::kTile, kThreads, PICKED>(p, sm.len, sm.prefix, sm.warp_sums, sm.warp_most);
-  const int total = sm.prefix[p.batch], share = share_of(total, int(gridDim.x)), units = p.batch * p.Hkv;
+  const int total = sm.prefix[p.batch], share = share_of(total, int(gridDim.x), kWarps), units = p.batch * p.Hkv;
   int lo = int(min(int64_t(total), int64_t(blockIdx.x) * share)), hi = min(total, lo + share);
   if (units <= int(gridDim.x) && most <= share + kCutCost) {   // a unit for each CTA
     const int u = min(int(blockIdx.x), units), b = u / p.Hkv, n = u < units ? (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv : 0;
@@ -687,9 +770,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     if (page < 0) return t;
     if (kCodes) t.at = int64_t(size_t(page) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride));   // (the head's block)
     else t.at = int64_t(paged_row(p, page, t.slot, g));
-    auto below = [](int n) { return n <= 0 ? 0u : n >= Sh::kTile ? (1u << Sh::kTile) - 1u : (1u << n) - 1u; };
+    auto below = [](int n) { return n <= 0 ? 0u : n >= Sh::kTile ? ~0u >> (32 - Sh::kTile) : (1u << n) - 1u; };
     t.rows = (below(len - t.slot) & ~below(st.vis_begin - t.slot)) | below(st.vis_end - t.slot);
-    if (p.new_k && len - 1 - t.slot < Sh::kTile) t.rows |= kFresh | uint32_t(len - 1 - t.slot) << 16;
+    if (!kCodes && p.new_k && len - 1 - t.slot < Sh::kTile) t.rows |= kFresh | uint32_t(len - 1 - t.slot) << 16;
     return t;
   };
   TileInfo now;
@@ -708,14 +791,17 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
         const int row = slots[S - 1] & ((1 << p.page_shift) - 1);
         const unsigned char *k = reinterpret_cast<const unsigned char *>(p.k) + at, *v = reinterpret_cast<const unsigned char *>(p.v) + at;
         const uint32_t dst = smem_u32(sm.ring[warp][i % S]);
+        k += row * (D / 2) + lane * 16, v += row * (D / 2) + lane * 16;
+        const uint32_t to_k = dst + lane * 16, to_v = dst + Sh::kHalf + Sh::at_v(lane);
 #pragma unroll
-        for (int c0 = 0; c0 < Sh::kCodes / 16; c0 += 32) {
-          const int c = c0 + lane;
-          cp_async16(dst + c * 16, k + row * (D / 2) + c * 16);
-          cp_async16(dst + Sh::kHalf + Sh::at_v(c), v + row * (D / 2) + c * 16);
+        for (int c = 0; c < Sh::kCodes; c += 512) {   // (32 pieces on, at_v is 512 on)
+          cp_async16(to_k + c, k + c);
+          cp_async16(to_v + c, v + c);
         }
-        const int levels = ((D / 2) << p.page_shift) + row * kLevelBytes + (lane & 3) * 16;
-        if (lane < 8) cp_async16(dst + (lane < 4 ? 0 : Sh::kHalf) + Sh::kCodes + (lane & 3) * 16, (lane < 4 ? k : v) + levels);
+        // the levels: TILE / 4 pieces of K's and of V's
+        constexpr int kEach = Sh::kTile / 4;
+        const int64_t levels = ((D / 2) << p.page_shift) + row * kLevelBytes - row * (D / 2) + (lane % kEach - lane) * 16;
+        if (lane < 2 * kEach) cp_async16(dst + (lane < kEach ? 0 : Sh::kHalf) + Sh::kCodes + (lane % kEach) * 16, (lane < kEach ? k : v) + levels);
         cp_async_commit();
         return;
       } else {
@@ -799,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
     while (lo + warp + cur * kWarps < end) {
       cp_async_wait<S - 1>();
       __syncwarp();
-      unit.tile(p, sm, sm.ring[warp][cur % S], rows[0] & 0xffffu, scores ? scores + size_t(slots[0]) * G : nullptr);
+      unit.tile(p, sm, sm.ring[warp][cur % S], kCodes ? rows[0] : rows[0] & 0xffffu, scores ? scores + size_t(slots[0]) * G : nullptr);
       __syncwarp();
       ask(cur + S);
       ++cur;
@@ -871,7 +957,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const __grid_
       if (cut[w] < 0 || !sm.last[w]) continue;
       const int b = seq_of(sm.prefix, p.batch, cut[w]), n = (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv, g = (cut[w] - sm.prefix[b]) / n;
       const int t0 = sm.prefix[b] + g * n;
-      add_records<T, D, G>(p, b, g, t0 / share, (t0 + n - 1) / share, t0, share, keep);
+      add_records<T, D, G, kThreads>(p, b, g, t0 / share, (t0 + n - 1) / share, t0, share, keep);
     }
   }
   dependents_may_start();
@@ -908,6 +994,7 @@ int launch(const PagedParams &p, cudaStream_t st) {
   using Sh = Shape<C, D>;
   // tiles that the sequences can have at most: no more CTAs than their warps can have
   const int64_t longest = PICKED ? std::min<int64_t>(p.most, int64_t(p.n_picks) << p.page_shift) : p.window < 0 ? p.most : std::min<int64_t>(p.most, int64_t(p.window) + p.n_sink + 2 * Sh::kTile);
+  constexpr int kWarps = Sh::kWarps, kThreads = kWarps * 32;
   const int64_t tiles = (longest / Sh::kTile + 2) * p.Hkv * p.batch;
   const int units = p.batch * p.Hkv;
   int grid = int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kWarps - 1) / kWarps, p.sm_count, kMaxGrid})));
@@ -930,7 +1017,9 @@ namespace {
 // f(what a page holds, D, G)
 template <typename F>
 int dispatch_pages(const glide_paged *h, F &&f) {
-  if (h->codes) return dispatch_config(GLIDE_BF16, h->cfg.head_dim, h->group, [&](auto, auto d, auto g) { return f(TypeTag<Code4>{}, d, g); });
+  if (h->codes)   // (no tile crosses a page)
+    return dispatch_config(GLIDE_BF16, h->cfg.head_dim, h->group,
+                           [&](auto, auto d, auto g) { return h->page_shift == 4 ? f(TypeTag<Codes<16>>{}, d, g) : f(TypeTag<Codes<32>>{}, d, g); });
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, h->group, f);
 }
 template <typename C, int D, int G, bool PICKED>
@@ -946,7 +1035,7 @@ int setup_paged_decode(const glide_paged *h) {
     using C = typename decltype(c)::type;
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     bool ok = setup<C, D, G, false>();
-    if constexpr (!std::is_same<C, Code4>::value) ok = ok && setup<C, D, G, true>();
+    if constexpr (std::is_same<C, Io<C>>::value) ok = ok && setup<C, D, G, true>();
     return ok ? int(GLIDE_OK) : int(GLIDE_ERR_CUDA);
   });
 }
@@ -955,7 +1044,7 @@ int launch_paged_decode(const glide_paged *h, const PagedParams &p, cudaStream_t
   return dispatch_pages(h, [&](auto c, auto d, auto g) {
     using C = typename decltype(c)::type;
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    if constexpr (!std::is_same<C, Code4>::value) {
+    if constexpr (std::is_same<C, Io<C>>::value) {
       if (p.picks) return launch<C, D, G, true>(p, st);
     }
     return launch<C, D, G, false>(p, st);

@@ -105,7 +105,7 @@ class Cache4:
 def reference4(c, window=-1, n_sink=0, layer=0, prompt=False):
     """Outputs and lse in fp64 and how far an implementation may be off them, with u = 2^-24, s the step, m = low + 8 s the middle level, n = code - 8,
     Q = sum |q|, all times the softmax scale:
-      a step of one token: 128 + code against q in fp32 on tensor cores, which may cut off: e = (d + 8) 2u Q (143 s + |low|);
+      a step of one token: codes against q in fp32 on tensor cores, which may cut off: e = (d + 8) 2u Q (15 s + |low|);
         weights times step are rounded to bf16: 2^-8 sum p |v - m|
       prompts: e = (d + 8) 2u Q (8 s + |m|) + 2^-20 Q |m| (two numbers of 22 bits) + d 2^-31 max|q| max|k| (queries below 2^-20 of a row's largest), and
         2^-19 Q max|k| for rows whose step is below 2^-8 of the largest key; weights rounded to fp16: 2^-11 sum p |v| + cnt 2^-25 max|v|; values:
@@ -140,7 +140,7 @@ def reference4(c, window=-1, n_sink=0, layer=0, prompt=False):
                 per_key = per_key + torch.where((step < 2.0 ** -8 * most.max()) & (step > 0), 2.0 ** -19 * most.max(), 0.0)
                 e = Q * torch.where(sees, per_key[None], 0.0).amax(1) + d * 2.0 ** -31 * q.abs().amax(1) * most.max() * scale
             else:
-                e = Q * torch.where(sees, ((d + 8) * 2 * U * (143 * step + low.abs()))[None], 0.0).amax(1)
+                e = Q * torch.where(sees, ((d + 8) * 2 * U * (15 * step + low.abs()))[None], 0.0).amax(1)
             total = torch.logsumexp(x, 1)
             p = torch.where(sees, torch.exp(x - torch.where(total == -math.inf, 0.0, total)[:, None]), 0.0)
             v0 = torch.where(sees.any(0)[:, None], fine(v), 0.0)
