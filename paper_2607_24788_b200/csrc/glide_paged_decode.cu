@@ -53,6 +53,7 @@ struct Shape {
   // and these SMs end last: 134 MB 33.9 us instead of 32.1, 2.1 GB 327 instead of 321.)
   static constexpr int kStages = 16384 / kTileBytes;
   static constexpr int kParts = 32 / kTile;                  // fp32: lanes per slot
+  static __device__ __forceinline__ int at_o(int c) { return c; }
   // position of 16-byte chunk c of row r: eight lanes that read together meet in different banks
   static __device__ __forceinline__ int at(int r, int c) {
     return r * kRowBytes + ((c ^ ((sizeof(T) == 4 ? r * kParts : r) & 7)) << 4);
@@ -68,6 +69,7 @@ struct Shape<Codes<TILE>, D> {
   static constexpr int kTileBytes = 2 * kHalf;
   static constexpr int kStages = 13312 / kTileBytes;
   static constexpr int kRowBytes = 2 * D;   // (of q)
+  static __device__ __forceinline__ int at_o(int c) { return c % (D / 8) * 8 + c / (D / 8); }   // place of column c where the warps meet: a warp's lanes side by side
   // where 16-byte piece i of V's codes lies: the eight slots 2c, 2c + 1, .. of a quarter warp in different banks
   static __device__ __forceinline__ int at_v(int i) { return ((i & ~7) | ((i & 7) ^ (D == 128 ? ((i >> 3) & 3) << 1 : ((i >> 3) & 1) << 1))) << 4; }
 };
@@ -214,8 +216,10 @@ struct WarpUnit {
   float o[D / 16][4];
   float m[2], l[2], x[2];   // maxima; sums of the rounded weights, which O has, and of the exact ones, which lse and the account want
 
+  struct Asked {};
+  static __device__ __forceinline__ void ask(const PagedParams &, int, int, Asked &) {}
   template <typename S>
-  __device__ __forceinline__ void begin(const PagedParams &p, S &, int b, int g) {
+  __device__ __forceinline__ void begin(const PagedParams &p, S &, int b, int g, const Asked &) {
     const int lane = threadIdx.x & 31, h = lane >> 2;
     const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + size_t(b) * size_t(p.q_stride) + size_t(g * G + h) * D + (lane & 3) * 2;
 #pragma unroll
@@ -336,17 +340,24 @@ struct WarpUnit<Codes<TILE>, D, G> {
   float fq[2], qs[2];       // 2^(133 - s) and sum q, in the scores' unit
   float fw;                 // 2^w; 0: no tile with a step yet
 
-  template <typename S>
-  __device__ __forceinline__ void begin(const PagedParams &p, S &, int b, int g) {
+  static constexpr int F = D / 4;   // features of a lane in a dot product
+  struct Asked {
+    uint4 w[F / 8];
+  };
+  static __device__ __forceinline__ void ask(const PagedParams &p, int b, int g, Asked &a) {
     const int lane = threadIdx.x & 31, h = lane >> 2;
-    constexpr int F = D / 4;   // features of a lane
     const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + size_t(b) * size_t(p.q_stride) +
                                                        size_t(g * G + h) * D + (lane & 3) * F);
+#pragma unroll
+    for (int j = 0; j < F / 8; ++j) a.w[j] = h < G ? src[j] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  template <typename S>
+  __device__ __forceinline__ void begin(const PagedParams &p, S &, int, int, const Asked &asked) {
+    const int lane = threadIdx.x & 31;
+    const uint4(&w)[F / 8] = asked.w;
     float sum = 0.f, top = 0.f;
-    uint4 w[F / 8];
 #pragma unroll
     for (int j = 0; j < F / 8; ++j) {
-      w[j] = h < G ? src[j] : make_uint4(0u, 0u, 0u, 0u);
       const uint32_t x4[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -551,8 +562,10 @@ struct WarpUnit<float, D, G> {
   static constexpr int E = D / 32;
   float o[G][E], m[G], l[G];
 
+  struct Asked {};
+  static __device__ __forceinline__ void ask(const PagedParams &, int, int, Asked &) {}
   template <typename S>
-  __device__ __forceinline__ void begin(const PagedParams &p, S &sm, int b, int g) {
+  __device__ __forceinline__ void begin(const PagedParams &p, S &sm, int b, int g, const Asked &) {
     // (every warp of the CTA comes here at the same unit, behind the meeting of the one before)
     for (int i = threadIdx.x; i < G * D; i += Shape<float, D>::kWarps * 32)
       sm.q[i / D][i % D] = reinterpret_cast<const float *>(p.q)[size_t(b) * size_t(p.q_stride) + size_t(g * G + i / D) * D + i % D] * p.scale_log2;
@@ -841,7 +854,12 @@ __global__ void __launch_bounds__(Shape<C, D>::kWarps * 32, 1) paged_decode_kern
   };
 
   // the first unit's queries, before the tiles that they would wait behind
-  if (lo < hi && warp == 0) {
+  typename WarpUnit<C, D, G>::Asked asked;
+  if (kCodes && lo < hi) {
+    const int b = seq_of(sm.prefix, p.batch, lo);
+    WarpUnit<C, D, G>::ask(p, b, (lo - sm.prefix[b]) / ((sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv), asked);
+  }
+  if (!kCodes && lo < hi && warp == 0) {
     const int b = seq_of(sm.prefix, p.batch, lo), g = (lo - sm.prefix[b]) / ((sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv);
     if (lane < G * Sh::kRowBytes / 128)
       asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char *>(reinterpret_cast<const T *>(p.q) + size_t(b) * size_t(p.q_stride) + size_t(g) * G * D) + lane * 128));
@@ -879,7 +897,8 @@ __global__ void __launch_bounds__(Shape<C, D>::kWarps * 32, 1) paged_decode_kern
     const int b = seq_of(sm.prefix, p.batch, at), n = (sm.prefix[b + 1] - sm.prefix[b]) / p.Hkv, g = (at - sm.prefix[b]) / n;
     const int t0 = sm.prefix[b] + g * n, end = min(hi, t0 + n);
     WarpUnit<C, D, G> unit;
-    unit.begin(p, sm, b, g);
+    if (at != lo) WarpUnit<C, D, G>::ask(p, b, g, asked);
+    unit.begin(p, sm, b, g, asked);
     float *scores = keep ? p.logits + size_t(b * p.Hkv + g) * size_t(p.most) * G : nullptr;
 #pragma unroll 1
     while (lo + warp + cur * kWarps < end) {
@@ -906,10 +925,10 @@ __global__ void __launch_bounds__(Shape<C, D>::kWarps * 32, 1) paged_decode_kern
     }
     unit.scale(factor);
     constexpr int kSlots = Smem<C, D, G>::kSlots;
-    if (warp >= kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - (kWarps - kSlots)][h][c] = x; });
+    if (warp >= kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp - (kWarps - kSlots)][h][Sh::at_o(c)] = x; });
     __syncthreads();
     if (kSlots < kWarps) {
-      if (warp < kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][c] += x; });
+      if (warp < kWarps - kSlots) unit.each([&](int h, int c, float x) { sm.o[warp][h][Sh::at_o(c)] += x; });
       __syncthreads();
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
@@ -920,7 +939,7 @@ __global__ void __launch_bounds__(Shape<C, D>::kWarps * 32, 1) paged_decode_kern
       const int h = i / D, c = i - h * D;   // (the same head in all lanes)
       float x = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) x += sm.o[s][h][c];
+      for (int s = 0; s < kSlots; ++s) x += sm.o[s][h][Sh::at_o(c)];
       const float f = __shfl_sync(0xffffffffu, inv, h);
       if (whole)
         from_f32(reinterpret_cast<T *>(p.out) + size_t(b) * size_t(p.out_stride) + size_t(g * G + h) * D + c, x * f);
