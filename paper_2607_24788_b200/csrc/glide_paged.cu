@@ -68,18 +68,32 @@ __global__ void __launch_bounds__(kWarps * 32) paged_join_kernel(const __grid_co
   float M = -CUDART_INF_F, L = 0.f, X = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int s = 0; s < splits; ++s) M = fmaxf(M, split_record(p, D, s, size_t(r), head)[D]);
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const float *rec = split_record(p, D, s, size_t(r), head);
-    const float4 tail = *reinterpret_cast<const float4 *>(rec + D);
-    if (tail.x == -CUDART_INF_F && tail.y == 0.f) continue;   // nothing seen there (and nothing of O written)
-    const float f = tail.x == -CUDART_INF_F ? 1.f : exp2f(tail.x - M);
-    float x[E];
-    load_elems<float, E>(rec + lane * E, x);
-    L = fmaf(tail.y, f, L), X = fmaf(tail.z, f, X);
+  // (what stands behind the records' O, a lane each, asked for together; up to 64 of them)
+  float4 tail[2];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(x[e], f, o[e]);
+  for (int i = 0; i < 2; ++i) {
+    const int s = i * 32 + lane;
+    tail[i] = s < splits ? *reinterpret_cast<const float4 *>(split_record(p, D, s, size_t(r), head) + D) : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+    M = fmaxf(M, tail[i].x);
+  }
+  M = warp_max(M);
+#pragma unroll 1
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    float x[8][E];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s0 + i < splits) load_elems<float, E>(split_record(p, D, s0 + i, size_t(r), head) + lane * E, x[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + i;
+      const float4 &mine = s0 < 32 ? tail[0] : tail[1];
+      const float tx = __shfl_sync(0xffffffffu, mine.x, s & 31), ty = __shfl_sync(0xffffffffu, mine.y, s & 31), tz = __shfl_sync(0xffffffffu, mine.z, s & 31);
+      if (s >= splits || (tx == -CUDART_INF_F && ty == 0.f)) continue;   // nothing seen there (and nothing of O written)
+      const float f = tx == -CUDART_INF_F ? 1.f : exp2f(tx - M);
+      L = fmaf(ty, f, L), X = fmaf(tz, f, X);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(x[i][e], f, o[e]);
+    }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   bool fine = true;

@@ -7,7 +7,8 @@
 //                         and mantissa, moved to where a double has them, are 2^-896 times the float (subnormal ones too); the queries are
 //                         multiplied by 2^448, so all scores by 2^-448.  Pages with a bound that is no number are computed once more by the
 //                         formula.  The bounds of the newest page take in the new key on the way.
-//   paged_pick_kernel     a block per (sequence, KV head): the n_picks largest by radix selection, equal ones by their place, written in order
+//                         The block that is the last of its (sequence, KV head) then picks the n_picks largest by radix selection, equal ones by
+//                         their place, and writes them in order.  (A kernel of its own for that: 4 us more.)
 // Bound: the bounds' bytes (2 / page_size of the keys'); of short caches the launches.
 #include <algorithm>
 #include <type_traits>
@@ -20,8 +21,10 @@ namespace {
 
 constexpr int kScoreThreads = 256;
 constexpr int kScorePages = kScoreThreads / 4;   // pages that a block looks at at once
-constexpr int kPickThreads = 512;
+constexpr int kScoreBlocks = 3;                  // blocks of an SM
 constexpr int kBins = 2048, kDigit = 11;
+constexpr int kHeld = 16;              // keys that a thread holds while they are looked through: of up to 4096 pages
+constexpr int kFew = 96;               // candidates among which each one's place is counted
 
 // scores as whole numbers in their order; NaN the largest
 __device__ __forceinline__ unsigned long long score_key(double x) {
@@ -61,11 +64,140 @@ __device__ __forceinline__ void load_bits(const T *src, uint32_t (&x)[8]) {
   }
 }
 
+struct PickSmem {
+  int bins[kBins];
+  unsigned long long bits_and[kScoreThreads / 32], bits_or[kScoreThreads / 32];
+  unsigned long long some[kFew];   // the candidates that are left, when they are few
+  int warp_sums[kScoreThreads / 32];
+  int n_some, bin, before;
+};
+
+// The sum of x over the threads before this one; total: over all
+__device__ __forceinline__ int scan_block(int x, int *warp_sums, int &total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int inc = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = inc;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kScoreThreads / 32; ++w) {
+    const int s = warp_sums[w];
+    if (w < warp) before += s;
+    total += s;
+  }
+  return before + inc - x;
+}
+
+// The choice of one (sequence, KV head) with more than n_picks pages, whose keys stand in memory; a block.
+__device__ __noinline__ void pick_pages(const PagedParams &p, PickSmem &sm, const SeqPages &s, const unsigned long long *keys, int32_t *out) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int c0 = s.sinks, c1 = s.n - 1;   // the columns to choose from, a run of them for each thread
+  const int per = (c1 - c0 + kScoreThreads - 1) / kScoreThreads, i0 = min(c1, c0 + tid * per), i1 = min(c1, i0 + per);
+  unsigned long long held[kHeld];         // their keys, where they are few enough
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) held[k] = per <= kHeld && i0 + k < i1 ? __ldcg(keys + i0 + k) : 0ull;
+  auto each = [&](auto &&f) {             // f(key, column) in order
+    if (per <= kHeld) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k)
+        if (i0 + k < i1) f(held[k], i0 + k);
+    } else {
+#pragma unroll 4
+      for (int i = i0; i < i1; ++i) f(__ldcg(keys + i), i);
+    }
+  };
+  int need = p.n_picks - 1 - s.sinks;     // of them; fewer than there are
+  // The least key that is chosen, and how many of those that equal it: digits from the first bit on that not all keys share
+  unsigned long long least = ~0ull;
+  int equal = 0;
+  if (need > 0) {
+    unsigned long long common = ~0ull, any = 0ull;
+    each([&](unsigned long long k, int) { common &= k, any |= k; });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) common &= __shfl_xor_sync(0xffffffffu, common, o), any |= __shfl_xor_sync(0xffffffffu, any, o);
+    if (lane == 0) sm.bits_and[warp] = common, sm.bits_or[warp] = any;
+    __syncthreads();
+    common = ~0ull, any = 0ull;
+#pragma unroll
+    for (int w = 0; w < kScoreThreads / 32; ++w) common &= sm.bits_and[w], any |= sm.bits_or[w];
+    int low = 64 - __clzll(common ^ any);   // bits below this one differ (0: none does)
+    unsigned long long prefix = low == 64 ? 0ull : common >> low << low;   // the digits so far
+    int left = c1 - c0;                     // keys with that prefix
+    while (low > 0 && left > kFew) {
+      const int shift = max(0, low - kDigit), width = low - shift;
+      for (int i = tid; i < kBins; i += kScoreThreads) sm.bins[i] = 0;
+      __syncthreads();
+      each([&](unsigned long long k, int) {
+        if (low == 64 || (k ^ prefix) >> low == 0) atomicAdd(&sm.bins[int(k >> shift) & ((1 << width) - 1)], 1);
+      });
+      __syncthreads();
+      // bins from the largest digit down, four for each thread
+      constexpr int kEach = kBins / kScoreThreads;
+      int mine[kEach], sum = 0, total;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) sum += mine[e] = sm.bins[kBins - 1 - (tid * kEach + e)];
+      int before = scan_block(sum, sm.warp_sums, total);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        if (before < need && before + mine[e] >= need) sm.bin = kBins - 1 - (tid * kEach + e), sm.before = before, sm.n_some = mine[e];
+        before += mine[e];
+      }
+      __syncthreads();
+      prefix |= static_cast<unsigned long long>(sm.bin) << shift;
+      need -= sm.before;
+      left = sm.n_some;
+      low = shift;
+      __syncthreads();
+    }
+    if (low == 0) {
+      least = prefix, equal = need;
+    } else {   // few are left: each one's place among them
+      if (tid == 0) sm.n_some = 0;
+      __syncthreads();
+      each([&](unsigned long long k, int) {
+        if (low == 64 || (k ^ prefix) >> low == 0) sm.some[atomicAdd(&sm.n_some, 1)] = k;
+      });
+      __syncthreads();
+      if (tid < left) {
+        const unsigned long long k = sm.some[tid];
+        int larger = 0, same = 0;
+        for (int i = 0; i < left; ++i) larger += sm.some[i] > k, same += sm.some[i] == k;
+        // (threads with the same key write the same)
+        if (larger < need && larger + same >= need) sm.bits_and[0] = k, sm.before = need - larger;
+      }
+      __syncthreads();
+      least = sm.bits_and[0], equal = sm.before;
+    }
+  }
+  // in order
+  int same = 0, larger = 0, total;
+  if (equal) each([&](unsigned long long k, int) { larger += k > least, same += k == least; });
+  const int same_before = scan_block(same, sm.warp_sums, total);
+  int at = s.sinks + scan_block(larger, sm.warp_sums, total) + min(same_before, equal), ties = same_before;
+  if (equal)
+    each([&](unsigned long long k, int i) {
+      const bool tie = k == least;
+      if (k > least || (tie && ties < equal)) out[at++] = i;
+      ties += tie;
+    });
+  for (int i = tid; i < s.sinks; i += kScoreThreads) out[i] = i;
+  if (tid == 0) out[p.n_picks - 1] = c1;
+}
+
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid_constant__ PagedParams p, T *bounds, unsigned long long *keys, int parts) {
+__global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) paged_score_kernel(const __grid_constant__ PagedParams p, T *bounds, unsigned long long *keys, int32_t *picks, int parts) {
   constexpr int kPieces = D / 8;
   // queries times 2^448; a piece takes 80 bytes, so that four threads' pieces lie in different banks
   __shared__ __align__(16) double q[G][kPieces][10];
+  __shared__ PickSmem pick;
+  __shared__ int last;
   const int tid = threadIdx.x, seg = tid & 3;
   const int u = int(blockIdx.x) / parts, part = int(blockIdx.x) - u * parts, b = u / p.Hkv, g = u - b * p.Hkv;
   wait_for_predecessor();
@@ -79,7 +211,6 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
     q[i / D][i % D / 8][i % 8] = double(x) * 0x1p448;
   }
   fine = __syncthreads_and(fine);
-  dependents_may_start();
   if (part == 0 && tid < D / 8 && len > 0) {   // the newest page's bounds
     const int page = paged_page(p, b, len - 1);
     if (page >= 0) {
@@ -96,19 +227,25 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
       }
     }
   }
-  if (s.n <= p.n_picks) return;   // all of them are chosen
+  int32_t *mine = picks + size_t(u) * size_t(p.n_picks);
+  if (s.n <= p.n_picks) {         // all of them are chosen
+    for (int i = tid; part == 0 && i < p.n_picks; i += kScoreThreads) mine[i] = i < s.n ? i : -1;
+    return;
+  }
   unsigned long long *out = keys + size_t(u) * size_t(p.n_cols);
-  for (int at = s.sinks + part * kScorePages; at < s.n - 1; at += parts * kScorePages) {
-    const int col = at + (tid >> 2);
+  const int32_t *table = p.table + size_t(b) * size_t(p.table_stride);
+  int col = s.sinks + part * kScorePages + (tid >> 2), next = col < s.n - 1 ? table[col] : -1;
+  for (int at = s.sinks + part * kScorePages; at < s.n - 1; at += parts * kScorePages, col += parts * kScorePages) {
     const bool there = col < s.n - 1;
-    int page = there ? p.table[size_t(b) * size_t(p.table_stride) + col] : -1;
+    int page = next;
+    next = col + parts * kScorePages < s.n - 1 ? table[col + parts * kScorePages] : -1;
     if (unsigned(page) >= unsigned(p.n_pages)) {
       if (there) atomicExch(p.status, kDevBadPage);
       page = 0;   // (memory of the pool)
     }
     const T *low = bounds + (size_t(page) * p.Hkv + g) * 2 * D;
     double sum[G];
-    uint32_t top = 0u;
+    float odd_sum = 0.f;   // NaN if a bound is no number
 #pragma unroll
     for (int h = 0; h < G; ++h) sum[h] = 0.0;
 #pragma unroll
@@ -118,7 +255,7 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
       load_bits(low + piece * 8, lo), load_bits(low + D + piece * 8, hi);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        top = max(top, max(lo[e] & 0x7fffffffu, hi[e] & 0x7fffffffu));
+        odd_sum = fmaf(__uint_as_float(lo[e]), 0.f, fmaf(__uint_as_float(hi[e]), 0.f, odd_sum));
         const double l = shifted(lo[e]), m = shifted(hi[e]);
 #pragma unroll
         for (int h = 0; h < G; ++h) {
@@ -127,7 +264,7 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
         }
       }
     }
-    bool odd = !fine || top >= 0x7f800000u;
+    bool odd = !fine || odd_sum != 0.f;
     odd = __shfl_xor_sync(0xffffffffu, int(odd), 1) || odd;
     odd = __shfl_xor_sync(0xffffffffu, int(odd), 2) || odd;
     if (__any_sync(0xffffffffu, odd)) {
@@ -155,134 +292,16 @@ __global__ void __launch_bounds__(kScoreThreads) paged_score_kernel(const __grid
     }
     if (there && seg == 0) out[col] = score_key(best);
   }
-}
-
-struct PickSmem {
-  int bins[kBins];
-  unsigned long long bits_and[kPickThreads / 32], bits_or[kPickThreads / 32];
-  unsigned long long some[kPickThreads];   // the candidates that are left, when they are few
-  int warp_sums[kPickThreads / 32];
-  int n_some, bin, before;
-};
-
-// The sum of x over the threads before this one; total: over all
-__device__ __forceinline__ int scan_block(int x, int *warp_sums, int &total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int inc = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += y;
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    last = atomicAdd(&p.tickets[u], 1) == parts - 1;
+    if (last) p.tickets[u] = 0;   // as the next call wants it: nobody else comes
+    __threadfence();
   }
   __syncthreads();
-  if (lane == 31) warp_sums[warp] = inc;
-  __syncthreads();
-  int before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kPickThreads / 32; ++w) {
-    const int s = warp_sums[w];
-    if (w < warp) before += s;
-    total += s;
-  }
-  return before + inc - x;
-}
-
-__global__ void __launch_bounds__(kPickThreads) paged_pick_kernel(const __grid_constant__ PagedParams p, const unsigned long long *all_keys, int32_t *picks) {
-  __shared__ PickSmem sm;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, u = int(blockIdx.x), b = u / p.Hkv;
-  wait_for_predecessor();
+  if (last) pick_pages(p, pick, s, out, mine);
   dependents_may_start();
-  const SeqPages s = pages_of(p, paged_len(p, b));
-  int32_t *out = picks + size_t(u) * size_t(p.n_picks);
-  if (s.n <= p.n_picks) {
-    for (int i = tid; i < p.n_picks; i += kPickThreads) out[i] = i < s.n ? i : -1;
-    return;
-  }
-  const unsigned long long *keys = all_keys + size_t(u) * size_t(p.n_cols);
-  const int c0 = s.sinks, c1 = s.n - 1;   // the columns to choose from
-  int need = p.n_picks - 1 - s.sinks;     // of them; fewer than there are
-  // The least key that is chosen, and how many of those that equal it: digits from the first bit on that not all keys share
-  unsigned long long least = ~0ull;
-  int equal = 0;
-  if (need > 0) {
-    unsigned long long common = ~0ull, any = 0ull;
-    for (int i = c0 + tid; i < c1; i += kPickThreads) common &= keys[i], any |= keys[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) common &= __shfl_xor_sync(0xffffffffu, common, o), any |= __shfl_xor_sync(0xffffffffu, any, o);
-    if (lane == 0) sm.bits_and[warp] = common, sm.bits_or[warp] = any;
-    __syncthreads();
-    common = ~0ull, any = 0ull;
-#pragma unroll
-    for (int w = 0; w < kPickThreads / 32; ++w) common &= sm.bits_and[w], any |= sm.bits_or[w];
-    int low = 64 - __clzll(common ^ any);   // bits below this one differ (0: none does)
-    unsigned long long prefix = low == 64 ? 0ull : common >> low << low;   // the digits so far
-    int left = c1 - c0;                     // keys with that prefix
-    while (low > 0 && left > kPickThreads) {
-      const int shift = max(0, low - kDigit), width = low - shift;
-      for (int i = tid; i < kBins; i += kPickThreads) sm.bins[i] = 0;
-      __syncthreads();
-      for (int i = c0 + tid; i < c1; i += kPickThreads) {
-        const unsigned long long k = keys[i];
-        if (low == 64 || (k ^ prefix) >> low == 0) atomicAdd(&sm.bins[int(k >> shift) & ((1 << width) - 1)], 1);
-      }
-      __syncthreads();
-      // bins from the largest digit down, four for each thread
-      constexpr int kEach = kBins / kPickThreads;
-      int mine[kEach], sum = 0, total;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) sum += mine[e] = sm.bins[kBins - 1 - (tid * kEach + e)];
-      int before = scan_block(sum, sm.warp_sums, total);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        if (before < need && before + mine[e] >= need) sm.bin = kBins - 1 - (tid * kEach + e), sm.before = before, sm.n_some = mine[e];
-        before += mine[e];
-      }
-      __syncthreads();
-      prefix |= static_cast<unsigned long long>(sm.bin) << shift;
-      need -= sm.before;
-      left = sm.n_some;
-      low = shift;
-      __syncthreads();
-    }
-    if (low == 0) {
-      least = prefix, equal = need;
-    } else {   // few are left: each one's place among them
-      if (tid == 0) sm.n_some = 0;
-      __syncthreads();
-      for (int i = c0 + tid; i < c1; i += kPickThreads) {
-        const unsigned long long k = keys[i];
-        if (low == 64 || (k ^ prefix) >> low == 0) sm.some[atomicAdd(&sm.n_some, 1)] = k;
-      }
-      __syncthreads();
-      if (tid < left) {
-        const unsigned long long k = sm.some[tid];
-        int larger = 0, same = 0;
-        for (int i = 0; i < left; ++i) larger += sm.some[i] > k, same += sm.some[i] == k;
-        // (threads with the same key write the same)
-        if (larger < need && larger + same >= need) sm.bits_and[0] = k, sm.before = need - larger;
-      }
-      __syncthreads();
-      least = sm.bits_and[0], equal = sm.before;
-    }
-  }
-  // in order: a run of columns for each thread
-  const int per = (c1 - c0 + kPickThreads - 1) / kPickThreads, i0 = min(c1, c0 + tid * per), i1 = min(c1, i0 + per);
-  int same = 0, larger = 0, total;
-  if (equal)
-    for (int i = i0; i < i1; ++i) larger += keys[i] > least, same += keys[i] == least;
-  const int same_before = scan_block(same, sm.warp_sums, total);
-  int at = s.sinks + scan_block(larger, sm.warp_sums, total) + min(same_before, equal), ties = same_before;
-  if (equal) {
-    for (int i = i0; i < i1; ++i) {
-      const unsigned long long k = keys[i];
-      const bool tie = k == least;
-      if (k > least || (tie && ties < equal)) out[at++] = i;
-      ties += tie;
-    }
-  }
-  for (int i = tid; i < s.sinks; i += kPickThreads) out[i] = i;
-  if (tid == 0) out[p.n_picks - 1] = c1;
 }
 
 }  // namespace
@@ -293,11 +312,10 @@ int launch_paged_select(const glide_paged *h, const PagedParams &p, void *bounds
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     const int units = p.batch * p.Hkv;
     const int64_t cols = std::min<int64_t>(p.n_cols, ((int64_t(p.most) - 1) >> p.page_shift) + 1);
-    // blocks of a unit: one for every 64 pages, but no more than the chip has places for
-    const int parts = int(std::max<int64_t>(1, std::min<int64_t>((cols + kScorePages - 1) / kScorePages, (int64_t(p.sm_count) * 8 + units - 1) / units)));
+    // blocks of a unit: one for every 64 pages, but no more than the chip has places for (to begin, a block takes as long as for 64 pages)
+    const int parts = int(std::max<int64_t>(1, std::min<int64_t>((cols + kScorePages - 1) / kScorePages, int64_t(p.sm_count) * kScoreBlocks / units)));
     unsigned long long *keys = reinterpret_cast<unsigned long long *>(scores);
-    const int rc = launch_status(launch_chained(paged_score_kernel<T, D, G>, unsigned(units * parts), kScoreThreads, 0, st, p, reinterpret_cast<T *>(bounds), keys, parts));
-    return rc ? rc : launch_status(launch_chained(paged_pick_kernel, unsigned(units), kPickThreads, 0, st, p, static_cast<const unsigned long long *>(keys), picks));
+    return launch_status(launch_chained(paged_score_kernel<T, D, G>, unsigned(units * parts), kScoreThreads, 0, st, p, reinterpret_cast<T *>(bounds), keys, picks, parts));
   });
 }
 

@@ -42,6 +42,7 @@ constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
 constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
+constexpr int kFar = 4;               // (pages in 4 bits) how many tiles ahead L2 is told
 constexpr int kLevelWarp = 19, kCodeThreads = 640, kUnpackWarps = 8, kRawStages = 2;   // pages in 4 bits
 // How far (in the exponent) scores may exceed a row's reference before it moves.  Weights, sums and O are floating numbers: the reference only
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
@@ -910,6 +911,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       if (w.seq < 0) break;
       set_work(w);
       int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
+      int far = CODES && kFar < n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(kFar), pieces, rows) : -1;
       // The first tiles may come while the piece before is still being written out, Q_X when its rows have been.
       auto ask_q = [&](int x) {
         if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed, moves));
@@ -932,6 +934,16 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       for (int k = 0; k < n_tiles && ok; ++k) {
         const int j0 = kt.slot(k), page = piece_page(p, next, tq0, tq_last, j0, pieces, rows, none);
         if (k + 1 < n_tiles) next = piece_entry(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows);
+        if constexpr (CODES) {   // a later tile's codes to L2 (a lane per piece): the buffers hold one tile of each kind
+          if (k + kFar < n_tiles && unsigned(far) < unsigned(p.n_pages)) {
+            const int off = (kt.slot(k + kFar) + lane * rows) & ((1 << p.page_shift) - 1);
+            const size_t at = size_t(far) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + size_t(off) * (D / 2);
+            const uint32_t bytes = uint32_t(rows) * (D / 2);
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const unsigned char *>(p.k) + at), "r"(bytes) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const unsigned char *>(p.v) + at), "r"(bytes) : "memory");
+          }
+          far = k + 1 + kFar < n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(k + 1 + kFar), pieces, rows) : -1;
+        }
 #pragma unroll 1
         for (int is_v = 0; is_v < 2 && ok; ++is_v) {
           const int job = jobs + 2 * k + is_v, slot = job % S;
