@@ -64,16 +64,18 @@ template <int D, bool CODES>
 struct PrefillSmem {
   static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
   static constexpr int kStages = CODES ? (D == 128 ? 4 : 6) : D == 128 ? 5 : 8;
-  static constexpr int kRaw = CODES ? kRawStages : 1, kRawKeys = kKT * (D / 2 + 2 * kLevelBytes);   // (with the keys come their and the values' levels)
+  static constexpr int kRaw = CODES ? kRawStages : 1, kRawBytes = kKT * D / 2;
   unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
   unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
-  alignas(16) unsigned char raw[CODES ? kRawKeys + kKT * D / 2 : 16];   // pages in 4 bits: a key tile's codes and levels; a value tile's codes
+  alignas(16) unsigned char raw[CODES ? kRaw * kRawBytes : 16];   // pages in 4 bits: a key tile's codes; a value tile's codes
+  alignas(16) uint32_t levels[CODES ? 2 : 1][CODES ? 2 * kKT : 4];  // of two key tiles and the value tiles behind them
+  uint64_t bar_lev[2];                   // they have landed (a tile's levels have been read when its codes have, before those of the tile after next come)
   uint64_t bar_raw[kRaw], bar_rawfree[kRaw];        // they have landed; the unpacking warps have read them
-  uint32_t raw_pieces[kRaw];             // bit i: piece i of the tile has been loaded
+  uint32_t pieces[4];                    // bit i: piece i of the tile has been loaded
   // the four further columns of Q_A, Q_B and of the key tiles, 16 bytes a row (a key tile's as long as its buffer), and the zeros that make them 16
   alignas(128) unsigned char more_q[CODES ? 2 : 1][CODES ? kRows * 16 : 16], more_k[CODES ? kStages / 2 : 1][CODES ? kKT * 16 : 16], zeros[CODES ? kRows * 16 : 16];
   float k_undo[4], v_undo[4];            // what undoes the last tiles' scales (read until the row tiles have the next one's scores)
-  uint2 steps[6][CODES ? kKT : 1];       // per slot, as fp16 pairs: 2^24 steps as the tile is scaled, what is added; of two key tiles, of four value tiles
+  uint2 steps[5][CODES ? kKT : 1];       // per slot, as fp16 pairs: 2^24 steps as the tile is scaled, what is added; of two key tiles, of three value tiles
   uint64_t bar_levels[4];                // all this of a key tile and the value tile behind it stands here (B may be two tiles behind warp 19)
   uint64_t bar_qmade[2];                 // Q_X is in fp16 (one arrival per warp)
   uint64_t bar_full[kStages];            // the buffer's K or V tile has landed (pages in 4 bits: has been made, one arrival per warp)
@@ -340,6 +342,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&sm.bar_levels[s]), 1);
     if (CODES)
       for (int s = 0; s < R; ++s) {
+        mbar_init(smem_u32(&sm.bar_lev[s]), 1);
         mbar_init(smem_u32(&sm.bar_raw[s]), 1), mbar_init(smem_u32(&sm.bar_rawfree[s]), kUnpackWarps);
         mbar_init(smem_u32(&sm.bar_qmade[s]), kSoftmaxThreads / 32 / 2);
       }
@@ -647,12 +650,10 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if (ok) ok = mbar_wait_long(smem_u32(&bar), phase & 1u, failed, moves);
         ok = __all_sync(0xffffffffu, ok);
       };
-      wait(sm.bar_levels[tile & 3], tile >> 2);     // (of keys their codes are there too then, and the buffer is free)
-      if (X) {
-        wait(sm.bar_raw[from], job / R);
-        if (job >= S) wait(sm.bar_free[slot], job / S - 1u);
-      }
-      if (ok) unpack_tile<D>(sm.kv[slot], sm.raw + from * Sm::kRawKeys, sm.steps[X ? 2 + (tile & 3) : tile & 1]);
+      wait(sm.bar_levels[tile & 3], tile >> 2);     // (a key tile's buffer is free too then)
+      wait(sm.bar_raw[from], job / R);
+      if (X && job >= S) wait(sm.bar_free[slot], job / S - 1u);
+      if (ok) unpack_tile<D>(sm.kv[slot], sm.raw + from * Sm::kRawBytes, sm.steps[X ? 2 + tile % 3u : tile & 1]);
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
@@ -716,7 +717,9 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
           const float undo = *const_cast<volatile float *>(&sm.v_undo[tile]), ratio = before < 0 ? 1.f : v_undo / undo;
           scale = q_undo * *const_cast<volatile float *>(&sm.k_undo[tile]);
           v_undo = undo;
-          if (whole) soft_half(std::false_type{}, v, before < 0, ratio);
+          // (32 rows of no token: whatever their weights are, nobody reads what comes of them.  8 tokens behind 131072, 32 / 8 heads, fill one warp of the four.)
+          if ((row & ~31) >= ntokX * G) hand_over();
+          else if (whole) soft_half(std::false_type{}, v, before < 0, ratio);
           else soft_half(std::true_type{}, v, before < 0, ratio);
         } else if (move) {
           soft_tile_masked(v, before < 0);
@@ -869,12 +872,12 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
   #pragma unroll 1
         for (int k = 0; k < n_tiles; ++k) {
           const int job = jobs + 2 * k, tile = job >> 1, j0 = kt.slot(k);
-          ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_raw[0]), uint32_t(tile) & 1u, failed, moves));
-          // (the further columns of the tile that had the buffer are free when that is)
+          ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_lev[tile & 1]), uint32_t(tile >> 1) & 1u, failed, moves));
+          // (the steps and the further columns of the tile that had the buffer are free when that is)
           if (ok && job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[job % S]), uint32_t(job / S - 1) & 1u, failed, moves));
           if (!ok) break;
-          const TileRows rows{*const_cast<volatile uint32_t *>(&sm.raw_pieces[0]), min(p.page_shift, 7), p.window < 0 ? 0 : tq0 - p.window + 1 - j0, tq_last + 1 - j0, p.n_sink - j0};
-          make_levels(reinterpret_cast<const uint32_t *>(sm.raw + kKT * (D / 2)), rows, v_scale, &sm.k_undo[tile & 3], &sm.v_undo[tile & 3], sm.steps[tile & 1], sm.steps[2 + (tile & 3)],
+          const TileRows rows{*const_cast<volatile uint32_t *>(&sm.pieces[tile & 3]), min(p.page_shift, 7), p.window < 0 ? 0 : tq0 - p.window + 1 - j0, tq_last + 1 - j0, p.n_sink - j0};
+          make_levels(sm.levels[tile & 1], rows, v_scale, &sm.k_undo[tile & 3], &sm.v_undo[tile & 3], sm.steps[tile & 1], sm.steps[2 + tile % 3],
                       sm.more_k[tile % (S / 2)]);
           fence_async_smem();
           __syncwarp();
@@ -889,6 +892,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const int tiles = count_tiles(p, TOKC), total = tiles * p.Hkv * parts;
     bool ok = true;
     AskedCopies asked;                             // Q, K and V tiles, tails so far
+    int asked_levels = 0;                          // tiles whose levels have been asked for
     uint32_t n_use[2] = {0, 0};                    // pieces with rows in X
     int drawn = 0;
     if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
@@ -952,12 +956,30 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             const int to = job % R;
             if (job >= R) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_rawfree[to]), uint32_t(job / R - 1) & 1u, failed, moves));
             if (!ok) break;
-            const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && page != none);
-            const uint32_t raw = smem_u32(sm.raw + to * Sm::kRawKeys), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2), levels = uint32_t(rows) * kLevelBytes;
-            if (leader) {
-              sm.raw_pieces[to] = there;
-              mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * (is_v ? codes : codes + 2 * levels));
+            // the levels of this tile (of the first of a piece) and of the next one
+            for (int ahead = k == 0 ? 0 : 1; ahead < 2 && !is_v && k + ahead < n_tiles; ++ahead) {
+              const int tile = (job >> 1) + ahead, j1 = kt.slot(k + ahead), pg = ahead ? piece_page(p, next, tq0, tq_last, j1, pieces, rows, none) : page;
+              const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && pg != none);
+              const uint32_t lev = smem_u32(sm.levels[tile & 1]), lev_bar = smem_u32(&sm.bar_lev[tile & 1]), bytes = uint32_t(rows) * kLevelBytes;
+              if (leader) {
+                sm.pieces[tile & 3] = there;
+                mbar_expect_tx(lev_bar, uint32_t(__popc(there)) * 2 * bytes);
+              }
+#pragma unroll 1
+              for (int i = 0; i < pieces; ++i) {
+                const int pi = __shfl_sync(0xffffffffu, pg, i);
+                if (leader && (there >> i) & 1u) {
+                  const size_t at = size_t(pi - p.page0) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + ((D / 2) << p.page_shift) +
+                                    ((j1 + i * rows) & ((1 << p.page_shift) - 1)) * kLevelBytes;
+                  bulk_load(lev + i * bytes, reinterpret_cast<const unsigned char *>(p.k) + at, bytes, lev_bar);
+                  bulk_load(lev + kKT * kLevelBytes + i * bytes, reinterpret_cast<const unsigned char *>(p.v) + at, bytes, lev_bar);
+                }
+              }
+              asked_levels = tile + 1;
             }
+            const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && page != none);
+            const uint32_t raw = smem_u32(sm.raw + to * Sm::kRawBytes), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2);
+            if (leader) mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * codes);
 #pragma unroll 1
             for (int i = 0; i < pieces; ++i) {
               const int pg = __shfl_sync(0xffffffffu, page, i);
@@ -965,12 +987,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
                 const int off = (j0 + i * rows) & ((1 << p.page_shift) - 1);
                 const unsigned char *block = reinterpret_cast<const unsigned char *>(is_v ? p.v : p.k) + size_t(pg - p.page0) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride);
                 bulk_load(raw + i * codes, block + off * (D / 2), codes, raw_bar);
-                const int at = ((D / 2) << p.page_shift) + off * kLevelBytes;
-                if (!is_v) {   // (with the keys' levels come the values')
-                  bulk_load(raw + kKT * (D / 2) + i * levels, block + at, levels, raw_bar);
-                  bulk_load(raw + kKT * (D / 2 + kLevelBytes) + i * levels, block + (reinterpret_cast<const unsigned char *>(p.v) - reinterpret_cast<const unsigned char *>(p.k)) + at, levels,
-                            raw_bar);
-                }
               }
             }
             ++asked.tiles;
@@ -1015,6 +1031,10 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
     }
     if (!ok) {   // after a time-out: no copy outlives the CTA
+      for (int tile = max(0, asked_levels - 2); CODES && tile < asked_levels; ++tile) {
+        int alone = 0;
+        mbar_wait(smem_u32(&sm.bar_lev[tile & 1]), uint32_t(tile >> 1) & 1u, &alone);
+      }
       wait_for_copies(asked, CODES ? R : S, [&](int what, int which, uint32_t parity) {
         int alone = 0;   // (whoever has given up)
         mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_q[which] : what == kCopyTile ? (CODES ? &sm.bar_raw[which] : &sm.bar_full[which]) : &sm.bar_tail), parity, &alone);
