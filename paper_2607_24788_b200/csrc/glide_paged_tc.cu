@@ -8,7 +8,7 @@
 //   warps 4-7, 12-15   softmax of tile B
 //   warps 16, 17       issue the tcgen05.mma of A and of B (one elected lane), in turns
 //   warp 18            draws and finds the work, loads Q, K and V by TMA, a box per page (or 128 slots of one) and 64 columns
-// Pages in 4 bits.  The loader fetches a tile's codes and levels, a piece per page, into a buffer for keys or one for values; the softmax
+// Pages in 4 bits.  The loader fetches a tile's codes, a piece per page, into a buffer for keys or one for values; the softmax
 // threads of A make the key tiles of them, two tiles ahead, those of B the value tiles, one ahead, when they have handed a tile's weights over and
 // would wait for its products.  (Four warps of their own: 862 us for 8001 tokens, 32 / 8 heads, of which 270 were waits for them.)
 //   A key is mid + step n with mid = low + 8 step and n = code - 8, -8 .. 7, three bits and a sign: step n is a number of 11
@@ -21,7 +21,8 @@
 // first tile on, until a tile has values four to eight times as large; then O is scaled as where a reference moves.  A key or value comes out of
 // one fused multiply-add for two codes where they lie in the word: four bits at the bottom of an fp16 number are code times its least
 // subnormal number, the next four 16 times that.  Which leaves the features of eight in the order 0 4 1 5 2 6 3 7, in keys, values, and so in
-// Q and O.  What a slot's codes are multiplied by, the scales and the further columns come from warp 19.
+// Q and O.  What a slot's codes are multiplied by, the scales and the further columns come from warp 19, which reads
+// the levels itself, a tile ahead.
 // Every mbarrier wait is bounded; on a time-out the CTA records kDevWaitTimeout, leaves its loops, frees its TMEM columns and returns.
 #include <algorithm>
 #include <cstring>
@@ -42,7 +43,6 @@ constexpr int kBoxBytes = 16384;      // 128 rows of 64 columns
 constexpr int kSoftmaxThreads = 512;
 constexpr int kThreads = 608;
 constexpr int kMmaWarp = 16, kLoadWarp = 18;   // (MMA warps: one per row tile)
-constexpr int kFar = 4;               // (pages in 4 bits) how many tiles ahead L2 is told
 constexpr int kLevelWarp = 19, kCodeThreads = 640, kUnpackWarps = 8, kRawStages = 2;   // pages in 4 bits
 // How far (in the exponent) scores may exceed a row's reference before it moves.  Weights, sums and O are floating numbers: the reference only
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
@@ -68,10 +68,7 @@ struct PrefillSmem {
   unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
   unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
   alignas(16) unsigned char raw[CODES ? kRaw * kRawBytes : 16];   // pages in 4 bits: a key tile's codes; a value tile's codes
-  alignas(16) uint32_t levels[CODES ? 2 : 1][CODES ? 2 * kKT : 4];  // of two key tiles and the value tiles behind them
-  uint64_t bar_lev[2];                   // they have landed (a tile's levels have been read when its codes have, before those of the tile after next come)
   uint64_t bar_raw[kRaw], bar_rawfree[kRaw];        // they have landed; the unpacking warps have read them
-  uint32_t pieces[4];                    // bit i: piece i of the tile has been loaded
   // the four further columns of Q_A, Q_B and of the key tiles, 16 bytes a row (a key tile's as long as its buffer), and the zeros that make them 16
   alignas(128) unsigned char more_q[CODES ? 2 : 1][CODES ? kRows * 16 : 16], more_k[CODES ? kStages / 2 : 1][CODES ? kKT * 16 : 16], zeros[CODES ? kRows * 16 : 16];
   float k_undo[4], v_undo[4];            // what undoes the last tiles' scales (read until the row tiles have the next one's scores)
@@ -262,23 +259,38 @@ __device__ __forceinline__ uint4 more_columns(float x, bool keys) {
 }
 
 // A tile of codes and levels becomes a tile of rows, 128-byte swizzle: keys as step n, with mid in more columns, both times a power of two of
-// the tile; values times one of the piece.  Slots that no query of the piece sees (by the window: of [lo, rows) and [0, sinks) some query sees
-// each) and those of pieces (of 2^piece_shift slots) that have not been loaded have levels 0, and so are 0.
-struct TileRows {
-  uint32_t pieces;
-  int piece_shift, lo, rows, sinks;
-  __device__ __forceinline__ bool has(int row) const { return row < rows && (row >= lo || row < sinks) && (pieces >> (row >> piece_shift)) & 1u; }
+// the tile; values times one of the piece.  Slots that no query of the piece sees have levels 0, and so are 0.
+// The levels of a key tile and of the value tile behind it, a lane has those of slots lane, lane + 32 ..; one warp.
+struct TileLevels {
+  uint32_t l[2][kKT / 32];
 };
-// The levels of a key tile and of the value tile behind it (levels [2][kKT]); one warp.
-__device__ __forceinline__ void make_levels(const uint32_t *levels, const TileRows &there, float &v_scale, float *k_undo, float *v_undo, uint2 *k_step, uint2 *v_step, unsigned char *more) {
+// Which pages they are on: -1 where no query of slots [q0, q1] sees the slot, or the id is bad (the loader records that)
+__device__ __forceinline__ void ask_entries(const PagedParams &p, int b, int q0, int q1, int j0, int (&entry)[kKT / 32]) {
+#pragma unroll
+  for (int i = 0; i < kKT / 32; ++i) {
+    const int slot = j0 + i * 32 + int(threadIdx.x & 31);
+    entry[i] = paged_seen_by(p, q0, q1, slot) ? p.table[size_t(b) * size_t(p.table_stride) + size_t(slot >> p.page_shift)] : -1;
+  }
+}
+template <int D>
+__device__ __forceinline__ void ask_levels(const PagedParams &p, int g, int j0, const int (&entry)[kKT / 32], TileLevels &t) {
+#pragma unroll
+  for (int i = 0; i < kKT / 32; ++i) {
+    const int off = (j0 + i * 32 + int(threadIdx.x & 31)) & ((1 << p.page_shift) - 1);
+    const size_t at = size_t(entry[i]) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + ((D / 2) << p.page_shift) + off * kLevelBytes;
+    const bool there = unsigned(entry[i]) < unsigned(p.n_pages);
+    t.l[0][i] = there ? *reinterpret_cast<const uint32_t *>(reinterpret_cast<const unsigned char *>(p.k) + at) : 0u;
+    t.l[1][i] = there ? *reinterpret_cast<const uint32_t *>(reinterpret_cast<const unsigned char *>(p.v) + at) : 0u;
+  }
+}
+__device__ __forceinline__ void make_levels(const TileLevels &t, float &v_scale, float *k_undo, float *v_undo, uint2 *k_step, uint2 *v_step, unsigned char *more) {
   const int lane = threadIdx.x & 31;
-  uint32_t l[2][kKT / 32], top[2] = {0u, 0u};
+  const auto &l = t.l;
+  uint32_t top[2] = {0u, 0u};
 #pragma unroll
   for (int which = 0; which < 2; ++which)
 #pragma unroll
     for (int i = 0; i < kKT / 32; ++i) {
-      const int row = i * 32 + lane;
-      l[which][i] = there.has(row) ? levels[which * kKT + row] : 0u;
       const float low = bf16_hi(l[which][i]), x = fmaxf(fabsf(low), fabsf(fmaf(15.f, bf16_lo(l[which][i]), low)));   // (a step is 2 / 15 of it at most)
       if (x < CUDART_INF_F) top[which] = max(top[which], __float_as_uint(x));   // (no NaN either)
     }
@@ -342,7 +354,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&sm.bar_levels[s]), 1);
     if (CODES)
       for (int s = 0; s < R; ++s) {
-        mbar_init(smem_u32(&sm.bar_lev[s]), 1);
         mbar_init(smem_u32(&sm.bar_raw[s]), 1), mbar_init(smem_u32(&sm.bar_rawfree[s]), kUnpackWarps);
         mbar_init(smem_u32(&sm.bar_qmade[s]), kSoftmaxThreads / 32 / 2);
       }
@@ -868,17 +879,24 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     if constexpr (CODES) {
       bool ok = true;
       for (int it = 0; ok && next_work(it); ++it) {
-        float v_scale = 0.f;                          // of the values since the piece's first tile, or one that was much larger
-  #pragma unroll 1
+        float v_scale = 0.f;                        // of the values since the piece's first tile, or one that was much larger
+        TileLevels now, next;                       // of a tile, and of the one behind it while they come
+        int entry[kKT / 32];                        // ... pages of the one behind that
+        if (n_tiles) {
+          ask_entries(p, b, tq0, tq_last, kt.slot(0), entry);
+          ask_levels<D>(p, g, kt.slot(0), entry, next);
+          if (n_tiles > 1) ask_entries(p, b, tq0, tq_last, kt.slot(1), entry);
+        }
+#pragma unroll 1
         for (int k = 0; k < n_tiles; ++k) {
-          const int job = jobs + 2 * k, tile = job >> 1, j0 = kt.slot(k);
-          ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_lev[tile & 1]), uint32_t(tile >> 1) & 1u, failed, moves));
+          const int job = jobs + 2 * k, tile = job >> 1;
+          now = next;
+          if (k + 1 < n_tiles) ask_levels<D>(p, g, kt.slot(k + 1), entry, next);
+          if (k + 2 < n_tiles) ask_entries(p, b, tq0, tq_last, kt.slot(k + 2), entry);
           // (the steps and the further columns of the tile that had the buffer are free when that is)
-          if (ok && job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[job % S]), uint32_t(job / S - 1) & 1u, failed, moves));
+          if (job >= S) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_free[job % S]), uint32_t(job / S - 1) & 1u, failed, moves));
           if (!ok) break;
-          const TileRows rows{*const_cast<volatile uint32_t *>(&sm.pieces[tile & 3]), min(p.page_shift, 7), p.window < 0 ? 0 : tq0 - p.window + 1 - j0, tq_last + 1 - j0, p.n_sink - j0};
-          make_levels(sm.levels[tile & 1], rows, v_scale, &sm.k_undo[tile & 3], &sm.v_undo[tile & 3], sm.steps[tile & 1], sm.steps[2 + tile % 3],
-                      sm.more_k[tile % (S / 2)]);
+          make_levels(now, v_scale, &sm.k_undo[tile & 3], &sm.v_undo[tile & 3], sm.steps[tile & 1], sm.steps[2 + tile % 3], sm.more_k[tile % (S / 2)]);
           fence_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&sm.bar_levels[tile & 3]));
@@ -892,7 +910,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
     const int tiles = count_tiles(p, TOKC), total = tiles * p.Hkv * parts;
     bool ok = true;
     AskedCopies asked;                             // Q, K and V tiles, tails so far
-    int asked_levels = 0;                          // tiles whose levels have been asked for
     uint32_t n_use[2] = {0, 0};                    // pieces with rows in X
     int drawn = 0;
     if (lane == 0) drawn = atomicAdd(p.status + 1, 1);
@@ -915,7 +932,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       if (w.seq < 0) break;
       set_work(w);
       int next = n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(0), pieces, rows) : 0;
-      int far = CODES && kFar < n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(kFar), pieces, rows) : -1;
       // The first tiles may come while the piece before is still being written out, Q_X when its rows have been.
       auto ask_q = [&](int x) {
         if (n_use[x]) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_qfree[x]), (n_use[x] - 1) & 1u, failed, moves));
@@ -938,16 +954,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       for (int k = 0; k < n_tiles && ok; ++k) {
         const int j0 = kt.slot(k), page = piece_page(p, next, tq0, tq_last, j0, pieces, rows, none);
         if (k + 1 < n_tiles) next = piece_entry(p, b, tq0, tq_last, kt.slot(k + 1), pieces, rows);
-        if constexpr (CODES) {   // a later tile's codes to L2 (a lane per piece): the buffers hold one tile of each kind
-          if (k + kFar < n_tiles && unsigned(far) < unsigned(p.n_pages)) {
-            const int off = (kt.slot(k + kFar) + lane * rows) & ((1 << p.page_shift) - 1);
-            const size_t at = size_t(far) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + size_t(off) * (D / 2);
-            const uint32_t bytes = uint32_t(rows) * (D / 2);
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const unsigned char *>(p.k) + at), "r"(bytes) : "memory");
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const unsigned char *>(p.v) + at), "r"(bytes) : "memory");
-          }
-          far = k + 1 + kFar < n_tiles ? piece_entry(p, b, tq0, tq_last, kt.slot(k + 1 + kFar), pieces, rows) : -1;
-        }
 #pragma unroll 1
         for (int is_v = 0; is_v < 2 && ok; ++is_v) {
           const int job = jobs + 2 * k + is_v, slot = job % S;
@@ -956,27 +962,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
             const int to = job % R;
             if (job >= R) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_rawfree[to]), uint32_t(job / R - 1) & 1u, failed, moves));
             if (!ok) break;
-            // the levels of this tile (of the first of a piece) and of the next one
-            for (int ahead = k == 0 ? 0 : 1; ahead < 2 && !is_v && k + ahead < n_tiles; ++ahead) {
-              const int tile = (job >> 1) + ahead, j1 = kt.slot(k + ahead), pg = ahead ? piece_page(p, next, tq0, tq_last, j1, pieces, rows, none) : page;
-              const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && pg != none);
-              const uint32_t lev = smem_u32(sm.levels[tile & 1]), lev_bar = smem_u32(&sm.bar_lev[tile & 1]), bytes = uint32_t(rows) * kLevelBytes;
-              if (leader) {
-                sm.pieces[tile & 3] = there;
-                mbar_expect_tx(lev_bar, uint32_t(__popc(there)) * 2 * bytes);
-              }
-#pragma unroll 1
-              for (int i = 0; i < pieces; ++i) {
-                const int pi = __shfl_sync(0xffffffffu, pg, i);
-                if (leader && (there >> i) & 1u) {
-                  const size_t at = size_t(pi - p.page0) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + ((D / 2) << p.page_shift) +
-                                    ((j1 + i * rows) & ((1 << p.page_shift) - 1)) * kLevelBytes;
-                  bulk_load(lev + i * bytes, reinterpret_cast<const unsigned char *>(p.k) + at, bytes, lev_bar);
-                  bulk_load(lev + kKT * kLevelBytes + i * bytes, reinterpret_cast<const unsigned char *>(p.v) + at, bytes, lev_bar);
-                }
-              }
-              asked_levels = tile + 1;
-            }
             const unsigned there = __ballot_sync(0xffffffffu, lane < pieces && page != none);
             const uint32_t raw = smem_u32(sm.raw + to * Sm::kRawBytes), raw_bar = smem_u32(&sm.bar_raw[to]), codes = uint32_t(rows) * (D / 2);
             if (leader) mbar_expect_tx(raw_bar, uint32_t(__popc(there)) * codes);
@@ -1031,10 +1016,6 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       }
     }
     if (!ok) {   // after a time-out: no copy outlives the CTA
-      for (int tile = max(0, asked_levels - 2); CODES && tile < asked_levels; ++tile) {
-        int alone = 0;
-        mbar_wait(smem_u32(&sm.bar_lev[tile & 1]), uint32_t(tile >> 1) & 1u, &alone);
-      }
       wait_for_copies(asked, CODES ? R : S, [&](int what, int which, uint32_t parity) {
         int alone = 0;   // (whoever has given up)
         mbar_wait(smem_u32(what == kCopyQ ? &sm.bar_q[which] : what == kCopyTile ? (CODES ? &sm.bar_raw[which] : &sm.bar_full[which]) : &sm.bar_tail), parity, &alone);
@@ -1409,8 +1390,8 @@ int launch_paged_prefill_tc(const glide_paged *h, const PagedParams &p, cudaStre
     const unsigned blocks = unsigned(std::min<int64_t>(grid * splits, p.sm_count));
     auto start = [&](auto codes) {
       constexpr bool CODES = decltype(codes)::value;
-      if (p.lse) paged_prefill_tc_kernel<D, G, true, CODES><<<blocks, CODES ? kCodeThreads : kThreads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
-      else paged_prefill_tc_kernel<D, G, false, CODES><<<blocks, CODES ? kCodeThreads : kThreads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
+      const auto kernel = p.lse ? paged_prefill_tc_kernel<D, G, true, CODES> : paged_prefill_tc_kernel<D, G, false, CODES>;
+      kernel<<<blocks, CODES ? kCodeThreads : kThreads, sizeof(PrefillSmem<D, CODES>), st>>>(p, maps, h->map_pages, splits);
     };
     if (h->codes) start(std::true_type{});
     else start(std::false_type{});
