@@ -63,7 +63,9 @@ struct Work {
 template <int D, bool CODES>
 struct PrefillSmem {
   static constexpr int kTileBytes = D * 256;                     // [D / 64 boxes][128 rows][64 bf16]
-  static constexpr int kStages = CODES ? (D == 128 ? 4 : 6) : D == 128 ? 5 : 8;
+  // (pages in 4 bits: a tile of each kind is made while another one is read.  What warp 19 writes for a key tile has rings that go by that: it waits until the
+  // tile two before has been read.)
+  static constexpr int kStages = CODES ? 4 : D == 128 ? 5 : 8;
   static constexpr int kRaw = CODES ? kRawStages : 1, kRawBytes = kKT * D / 2;
   unsigned char q[2][kTileBytes];        // Q_A, Q_B; then the output rows on their way out
   unsigned char kv[kStages][kTileBytes]; // K and V tiles in turn
@@ -297,12 +299,13 @@ __device__ __forceinline__ void make_levels(const TileLevels &t, float &v_scale,
   float undo, v_back;
   const float scale = scale_to(__uint_as_float(__reduce_max_sync(0xffffffffu, top[0])), -7, undo);
   const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, top[1]));
-  if (v_scale == 0.f || most * v_scale >= 0x1p-6f) v_scale = scale_to(most, -9, v_back);
-  if (lane == 0) *k_undo = undo, *v_undo = 1.f / v_scale;
+  if (most > 0.f && (v_scale == 0.f || most * v_scale >= 0x1p-6f)) v_scale = scale_to(most, -9, v_back);
+  const float vs1 = v_scale == 0.f ? 1.f : v_scale;   // (nothing but zeros so far)
+  if (lane == 0) *k_undo = undo, *v_undo = 1.f / vs1;
 #pragma unroll
   for (int i = 0; i < kKT / 32; ++i) {
     const int row = i * 32 + lane;
-    const float ks = bf16_lo(l[0][i]) * scale * 0x1p24f, vs = bf16_lo(l[1][i]) * v_scale * 0x1p24f, low = bf16_hi(l[1][i]) * v_scale;
+    const float ks = bf16_lo(l[0][i]) * scale * 0x1p24f, vs = bf16_lo(l[1][i]) * vs1 * 0x1p24f, low = bf16_hi(l[1][i]) * vs1;
     k_step[row] = make_uint2(pack_f16x2(ks, ks), pack_f16x2(ks * -0x1p-21f, ks * -0x1p-21f));
     v_step[row] = make_uint2(pack_f16x2(vs, vs), pack_f16x2(low, low));
     *reinterpret_cast<uint4 *>(more + row * 16) = more_columns(fmaf(8.f, bf16_lo(l[0][i]), bf16_hi(l[0][i])) * (scale * kMoreScale), true);

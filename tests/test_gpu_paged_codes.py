@@ -172,6 +172,37 @@ def test_values_and_scores_that_grow_along_the_cache():
     check_decode(Cache4([1600], [1], 4, 2, 128, 64, rows=rows, amp=6.0))
 
 
+@pytest.mark.parametrize("zeros", [1, 128, 300])
+def test_a_cache_that_begins_with_zeros(zeros):
+    """Keys and values of nothing but zeros, then small ones: no scale goes by the zeros."""
+    def rows(b, k, v):
+        k, v = k.clone(), (v.double() * 2.0 ** -30).to(BF16)
+        k[:zeros], v[:zeros] = 0.0, 0.0
+        return k, v
+    check_prefill(Cache4([400, 0], [60, 450], 4, 2, 128, 64, rows=rows))
+    check_prefill(Cache4([400], [60], 4, 2, 64, 16, rows=rows), 250, 2)
+    check_decode(Cache4([400, zeros - 1], [1, 1], 4, 2, 128, 64, rows=rows))
+
+
+@pytest.mark.parametrize("d,H,Hkv,page", [(64, 16, 4, 64), (128, 16, 4, 64), (64, 4, 4, 16), (128, 8, 1, 32)])
+@pytest.mark.parametrize("before,new", [(3000, 300), (0, 900), (6000, 3)])
+def test_calls_that_follow_one_another(d, H, Hkv, page, before, new):
+    """Two handles' calls in turns that nothing waits between give what they give by themselves, bit for bit."""
+    pairs = [Cache4([before, before // 2], [new, new], H, Hkv, d, page, seed=i) for i in range(2)]
+    run = lambda c, out: c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, None, None, out)  # noqa: E731
+    alone = []
+    for c in pairs:
+        alone.append(torch.empty_like(c.q))
+        run(c, alone[-1])
+        torch.cuda.synchronize()
+    outs = [[torch.full_like(c.q, 7.0) for c in pairs] for _ in range(20)]
+    for out in outs:
+        for c, o in zip(pairs, out):
+            run(c, o)
+    for out in outs:
+        assert all(torch.equal(o, a) for o, a in zip(out, alone))
+
+
 def test_layers_and_strides():
     """A second layer of padded blocks, queries and outputs that are views."""
     c = Cache4([200, 10], [30, 60], 8, 2, 128, 32, layers=3, gap=48)
