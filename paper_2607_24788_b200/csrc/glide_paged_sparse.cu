@@ -293,6 +293,7 @@ __device__ __noinline__ void pick_pages(const PagedParams &p, PickSmem &sm, cons
           if (a > above) keys.at[i] = ~0ull;
           else if (a < below) keys.at[i] = 0ull;
         });
+        __syncthreads();   // (what is stored from here on is no such pair: no warp may still be looking at those of others' runs)
         for (int j = warp; j < n_band; j += kScoreThreads / 32) {
           const unsigned long long k = exact_key<T, D, G>(p, bounds, q, b, g, c0 + sm.band[j]);
           if (lane == 0) keys.at[sm.band[j]] = min(max(k, 1ull), ~1ull);
