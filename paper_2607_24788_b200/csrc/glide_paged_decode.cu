@@ -329,10 +329,16 @@ struct WarpUnit {
 
 // Rows in 4 bits.  Thread (r = lane / 4, c = lane % 4) has scores as above, of every 16 slots; of O^T, features r D / 8 + 2k and + 2k + 1 of every k.
 // Codes are operands as they lie in their words, bf16 numbers below the least normal one, against queries times 2^s (so that a head's
-// largest is near 2^100) and weights times step 2^w (so that a step is).  A tile's products are added up from 0 and then to O, in which nothing is cut off.
+// largest is near 2^100) and weights times step 2^w.  A tile's products are added up from 0 and then to O, in which nothing is cut off.
+//   2^w brings the largest step of the warp's first tile that has one to [2^76, 2^77) and moves when a step reaches 2^92.  So the sums y of at most
+// 2^30 / 12 weights of at most 2^kLazy each, times step 2^w, end below 2^92 2^8 2^27 = 2^127; and O, 2^-133 times that, keeps all its bits of rows whose weight
+// times step is 2^-60 of the largest or more.
 template <int TILE, int D, int G>
 struct WarpUnit<Codes<TILE>, D, G> {
   static constexpr int N = TILE / 16;
+  static constexpr int kStepAt = 76;               // exponent that 2^w gives the largest step
+  static constexpr float kMostStep = 0x1p92f;
+  static_assert(kLazy <= 8.0f, "the range of y");
   uint32_t q[D / 16][2];
   float o[D / 16][4];       // times 2^(w - 133), odd features 16 times that
   float m[2], x[2], z[2];   // maxima; sums of the weights; of the weights times the middle levels of their rows, low + 8 step
@@ -440,11 +446,11 @@ struct WarpUnit<Codes<TILE>, D, G> {
       step = fmaxf(step, fmaxf(bf16_lo(vl[t][0]), bf16_lo(vl[t][1])));   // (a NaN is left out)
     }
     // (-infinity + 8 is -infinity: a head without a maximum moves with its first score; an infinite step is none)
-    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy || (fw == 0.f ? step > 0.f : step * fw >= 0x1p116f))) {
+    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy || (fw == 0.f ? step > 0.f : step * fw >= kMostStep))) {
       float go = 1.f;   // what the weights' scale makes of O
       const float most = warp_max(step);
-      if (fw == 0.f ? most > 0.f : most * fw >= 0x1p116f) {
-        const float now = power_of_2(100 - exponent_of(most));
+      if (fw == 0.f ? most > 0.f : most * fw >= kMostStep) {
+        const float now = power_of_2(kStepAt - exponent_of(most));
         go = fw == 0.f ? 1.f : now / fw;
         fw = now;
       }
