@@ -4,9 +4,8 @@
 // the KV head's query heads: the products of the query's negative features with the lows and of the others with the highs.  Which page comes before
 // which is decided by sums in 64 bits, in which the products of 16-bit numbers are exact and their sums all but exact.
 //   bf16   S = [lows | highs] [q- | q+]^T by mma.sync (16 pages on M, the KV head's query heads on N), and the same of the absolute values, which
-//          says how far S may be off: 2^-17 of it is sixteen times what 256 sums of 23 bits can lose.  The block that is the last of its (sequence,
-//          KV head) finds the n-th largest S by radix selection; only pages within twice the error of it, a few or none, are summed in 64 bits.  Bounds that
-//          are no numbers, or more than 256 such pages: all are.
+//          says how far S may be off (off_by).  The block that is the last of its (sequence, KV head) finds the n-th largest S by radix selection; only
+//          pages within twice the error of it, a few or none, are summed in 64 bits.  Bounds that are no numbers, or more than 256 such pages: all are.
 //   fp32   in 64 bits from the start: four threads per page, pieces of 8 features in turns; the bounds become doubles by their bits: a float's
 //          exponent and mantissa, moved to where a double has them, are 2^-896 times the float (subnormal ones too); the queries are multiplied by
 //          2^448, so all scores by 2^-448.  Pages with a bound that is no number are computed once more by the formula.
@@ -370,6 +369,13 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// How far an approximate score may be off, as a part of the sum of its products' absolute values, A.  The products of 16-bit numbers are exact.  Of the adder
+// no more is taken for granted than single precision, and that it may cut off: each of the 2 D additions loses less than 2^-23 of the largest number in
+// it, which is A at most, so the sum loses less than 2 D 2^-23 A; A's own sum as much of itself.  Twice that covers both, and the roundings of the borders that
+// are made of it.  (2^-14 for D = 128.  A large product and ones just below what 2^-23 of it would keep lose half of it in such an adder.)
+template <int D>
+__device__ constexpr float off_by() { return 2.f * (2 * D) * 0x1p-23f; }
+
 // bf16.  A warp has 16 pages at a time; thread (r = lane / 4, c = lane % 4) reads pieces 4j + c of the bounds of pages r and r + 8, whose features are
 // the columns 2c, 2c + 1, 2c + 8, 2c + 9 of two products, the queries' in the same order.
 template <int D, int G>
@@ -455,7 +461,7 @@ paged_score_tc_kernel(const __grid_constant__ PagedParams p, __nv_bfloat16 *boun
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o)), err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
         odd = __shfl_xor_sync(0xffffffffu, int(odd), o) || odd;
       }
-      err = odd ? CUDART_INF_F : fmaf(err, 0x1p-17f, 0x1p-117f);   // (and what products below the least normal number lose)
+      err = odd ? CUDART_INF_F : fmaf(err, off_by<D>(), 0x1p-117f);   // (and what products below the least normal number lose)
       const int col = base + r + 8 * i;
       if (c == 0 && col < end) keys[col] = static_cast<unsigned long long>(__float_as_uint(err)) << 32 | order_of(odd ? 0.f : best);
     }

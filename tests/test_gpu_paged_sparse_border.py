@@ -45,3 +45,32 @@ def test_the_choice_does_not_depend_on_timing(pages, n_near, where):
         s.step(c.k, c.v)
         all_picks.append(s.picks[0].clone())
     assert all(torch.equal(p, want) for p in all_picks)
+
+
+@pytest.mark.parametrize("d,H", [(128, 1), (128, 8), (64, 2)])
+@pytest.mark.parametrize("below", [22, 23, 24, 25, 26])
+def test_sums_that_lose_what_an_adder_can(d, H, below):
+    """One large product and others just below 2^-below of it, which an adder of so many bits cuts off one by one: the choice is that of sums in 64 bits.  The bound
+    that a score goes by (beside it in the work space: bits of a float above those of the score in order) covers what 2 d additions of 23 bits can lose."""
+    pages = 300
+    g = torch.Generator().manual_seed(below)
+    at = torch.arange(pages)
+
+    def make(k):
+        key = torch.full((pages, 1, d), (2 - 2.0 ** -7) * 2.0 ** -below, dtype=torch.float64)
+        key[torch.rand((pages, 1, d), generator=g) < 0.2] = 0.0
+        key[at, 0, at % d] = 1.0
+        return key.repeat_interleave(16, 0).to(BF16).cuda()
+    c = with_keys(Cache([16 * pages], [1], H, 1, d, BF16, 16), make)
+    c.q = torch.ones_like(c.q)
+    c.q[:, 1::2] = 0.5
+    s = Sparse(c, 40)
+    s.step(c.k, c.v)
+    s.check()
+    key = s.scores.view(torch.int64)[0, 0, :pages]
+    order, err = key & 0xffffffff, (key >> 32).to(torch.int32).view(torch.float32).double()
+    bits = torch.where(order >= 1 << 31, order - (1 << 31), 0xffffffff - order)
+    got = torch.where(bits >= 1 << 31, bits - (1 << 32), bits).to(torch.int32).view(torch.float32).double()
+    want = page_scores(c.q[0], s.bounds, c.table[0], pages)[0]   # (of numbers that are not negative: their absolute values' sum too)
+    assert ((got - want).abs() <= err).all()
+    assert (err >= 2 * d * 2.0 ** -23 * want).all()
