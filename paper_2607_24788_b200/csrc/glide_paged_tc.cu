@@ -17,7 +17,7 @@
 // to below 2^-6, a query row by the threads that it belongs to, to below 2^7, and the scores are scaled back where they are multiplied by the
 // softmax scale anyway.  (Exact for rows whose step is 2^-8 of the tile's largest key or more, others are off by 2^-19 of that at most.  Keys
 // rounded to bf16 put scores off by 0.005, outputs by 0.006 of their norm.)  A value is rounded to fp16 once, and so are the weights: off by at most
-// 2^-11 of themselves, or a value by 2^-16 of the largest that its scale went by.  The values' scale is a power of two as well, from the piece's
+// 2^-11 of themselves, or a value by 2^-16 of the largest that its scale went by, a weight by 2^-30 of the row's largest (kRoomHalf).  The values' scale is a power of two as well, from the piece's
 // first tile on, until a tile has values four to eight times as large; then O is scaled as where a reference moves.  A key or value comes out of
 // one fused multiply-add for two codes where they lie in the word: four bits at the bottom of an fp16 number are code times its least
 // subnormal number, the next four 16 times that.  Which leaves the features of eight in the order 0 4 1 5 2 6 3 7, in keys, values, and so in
@@ -48,7 +48,11 @@ constexpr int kLevelWarp = 19, kCodeThreads = 640, kUnpackWarps = 8, kRawStages 
 // has to keep them inside the range (values above 2^90 or so would leave it; such a row is computed by itself).  A move takes a second
 // pass over the tile: 8 sequences of up to 2048 tokens, windows of 256 with 4 first tokens 228 us with 8, 169 with 32, 171 with 64.
 constexpr float kLazy = 32.0f, kMostWeight = 0x1p32f;
-constexpr float kLazyHalf = 14.0f;    // ... of weights that are fp16 numbers
+// Weights that are fp16 numbers: a reference that moves goes to 2^5 below the row's largest score so far, and may be exceeded by 2^15.5.  So the largest
+// weight stands at 2^5 or more, and others have 11 bits down to 2^-19 of it and are 0 from 2^-30 on: 128K slots that are alike, beside a first token that
+// takes most of the weight, are off by 2^-13 of it in all, 1M by 2^-10.  (A reference at the largest score, exceeded by 2^14, lost 0.4 % of 128K.  2^6, 2^7 and 2^8 below
+// it: it moves more often, 750, 760 and 772 us for 8001 tokens, 32 / 8 heads, instead of 744; a reference at the largest one 742.)
+constexpr float kRoomHalf = 5.0f, kLazyHalf = 15.5f;
 constexpr int kMostSlots = 1 << 30;
 
 struct PagedMaps {
@@ -598,7 +602,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
       if (LSE) x_sum += ex0 + ex1;
     };
     // Pages in 4 bits: weights as fp16 numbers, so the reference moves first where it has to, and O with it; O too where the values' scale has
-    // moved.  Sums of the weights as they are: rounding puts them off by 2^-11 each.
+    // moved.  Sums of the weights as they are: rounding puts them off by 2^-11 each, or by 2^-25, which is 2^-30 of the largest or less.
     auto soft_half = [&](auto masked, const Bounds &v, bool first, float v_ratio) {
       float mx = -CUDART_INF_F;
 #pragma unroll
@@ -624,6 +628,7 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         float f = 1.f;
         if (grows()) {
           mx *= scale;
+          mx -= kRoomHalf;
           f = m_ref == -CUDART_INF_F ? 0.f : ex2(m_ref - mx);
           m_ref = mx;
           x_sum *= f;
