@@ -460,6 +460,7 @@ class GlideRotation:
 
 
 _I32, _F32 = torch.int32, torch.float32
+_MOST_TOKENS = 1 << 30   # of a call
 # a call's fields as bytes of its own (one pack instead of a store per field: a step's host time is what counts where the cache is short)
 _pack_call = struct.Struct("@iiPiiqPPqqqqqPPPq").pack
 assert struct.calcsize("@iiPiiqPPqqqqqPPPq") == ctypes.sizeof(glide_paged_call)
@@ -640,8 +641,9 @@ class GlidePaged:
 
     def glide_paged_bounds(self, table, lens, starts, bounds, n_tokens: Optional[int] = None, layer: int = 0, stream=None) -> None:
         """bounds [n_pages][H_kv][2][d], of the layer: least and largest key values of the pages that hold the tokens that starts names (None: the
-        newest of each sequence).  n_tokens: starts[B] or more (None: as many as the sequences can hold, which only costs time)."""
-        most = min(self.max_tokens, table.shape[1] * self.page_size) * table.shape[0]
+        newest of each sequence).  n_tokens: starts[B] or more; None: as many as the sequences can hold, for which a block for each of the table's entries
+        is launched."""
+        most = min(min(self.max_tokens, table.shape[1] * self.page_size) * table.shape[0], _MOST_TOKENS)
         rows = None if starts is None else most if n_tokens is None else int(n_tokens)
         call = self._packed_call(layer, table, lens, starts, rows, (0, 0, 0), -1, 0, None, None, None)
         self._run("glide_paged_bounds", stream, self.lib.glide_paged_bounds, call, self._bounds(bounds))
