@@ -328,8 +328,9 @@ struct WarpUnit {
 };
 
 // Rows in 4 bits.  Thread (r = lane / 4, c = lane % 4) has scores as above, of every 16 slots; of O^T, features r D / 8 + 2k and + 2k + 1 of every k.
-// Codes are operands as they lie in their words, bf16 numbers below the least normal one, against queries times 2^s (so that a head's
-// largest is near 2^100) and weights times step 2^w.  A tile's products are added up from 0 and then to O, in which nothing is cut off.
+// Codes are operands as they lie in their words, bf16 numbers below the least normal one, against queries times 2^s and weights times step 2^w.  A tile's products
+// are added up from 0 and then to O, in which nothing is cut off.
+//   2^s brings a head's largest query to 2^126 or so: what undoes it together with a step, 2^(133 - s) step, is a number as long as scores are below 2^118 or so.
 //   2^w brings the largest step of the warp's first tile that has one to [2^76, 2^77) and moves when a step reaches 2^92.  So the sums y of at most
 // 2^30 / 12 weights of at most 2^kLazy each, times step 2^w, end below 2^92 2^8 2^27 = 2^127; and O, 2^-133 times that, keeps all its bits of rows whose weight
 // times step is 2^-60 of the largest or more.
@@ -374,7 +375,7 @@ struct WarpUnit<Codes<TILE>, D, G> {
 #pragma unroll
     for (int o2 = 1; o2 < 4; o2 <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o2), top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o2));
     const int e_top = max(exponent_of(top), -126);                            // (an infinity: 128)
-    const int up = max(100 - e_top, 6);                                       // (2^(133 - up) is a number)
+    const int up = max(126 - e_top, 6);                                       // (2^(133 - up) is a number; queries of 2^122 leave the range)
     const float f0 = power_of_2(up / 2), f1 = power_of_2(up - up / 2);        // (2^up may be none)
     auto scaled = [&](uint32_t a, uint32_t b2, bool high, float f) {           // features of two words, one each, as a pair
       return high ? pack_bf16x2(bf16_hi(a) * f0 * f1 * f, bf16_hi(b2) * f0 * f1 * f) : pack_bf16x2(bf16_lo(a) * f0 * f1 * f, bf16_lo(b2) * f0 * f1 * f);

@@ -51,3 +51,17 @@ def test_values_that_grow_behind_a_warps_first_tile(slots, small, factor, score,
     check(out, want.expand_as(q), tol.expand_as(q), "out")
     check(lse, want_lse.expand(B, H), lse_tol.expand(B, H), "lse")
     assert handle.glide_paged_device_status() == 0
+
+
+@pytest.mark.parametrize("of_q,of_k", [(2.0 ** 50, 2.0 ** 50), (2.0 ** 60, 2.0 ** 55), (2.0 ** 118, 2.0 ** -118), (2.0 ** -118, 2.0 ** 118), (2.0 ** -60, 2.0 ** -60)])
+@pytest.mark.parametrize("d,H,Hkv", [(128, 4, 2), (64, 8, 1)])
+def test_very_large_and_very_small_scores(of_q, of_k, d, H, Hkv):
+    """Scores near 2^100 and 2^115, of which one slot takes all the weight; products that come out ordinary; scores of nothing."""
+    c = Cache4([700, 5, 2000], [1, 1, 1], H, Hkv, d, 32, rows=lambda b, k, v: ((k.double() * of_k).to(BF16), v))
+    c.q = (c.q.double() * of_q).to(BF16)
+    out, lse = torch.full_like(c.q, 7.0), torch.full(c.q.shape[:2], 7.0, device="cuda")
+    c.handle.glide_paged_decode(c.table, c.lens_dev, c.q, None, None, out, lse=lse)
+    want, tol, want_lse, lse_tol = reference4(c)
+    check(out, want, tol, "out")
+    check(lse, want_lse, lse_tol, "lse")
+    assert c.handle.glide_paged_device_status() == 0
