@@ -53,6 +53,9 @@ constexpr float kLazy = 32.0f, kMostWeight = 0x1p32f;
 // takes most of the weight, are off by 2^-13 of it in all, 1M by 2^-10.  (A reference at the largest score, exceeded by 2^14, lost 0.4 % of 128K.  2^6, 2^7 and 2^8 below
 // it: it moves more often, 750, 760 and 772 us for 8001 tokens, 32 / 8 heads, instead of 744; a reference at the largest one 742.)
 constexpr float kRoomHalf = 5.0f, kLazyHalf = 15.5f;
+// What a row's sum is at least, since the largest weight was 1 (2^kRoomHalf) when the reference moved.  It is less where scores are so large, 2^26 or more, that the
+// reference, a rounded product, is whole powers of two off the score that it was made of: then all weights may be 0, or (fp16) too small.
+constexpr float kLeast = 0x1p-100f, kLeastHalf = 0x1p4f;
 constexpr int kMostSlots = 1 << 30;
 
 struct PagedMaps {
@@ -753,8 +756,9 @@ paged_prefill_tc_kernel(const __grid_constant__ PagedParams p, const __grid_cons
         if constexpr (CODES) unpack(k + 2 - X);
       }
       if (CODES && ntokX == 0) continue;
-      const float l_row = row_sum_of(CODES ? x_sum : l_sum);
-      const float x_row = CODES ? l_row : LSE ? row_sum_of(x_sum) : 0.f;
+      float l_row = row_sum_of(CODES ? x_sum : l_sum);
+      float x_row = CODES ? l_row : LSE ? row_sum_of(x_sum) : 0.f;
+      if (m_ref > -CUDART_INF_F && !(l_row >= (CODES ? kLeastHalf : kLeast))) l_row = x_row = CUDART_NAN_F;   // (for the row to be computed by itself)
       if (before >= 0) wait_s();                    // every product of X has completed
       else if (!CODES && n_tiles && ok) ok = __all_sync(0xffffffffu, mbar_wait_long(smem_u32(&sm.bar_q[X]), n_q & 1u, failed, moves));   // (Q, which no product has waited for)
       n_q += n_tiles != 0;

@@ -1,11 +1,11 @@
-"""Prompts over a cache in 4 bits whose weights spread over many powers of two: small ones are not lost beside a large one."""
+"""Prompts whose weights spread over many powers of two: over a cache in 4 bits small ones are not lost beside a large one; no row loses all of them."""
 import math
 
 import pytest
 import torch
 
-from tests.paged_more_util import BF16, Cache4, levels
-from tests.paged_util import check
+from tests.paged_more_util import BF16, Cache4, levels, reference4
+from tests.paged_util import Cache, check, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -41,4 +41,31 @@ def test_a_first_token_that_takes_most_of_a_prompts_weight(d, H, before, new, fi
     check(out, want, tol, "out")
     total = (i + x.exp()).log().squeeze(2)
     check(lse, total.expand(new, H), (e + 8 * U * x + 8 * U + n * 2 * U + 2 * U * total).expand(new, H), "lse")
+    assert c.handle.glide_paged_device_status() == 0
+
+
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("of_q,of_k", [(2.0 ** 14, 2.0 ** 14), (2.0 ** 16, 2.0 ** 15), (2.0 ** 50, 2.0 ** 50), (2.0 ** 60, 2.0 ** 50), (2.0 ** -60, 2.0 ** -60)])
+@pytest.mark.parametrize("d,H,Hkv,before,new", [(128, 4, 2, [700, 0], [40, 130]), (64, 8, 1, [9000], [5])])
+def test_scores_beyond_what_a_reference_can_hold(codes, of_q, of_k, d, H, Hkv, before, new):
+    """Scores so large that a number next to the largest one is whole powers of two away: one slot takes all the weight, and none is lost.  In tiles and in
+    parts of the key tiles."""
+    scaled = lambda x, f: (x.double() * f).to(BF16)  # noqa: E731
+    if codes:
+        c = Cache4(before, new, H, Hkv, d, 32, rows=lambda b, k, v: (scaled(k, of_k), v))
+    else:
+        c = Cache(before, new, H, Hkv, d, BF16, 32)
+        c.dense = [[(scaled(k, of_k), v) for k, v in rows] for rows in c.dense]
+        c.k = scaled(c.k, of_k)
+        for b, n in enumerate(c.lens):
+            at, off = c.place(b, torch.arange(n, device="cuda"))
+            for pool, x in zip((c.k_pages, c.v_pages), c.rows(0, b)):
+                pool[0][at, :, off] = x
+    c.q = scaled(c.q, of_q)
+    out, lse = torch.full_like(c.q, 7.0), torch.full(c.q.shape[:2], 7.0, device="cuda")
+    for with_lse in (lse, None):
+        c.handle.glide_paged_prefill(c.table, c.lens_dev, c.starts, c.q, None, None, out, lse=with_lse)
+        want, tol, want_lse, lse_tol = (reference4(c, prompt=True) if codes else reference(c))[:4]
+        check(out, want, tol, "out")
+    check(lse, want_lse, lse_tol, "lse")
     assert c.handle.glide_paged_device_status() == 0
