@@ -305,72 +305,79 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// A block per page that got tokens (the grid has as many as there can be), a warp per KV head in turns: a team per row, the teams' values
-// joined at the end.  A page's old tokens are read too: nothing is taken over from bounds that an eviction or another sequence may have
-// left.  Bound: the pages' bytes.
+// A block per page that got tokens, a warp per KV head in turns: a team per row, the teams' values joined at the end.  How many pages there are is only known
+// here: the blocks are no more than kBoundsBlocks for each SM and take pages in turns, so that a call which may bring far more tokens than it does costs
+// little.  (256 sequences of 40 tokens, table entries for 8192 pages each: with a block for each of those 16 ms; with 64, 256 blocks 23, 49 us, and 16 where the
+// call names the tokens.  256 sequences of 3000 tokens, 48128 pages: 74 and 71 us.)  A page's old tokens are read too: nothing is taken over from bounds that an eviction or another sequence may have left.  Bound:
+// the pages' bytes.
+constexpr int kBoundsBlocks = 128;
 template <typename T, int D>
-__global__ void __launch_bounds__(kWarps * 32) paged_bounds_kernel(const __grid_constant__ PagedParams p, T *bounds) {
+__global__ void __launch_bounds__(kWarps * 32) paged_bounds_kernel(const __grid_constant__ PagedParams p, T *bounds, int most) {
   constexpr int kTeam = D / 16, kTeams = 32 / kTeam;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane % kTeam, team = lane / kTeam;
   wait_for_predecessor();
-  // the block's page: of all sequences' pages with new tokens, in order, the one of the block's number
-  int want = int(blockIdx.x), b = -1, len = 0, col = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const int i = b0 + lane;
-    int row0, n = 0, l = 0;
-    if (i < p.batch) {
-      l = paged_len(p, i);
-      n = p.starts ? paged_new(p, i, l, row0) : min(l, 1);
-    }
-    const int first = (l - n) >> p.page_shift, pages = n ? ((l - 1) >> p.page_shift) - first + 1 : 0;
-    int inc = pages;
+  const int end = p.starts ? min(most, (max(p.starts[p.batch], 0) >> p.page_shift) + 2 * p.batch) : most;   // (pages of a sequence's n tokens: n / page_size + 2 at most)
+#pragma unroll 1
+  for (int item = int(blockIdx.x); item < end; item += int(gridDim.x)) {
+    // the item's page: of all sequences' pages with new tokens, in order, the one of its number
+    int want = item, b = -1, len = 0, col = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+      const int i = b0 + lane;
+      int row0, n = 0, l = 0;
+      if (i < p.batch) {
+        l = paged_len(p, i);
+        n = p.starts ? paged_new(p, i, l, row0) : min(l, 1);
+      }
+      const int first = (l - n) >> p.page_shift, pages = n ? ((l - 1) >> p.page_shift) - first + 1 : 0;
+      int inc = pages;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      const unsigned here = __ballot_sync(0xffffffffu, want < inc);
+      if (here) {
+        const int s = __ffs(int(here)) - 1;
+        b = b0 + s, len = __shfl_sync(0xffffffffu, l, s);
+        col = __shfl_sync(0xffffffffu, first, s) + want - __shfl_sync(0xffffffffu, inc - pages, s);
+        break;
+      }
+      want -= __shfl_sync(0xffffffffu, inc, 31);
     }
-    const unsigned here = __ballot_sync(0xffffffffu, want < inc);
-    if (here) {
-      const int s = __ffs(int(here)) - 1;
-      b = b0 + s, len = __shfl_sync(0xffffffffu, l, s);
-      col = __shfl_sync(0xffffffffu, first, s) + want - __shfl_sync(0xffffffffu, inc - pages, s);
-      break;
-    }
-    want -= __shfl_sync(0xffffffffu, inc, 31);
-  }
-  dependents_may_start();
-  if (b < 0) return;
-  const int pg = paged_page(p, b, col << p.page_shift);
-  if (pg < 0) return;
-  const int n = min(len - (col << p.page_shift), 1 << p.page_shift);   // slots of the page
-  for (int g = warp; g < p.Hkv; g += int(blockDim.x) / 32) {
-    const T *src = reinterpret_cast<const T *>(p.k) + size_t(pg) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + t * 16;
-    float lo[16], hi[16];
+    dependents_may_start();
+    if (b < 0) return;
+    const int pg = paged_page(p, b, col << p.page_shift);
+    if (pg < 0) continue;
+    const int n = min(len - (col << p.page_shift), 1 << p.page_shift);   // slots of the page
+    for (int g = warp; g < p.Hkv; g += int(blockDim.x) / 32) {
+      const T *src = reinterpret_cast<const T *>(p.k) + size_t(pg) * size_t(p.page_stride) + size_t(g) * size_t(p.head_stride) + t * 16;
+      float lo[16], hi[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) lo[e] = CUDART_INF_F, hi[e] = -CUDART_INF_F;
+      for (int e = 0; e < 16; ++e) lo[e] = CUDART_INF_F, hi[e] = -CUDART_INF_F;
 #pragma unroll 8
-    for (int i = team; i < n; i += kTeams) {
-      float x0[8], x1[8];
-      load8(src + size_t(i) * size_t(p.row_stride), x0), load8(src + size_t(i) * size_t(p.row_stride) + 8, x1);
+      for (int i = team; i < n; i += kTeams) {
+        float x0[8], x1[8];
+        load8(src + size_t(i) * size_t(p.row_stride), x0), load8(src + size_t(i) * size_t(p.row_stride) + 8, x1);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lo[e] = min_nan(lo[e], x0[e]), hi[e] = max_nan(hi[e], x0[e]);
-        lo[8 + e] = min_nan(lo[8 + e], x1[e]), hi[8 + e] = max_nan(hi[8 + e], x1[e]);
+        for (int e = 0; e < 8; ++e) {
+          lo[e] = min_nan(lo[e], x0[e]), hi[e] = max_nan(hi[e], x0[e]);
+          lo[8 + e] = min_nan(lo[8 + e], x1[e]), hi[8 + e] = max_nan(hi[8 + e], x1[e]);
+        }
       }
-    }
 #pragma unroll
-    for (int o = kTeam; o < 32; o <<= 1)
+      for (int o = kTeam; o < 32; o <<= 1)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        lo[e] = min_nan(lo[e], __shfl_xor_sync(0xffffffffu, lo[e], o));
-        hi[e] = max_nan(hi[e], __shfl_xor_sync(0xffffffffu, hi[e], o));
+        for (int e = 0; e < 16; ++e) {
+          lo[e] = min_nan(lo[e], __shfl_xor_sync(0xffffffffu, lo[e], o));
+          hi[e] = max_nan(hi[e], __shfl_xor_sync(0xffffffffu, hi[e], o));
+        }
+      if (team < 2) {   // one writes the least values, one the largest
+        T *dst = bounds + ((size_t(pg) * p.Hkv + g) * 2 + team) * D + t * 16;
+        float x0[8], x1[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x0[e] = team ? hi[e] : lo[e], x1[e] = team ? hi[8 + e] : lo[8 + e];
+        store8(dst, x0), store8(dst + 8, x1);
       }
-    if (team < 2) {   // one writes the least values, one the largest
-      T *dst = bounds + ((size_t(pg) * p.Hkv + g) * 2 + team) * D + t * 16;
-      float x0[8], x1[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x0[e] = team ? hi[e] : lo[e], x1[e] = team ? hi[8 + e] : lo[8 + e];
-      store8(dst, x0), store8(dst + 8, x1);
     }
   }
 }
@@ -413,9 +420,10 @@ int launch_paged_read(const glide_paged *h, const PagedParams &p, void *k, void 
 int launch_paged_bounds(const glide_paged *h, const PagedParams &p, void *bounds, cudaStream_t st) {
   return dispatch_config(h->cfg.io_dtype, h->cfg.head_dim, 1, [&](auto t, auto d, auto) {
     using T = typename decltype(t)::type;
-    const int64_t cols = ((int64_t(p.most) - 1) >> p.page_shift) + 1, most = p.starts ? (p.n_tokens >> p.page_shift) + 2 * int64_t(p.batch) : p.batch;
-    return launch_status(launch_chained(paged_bounds_kernel<T, decltype(d)::value>, unsigned(std::min<int64_t>(most, cols * p.batch)),
-                                        unsigned(std::min(p.Hkv, kWarps)) * 32, 0, st, p, reinterpret_cast<T *>(bounds)));
+    const int64_t cols = ((int64_t(p.most) - 1) >> p.page_shift) + 1;
+    const int most = int(std::min<int64_t>(p.starts ? (p.n_tokens >> p.page_shift) + 2 * int64_t(p.batch) : p.batch, cols * p.batch));
+    return launch_status(launch_chained(paged_bounds_kernel<T, decltype(d)::value>, unsigned(std::min(most, p.sm_count * kBoundsBlocks)),
+                                        unsigned(std::min(p.Hkv, kWarps)) * 32, 0, st, p, reinterpret_cast<T *>(bounds), most));
   });
 }
 

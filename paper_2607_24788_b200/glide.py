@@ -641,8 +641,7 @@ class GlidePaged:
 
     def glide_paged_bounds(self, table, lens, starts, bounds, n_tokens: Optional[int] = None, layer: int = 0, stream=None) -> None:
         """bounds [n_pages][H_kv][2][d], of the layer: least and largest key values of the pages that hold the tokens that starts names (None: the
-        newest of each sequence).  n_tokens: starts[B] or more; None: as many as the sequences can hold, for which a block for each of the table's entries
-        is launched."""
+        newest of each sequence).  n_tokens: starts[B] or more (None: as many as the sequences can hold)."""
         most = min(min(self.max_tokens, table.shape[1] * self.page_size) * table.shape[0], _MOST_TOKENS)
         rows = None if starts is None else most if n_tokens is None else int(n_tokens)
         call = self._packed_call(layer, table, lens, starts, rows, (0, 0, 0), -1, 0, None, None, None)
