@@ -15,14 +15,14 @@
 // bits, which fp16 has.  So S = sum q (step n) + mid sum q is computed as it stands: both as fp16 operands, the second term as four more
 // columns of the product, (hi, lo) of mid against (hi, lo) of sum q.  fp16 is short of exponents, so a key tile is scaled by a power of two
 // to below 2^-6, a query row by the threads that it belongs to, to below 2^7, and the scores are scaled back where they are multiplied by the
-// softmax scale anyway.  (Exact for rows whose step is 2^-8 of the tile's largest key or more, others are off by 2^-19 of that at most.  Keys
-// rounded to bf16 put scores off by 0.005, outputs by 0.006 of their norm.)  A value is rounded to fp16 once, and so are the weights: off by at most
-// 2^-11 of themselves, or a value by 2^-16 of the largest that its scale went by, a weight by 2^-30 of the row's largest (kRoomHalf).  The values' scale is a power of two as well, from the piece's
-// first tile on, until a tile has values four to eight times as large; then O is scaled as where a reference moves.  A key or value comes out of
-// one fused multiply-add for two codes where they lie in the word: four bits at the bottom of an fp16 number are code times its least
-// subnormal number, the next four 16 times that.  Which leaves the features of eight in the order 0 4 1 5 2 6 3 7, in keys, values, and so in
-// Q and O.  What a slot's codes are multiplied by, the scales and the further columns come from warp 19, which reads
-// the levels itself, a tile ahead.
+// softmax scale anyway.  (step n is exact for rows whose step is 2^-8 of the tile's largest key or more, others are off by 2^-19 of that at most; mid
+// and sum q have 22 bits each, which puts a score off by 2^-20 sum |q| |mid|.  Keys rounded to bf16 put scores off by 0.005, outputs by 0.006 of
+// their norm.)  A value is rounded to fp16 once, and so are the weights: off by at most 2^-11 of themselves, or a value by 2^-16 of the largest that
+// its scale went by, a weight by 2^-30 of the row's largest (kRoomHalf).  The values' scale is a power of two as well, from the piece's first tile on,
+// until a tile has values four to eight times as large; then O is scaled as where a reference moves.  A key or value comes out of one fused multiply-add
+// for two codes where they lie in the word: four bits at the bottom of an fp16 number are code times its least subnormal number, the next four 16
+// times that.  Which leaves the features of eight in the order 0 4 1 5 2 6 3 7, in keys, values, and so in Q and O.  What a slot's codes are
+// multiplied by, the scales and the further columns come from warp 19, which reads the levels itself, a tile ahead.
 // Every mbarrier wait is bounded; on a time-out the CTA records kDevWaitTimeout, leaves its loops, frees its TMEM columns and returns.
 #include <algorithm>
 #include <cstring>
